@@ -1,0 +1,102 @@
+// What the kernels of the language-model operators (grim_lm.h) share: element types, vector loads and stores that need no
+// alignment beyond the element's, reductions over a wave and a workgroup.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include "grim_lm.h"
+
+namespace grim {
+namespace lm {
+
+using bf16 = __bf16;
+using f16 = _Float16;
+
+constexpr int kComputeUnits = 256;
+constexpr int kMaxGrid = 0x7fffffff;
+
+// V elements of T as one value whose alignment is the element's: rows may start anywhere (odd widths, leading dimensions and
+// offsets), and the hardware takes a 16-byte access at any address, so rows that are not aligned run on the same kernels.
+template <typename T, int V>
+struct __attribute__((packed, aligned(sizeof(T)))) Pack {
+    T at[V];
+};
+
+template <int V, typename T>
+__device__ __forceinline__ void unpack(const Pack<T, V> &p, float (&out)[V]) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) out[j] = (float)p.at[j];
+}
+
+template <int V, typename T>
+__device__ __forceinline__ Pack<T, V> load(const T *p) {
+    Pack<T, V> r;
+    __builtin_memcpy(&r, p, sizeof(r));
+    return r;
+}
+
+template <int V, typename T>
+__device__ __forceinline__ void store(T *p, const float (&v)[V]) {
+    Pack<T, V> r;
+#pragma unroll
+    for (int j = 0; j < V; ++j) r.at[j] = (T)v[j];       // one rounding, to nearest even
+    __builtin_memcpy(p, &r, sizeof(r));
+}
+
+// The same values as far as the program goes, but not for the compiler: what was unpacked before is unpacked again after,
+// instead of being held in twice the registers meanwhile.
+template <typename T, int V>
+__device__ __forceinline__ void forget(Pack<T, V> &p) {
+    constexpr int n = (int)(sizeof(p) + 3) / 4;
+    unsigned int w[n] = {};
+    __builtin_memcpy(w, &p, sizeof(p));
+#pragma unroll
+    for (int i = 0; i < n; ++i) asm volatile("" : "+v"(w[i]));
+    __builtin_memcpy(&p, w, sizeof(p));
+}
+
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d, 64);
+    return v;
+}
+
+__device__ __forceinline__ float wave_max(float v) {
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) v = fmaxf(v, __shfl_xor(v, d, 64));
+    return v;
+}
+
+// Sums over a workgroup of W waves, in the order of the waves; `room` holds W floats that nobody uses until the next barrier
+// of the caller.
+template <int W>
+__device__ __forceinline__ float group_sum(float v, float *room) {
+    v = wave_sum(v);
+    if (W == 1) return v;
+    if ((threadIdx.x & 63) == 0) room[threadIdx.x >> 6] = v;
+    __syncthreads();
+    float s = 0.f;
+#pragma unroll
+    for (int w = 0; w < W; ++w) s += room[w];
+    return s;
+}
+
+template <int W>
+__device__ __forceinline__ float group_max(float v, float *room) {
+    v = wave_max(v);
+    if (W == 1) return v;
+    if ((threadIdx.x & 63) == 0) room[threadIdx.x >> 6] = v;
+    __syncthreads();
+    float s = room[0];
+#pragma unroll
+    for (int w = 1; w < W; ++w) s = fmaxf(s, room[w]);
+    return s;
+}
+
+inline bool known(grim_dtype dt) { return dt == GRIM_F32 || dt == GRIM_F16 || dt == GRIM_BF16; }
+inline grim_status launched() { return hipGetLastError() == hipSuccess ? GRIM_OK : GRIM_ERR_DEVICE; }
+
+// rows x ld elements stay far below what a 64-bit byte offset holds
+inline bool fits(int64_t rows, int64_t ld) { return ld >= 0 && ld <= (int64_t(1) << 40) && (rows <= 1 || ld <= (int64_t(1) << 56) / rows); }
+
+}  // namespace lm
+}  // namespace grim
