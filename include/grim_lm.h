@@ -71,7 +71,7 @@ grim_status grim_layer_norm_backward(const void *dy_dev, int64_t lddy, const voi
  * grim_glr_step is one token for `batch` callers at once, in the layout of grim_lstm_cell: gates 3H x batch fp32 as
  * grim_bcr_spmv leaves them (ldg >= batch), states H x batch fp32 (h_new_dev may be h_dev itself), y H x batch of element
  * type dt (what the next product reads), or NULL.
- * Errors: NULL, SHAPE (N < 0, N >= 2^31, H < 1, nseq < 1, leading dimension or a buffer too small), DTYPE, DEVICE.
+ * Errors: NULL, SHAPE (N < 0, N > 2^30, H < 1, H > 2^21, nseq < 1, nseq > 1 without starts, leading dimension or a buffer too small), DTYPE, DEVICE.
  */
 int64_t grim_glr_states(int64_t N, int64_t H);
 int64_t grim_glr_workspace(int64_t N, int64_t H);

@@ -8,4 +8,6 @@ from .binding import (  # noqa: F401
     BcrMatrix, BcrGroup, GrimError, lib_path, load_library, pack, conv2d, conv2d_act, ConvPlan, conv2d_plan, conv2d_kernel_name, export_bcrc, lstm_cell, lstm_step, rnn_step_launches, rnn_sequence_supported, lstm_sequence, lstm_sequence_noalloc, gru_sequence, lstm_sequence_batch, gru_sequence_batch, gru_cell, gru_step, spmm, spmm_kernel_name, spmv, spmv_batched,
     F32, F16, BF16, STATUS_NAMES,
 )
-from .lm import layer_norm, layer_norm_backward, layer_norm_workspace  # noqa: F401
+from .lm import (  # noqa: F401
+    glr_sequence, glr_sequence_backward, glr_states, glr_step, glr_workspace, layer_norm, layer_norm_backward, layer_norm_workspace,
+)

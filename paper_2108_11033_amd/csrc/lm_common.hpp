@@ -92,6 +92,9 @@ __device__ __forceinline__ float group_max(float v, float *room) {
     return s;
 }
 
+// out0[c], out1[c - C0]: sums of part[i * (C0 + C1) + c] over i < groups, in a fixed order (lm_norm.hip).
+grim_status join_columns(const float *part, int64_t groups, int64_t C0, float *out0, int64_t C1, float *out1, hipStream_t stream);
+
 inline bool known(grim_dtype dt) { return dt == GRIM_F32 || dt == GRIM_F16 || dt == GRIM_BF16; }
 inline grim_status launched() { return hipGetLastError() == hipSuccess ? GRIM_OK : GRIM_ERR_DEVICE; }
 

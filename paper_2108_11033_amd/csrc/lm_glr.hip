@@ -1,0 +1,687 @@
+// Gated linear recurrence over packed sequences, forward and backward, and its single-token step.
+//
+//     f = sigmoid(u)    h_t = f h_(t-1) + (1 - f) c    y = sigmoid(v) h
+//     G_t = dy_t sigmoid(v_t) + R_t,  R_(t-1) = f_t G_t     (R after the last token: dh_last)
+//     du = G f (1 - f) (h_(t-1) - c)    dc = G (1 - f)    dv = dy h sigmoid(v) (1 - sigmoid(v))    dh0 = f_0 G_0
+//
+// Both directions are linear in the state that is handed on: what a run of tokens does to it is a map S -> A S + B per unit, and
+// maps compose.  The rows of all sequences are cut alike, whatever their lengths, into chunks (one wave, 64 or 128 units)
+// and sets of kWaves chunks (one workgroup).  A first launch forms the maps of the chunks and sets; the second composes the maps of the
+// sets in front of its own, which gives every wave its state, and walks its rows again.  That reads u and c (backward: u, v
+// and dy) twice, the price of the parallelism along the sequence; the sets are walked in the opposite order so that what was
+// read last is still in the last-level cache.  A sequence that starts inside a run makes the map forget what came before: A = -0, told
+// apart from a product of gates that has underflowed, so that an infinity or NaN crosses underflow but no start.
+//
+// The backward pass needs h_(t-1).  The forward pass leaves the state in front of every kGroup-th row (fp32: 4 bytes for 8 rows of
+// 2 to 4 bytes each), from which a group's states are formed again in registers.
+#include "lm_common.hpp"
+
+namespace grim {
+namespace lm {
+
+constexpr int kWaves = 8;       // waves, and chunks, of a workgroup
+constexpr int kGroup = 8;       // rows whose loads are in flight together, and between two saved states
+constexpr float kLog2e = 1.44269504088896340736f;
+
+struct GlrParams {
+    const void *gates;
+    const float *bias, *h0;
+    const int32_t *seq;             // nseq + 1 starts, or NULL: one sequence
+    void *y;
+    float *h_last, *states;
+    const void *dy;
+    const float *dh_last;
+    void *dgates;
+    float *dh0, *dbias_part;        // [set][3H]
+    float *chunk_maps, *set_maps;   // [chunk or set][A | B][H]
+    int64_t ldg, ldy, lddy, lddg, N, H;
+    int32_t nseq, L, sets;          // rows of a chunk (a multiple of kGroup), sets of kWaves chunks
+};
+
+// f = sigmoid(z) and k = 1 - f = sigmoid(-z) of t = -z log2(e), without cancellation: k = 2^t f.  2^126 is as good as
+// infinity for f, and keeps k = 1 there; a NaN stays one.
+__device__ __forceinline__ void gate(float t, float &f, float &k) {
+    t = t > 126.f ? 126.f : t;
+    const float e = __builtin_amdgcn_exp2f(t);
+    f = __builtin_amdgcn_rcpf(1.f + e);
+    k = e * f;
+}
+
+__device__ __forceinline__ bool forgets(float a) { return __builtin_bit_cast(unsigned, a) == 0x80000000u; }
+__device__ __forceinline__ float apply(float a, float b, float s) { return forgets(a) ? b : __builtin_fmaf(a, s, b); }
+// (a, b) after (a0, b0)
+__device__ __forceinline__ void compose(float a0, float b0, float &a, float &b) {
+    b = apply(a, b, b0);
+    a = forgets(a) ? a : a0 * a;
+}
+
+// ---------------------------------------------------------------------------------------------- where sequences start
+struct Starts {
+    const int32_t *seq;
+    int32_t nseq, N;
+    __device__ __forceinline__ int at(int i) const { return seq ? seq[i] : i ? N : 0; }
+    // how many of the starts of sequences 0 .. nseq - 1 lie below `row`; the whole wave asks
+    __device__ __forceinline__ int below(int row) const {
+        if (!seq) return row > 0 ? 1 : 0;
+        const int lane = threadIdx.x & 63;
+        int lo = 0, n = nseq;
+        while (n > 64) {
+            const int step = (n + 63) / 64;
+            const bool under = lane * step < n && seq[lo + lane * step] < row;
+            const int c = __popcll(__ballot(under));
+            if (c == 0) return lo;
+            lo += (c - 1) * step;
+            n = min(step, n - (c - 1) * step);
+        }
+        return __builtin_amdgcn_readfirstlane(lo + __popcll(__ballot(lane < n && seq[lo + lane] < row)));
+    }
+};
+
+// The unit(s) of a lane: VEC side by side.  Lanes past the last unit repeat it and write nothing; a last lane that would reach past it
+// is moved back and shares units with its neighbour (same values, same bits).
+template <int VEC>
+struct Units {
+    int64_t at;
+    bool live;
+    __device__ __forceinline__ Units(int tile, int64_t H) {
+        at = ((int64_t)tile * 64 + (threadIdx.x & 63)) * VEC;
+        live = at < H;
+        if (at > H - VEC) at = H - VEC;
+    }
+};
+
+template <int VEC>
+__device__ __forceinline__ void take(const float *from, float (&v)[VEC]) {
+    unpack(load<VEC>(from), v);
+}
+
+// Scaled biases: the gates' exponents are one multiply-add each.
+template <int VEC>
+struct Bias {
+    float u[VEC], c[VEC], v[VEC];
+    __device__ __forceinline__ Bias(const GlrParams &p, int64_t at) {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) u[j] = c[j] = v[j] = 0.f;
+        if (p.bias) {
+            take<VEC>(p.bias + at, u);
+            take<VEC>(p.bias + p.H + at, c);
+            take<VEC>(p.bias + 2 * p.H + at, v);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) u[j] *= -kLog2e, v[j] *= -kLog2e;
+        }
+    }
+};
+
+// Rows g .. of a group, at most `have` of them (the last is read again for those that are missing), of one column block.
+template <typename T, int VEC>
+struct Rows {
+    Pack<T, VEC> r[kGroup];
+    __device__ __forceinline__ void fetch(const void *base, int64_t ld, int64_t column, int g, int have) {
+        const T *p = static_cast<const T *>(base) + (int64_t)g * ld;
+#pragma unroll
+        for (int i = 0; i < kGroup; ++i) r[i] = load<VEC>(p + (int64_t)min(i, have - 1) * ld + column);
+    }
+};
+
+// ---------------------------------------------------------------------------------------------- maps of the chunks
+// What rows r0 .. r1 - 1 do to the state that enters in front of them.
+template <typename T, int VEC>
+__device__ __forceinline__ void forward_map(const GlrParams &p, const Units<VEC> &un, const Bias<VEC> &bias, int r0, int r1,
+                                            float (&A)[VEC], float (&B)[VEC]) {
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) A[j] = 1.f, B[j] = 0.f;
+    if (r0 >= r1) return;
+    const Starts starts{p.seq, p.nseq, (int32_t)p.N};
+    int s = starts.below(r0) - 1, bound = starts.at(s + 1);
+    Rows<T, VEC> u, c, un_, cn;
+    un_.fetch(p.gates, p.ldg, un.at, r0, r1 - r0);
+    cn.fetch(p.gates, p.ldg, p.H + un.at, r0, r1 - r0);
+    for (int g = r0; g < r1; g += kGroup) {
+        u = un_, c = cn;
+        if (g + kGroup < r1) {
+            un_.fetch(p.gates, p.ldg, un.at, g + kGroup, r1 - g - kGroup);
+            cn.fetch(p.gates, p.ldg, p.H + un.at, g + kGroup, r1 - g - kGroup);
+        }
+#pragma unroll
+        for (int i = 0; i < kGroup; ++i) {
+            const int r = g + i;
+            if (r < r1) {
+                if (r == bound && s + 1 < p.nseq) {
+                    do ++s;
+                    while (s + 1 < p.nseq && starts.at(s + 1) <= r);
+                    bound = starts.at(s + 1);
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) A[j] = -0.f, B[j] = 0.f;
+                    if (p.h0) take<VEC>(p.h0 + s * p.H + un.at, B);
+                }
+                float zu[VEC], zc[VEC];
+                unpack(u.r[i], zu);
+                unpack(c.r[i], zc);
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    float f, k;
+                    gate(__builtin_fmaf(zu[j], -kLog2e, bias.u[j]), f, k);
+                    A[j] *= f;
+                    B[j] = __builtin_fmaf(f, B[j], k * (zc[j] + bias.c[j]));
+                }
+            }
+        }
+    }
+}
+
+// What rows r1 - 1 .. r0 do to the gradient R that enters behind them.
+template <typename T, int VEC>
+__device__ __forceinline__ void backward_map(const GlrParams &p, const Units<VEC> &un, const Bias<VEC> &bias, int r0, int r1,
+                                             float (&A)[VEC], float (&B)[VEC]) {
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) A[j] = 1.f, B[j] = 0.f;
+    if (r0 >= r1) return;
+    const Starts starts{p.seq, p.nseq, (int32_t)p.N};
+    int s = starts.below(r1) - 1;                               // the sequence of row r1 - 1, and where it ends and starts
+    int end = s >= 0 ? starts.at(s + 1) : -1, begin = s >= 0 ? starts.at(s) : 0;
+    Rows<T, VEC> u, v, d, un_, vn, dn;
+    int g = r0 + (r1 - 1 - r0) / kGroup * kGroup;
+    auto fetch = [&](int at) {
+        un_.fetch(p.gates, p.ldg, un.at, at, r1 - at);
+        vn.fetch(p.gates, p.ldg, 2 * p.H + un.at, at, r1 - at);
+        dn.fetch(p.dy, p.lddy, un.at, at, r1 - at);
+    };
+    fetch(g);
+    for (; g >= r0; g -= kGroup) {
+        u = un_, v = vn, d = dn;
+        if (g > r0) fetch(g - kGroup);
+#pragma unroll
+        for (int i = kGroup - 1; i >= 0; --i) {
+            const int r = g + i;
+            if (r < r1) {
+                if (r < begin && s > 0) {
+                    do --s;
+                    while (s > 0 && starts.at(s) > r);
+                    end = starts.at(s + 1), begin = starts.at(s);
+                }
+                if (r + 1 == end) {
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) A[j] = -0.f, B[j] = 0.f;
+                    if (p.dh_last) take<VEC>(p.dh_last + s * p.H + un.at, B);
+                }
+                float zu[VEC], zv[VEC], dy[VEC];
+                unpack(u.r[i], zu);
+                unpack(v.r[i], zv);
+                unpack(d.r[i], dy);
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    float f, k, o, ko;
+                    gate(__builtin_fmaf(zu[j], -kLog2e, bias.u[j]), f, k);
+                    gate(__builtin_fmaf(zv[j], -kLog2e, bias.v[j]), o, ko);
+                    A[j] *= f;
+                    B[j] = f * __builtin_fmaf(dy[j], o, B[j]);
+                }
+            }
+        }
+    }
+}
+
+// The maps of a workgroup's chunks in the order that the state passes them (wave `place` is the place-th), from LDS: what those in front of
+// this one do together (A, B), and what all do (SA, SB).
+template <int VEC>
+__device__ __forceinline__ void compose_chunks(float (*maps)[2][64 * VEC], int place, const float (&a)[VEC], const float (&b)[VEC],
+                                               float (&A)[VEC], float (&B)[VEC], float (&SA)[VEC], float (&SB)[VEC]) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) maps[place][0][lane * VEC + j] = a[j], maps[place][1][lane * VEC + j] = b[j];
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) A[j] = SA[j] = 1.f, B[j] = SB[j] = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        if (w == place) {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) A[j] = SA[j], B[j] = SB[j];
+        }
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            float na = maps[w][0][lane * VEC + j], nb = maps[w][1][lane * VEC + j];
+            compose(SA[j], SB[j], na, nb);
+            SA[j] = na, SB[j] = nb;
+        }
+    }
+}
+
+// Rows of this wave's chunk.
+struct Chunk {
+    int wave, index, r0, r1;
+    __device__ __forceinline__ Chunk(const GlrParams &p, int set) {
+        wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        index = set * kWaves + wave;
+        const int64_t a = (int64_t)index * p.L, b = a + p.L;
+        r0 = (int)(a < p.N ? a : p.N), r1 = (int)(b < p.N ? b : p.N);
+    }
+};
+
+template <typename T, int VEC, bool BACK>
+__global__ void __launch_bounds__(64 * kWaves) glr_maps(GlrParams p) {
+    __shared__ float maps[kWaves][2][64 * VEC];
+    const int set = blockIdx.x;
+    const Units<VEC> un(blockIdx.y, p.H);
+    const Bias<VEC> bias(p, un.at);
+    const Chunk ch(p, set);
+    float a[VEC], b[VEC], A[VEC], B[VEC], SA[VEC], SB[VEC];
+    if (BACK) backward_map<T, VEC>(p, un, bias, ch.r0, ch.r1, a, b);
+    else forward_map<T, VEC>(p, un, bias, ch.r0, ch.r1, a, b);
+    const int place = BACK ? kWaves - 1 - ch.wave : ch.wave;
+    compose_chunks<VEC>(maps, place, a, b, A, B, SA, SB);
+    if (!un.live) return;
+    float *mine = p.chunk_maps + (int64_t)ch.index * 2 * p.H + un.at;
+    store(mine, A);
+    store(mine + p.H, B);
+    if (place == kWaves - 1) {
+        float *all = p.set_maps + (int64_t)set * 2 * p.H + un.at;
+        store(all, SA);
+        store(all + p.H, SB);
+    }
+}
+
+// The state that enters this wave's chunk: the sets in front of its own (first, in steps of `dir`, to the one before `set`) dealt to the
+// waves as runs, composed through LDS, then the chunk's own prefix.  Nothing enters the first set: A counts for nothing there.
+template <int VEC>
+__device__ __forceinline__ void entering(const GlrParams &p, float (*maps)[2][64 * VEC], const Units<VEC> &un, const Chunk &ch, int set,
+                                         int first, int dir, int ahead, float (&S)[VEC]) {
+    float a[VEC], b[VEC], pa[VEC], pb[VEC];
+    const float *prefix = p.chunk_maps + (int64_t)ch.index * 2 * p.H + un.at;
+    take<VEC>(prefix, pa);
+    take<VEC>(prefix + p.H, pb);
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) a[j] = 1.f, b[j] = 0.f;
+    const int per = (ahead + kWaves - 1) / kWaves;
+    const int from = min(ch.wave * per, ahead), to = min(from + per, ahead);
+#pragma unroll 4
+    for (int i = from; i < to; ++i) {
+        const float *m = p.set_maps + (int64_t)(first + dir * i) * 2 * p.H + un.at;
+        float na[VEC], nb[VEC];
+        take<VEC>(m, na);
+        take<VEC>(m + p.H, nb);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            compose(a[j], b[j], na[j], nb[j]);
+            a[j] = na[j], b[j] = nb[j];
+        }
+    }
+    float A[VEC], B[VEC], SA[VEC], SB[VEC];
+    compose_chunks<VEC>(maps, ch.wave, a, b, A, B, SA, SB);
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) S[j] = apply(pa[j], pb[j], SB[j]);
+}
+
+// ---------------------------------------------------------------------------------------------- forward
+// ALONE: one set holds all rows, and its workgroup forms the maps of its chunks itself.
+template <typename T, int VEC, bool ALONE>
+__global__ void __launch_bounds__(64 * kWaves) glr_forward(GlrParams p) {
+    __shared__ float maps[kWaves][2][64 * VEC];
+    const int set = ALONE ? 0 : p.sets - 1 - blockIdx.x;
+    const Units<VEC> un(blockIdx.y, p.H);
+    const Bias<VEC> bias(p, un.at);
+    const Chunk ch(p, set);
+    const Starts starts{p.seq, p.nseq, (int32_t)p.N};
+    float h[VEC];
+    if (ALONE) {
+        float a[VEC], b[VEC], A[VEC], SA[VEC], SB[VEC];
+        forward_map<T, VEC>(p, un, bias, ch.r0, ch.r1, a, b);
+        compose_chunks<VEC>(maps, ch.wave, a, b, A, h, SA, SB);
+    } else {
+        entering<VEC>(p, maps, un, ch, set, 0, 1, set, h);
+    }
+    if (p.h_last)                                               // sequences without a token keep their state
+        for (int s = ch.index; s < p.nseq; s += p.sets * kWaves)
+            if (starts.at(s) == starts.at(s + 1) && un.live) {
+                float v[VEC] = {};
+                if (p.h0) take<VEC>(p.h0 + s * p.H + un.at, v);
+                store(p.h_last + s * p.H + un.at, v);
+            }
+    const int r0 = ch.r0, r1 = ch.r1;
+    if (r0 >= r1) return;
+    int s = starts.below(r0) - 1, bound = starts.at(s + 1);
+    Rows<T, VEC> u, c, v, un_, cn, vn;
+    auto fetch = [&](int at) {
+        un_.fetch(p.gates, p.ldg, un.at, at, r1 - at);
+        cn.fetch(p.gates, p.ldg, p.H + un.at, at, r1 - at);
+        vn.fetch(p.gates, p.ldg, 2 * p.H + un.at, at, r1 - at);
+    };
+    fetch(r0);
+    T *y = static_cast<T *>(p.y) + un.at;
+    for (int g = r0; g < r1; g += kGroup) {
+        u = un_, c = cn, v = vn;
+        if (g + kGroup < r1) fetch(g + kGroup);
+        if (p.states && un.live) store(p.states + (int64_t)(g / kGroup) * p.H + un.at, h);
+#pragma unroll
+        for (int i = 0; i < kGroup; ++i) {
+            const int r = g + i;
+            if (r < r1) {
+                if (r == bound && s + 1 < p.nseq) {
+                    do ++s;
+                    while (s + 1 < p.nseq && starts.at(s + 1) <= r);
+                    bound = starts.at(s + 1);
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) h[j] = 0.f;
+                    if (p.h0) take<VEC>(p.h0 + s * p.H + un.at, h);
+                }
+                float zu[VEC], zc[VEC], zv[VEC], out[VEC];
+                unpack(u.r[i], zu);
+                unpack(c.r[i], zc);
+                unpack(v.r[i], zv);
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    float f, k, o, ko;
+                    gate(__builtin_fmaf(zu[j], -kLog2e, bias.u[j]), f, k);
+                    gate(__builtin_fmaf(zv[j], -kLog2e, bias.v[j]), o, ko);
+                    h[j] = __builtin_fmaf(f, h[j], k * (zc[j] + bias.c[j]));
+                    out[j] = o * h[j];
+                }
+                if (un.live) {
+                    store(y + (int64_t)r * p.ldy, out);
+                    if (p.h_last && s >= 0 && r + 1 == bound) store(p.h_last + s * p.H + un.at, h);
+                }
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- backward
+template <typename T, int VEC, bool ALONE>
+__global__ void __launch_bounds__(64 * kWaves) glr_backward(GlrParams p) {
+    __shared__ float maps[kWaves][2][64 * VEC];
+    __shared__ float sums[3][64 * VEC];
+    const int set = ALONE ? 0 : p.sets - 1 - blockIdx.x;
+    const Units<VEC> un(blockIdx.y, p.H);
+    const Bias<VEC> bias(p, un.at);
+    const Chunk ch(p, set);
+    const Starts starts{p.seq, p.nseq, (int32_t)p.N};
+    float R[VEC];
+    if (ALONE) {
+        float a[VEC], b[VEC], A[VEC], SA[VEC], SB[VEC];
+        backward_map<T, VEC>(p, un, bias, ch.r0, ch.r1, a, b);
+        compose_chunks<VEC>(maps, kWaves - 1 - ch.wave, a, b, A, R, SA, SB);
+    } else {
+        entering<VEC>(p, maps, un, ch, set, p.sets - 1, -1, p.sets - 1 - set, R);
+    }
+    if (p.dh0)
+        for (int s = ch.index; s < p.nseq; s += p.sets * kWaves)
+            if (starts.at(s) == starts.at(s + 1) && un.live) {
+                float v[VEC] = {};
+                if (p.dh_last) take<VEC>(p.dh_last + s * p.H + un.at, v);
+                store(p.dh0 + s * p.H + un.at, v);
+            }
+    float bu[VEC], bc[VEC], bv[VEC];
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) bu[j] = bc[j] = bv[j] = 0.f;
+    const int r0 = ch.r0, r1 = ch.r1;
+    if (r0 < r1) {
+        int s = starts.below(r1) - 1;                           // the sequence of the row in hand, its first row and its end
+        int begin = s >= 0 ? starts.at(s) : 0, end = s >= 0 ? starts.at(s + 1) : -1;
+        for (int g = r0 + (r1 - 1 - r0) / kGroup * kGroup; g >= r0; g -= kGroup) {
+            const int have = min(r1 - g, kGroup);
+            Rows<T, VEC> u, c, v, d;
+            u.fetch(p.gates, p.ldg, un.at, g, have);
+            c.fetch(p.gates, p.ldg, p.H + un.at, g, have);
+            v.fetch(p.gates, p.ldg, 2 * p.H + un.at, g, have);
+            d.fetch(p.dy, p.lddy, un.at, g, have);
+            float before[VEC];                                  // the state in front of the row
+            take<VEC>(p.states + (int64_t)(g / kGroup) * p.H + un.at, before);
+            // the group's states again, and its gates; `first` marks the rows that begin a sequence
+            float h[kGroup][VEC], f[kGroup][VEC], k[kGroup][VEC];
+            unsigned first = 0;
+            int q = s, next = -1;                               // (no start inside: nothing to look for)
+            if (begin >= g) {
+                q = starts.below(g) - 1;
+                next = starts.at(q + 1);
+            }
+#pragma unroll
+            for (int i = 0; i < kGroup; ++i) {
+                if (i < have) {
+                    if (g + i == next && q + 1 < p.nseq) {
+                        do ++q;
+                        while (q + 1 < p.nseq && starts.at(q + 1) <= g + i);
+                        next = starts.at(q + 1);
+                        first |= 1u << i;
+#pragma unroll
+                        for (int j = 0; j < VEC; ++j) before[j] = 0.f;
+                        if (p.h0) take<VEC>(p.h0 + q * p.H + un.at, before);
+                    }
+                    float zu[VEC], zc[VEC];
+                    unpack(u.r[i], zu);
+                    unpack(c.r[i], zc);
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) {
+                        gate(__builtin_fmaf(zu[j], -kLog2e, bias.u[j]), f[i][j], k[i][j]);
+                        h[i][j] = before[j];
+                        before[j] = __builtin_fmaf(f[i][j], before[j], k[i][j] * (zc[j] + bias.c[j]));
+                    }
+                }
+            }
+#pragma unroll
+            for (int i = kGroup - 1; i >= 0; --i) {
+                if (i < have) {
+                    const int r = g + i;
+                    if (r < begin && s > 0) {
+                        do --s;
+                        while (s > 0 && starts.at(s) > r);
+                        end = starts.at(s + 1), begin = starts.at(s);
+                    }
+                    if (r + 1 == end) {
+#pragma unroll
+                        for (int j = 0; j < VEC; ++j) R[j] = 0.f;
+                        if (p.dh_last) take<VEC>(p.dh_last + s * p.H + un.at, R);
+                    }
+                    float zc[VEC], zv[VEC], dy[VEC], du[VEC], dc[VEC], dv[VEC];
+                    unpack(c.r[i], zc);
+                    unpack(v.r[i], zv);
+                    unpack(d.r[i], dy);
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) {
+                        float o, ko;
+                        gate(__builtin_fmaf(zv[j], -kLog2e, bias.v[j]), o, ko);
+                        const float cc = zc[j] + bias.c[j];
+                        const float dyo = dy[j] * o, G = dyo + R[j];
+                        const float hh = __builtin_fmaf(f[i][j], h[i][j], k[i][j] * cc);
+                        dc[j] = G * k[i][j];
+                        R[j] = G * f[i][j];
+                        du[j] = dc[j] * f[i][j] * (h[i][j] - cc);
+                        dv[j] = dyo * ko * hh;
+                        bu[j] += du[j], bc[j] += dc[j], bv[j] += dv[j];
+                    }
+                    if (un.live) {
+                        T *out = static_cast<T *>(p.dgates) + (int64_t)r * p.lddg + un.at;
+                        store(out, du);
+                        store(out + p.H, dc);
+                        store(out + 2 * p.H, dv);
+                        if (p.dh0 && s >= 0 && (first >> i & 1)) store(p.dh0 + s * p.H + un.at, R);
+                    }
+                }
+            }
+        }
+    }
+    if (!p.dbias_part) return;
+    const int lane = threadIdx.x & 63;
+    for (int w = 0; w < kWaves; ++w) {                          // the waves' sums, in the order of the waves
+        if (ch.wave == w) {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                const int at = lane * VEC + j;
+                sums[0][at] = w ? sums[0][at] + bu[j] : bu[j];
+                sums[1][at] = w ? sums[1][at] + bc[j] : bc[j];
+                sums[2][at] = w ? sums[2][at] + bv[j] : bv[j];
+            }
+        }
+        __syncthreads();
+    }
+    if (ch.wave < 3 && un.live) {
+        float out[VEC];
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) out[j] = sums[ch.wave][lane * VEC + j];
+        store(p.dbias_part + ((int64_t)set * 3 + ch.wave) * p.H + un.at, out);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- one token
+struct GlrStepParams {
+    const float *gates, *bias, *h;
+    float *h_new;
+    void *y;
+    int64_t ldg, ldh, ldh_new, ldy, H;
+    int32_t batch;
+};
+
+template <typename T>
+__global__ void __launch_bounds__(256) glr_step_kernel(GlrStepParams p) {
+    const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (e >= p.H * p.batch) return;
+    const int64_t r = e >> 32 ? e / p.batch : (int64_t)((uint32_t)e / (uint32_t)p.batch);
+    const int64_t b = e - r * p.batch;
+    float zu = p.gates[r * p.ldg + b], zc = p.gates[(p.H + r) * p.ldg + b], zv = p.gates[(2 * p.H + r) * p.ldg + b];
+    if (p.bias) zu += p.bias[r], zc += p.bias[p.H + r], zv += p.bias[2 * p.H + r];
+    float f, k, o, ko;
+    gate(zu * -kLog2e, f, k);
+    gate(zv * -kLog2e, o, ko);
+    const float h = __builtin_fmaf(f, p.h[r * p.ldh + b], k * zc);
+    p.h_new[r * p.ldh_new + b] = h;
+    if (p.y) static_cast<T *>(p.y)[r * p.ldy + b] = (T)(o * h);
+}
+
+// ---------------------------------------------------------------------------------------------- launches
+// How the rows are cut.  Chunks as short as give some 1024 workgroups (four per compute unit, so that they even out), but
+// of no more than 128 sets, whose maps every workgroup reads, and no shorter than a group.
+struct Cut {
+    int vec;
+    int32_t L, sets, tiles;
+};
+
+inline Cut cut_rows(int64_t N, int64_t H) {
+    Cut c;
+    // one unit a lane where two would leave compute units without a workgroup
+    c.vec = H >= 2 && N * H >= (int64_t)1 << 20 ? 2 : 1;
+    c.tiles = (int32_t)((H + 64 * c.vec - 1) / (64 * c.vec));
+    const int64_t even = (N * c.tiles + kWaves * 1024 - 1) / (kWaves * 1024), few = (N + kWaves * 128 - 1) / (kWaves * 128);
+    int64_t L = even > few ? even : few;
+    if (N <= 2 * kWaves * kGroup) L = (N + kWaves - 1) / kWaves;          // one set, one launch
+    L = (L + kGroup - 1) / kGroup * kGroup;
+    c.L = (int32_t)(L < kGroup ? kGroup : L);
+    const int64_t rows = (int64_t)c.L * kWaves;
+    c.sets = N > 0 ? (int32_t)((N + rows - 1) / rows) : 1;
+    return c;
+}
+
+inline int64_t map_floats(const Cut &c, int64_t H) { return ((int64_t)c.sets * (kWaves + 1)) * 2 * H; }
+
+template <typename T, int VEC>
+grim_status glr_launch(const GlrParams &p, const Cut &c, bool back, hipStream_t stream) {
+    const dim3 grid((unsigned)c.sets, (unsigned)c.tiles), block(64 * kWaves);
+    if (c.sets == 1) {
+        if (back) hipLaunchKernelGGL((glr_backward<T, VEC, true>), grid, block, 0, stream, p);
+        else hipLaunchKernelGGL((glr_forward<T, VEC, true>), grid, block, 0, stream, p);
+        return launched();
+    }
+    if (back) hipLaunchKernelGGL((glr_maps<T, VEC, true>), grid, block, 0, stream, p);
+    else hipLaunchKernelGGL((glr_maps<T, VEC, false>), grid, block, 0, stream, p);
+    const grim_status st = launched();
+    if (st != GRIM_OK) return st;
+    if (back) hipLaunchKernelGGL((glr_backward<T, VEC, false>), grid, block, 0, stream, p);
+    else hipLaunchKernelGGL((glr_forward<T, VEC, false>), grid, block, 0, stream, p);
+    return launched();
+}
+
+grim_status glr_run(GlrParams p, grim_dtype dt, bool back, hipStream_t stream) {
+    const Cut c = cut_rows(p.N, p.H);
+    p.L = c.L, p.sets = c.sets;
+    p.set_maps = p.chunk_maps + (int64_t)c.sets * kWaves * 2 * p.H;
+    switch (dt) {
+        case GRIM_F32: return c.vec == 2 ? glr_launch<float, 2>(p, c, back, stream) : glr_launch<float, 1>(p, c, back, stream);
+        case GRIM_F16: return c.vec == 2 ? glr_launch<f16, 2>(p, c, back, stream) : glr_launch<f16, 1>(p, c, back, stream);
+        default: return c.vec == 2 ? glr_launch<bf16, 2>(p, c, back, stream) : glr_launch<bf16, 1>(p, c, back, stream);
+    }
+}
+
+inline bool glr_sizes(int64_t N, int64_t H, int32_t nseq, const int32_t *seq) {
+    // (row numbers in 32 bits with room for a group more; column blocks in one grid dimension)
+    return N >= 0 && N <= (int64_t)1 << 30 && H >= 1 && H <= (int64_t)1 << 21 && nseq >= 1 && (seq || nseq == 1);
+}
+
+}  // namespace lm
+}  // namespace grim
+
+extern "C" {
+
+int64_t grim_glr_states(int64_t N, int64_t H) {
+    using namespace grim::lm;
+    return glr_sizes(N, H, 1, nullptr) ? (N + kGroup - 1) / kGroup * H * (int64_t)sizeof(float) : 0;
+}
+
+int64_t grim_glr_workspace(int64_t N, int64_t H) {
+    using namespace grim::lm;
+    if (!glr_sizes(N, H, 1, nullptr)) return 0;
+    const Cut c = cut_rows(N, H);
+    return (map_floats(c, H) + (int64_t)c.sets * 3 * H) * (int64_t)sizeof(float);
+}
+
+grim_status grim_glr_sequence(const void *gates_dev, grim_dtype dt, int64_t ldg, const float *bias_dev, const float *h0_dev,
+                              const int32_t *seq_start_dev, int32_t nseq, int64_t N, int64_t H, void *y_dev, int64_t ldy,
+                              float *h_last_dev, void *states_dev, void *workspace, int64_t workspace_bytes,
+                              void *hip_stream) {
+    using namespace grim::lm;
+    if (!known(dt)) return GRIM_ERR_DTYPE;
+    if (!glr_sizes(N, H, nseq, seq_start_dev) || ldg < 3 * H || ldy < H || !fits(N, ldg) || !fits(N, ldy)) return GRIM_ERR_SHAPE;
+    if ((N > 0 && (!gates_dev || !y_dev)) || !workspace) return GRIM_ERR_NULL;
+    if (workspace_bytes < grim_glr_workspace(N, H)) return GRIM_ERR_SHAPE;
+    GlrParams p{};
+    p.gates = gates_dev, p.bias = bias_dev, p.h0 = h0_dev, p.seq = seq_start_dev, p.nseq = nseq;
+    p.y = y_dev, p.h_last = h_last_dev, p.states = static_cast<float *>(states_dev);
+    p.chunk_maps = static_cast<float *>(workspace);
+    p.ldg = ldg, p.ldy = ldy, p.N = N, p.H = H;
+    return glr_run(p, dt, false, static_cast<hipStream_t>(hip_stream));
+}
+
+grim_status grim_glr_sequence_backward(const void *gates_dev, grim_dtype dt, int64_t ldg, const float *bias_dev,
+                                       const float *h0_dev, const int32_t *seq_start_dev, int32_t nseq, int64_t N, int64_t H,
+                                       const void *states_dev, const void *dy_dev, int64_t lddy, const float *dh_last_dev,
+                                       void *dgates_dev, int64_t lddg, float *dbias_dev, float *dh0_dev, void *workspace,
+                                       int64_t workspace_bytes, void *hip_stream) {
+    using namespace grim::lm;
+    if (!known(dt)) return GRIM_ERR_DTYPE;
+    if (!glr_sizes(N, H, nseq, seq_start_dev) || ldg < 3 * H || lddy < H || lddg < 3 * H || !fits(N, ldg) || !fits(N, lddy) ||
+        !fits(N, lddg))
+        return GRIM_ERR_SHAPE;
+    if ((N > 0 && (!gates_dev || !states_dev || !dy_dev || !dgates_dev)) || !workspace) return GRIM_ERR_NULL;
+    if (workspace_bytes < grim_glr_workspace(N, H)) return GRIM_ERR_SHAPE;
+    const Cut c = cut_rows(N, H);
+    GlrParams p{};
+    p.gates = gates_dev, p.bias = bias_dev, p.h0 = h0_dev, p.seq = seq_start_dev, p.nseq = nseq;
+    p.states = static_cast<float *>(const_cast<void *>(states_dev));
+    p.dy = dy_dev, p.dh_last = dh_last_dev, p.dgates = dgates_dev, p.dh0 = dh0_dev;
+    p.chunk_maps = static_cast<float *>(workspace);
+    p.dbias_part = dbias_dev ? p.chunk_maps + map_floats(c, H) : nullptr;
+    p.ldg = ldg, p.lddy = lddy, p.lddg = lddg, p.N = N, p.H = H;
+    const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    const grim_status st = glr_run(p, dt, true, stream);
+    if (st != GRIM_OK || !dbias_dev) return st;
+    return join_columns(p.dbias_part, c.sets, 3 * H, dbias_dev, 0, nullptr, stream);
+}
+
+grim_status grim_glr_step(const float *gates_dev, int64_t ldg, const float *bias_dev, const float *h_dev, int64_t ldh,
+                          float *h_new_dev, int64_t ldh_new, void *y_dev, grim_dtype dt, int64_t ldy, int64_t H,
+                          int32_t batch, void *hip_stream) {
+    using namespace grim::lm;
+    if (!known(dt)) return GRIM_ERR_DTYPE;
+    if (H < 1 || batch < 0 || ldg < batch || ldh < batch || ldh_new < batch || (y_dev && ldy < batch) || H > (int64_t)1 << 32 ||
+        !fits(3 * H, ldg) || !fits(H, ldh) || !fits(H, ldh_new) || (y_dev && !fits(H, ldy)))
+        return GRIM_ERR_SHAPE;
+    if (batch == 0) return GRIM_OK;
+    if (!gates_dev || !h_dev || !h_new_dev) return GRIM_ERR_NULL;
+    if (H > (int64_t)kMaxGrid * 256 / batch) return GRIM_ERR_SHAPE;
+    const GlrStepParams p{gates_dev, bias_dev, h_dev, h_new_dev, y_dev, ldg, ldh, ldh_new, ldy, H, batch};
+    const dim3 grid((unsigned)((H * batch + 255) / 256)), block(256);
+    const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    if (dt == GRIM_F32) hipLaunchKernelGGL(glr_step_kernel<float>, grid, block, 0, stream, p);
+    else if (dt == GRIM_F16) hipLaunchKernelGGL(glr_step_kernel<f16>, grid, block, 0, stream, p);
+    else hipLaunchKernelGGL(glr_step_kernel<bf16>, grid, block, 0, stream, p);
+    return launched();
+}
+
+}  // extern "C"

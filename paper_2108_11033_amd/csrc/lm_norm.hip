@@ -258,24 +258,32 @@ __global__ void __launch_bounds__(256) norm_back_columns(NormBackParams p, int64
 }
 
 // Sums of the workgroups' columns, in a fixed order: 64 columns by 16 waves, each wave every 16th workgroup's.
-__global__ void __launch_bounds__(1024) norm_back_join(const float *part, int64_t groups, int64_t C, float *dgamma, float *dbeta) {
+__global__ void __launch_bounds__(1024) join_columns_kernel(const float *part, int64_t groups, int64_t C0, float *out0, int64_t C1,
+                                                            float *out1) {
     __shared__ float sums[16][64];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int64_t c = (int64_t)blockIdx.x * 64 + lane;
+    const int64_t c = (int64_t)blockIdx.x * 64 + lane, width = C0 + C1;
     float s = 0.f;
-    if (c < 2 * C) {
+    if (c < width) {
 #pragma unroll 8
-        for (int64_t i = w; i < groups; i += 16) s += part[i * 2 * C + c];
+        for (int64_t i = w; i < groups; i += 16) s += part[i * width + c];
     }
     sums[w][lane] = s;
     __syncthreads();
-    if (w || c >= 2 * C) return;
+    if (w || c >= width) return;
     s = 0.f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) s += sums[i][lane];
-    if (c < C) {
-        if (dgamma) dgamma[c] = s;
-    } else if (dbeta) dbeta[c - C] = s;
+    if (c < C0) {
+        if (out0) out0[c] = s;
+    } else if (out1) out1[c - C0] = s;
+}
+
+grim_status join_columns(const float *part, int64_t groups, int64_t C0, float *out0, int64_t C1, float *out1, hipStream_t stream) {
+    const int64_t grid = (C0 + C1 + 63) / 64;
+    if (grid > kMaxGrid) return GRIM_ERR_SHAPE;
+    hipLaunchKernelGGL(join_columns_kernel, dim3((unsigned)grid), dim3(1024), 0, stream, part, groups, C0, out0, C1, out1);
+    return launched();
 }
 
 // Threads per row: one wave while four pieces a thread hold the row, then 4 waves, then 16; 0: the walking kernels.
@@ -372,10 +380,7 @@ grim_status norm_back_typed(const NormBackParams &p, float *dgamma, float *dbeta
         }
     }
     if (st != GRIM_OK || !p.part) return st;
-    const int64_t grid = (2 * p.C + 63) / 64;
-    if (grid > kMaxGrid) return GRIM_ERR_SHAPE;
-    hipLaunchKernelGGL(norm_back_join, dim3((unsigned)grid), dim3(1024), 0, stream, p.part, p.N > 0 ? groups : 0, p.C, dgamma, dbeta);
-    return launched();
+    return join_columns(p.part, p.N > 0 ? groups : 0, p.C, dgamma, p.C, dbeta, stream);
 }
 
 }  // namespace lm

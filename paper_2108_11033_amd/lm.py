@@ -26,6 +26,11 @@ ARGTYPES = {
     "grim_layer_norm": [_P, _I32, _I64, _P, _P, _F, _I64, _I64, _P, _I64, _P, _P, _P],
     "grim_layer_norm_backward": [_P, _I64, _P, _I64, _I32, _P, _P, _P, _I64, _I64, _P, _I64, _P, _P, _P, _I64, _P],
     "grim_layer_norm_workspace": [_I64, _I64],
+    "grim_glr_states": [_I64, _I64],
+    "grim_glr_workspace": [_I64, _I64],
+    "grim_glr_sequence": [_P, _I32, _I64, _P, _P, _P, _I32, _I64, _I64, _P, _I64, _P, _P, _P, _I64, _P],
+    "grim_glr_sequence_backward": [_P, _I32, _I64, _P, _P, _P, _I32, _I64, _I64, _P, _P, _I64, _P, _P, _I64, _P, _P, _P, _I64, _P],
+    "grim_glr_step": [_P, _I64, _P, _P, _I64, _P, _I64, _P, _I32, _I64, _I64, _I32, _P],
 }
 
 
@@ -64,3 +69,37 @@ def layer_norm_backward(dy, lddy: int, x, ldx: int, dtype, gamma, mean, rstd, N:
     _check(_lib().grim_layer_norm_backward(_addr(dy), lddy, _addr(x), ldx, _DT_CODE[dtype], _addr(gamma), _addr(mean), _addr(rstd),
                                            N, C, _addr(dx), lddx, _addr(dgamma), _addr(dbeta), ws, room, _stream(stream)),
            "grim_layer_norm_backward")
+
+
+def glr_states(N: int, H: int) -> int:
+    """grim_glr_states: bytes of the states that glr_sequence leaves for its backward pass."""
+    return int(_lib().grim_glr_states(N, H))
+
+
+def glr_workspace(N: int, H: int) -> int:
+    """grim_glr_workspace: bytes that either direction of glr_sequence needs."""
+    return int(_lib().grim_glr_workspace(N, H))
+
+
+def glr_sequence(gates, dtype, ldg: int, bias, h0, seq_start, nseq: int, N: int, H: int, y, ldy: int, h_last, states, workspace,
+                 stream=None):
+    """grim_glr_sequence: enqueue the gated linear recurrence over N packed rows of gates [forget | candidate | output].
+    `states` (a buffer of glr_states bytes, or None) is what the backward pass reads."""
+    ws, room = _room(workspace)
+    _check(_lib().grim_glr_sequence(_addr(gates), _DT_CODE[dtype], ldg, _addr(bias), _addr(h0), _addr(seq_start), nseq, N, H, _addr(y),
+                                    ldy, _addr(h_last), _addr(states), ws, room, _stream(stream)), "grim_glr_sequence")
+
+
+def glr_sequence_backward(gates, dtype, ldg: int, bias, h0, seq_start, nseq: int, N: int, H: int, states, dy, lddy: int, dh_last,
+                          dgates, lddg: int, dbias, dh0, workspace, stream=None):
+    """grim_glr_sequence_backward: enqueue the gradients of the gates, the bias and the states before the first tokens."""
+    ws, room = _room(workspace)
+    _check(_lib().grim_glr_sequence_backward(_addr(gates), _DT_CODE[dtype], ldg, _addr(bias), _addr(h0), _addr(seq_start), nseq, N, H,
+                                             _addr(states), _addr(dy), lddy, _addr(dh_last), _addr(dgates), lddg, _addr(dbias),
+                                             _addr(dh0), ws, room, _stream(stream)), "grim_glr_sequence_backward")
+
+
+def glr_step(gates, ldg: int, bias, h, ldh: int, h_new, ldh_new: int, y, dtype, ldy: int, H: int, batch: int, stream=None):
+    """grim_glr_step: one token for `batch` callers; gates 3H x batch and states H x batch in fp32, as grim_lstm_cell has them."""
+    _check(_lib().grim_glr_step(_addr(gates), ldg, _addr(bias), _addr(h), ldh, _addr(h_new), ldh_new, _addr(y), _DT_CODE[dtype], ldy,
+                                H, batch, _stream(stream)), "grim_glr_step")
