@@ -9,5 +9,6 @@ from .binding import (  # noqa: F401
     F32, F16, BF16, STATUS_NAMES,
 )
 from .lm import (  # noqa: F401
-    glr_sequence, glr_sequence_backward, glr_states, glr_step, glr_workspace, layer_norm, layer_norm_backward, layer_norm_workspace,
+    distill_topk, distill_topk_workspace, glr_sequence, glr_sequence_backward, glr_states, glr_step, glr_workspace, layer_norm,
+    layer_norm_backward, layer_norm_workspace, logit_rules,
 )

@@ -14,44 +14,77 @@ using f16 = _Float16;
 constexpr int kComputeUnits = 256;
 constexpr int kMaxGrid = 0x7fffffff;
 
-// V elements of T as one value whose alignment is the element's: rows may start anywhere (odd widths, leading dimensions and
-// offsets), and the hardware takes a 16-byte access at any address, so rows that are not aligned run on the same kernels.
+// V elements of T as they lie in memory, in words: what waits in registers keeps two 16-bit elements in each.  They are read
+// and written at any address that an element may have: rows may start anywhere (odd widths, leading dimensions and offsets), the
+// hardware takes a 16-byte access at any address, and so rows that are not aligned run on the same kernels.
 template <typename T, int V>
-struct __attribute__((packed, aligned(sizeof(T)))) Pack {
-    T at[V];
+struct Pack {
+    static constexpr int W = (V * (int)sizeof(T) + 3) / 4;
+    uint32_t w[W];
 };
 
-template <int V, typename T>
-__device__ __forceinline__ void unpack(const Pack<T, V> &p, float (&out)[V]) {
-#pragma unroll
-    for (int j = 0; j < V; ++j) out[j] = (float)p.at[j];
-}
+template <typename T, int V>
+struct __attribute__((packed, aligned(sizeof(T)), may_alias)) Loose {
+    uint32_t w[Pack<T, V>::W];
+};
 
 template <int V, typename T>
 __device__ __forceinline__ Pack<T, V> load(const T *p) {
     Pack<T, V> r;
-    __builtin_memcpy(&r, p, sizeof(r));
+    if constexpr (V * sizeof(T) >= 4) {
+        const Loose<T, V> l = *reinterpret_cast<const Loose<T, V> *>(p);
+#pragma unroll
+        for (int i = 0; i < r.W; ++i) r.w[i] = l.w[i];
+    } else {
+        r.w[0] = __builtin_bit_cast(uint16_t, *p);
+    }
     return r;
 }
 
 template <int V, typename T>
-__device__ __forceinline__ void store(T *p, const float (&v)[V]) {
-    Pack<T, V> r;
-#pragma unroll
-    for (int j = 0; j < V; ++j) r.at[j] = (T)v[j];       // one rounding, to nearest even
-    __builtin_memcpy(p, &r, sizeof(r));
+__device__ __forceinline__ float element(const Pack<T, V> &p, int j) {
+    if constexpr (sizeof(T) == 4) return __builtin_bit_cast(float, p.w[j]);
+    const uint32_t w = p.w[j / 2];
+    if constexpr (__is_same(T, bf16)) return __builtin_bit_cast(float, j % 2 ? w & 0xffff0000u : w << 16);
+    return (float)__builtin_bit_cast(f16, (uint16_t)(j % 2 ? w >> 16 : w));
 }
 
-// The same values as far as the program goes, but not for the compiler: what was unpacked before is unpacked again after,
+template <int V, typename T>
+__device__ __forceinline__ void unpack(const Pack<T, V> &p, float (&out)[V]) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) out[j] = element(p, j);
+}
+
+template <int V, typename T>
+__device__ __forceinline__ void put(Pack<T, V> &p, int j, T v) {
+    if constexpr (sizeof(T) == 4) p.w[j] = __builtin_bit_cast(uint32_t, v);
+    else {
+        const uint32_t b = __builtin_bit_cast(uint16_t, v);
+        p.w[j / 2] = j % 2 ? (p.w[j / 2] & 0xffffu) | b << 16 : (p.w[j / 2] & 0xffff0000u) | b;
+    }
+}
+
+// One rounding, to nearest even.
+template <int V, typename T>
+__device__ __forceinline__ void store(T *p, const float (&v)[V]) {
+    if constexpr (V * sizeof(T) >= 4) {
+        T t[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) t[j] = (T)v[j];
+        Loose<T, V> l;
+        __builtin_memcpy(&l, t, sizeof(l));
+        *reinterpret_cast<Loose<T, V> *>(p) = l;
+    } else {
+        *p = (T)v[0];
+    }
+}
+
+// The same words as far as the program goes, but not for the compiler: what was unpacked before is unpacked again after,
 // instead of being held in twice the registers meanwhile.
 template <typename T, int V>
 __device__ __forceinline__ void forget(Pack<T, V> &p) {
-    constexpr int n = (int)(sizeof(p) + 3) / 4;
-    unsigned int w[n] = {};
-    __builtin_memcpy(w, &p, sizeof(p));
 #pragma unroll
-    for (int i = 0; i < n; ++i) asm volatile("" : "+v"(w[i]));
-    __builtin_memcpy(&p, w, sizeof(p));
+    for (int i = 0; i < p.W; ++i) asm volatile("" : "+v"(p.w[i]));
 }
 
 __device__ __forceinline__ float wave_sum(float v) {

@@ -1,0 +1,429 @@
+// Distillation from a teacher's top logits: loss and gradient in one pass over the student's logits.
+//
+//     p = softmax(top / tau) over the listed entries    q = softmax(z / tau) over all V
+//     loss = w tau^2 sum_i p_i (log p_i - log q[id_i])    dz_j = w tau (q_j - sum of p_i with id_i = j)
+//
+// Bound by memory: z read once, dz written once.  Where the rows fill the compute units a workgroup keeps its row in registers
+// between the maximum, the sum and the gradient.  With few rows, or rows that do not fit, a row is cut into slices: a first launch
+// leaves every slice's maximum, sum and share of the loss, and the second joins them and writes the gradient from a second
+// read of z, which a few rows leave in the caches.  Exponents are taken of differences from the maximum, (z - max) / tau, so that
+// masks of the type's lowest value do not overflow on the way.
+#include "lm_common.hpp"
+
+namespace grim {
+namespace lm {
+
+constexpr int kMostEntries = 1024, kTable = 2048;
+constexpr float kLn2 = 0.69314718055994530942f;
+
+struct DistillParams {
+    const void *z;
+    const float *top, *weight;
+    const int32_t *ids;
+    float *loss;
+    void *dz;
+    float *part;                // [row][slice][maximum, sum, share of the loss, probability listed in it]
+    int64_t ldz, lddz, ldt, N, V;
+    int32_t k, slices;
+    float tau, scale;           // scale = log2(e) / tau
+};
+
+// The teacher's side of a row in LDS: words (-1: absent), probabilities, the sums of the probabilities of entries that list the
+// same word, and log2 p = (top - best) scale - log2(total) kept as its first part.
+struct Entries {
+    int32_t id[kMostEntries];
+    float p[kMostEntries], sum[kMostEntries], log[kMostEntries];
+    uint16_t table[kTable];
+    float total;                // sum of exponentials (0: nothing is listed; NaN: a listed logit is)
+};
+
+// Formed by one wave.
+__device__ __forceinline__ void teacher(const DistillParams &p, int64_t n, Entries &e) {
+    const int lane = threadIdx.x & 63;
+    const float *t = p.top + n * p.ldt;
+    const int32_t *ids = p.ids + n * p.ldt;
+    float m = -INFINITY;
+    bool nan = false;
+    for (int i = lane; i < p.k; i += 64) {
+        const int32_t id = ids[i];
+        const bool there = id >= 0 && id < p.V;
+        const float v = there ? t[i] : -INFINITY;
+        e.id[i] = there ? id : -1;
+        e.log[i] = v;
+        nan |= v != v;
+        m = fmaxf(m, v);
+    }
+    m = wave_max(m);
+    if (__any(nan)) m = NAN;
+    float s = 0.f;
+    for (int i = lane; i < p.k; i += 64) {
+        const float v = e.log[i];
+        const float d = v == -INFINITY ? -INFINITY : (v - m) * p.scale;
+        const float x = v == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(d);
+        e.log[i] = d;
+        e.p[i] = x;
+        s += x;
+    }
+    s = wave_sum(s);
+    if (lane == 0) e.total = s;
+    // Words listed twice.  Every entry leaves its number in a table at its word's hash; one that finds another's there
+    // either lists the same word (both have company) or has to look.  Those few are looked up by the whole wave.
+    const float r = 1.f / s;
+    for (int i = lane; i < p.k; i += 64) {
+        const float x = s > 0.f ? e.p[i] * r : s;                        // (s: 0, or NaN)
+        e.p[i] = x;
+        e.sum[i] = x;
+        if (e.id[i] >= 0) e.table[e.id[i] & (kTable - 1)] = (uint16_t)i;
+    }
+    __builtin_amdgcn_wave_barrier();
+    __threadfence_block();
+    for (int i0 = 0; i0 < p.k; i0 += 64) {
+        const int i = i0 + lane;
+        const int32_t id = i < p.k ? e.id[i] : -1;
+        const int other = id >= 0 ? e.table[id & (kTable - 1)] : i;
+        unsigned long long look = __ballot(id >= 0 && other != i);
+        while (look) {
+            const int l = __builtin_ctzll(look);
+            look &= look - 1;
+            const int32_t word = __shfl(id, l, 64);
+            float sum = 0.f;
+            for (int j0 = 0; j0 < p.k; j0 += 64) {
+                const int j = j0 + lane;
+                const float x = j < p.k && e.id[j] == word ? e.p[j] : 0.f;
+                sum += wave_sum(x);
+            }
+            for (int j = lane; j < p.k; j += 64)
+                if (e.id[j] == word) e.sum[j] = sum;
+        }
+    }
+}
+
+template <typename T>
+constexpr int piece() { return 16 / (int)sizeof(T); }
+
+template <typename T>
+__device__ __forceinline__ void zero_row(T *dz, int64_t lo, int64_t hi) {
+    constexpr int V = piece<T>();
+    const float none[V] = {};
+    for (int64_t c = lo + (int64_t)threadIdx.x * V; c < hi; c += (int64_t)blockDim.x * V) {
+        if (c + V <= hi) store(dz + c, none);
+        else
+            for (int j = 0; c + j < hi; ++j) dz[c + j] = (T)0.f;
+    }
+}
+
+// weight tau (q_j - p_j) at the listed words, over what was streamed there.  zl: z at the entries' words.
+template <typename T>
+__device__ __forceinline__ void write_listed(const DistillParams &p, const Entries &e, T *dz, const float *zl, float peak, float rsum,
+                                             float factor, int64_t lo, int64_t hi) {
+    for (int i = threadIdx.x; i < p.k; i += blockDim.x) {
+        const int32_t id = e.id[i];
+        if (id >= lo && id < hi) dz[id] = (T)(factor * (__builtin_amdgcn_exp2f((zl[i] - peak) * p.scale) * rsum - e.sum[i]));
+    }
+}
+
+// -------------------------------------------------------------------------------------------------- one workgroup per row
+// W waves, at most PER pieces of 16 bytes a thread: pieces k < full are whole for all threads, piece `full` for some, the
+// others are empty.  A piece that reaches past the row is moved back to end with it; what it shares counts in the other.
+template <typename T, int W, int PER>
+__global__ void __launch_bounds__(64 * W) distill_rows(DistillParams p) {
+    constexpr int V = piece<T>(), TPR = 64 * W;
+    __shared__ Entries e;
+    __shared__ float listed[kMostEntries];                  // z at the listed words
+    __shared__ float room[2][W];
+    const int64_t n = blockIdx.x;
+    const T *z = static_cast<const T *>(p.z) + n * p.ldz;
+    T *dz = p.dz ? static_cast<T *>(p.dz) + n * p.lddz : nullptr;
+    const float weight = p.weight ? p.weight[n] : 1.f;
+    if (weight == 0.f) {
+        if (threadIdx.x == 0) p.loss[n] = 0.f;
+        if (dz) zero_row(dz, 0, p.V);
+        return;
+    }
+    const int full = (int)(p.V / (TPR * V));
+    const int mine = full * TPR * V + (int)threadIdx.x * V;   // where piece `full` would start
+    const bool some = mine < p.V;
+    const int tail = (int)min((int64_t)mine, p.V - V), first = mine - tail;
+    Pack<T, V> raw[PER];
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        if (k < full) raw[k] = load<V>(z + k * TPR * V + (int)threadIdx.x * V);
+        else if (k == full && some) raw[k] = load<V>(z + tail);
+    }
+    if (threadIdx.x < 64) {
+        teacher(p, n, e);
+        for (int i = threadIdx.x; i < p.k; i += 64) listed[i] = e.id[i] >= 0 ? (float)z[e.id[i]] : 0.f;
+    }
+    // f(k, j, value) over the thread's own elements
+    auto own = [&](auto f) {
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            if (k > full || (k == full && !some)) continue;
+            float v[V];
+            forget(raw[k]);
+            unpack(raw[k], v);
+            if (k < full) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) f(v[j]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    if (j >= first) f(v[j]);
+            }
+        }
+    };
+    float peak = -INFINITY, sum = 0.f;
+    own([&](float v) { peak = fmaxf(peak, v); });
+    peak = group_max<W>(peak, room[0]);
+    own([&](float v) { sum += __builtin_amdgcn_exp2f((v - peak) * p.scale); });
+    sum = group_sum<W>(sum, room[1]);                       // (its barrier also shows the teacher's side to all)
+    if (W == 1) __syncthreads();
+    const float total = e.total;
+    if (total == 0.f) {
+        if (threadIdx.x == 0) p.loss[n] = 0.f;
+        if (dz) zero_row(dz, 0, p.V);
+        return;
+    }
+    const float rsum = 1.f / sum;
+    const float factor = weight * p.tau * (total / total);  // (a NaN of the teacher reaches the whole row)
+    if (dz) {
+        const float slope = factor * rsum;
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            if (k > full || (k == full && !some)) continue;
+            float v[V], out[V];
+            forget(raw[k]);
+            unpack(raw[k], v);
+#pragma unroll
+            for (int j = 0; j < V; ++j) out[j] = slope * __builtin_amdgcn_exp2f((v[j] - peak) * p.scale);
+            store(dz + (k < full ? k * TPR * V + (int)threadIdx.x * V : tail), out);
+        }
+        __syncthreads();                                    // the listed words' places were written by other threads
+        write_listed(p, e, dz, listed, peak, rsum, factor, 0, p.V);
+    }
+    if (threadIdx.x < 64) {
+        const float lse = log2f(sum), ltotal = log2f(total);
+        float loss = 0.f;
+        for (int i = threadIdx.x; i < p.k; i += 64)
+            if (e.p[i] != 0.f) loss += e.p[i] * ((e.log[i] - ltotal) - ((listed[i] - peak) * p.scale - lse));
+        loss = wave_sum(loss);
+        if (threadIdx.x == 0) p.loss[n] = weight * p.tau * p.tau * (kLn2 * loss);
+    }
+}
+
+// -------------------------------------------------------------------------------------------------- slices of rows
+constexpr int kSliceWaves = 4, kSlicePer = 4;               // a slice: 4 pieces of 16 bytes a thread
+
+template <typename T>
+constexpr int64_t slice_elements() { return 64 * kSliceWaves * kSlicePer * piece<T>(); }
+
+// The pieces of a slice [lo, hi), element by element at its end.
+template <typename T>
+struct Slice {
+    static constexpr int V = piece<T>();
+    Pack<T, V> raw[kSlicePer];
+    int have[kSlicePer];
+    __device__ __forceinline__ static int64_t at(int64_t lo, int k) { return lo + (int64_t)(k * 64 * kSliceWaves + threadIdx.x) * V; }
+    __device__ __forceinline__ Slice(const T *z, int64_t lo, int64_t hi) {
+#pragma unroll
+        for (int k = 0; k < kSlicePer; ++k) {
+            const int64_t c = at(lo, k), left = hi - c;
+            have[k] = left >= V ? V : left > 0 ? (int)left : 0;
+            if (have[k] == V) raw[k] = load<V>(z + c);
+            else
+#pragma unroll
+                for (int j = 0; j < V; ++j) put(raw[k], j, j < have[k] ? z[c + j] : (T)-INFINITY);
+        }
+    }
+};
+
+template <typename T>
+__global__ void __launch_bounds__(64 * kSliceWaves) distill_slices(DistillParams p) {
+    constexpr int V = piece<T>(), W = kSliceWaves;
+    __shared__ Entries e;
+    __shared__ float room[2][W];
+    const int64_t n = blockIdx.x / p.slices, s = blockIdx.x % p.slices;
+    if (p.weight && p.weight[n] == 0.f) return;
+    const T *z = static_cast<const T *>(p.z) + n * p.ldz;
+    const int64_t lo = s * slice_elements<T>(), hi = lo + slice_elements<T>() < p.V ? lo + slice_elements<T>() : p.V;
+    Slice<T> sl(z, lo, hi);
+    if (threadIdx.x < 64) teacher(p, n, e);
+    float peak = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < kSlicePer; ++k) {
+        float v[V];
+        unpack(sl.raw[k], v);
+#pragma unroll
+        for (int j = 0; j < V; ++j) peak = fmaxf(peak, v[j]);
+    }
+    peak = group_max<W>(peak, room[0]);
+    // (a slice of nothing but -infinity has the sum 0; one NaN makes the sum NaN)
+    const float base = peak == -INFINITY ? 0.f : peak;
+#pragma unroll
+    for (int k = 0; k < kSlicePer; ++k) {
+        float v[V];
+        forget(sl.raw[k]);
+        unpack(sl.raw[k], v);
+#pragma unroll
+        for (int j = 0; j < V; ++j) sum += __builtin_amdgcn_exp2f((v[j] - base) * p.scale);
+    }
+    sum = group_sum<W>(sum, room[1]);
+    if (threadIdx.x >= 64) return;
+    // sum of p (log2 p - (z - peak) scale) over the words in this slice, and of p
+    float share = 0.f, there = 0.f;
+    for (int i = threadIdx.x; i < p.k; i += 64) {
+        const int32_t id = e.id[i];
+        if (id >= lo && id < hi && e.p[i] != 0.f) {
+            share += e.p[i] * (e.log[i] - ((float)z[id] - base) * p.scale);
+            there += e.p[i];
+        }
+    }
+    share = wave_sum(share);
+    there = wave_sum(there);
+    if (threadIdx.x == 0) {
+        float *part = p.part + (int64_t)blockIdx.x * 4;
+        part[0] = peak, part[1] = sum, part[2] = share, part[3] = there;
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(64 * kSliceWaves) distill_join(DistillParams p) {
+    constexpr int V = piece<T>();
+    __shared__ Entries e;
+    __shared__ float listed[kMostEntries];
+    __shared__ float joined[2];
+    const int64_t n = blockIdx.x / p.slices, s = blockIdx.x % p.slices;
+    const T *z = static_cast<const T *>(p.z) + n * p.ldz;
+    T *dz = p.dz ? static_cast<T *>(p.dz) + n * p.lddz : nullptr;
+    const int64_t lo = s * slice_elements<T>(), hi = lo + slice_elements<T>() < p.V ? lo + slice_elements<T>() : p.V;
+    const float weight = p.weight ? p.weight[n] : 1.f;
+    if (weight == 0.f) {
+        if (threadIdx.x == 0 && s == 0) p.loss[n] = 0.f;
+        if (dz) zero_row(dz, lo, hi);
+        return;
+    }
+    if (threadIdx.x < 64) {
+        const int lane = threadIdx.x;
+        teacher(p, n, e);
+        // (only of this slice: other slices' places may hold their gradient already, where dz is z)
+        for (int i = lane; i < p.k; i += 64) listed[i] = e.id[i] >= lo && e.id[i] < hi ? (float)z[e.id[i]] : 0.f;
+        const float *part = p.part + n * p.slices * 4;
+        float peak = -INFINITY, sum = 0.f, share = 0.f;
+        for (int i = lane; i < p.slices; i += 64) peak = fmaxf(peak, part[4 * i]);
+        peak = wave_max(peak);
+        for (int i = lane; i < p.slices; i += 64) {
+            const float m = part[4 * i] == -INFINITY ? peak : part[4 * i];
+            sum += part[4 * i + 1] * __builtin_amdgcn_exp2f((m - peak) * p.scale);
+        }
+        sum = wave_sum(sum);
+        if (lane == 0) joined[0] = peak, joined[1] = sum;
+        if (s == 0) {
+            // log2 q = (z - base_i) scale + (base_i - peak) scale - log2 sum
+            const float extra = log2f(sum) - log2f(e.total);
+            for (int i = lane; i < p.slices; i += 64) {
+                const float base = part[4 * i] == -INFINITY ? 0.f : part[4 * i], there = part[4 * i + 3];
+                if (there != 0.f) share += part[4 * i + 2] + there * ((peak - base) * p.scale + extra);
+            }
+            share = wave_sum(share);
+            if (lane == 0) p.loss[n] = e.total == 0.f ? 0.f : weight * p.tau * p.tau * (kLn2 * share);
+        }
+    }
+    if (!dz) return;
+    __syncthreads();
+    const float total = e.total, peak = joined[0], rsum = 1.f / joined[1];
+    if (total == 0.f) {
+        zero_row(dz, lo, hi);
+        return;
+    }
+    const float factor = weight * p.tau * (total / total), slope = factor * rsum;
+    const Slice<T> sl(z, lo, hi);
+#pragma unroll
+    for (int k = 0; k < kSlicePer; ++k) {
+        float v[V], out[V];
+        unpack(sl.raw[k], v);
+#pragma unroll
+        for (int j = 0; j < V; ++j) out[j] = slope * __builtin_amdgcn_exp2f((v[j] - peak) * p.scale);
+        T *to = dz + Slice<T>::at(lo, k);
+        if (sl.have[k] == V) store(to, out);
+        else
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                if (j < sl.have[k]) to[j] = (T)out[j];
+    }
+    __syncthreads();
+    write_listed(p, e, dz, listed, peak, rsum, factor, lo, hi);
+}
+
+// -------------------------------------------------------------------------------------------------- launches
+template <typename T>
+int64_t slices_of(int64_t V) { return (V + slice_elements<T>() - 1) / slice_elements<T>(); }
+
+// A workgroup per row where its registers hold the row: 16 pieces a thread of 16 waves.
+template <typename T>
+bool row_fits(int64_t V) { return V >= piece<T>() && V <= (int64_t)16 * 1024 * piece<T>(); }
+
+template <typename T>
+bool by_rows(int64_t N, int64_t V) { return row_fits<T>(V) && (N >= 128 || slices_of<T>(V) <= 2); }
+
+template <typename T>
+grim_status distill_typed(DistillParams p, hipStream_t stream) {
+    if (by_rows<T>(p.N, p.V)) {
+        if (p.N > kMaxGrid) return GRIM_ERR_SHAPE;
+        const dim3 g((unsigned)p.N);
+        const int64_t pieces = (p.V + piece<T>() - 1) / piece<T>();
+        if (pieces <= 256) hipLaunchKernelGGL((distill_rows<T, 4, 1>), g, dim3(256), 0, stream, p);
+        else if (pieces <= 512) hipLaunchKernelGGL((distill_rows<T, 4, 2>), g, dim3(256), 0, stream, p);
+        else if (pieces <= 1024) hipLaunchKernelGGL((distill_rows<T, 4, 4>), g, dim3(256), 0, stream, p);
+        else if (pieces <= 2048) hipLaunchKernelGGL((distill_rows<T, 8, 4>), g, dim3(512), 0, stream, p);
+        else if (pieces <= 4096) hipLaunchKernelGGL((distill_rows<T, 8, 8>), g, dim3(512), 0, stream, p);
+        else if (pieces <= 8192) hipLaunchKernelGGL((distill_rows<T, 8, 16>), g, dim3(512), 0, stream, p);
+        else hipLaunchKernelGGL((distill_rows<T, 16, 16>), g, dim3(1024), 0, stream, p);
+        return launched();
+    }
+    p.slices = (int32_t)slices_of<T>(p.V);
+    if (p.N > kMaxGrid / p.slices) return GRIM_ERR_SHAPE;
+    const dim3 g((unsigned)(p.N * p.slices)), b(64 * kSliceWaves);
+    hipLaunchKernelGGL(distill_slices<T>, g, b, 0, stream, p);
+    const grim_status st = launched();
+    if (st != GRIM_OK) return st;
+    hipLaunchKernelGGL(distill_join<T>, g, b, 0, stream, p);
+    return launched();
+}
+
+}  // namespace lm
+}  // namespace grim
+
+extern "C" {
+
+int64_t grim_distill_topk_workspace(int64_t N, int64_t V) {
+    using namespace grim::lm;
+    if (N < 0 || V < 1 || V >= (int64_t)1 << 31) return 0;
+    // (whichever type comes: of fp32 a slice holds the fewest elements)
+    int64_t bytes = 16;
+    if (!by_rows<float>(N, V)) bytes += N * slices_of<float>(V) * 16;
+    else if (!by_rows<f16>(N, V)) bytes += N * slices_of<f16>(V) * 16;
+    return bytes;
+}
+
+grim_status grim_distill_topk(const void *z_dev, grim_dtype dt, int64_t ldz, const float *top_logits_dev,
+                              const int32_t *top_ids_dev, int32_t k, int64_t ldt, float temperature,
+                              const float *weight_dev, int64_t N, int64_t V, float *loss_dev, void *dz_dev, int64_t lddz,
+                              void *workspace, int64_t workspace_bytes, void *hip_stream) {
+    using namespace grim::lm;
+    if (!known(dt)) return GRIM_ERR_DTYPE;
+    if (N < 0 || V < 1 || V >= (int64_t)1 << 31 || k < 1 || ldz < V || ldt < k || (dz_dev && lddz < V) || !fits(N, ldz) ||
+        !fits(N, ldt) || (dz_dev && !fits(N, lddz)) || !(temperature > 0.f) || temperature > 3.4e38f)
+        return GRIM_ERR_SHAPE;
+    if (k > kMostEntries) return GRIM_ERR_UNSUPPORTED;
+    if (N == 0) return GRIM_OK;
+    if (!z_dev || !top_logits_dev || !top_ids_dev || !loss_dev || !workspace) return GRIM_ERR_NULL;
+    if (workspace_bytes < grim_distill_topk_workspace(N, V)) return GRIM_ERR_SHAPE;
+    const DistillParams p{z_dev, top_logits_dev, weight_dev, top_ids_dev, loss_dev, dz_dev, static_cast<float *>(workspace),
+                          ldz, lddz, ldt, N, V, k, 0, temperature, 1.44269504088896340736f / temperature};
+    const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    return dt == GRIM_F32   ? distill_typed<float>(p, stream)
+           : dt == GRIM_F16 ? distill_typed<f16>(p, stream)
+                            : distill_typed<bf16>(p, stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,193 @@
+// Rules applied to the logits of a served step: penalties for words of the history, biases, a grammar's mask.
+//
+//     z -> (z > 0 ? z / repetition : z repetition) - frequency count - presence      where count > 0
+//     z -> z + bias    z -> -infinity where the word is not allowed
+//
+// One pass over the logits, bound by memory or, for a caller or two, by the launch.  A workgroup takes a tile of words and
+// callers, counts the histories' words that fall into it in LDS (whole-number atomics: the order cannot matter), and then
+// transforms the tile.  Every tile reads its callers' whole histories again (from L2), which costs less than a table of counts in memory, cleared,
+// filled and read by three launches.
+#include "lm_common.hpp"
+
+namespace grim {
+namespace lm {
+
+constexpr int kMostBias = 1024;
+
+struct RuleParams {
+    const void *z;
+    void *out;
+    int64_t ldz, ldo, V;
+    int32_t batch;
+    grim_logit_rules r;
+};
+
+struct CallerRules {
+    float repetition, frequency, presence;
+    __device__ __forceinline__ CallerRules(const grim_logit_rules &r, int64_t b)
+        : repetition(r.repetition ? r.repetition[b] : 1.f), frequency(r.frequency ? r.frequency[b] : 0.f),
+          presence(r.presence ? r.presence[b] : 0.f) {}
+    __device__ __forceinline__ float apply(float z, uint32_t count, float bias, bool allowed) const {
+        if (count) z = (z > 0.f ? z / repetition : z * repetition) - frequency * (float)count - presence;
+        return allowed ? z + bias : -INFINITY;
+    }
+};
+
+// Words lo .. hi - 1 of caller b into count[(word - lo) << shift] and bias[...]; the whole workgroup, with barriers.
+__device__ __forceinline__ void gather_rules(const grim_logit_rules &r, int64_t b, int64_t lo, int64_t hi, uint32_t *count, float *bias,
+                                             int shift, int32_t *staged) {
+    const int span = (int)(hi - lo), first = (int)lo;
+    if (r.history && r.max_history > 0) {
+        const int32_t *h = r.history + b * r.ld_history;
+        const int len = r.history_len ? min(max(r.history_len[b], 0), r.max_history) : r.max_history;
+        const auto tally = [&](int32_t id) {
+            // (a word below lo wraps around to a large number; words of 2^31 and more do not exist)
+            const uint32_t at = (uint32_t)id - (uint32_t)first;
+            if (id >= 0 && at < (uint32_t)span) atomicAdd(&count[at << shift], 1u);
+        };
+        int i = threadIdx.x * 4;
+        for (; i + 4 <= len; i += blockDim.x * 4) {
+            const Pack<int32_t, 4> ids = load<4>(h + i);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) tally((int32_t)ids.w[j]);
+        }
+        for (; i < len; ++i) tally(h[i]);                       // the last, short piece is one thread's
+    }
+    if (!r.bias_ids || !r.bias_values || r.nbias <= 0) return;
+    const int32_t *ids = r.bias_ids + b * r.ld_bias;
+    const float *values = r.bias_values + b * r.ld_bias;
+    for (int i = threadIdx.x; i < r.nbias; i += blockDim.x) staged[i] = ids[i];
+    __syncthreads();
+    for (int i = threadIdx.x; i < r.nbias; i += blockDim.x) {
+        const int32_t id = staged[i];
+        const uint32_t at = (uint32_t)id - (uint32_t)first;
+        if (id < 0 || at >= (uint32_t)span) continue;
+        // the first entry of a word adds up all of them, in the list's order
+        bool earlier = false;
+        for (int j = 0; j < i; ++j) earlier |= staged[j] == id;
+        if (earlier) continue;
+        float sum = values[i];
+        for (int j = i + 1; j < r.nbias; ++j)
+            if (staged[j] == id) sum += values[j];
+        bias[at << shift] = sum;
+    }
+    __syncthreads();                                            // (staged is free again)
+}
+
+// A row per caller: TILE words of one caller.
+template <typename T, int TILE, int THREADS>
+__global__ void __launch_bounds__(THREADS) rules_rows(RuleParams p, int tiles) {
+    constexpr int V = 16 / (int)sizeof(T), PER = TILE / (THREADS * V);
+    __shared__ __attribute__((aligned(16))) uint32_t count[TILE];
+    __shared__ __attribute__((aligned(16))) float bias[TILE];
+    __shared__ int32_t staged[kMostBias];
+    const int64_t b = blockIdx.x / tiles, lo = (int64_t)(blockIdx.x % tiles) * TILE;
+    const int64_t hi = lo + TILE < p.V ? lo + TILE : p.V;
+    const T *z = static_cast<const T *>(p.z) + b * p.ldz + lo;
+    T *out = static_cast<T *>(p.out) + b * p.ldo + lo;
+    const int span = (int)(hi - lo);
+    Pack<T, V> raw[PER];
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        const int c = (k * THREADS + threadIdx.x) * V;
+        if (c + V <= span) raw[k] = load<V>(z + c);
+        else
+#pragma unroll
+            for (int j = 0; j < V; ++j) put(raw[k], j, c + j < span ? z[c + j] : (T)0.f);
+    }
+    for (int i = threadIdx.x; i < TILE; i += THREADS) count[i] = 0, bias[i] = 0.f;
+    __syncthreads();
+    gather_rules(p.r, b, lo, hi, count, bias, 0, staged);
+    __syncthreads();
+    const CallerRules rules(p.r, b);
+    const uint32_t *allowed = p.r.allowed ? p.r.allowed + b * p.r.ld_allowed + lo / 32 : nullptr;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        const int c = (k * THREADS + threadIdx.x) * V;
+        if (c >= span) continue;
+        const uint32_t bits = allowed ? allowed[c / 32] >> (c % 32) : 0xffffffffu;
+        float v[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[j] = rules.apply(element(raw[k], j), count[c + j], bias[c + j], bits >> j & 1);
+        if (c + V <= span) store(out + c, v);
+        else
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                if (c + j < span) out[c + j] = (T)v[j];
+    }
+}
+
+// A column per caller: TILE >> shift words of up to 1 << shift callers.
+template <typename T, int TILE, int THREADS>
+__global__ void __launch_bounds__(THREADS) rules_columns(RuleParams p, int tiles, int shift) {
+    __shared__ uint32_t count[TILE];
+    __shared__ float bias[TILE];
+    __shared__ int32_t staged[kMostBias];
+    const int words = TILE >> shift;
+    const int64_t b0 = (int64_t)(blockIdx.x / tiles) << shift, lo = (int64_t)(blockIdx.x % tiles) * words;
+    const int64_t hi = lo + words < p.V ? lo + words : p.V;
+    const int callers = (int)min((int64_t)1 << shift, p.batch - b0);
+    for (int i = threadIdx.x; i < TILE; i += THREADS) count[i] = 0, bias[i] = 0.f;
+    __syncthreads();
+    for (int b = 0; b < callers; ++b) gather_rules(p.r, b0 + b, lo, hi, count + b, bias + b, shift, staged);
+    __syncthreads();
+    const int b = threadIdx.x & ((1 << shift) - 1);             // (THREADS is a multiple of 1 << shift: a thread keeps its caller)
+    if (b >= callers) return;
+    const CallerRules rules(p.r, b0 + b);
+    const uint32_t *allowed = p.r.allowed ? p.r.allowed + (b0 + b) * p.r.ld_allowed : nullptr;
+    const T *z = static_cast<const T *>(p.z) + b0 + b;
+    T *out = static_cast<T *>(p.out) + b0 + b;
+#pragma unroll 4
+    for (int i = threadIdx.x; i < TILE; i += THREADS) {
+        const int64_t word = lo + (i >> shift);
+        if (word >= hi) break;
+        const bool may = !allowed || (allowed[word / 32] >> (word % 32) & 1);
+        out[word * p.ldo] = (T)rules.apply((float)z[word * p.ldz], count[i], bias[i], may);
+    }
+}
+
+template <typename T, int TILE, int THREADS>
+grim_status rules_launch(const RuleParams &p, bool columns, hipStream_t stream) {
+    int shift = 0;
+    if (columns)
+        while (shift < 3 && (1 << shift) < p.batch) ++shift;    // up to 8 callers: 16 or 32 bytes of a row
+    const int64_t words = TILE >> shift, tiles = (p.V + words - 1) / words;
+    const int64_t grid = tiles * ((p.batch + (1 << shift) - 1) >> shift);
+    if (grid > kMaxGrid) return GRIM_ERR_SHAPE;
+    if (columns) hipLaunchKernelGGL((rules_columns<T, TILE, THREADS>), dim3((unsigned)grid), dim3(THREADS), 0, stream, p, (int)tiles, shift);
+    else hipLaunchKernelGGL((rules_rows<T, TILE, THREADS>), dim3((unsigned)grid), dim3(THREADS), 0, stream, p, (int)tiles);
+    return launched();
+}
+
+// Tiles of 4096 words and callers; of 2048 where those would leave compute units without one.
+template <typename T>
+grim_status rules_typed(const RuleParams &p, bool columns, hipStream_t stream) {
+    return p.V * p.batch >= (int64_t)4096 * kComputeUnits ? rules_launch<T, 4096, 512>(p, columns, stream)
+                                                          : rules_launch<T, 2048, 256>(p, columns, stream);
+}
+
+}  // namespace lm
+}  // namespace grim
+
+extern "C" grim_status grim_apply_logit_rules(const void *z_dev, grim_dtype dt, int32_t columns, int64_t ldz, int64_t V, int32_t batch,
+                                              const grim_logit_rules *rules, void *out_dev, int64_t ldo, void *hip_stream) {
+    using namespace grim::lm;
+    if (!rules) return GRIM_ERR_NULL;
+    if (!known(dt)) return GRIM_ERR_DTYPE;
+    if (V < 1 || V >= (int64_t)1 << 31 || batch < 0 || rules->max_history < 0 || rules->max_history > 1 << 30 ||
+        rules->nbias < 0) return GRIM_ERR_SHAPE;
+    const int64_t width = columns ? batch : V, rows = columns ? V : batch;
+    if (ldz < width || ldo < width || !fits(rows, ldz) || !fits(rows, ldo)) return GRIM_ERR_SHAPE;
+    if (rules->history && (rules->ld_history < rules->max_history || !fits(batch, rules->ld_history))) return GRIM_ERR_SHAPE;
+    if (rules->nbias > 0 && (rules->ld_bias < rules->nbias || !fits(batch, rules->ld_bias))) return GRIM_ERR_SHAPE;
+    if (rules->allowed && (rules->ld_allowed < (V + 31) / 32 || !fits(batch, rules->ld_allowed))) return GRIM_ERR_SHAPE;
+    if (rules->nbias > kMostBias) return GRIM_ERR_UNSUPPORTED;
+    if (rules->nbias > 0 && (!rules->bias_ids || !rules->bias_values)) return GRIM_ERR_NULL;
+    if (batch == 0) return GRIM_OK;
+    if (!z_dev || !out_dev) return GRIM_ERR_NULL;
+    const RuleParams p{z_dev, out_dev, ldz, ldo, V, batch, *rules};
+    const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    return dt == GRIM_F32   ? rules_typed<float>(p, columns != 0, stream)
+           : dt == GRIM_F16 ? rules_typed<f16>(p, columns != 0, stream)
+                            : rules_typed<bf16>(p, columns != 0, stream);
+}

@@ -31,6 +31,9 @@ ARGTYPES = {
     "grim_glr_sequence": [_P, _I32, _I64, _P, _P, _P, _I32, _I64, _I64, _P, _I64, _P, _P, _P, _I64, _P],
     "grim_glr_sequence_backward": [_P, _I32, _I64, _P, _P, _P, _I32, _I64, _I64, _P, _P, _I64, _P, _P, _I64, _P, _P, _P, _I64, _P],
     "grim_glr_step": [_P, _I64, _P, _P, _I64, _P, _I64, _P, _I32, _I64, _I64, _I32, _P],
+    "grim_distill_topk_workspace": [_I64, _I64],
+    "grim_distill_topk": [_P, _I32, _I64, _P, _P, _I32, _I64, _F, _P, _I64, _I64, _P, _P, _I64, _P, _I64, _P],
+    "grim_apply_logit_rules": [_P, _I32, _I32, _I64, _I64, _I32, ctypes.POINTER(LogitRules), _P, _I64, _P],
 }
 
 
@@ -103,3 +106,27 @@ def glr_step(gates, ldg: int, bias, h, ldh: int, h_new, ldh_new: int, y, dtype, 
     """grim_glr_step: one token for `batch` callers; gates 3H x batch and states H x batch in fp32, as grim_lstm_cell has them."""
     _check(_lib().grim_glr_step(_addr(gates), ldg, _addr(bias), _addr(h), ldh, _addr(h_new), ldh_new, _addr(y), _DT_CODE[dtype], ldy,
                                 H, batch, _stream(stream)), "grim_glr_step")
+
+
+def distill_topk_workspace(N: int, V: int) -> int:
+    """grim_distill_topk_workspace: bytes that distill_topk needs."""
+    return int(_lib().grim_distill_topk_workspace(N, V))
+
+
+def distill_topk(z, dtype, ldz: int, top_logits, top_ids, k: int, ldt: int, temperature: float, weight, N: int, V: int, loss, dz,
+                 lddz: int, workspace, stream=None):
+    """grim_distill_topk: enqueue every row's distillation loss and (dz not None) the gradient of their sum."""
+    ws, room = _room(workspace)
+    _check(_lib().grim_distill_topk(_addr(z), _DT_CODE[dtype], ldz, _addr(top_logits), _addr(top_ids), k, ldt, temperature,
+                                    _addr(weight), N, V, _addr(loss), _addr(dz), lddz, ws, room, _stream(stream)),
+           "grim_distill_topk")
+
+
+def logit_rules(z, dtype, ldz: int, V: int, batch: int, out, ldo: int, *, columns: bool = False, history=None, ld_history: int = 0,
+                max_history: int = 0, history_len=None, repetition=None, frequency=None, presence=None, bias_ids=None,
+                bias_values=None, nbias: int = 0, ld_bias: int = 0, allowed=None, ld_allowed: int = 0, stream=None):
+    """grim_apply_logit_rules: enqueue repetition, frequency and presence penalties, biases and the grammar's mask."""
+    rules = LogitRules(_addr(history), _addr(history_len), ld_history, max_history, nbias, _addr(repetition), _addr(frequency),
+                       _addr(presence), _addr(bias_ids), _addr(bias_values), ld_bias, _addr(allowed), ld_allowed)
+    _check(_lib().grim_apply_logit_rules(_addr(z), _DT_CODE[dtype], int(bool(columns)), ldz, V, batch, ctypes.byref(rules), _addr(out),
+                                         ldo, _stream(stream)), "grim_apply_logit_rules")
