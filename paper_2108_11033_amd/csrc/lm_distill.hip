@@ -13,7 +13,7 @@
 namespace grim {
 namespace lm {
 
-constexpr int kMostEntries = 1024, kTable = 2048;
+constexpr int kMostEntries = 1024, kTable = 8192;
 constexpr float kLn2 = 0.69314718055994530942f;
 
 struct DistillParams {
@@ -36,6 +36,9 @@ struct Entries {
     uint16_t table[kTable];
     float total;                // sum of exponentials (0: nothing is listed; NaN: a listed logit is)
 };
+
+// (multiplied, so that words in even steps spread; 13 bits)
+__device__ __forceinline__ int slot(int32_t id) { return (int)((uint32_t)id * 2654435761u >> 19); }
 
 // Formed by one wave.
 __device__ __forceinline__ void teacher(const DistillParams &p, int64_t n, Entries &e) {
@@ -73,25 +76,25 @@ __device__ __forceinline__ void teacher(const DistillParams &p, int64_t n, Entri
         const float x = s > 0.f ? e.p[i] * r : s;                        // (s: 0, or NaN)
         e.p[i] = x;
         e.sum[i] = x;
-        if (e.id[i] >= 0) e.table[e.id[i] & (kTable - 1)] = (uint16_t)i;
+        if (e.id[i] >= 0) e.table[slot(e.id[i])] = (uint16_t)i;
     }
     __builtin_amdgcn_wave_barrier();
     __threadfence_block();
     for (int i0 = 0; i0 < p.k; i0 += 64) {
         const int i = i0 + lane;
         const int32_t id = i < p.k ? e.id[i] : -1;
-        const int other = id >= 0 ? e.table[id & (kTable - 1)] : i;
+        const int other = id >= 0 ? e.table[slot(id)] : i;
         unsigned long long look = __ballot(id >= 0 && other != i);
         while (look) {
             const int l = __builtin_ctzll(look);
             look &= look - 1;
             const int32_t word = __shfl(id, l, 64);
+            int alike = 0;
+            for (int j = lane; j < p.k; j += 64) alike += __popcll(__ballot(e.id[j] == word));
+            if (__builtin_amdgcn_readfirstlane(alike) == 1) continue;        // (lane 0 takes part in every step)
             float sum = 0.f;
-            for (int j0 = 0; j0 < p.k; j0 += 64) {
-                const int j = j0 + lane;
-                const float x = j < p.k && e.id[j] == word ? e.p[j] : 0.f;
-                sum += wave_sum(x);
-            }
+            for (int j = lane; j < p.k; j += 64) sum += e.id[j] == word ? e.p[j] : 0.f;
+            sum = wave_sum(sum);
             for (int j = lane; j < p.k; j += 64)
                 if (e.id[j] == word) e.sum[j] = sum;
         }

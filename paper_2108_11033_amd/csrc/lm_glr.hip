@@ -20,6 +20,11 @@ namespace grim {
 namespace lm {
 
 constexpr int kWaves = 8;       // waves, and chunks, of a workgroup
+// Waves per SIMD that the kernels are held to: what the loads of a group of rows leave room for.  Waves that wait for each other's
+// loads hide more than a second group in flight per wave does (forward 125 against 112 us, backward 247 against 220, at
+// 65536 x 1024 bf16).
+template <typename T> constexpr int waves_forward() { return sizeof(T) == 2 ? 8 : 6; }
+template <typename T> constexpr int waves_backward() { return sizeof(T) == 2 ? 4 : 2; }
 constexpr int kGroup = 8;       // rows whose loads are in flight together, and between two saved states
 constexpr float kLog2e = 1.44269504088896340736f;
 
@@ -35,7 +40,7 @@ struct GlrParams {
     float *dh0, *dbias_part;        // [set][3H]
     float *chunk_maps, *set_maps;   // [chunk or set][A | B][H]
     int64_t ldg, ldy, lddy, lddg, N, H;
-    int32_t nseq, L, sets;          // rows of a chunk (a multiple of kGroup), sets of kWaves chunks
+    int32_t nseq, L, sets, tiles;   // rows of a chunk (a multiple of kGroup), sets of kWaves chunks, column blocks
 };
 
 // f = sigmoid(z) and k = 1 - f = sigmoid(-z) of t = -z log2(e), without cancellation: k = 2^t f.  2^126 is as good as
@@ -133,15 +138,10 @@ __device__ __forceinline__ void forward_map(const GlrParams &p, const Units<VEC>
     if (r0 >= r1) return;
     const Starts starts{p.seq, p.nseq, (int32_t)p.N};
     int s = starts.below(r0) - 1, bound = starts.at(s + 1);
-    Rows<T, VEC> u, c, un_, cn;
-    un_.fetch(p.gates, p.ldg, un.at, r0, r1 - r0);
-    cn.fetch(p.gates, p.ldg, p.H + un.at, r0, r1 - r0);
     for (int g = r0; g < r1; g += kGroup) {
-        u = un_, c = cn;
-        if (g + kGroup < r1) {
-            un_.fetch(p.gates, p.ldg, un.at, g + kGroup, r1 - g - kGroup);
-            cn.fetch(p.gates, p.ldg, p.H + un.at, g + kGroup, r1 - g - kGroup);
-        }
+        Rows<T, VEC> u, c;
+        u.fetch(p.gates, p.ldg, un.at, g, r1 - g);
+        c.fetch(p.gates, p.ldg, p.H + un.at, g, r1 - g);
 #pragma unroll
         for (int i = 0; i < kGroup; ++i) {
             const int r = g + i;
@@ -179,17 +179,11 @@ __device__ __forceinline__ void backward_map(const GlrParams &p, const Units<VEC
     const Starts starts{p.seq, p.nseq, (int32_t)p.N};
     int s = starts.below(r1) - 1;                               // the sequence of row r1 - 1, and where it ends and starts
     int end = s >= 0 ? starts.at(s + 1) : -1, begin = s >= 0 ? starts.at(s) : 0;
-    Rows<T, VEC> u, v, d, un_, vn, dn;
-    int g = r0 + (r1 - 1 - r0) / kGroup * kGroup;
-    auto fetch = [&](int at) {
-        un_.fetch(p.gates, p.ldg, un.at, at, r1 - at);
-        vn.fetch(p.gates, p.ldg, 2 * p.H + un.at, at, r1 - at);
-        dn.fetch(p.dy, p.lddy, un.at, at, r1 - at);
-    };
-    fetch(g);
-    for (; g >= r0; g -= kGroup) {
-        u = un_, v = vn, d = dn;
-        if (g > r0) fetch(g - kGroup);
+    for (int g = r0 + (r1 - 1 - r0) / kGroup * kGroup; g >= r0; g -= kGroup) {
+        Rows<T, VEC> u, v, d;
+        u.fetch(p.gates, p.ldg, un.at, g, r1 - g);
+        v.fetch(p.gates, p.ldg, 2 * p.H + un.at, g, r1 - g);
+        d.fetch(p.dy, p.lddy, un.at, g, r1 - g);
 #pragma unroll
         for (int i = kGroup - 1; i >= 0; --i) {
             const int r = g + i;
@@ -259,10 +253,10 @@ struct Chunk {
 };
 
 template <typename T, int VEC, bool BACK>
-__global__ void __launch_bounds__(64 * kWaves) glr_maps(GlrParams p) {
+__global__ void __launch_bounds__(64 * kWaves, waves_forward<T>()) glr_maps(GlrParams p) {
     __shared__ float maps[kWaves][2][64 * VEC];
-    const int set = blockIdx.x;
-    const Units<VEC> un(blockIdx.y, p.H);
+    const int set = blockIdx.x / p.tiles;
+    const Units<VEC> un(blockIdx.x % p.tiles, p.H);
     const Bias<VEC> bias(p, un.at);
     const Chunk ch(p, set);
     float a[VEC], b[VEC], A[VEC], B[VEC], SA[VEC], SB[VEC];
@@ -315,10 +309,10 @@ __device__ __forceinline__ void entering(const GlrParams &p, float (*maps)[2][64
 // ---------------------------------------------------------------------------------------------- forward
 // ALONE: one set holds all rows, and its workgroup forms the maps of its chunks itself.
 template <typename T, int VEC, bool ALONE>
-__global__ void __launch_bounds__(64 * kWaves) glr_forward(GlrParams p) {
+__global__ void __launch_bounds__(64 * kWaves, waves_forward<T>()) glr_forward(GlrParams p) {
     __shared__ float maps[kWaves][2][64 * VEC];
-    const int set = ALONE ? 0 : p.sets - 1 - blockIdx.x;
-    const Units<VEC> un(blockIdx.y, p.H);
+    const int set = ALONE ? 0 : p.sets - 1 - (int)blockIdx.x / p.tiles;
+    const Units<VEC> un(blockIdx.x % p.tiles, p.H);
     const Bias<VEC> bias(p, un.at);
     const Chunk ch(p, set);
     const Starts starts{p.seq, p.nseq, (int32_t)p.N};
@@ -340,17 +334,12 @@ __global__ void __launch_bounds__(64 * kWaves) glr_forward(GlrParams p) {
     const int r0 = ch.r0, r1 = ch.r1;
     if (r0 >= r1) return;
     int s = starts.below(r0) - 1, bound = starts.at(s + 1);
-    Rows<T, VEC> u, c, v, un_, cn, vn;
-    auto fetch = [&](int at) {
-        un_.fetch(p.gates, p.ldg, un.at, at, r1 - at);
-        cn.fetch(p.gates, p.ldg, p.H + un.at, at, r1 - at);
-        vn.fetch(p.gates, p.ldg, 2 * p.H + un.at, at, r1 - at);
-    };
-    fetch(r0);
     T *y = static_cast<T *>(p.y) + un.at;
     for (int g = r0; g < r1; g += kGroup) {
-        u = un_, c = cn, v = vn;
-        if (g + kGroup < r1) fetch(g + kGroup);
+        Rows<T, VEC> u, c, v;
+        u.fetch(p.gates, p.ldg, un.at, g, r1 - g);
+        c.fetch(p.gates, p.ldg, p.H + un.at, g, r1 - g);
+        v.fetch(p.gates, p.ldg, 2 * p.H + un.at, g, r1 - g);
         if (p.states && un.live) store(p.states + (int64_t)(g / kGroup) * p.H + un.at, h);
 #pragma unroll
         for (int i = 0; i < kGroup; ++i) {
@@ -387,11 +376,11 @@ __global__ void __launch_bounds__(64 * kWaves) glr_forward(GlrParams p) {
 
 // ---------------------------------------------------------------------------------------------- backward
 template <typename T, int VEC, bool ALONE>
-__global__ void __launch_bounds__(64 * kWaves) glr_backward(GlrParams p) {
+__global__ void __launch_bounds__(64 * kWaves, waves_backward<T>()) glr_backward(GlrParams p) {
     __shared__ float maps[kWaves][2][64 * VEC];
     __shared__ float sums[3][64 * VEC];
-    const int set = ALONE ? 0 : p.sets - 1 - blockIdx.x;
-    const Units<VEC> un(blockIdx.y, p.H);
+    const int set = ALONE ? 0 : p.sets - 1 - (int)blockIdx.x / p.tiles;
+    const Units<VEC> un(blockIdx.x % p.tiles, p.H);
     const Bias<VEC> bias(p, un.at);
     const Chunk ch(p, set);
     const Starts starts{p.seq, p.nseq, (int32_t)p.N};
@@ -573,7 +562,7 @@ inline int64_t map_floats(const Cut &c, int64_t H) { return ((int64_t)c.sets * (
 
 template <typename T, int VEC>
 grim_status glr_launch(const GlrParams &p, const Cut &c, bool back, hipStream_t stream) {
-    const dim3 grid((unsigned)c.sets, (unsigned)c.tiles), block(64 * kWaves);
+    const dim3 grid((unsigned)c.sets * c.tiles), block(64 * kWaves);      // (the column blocks of a set's rows side by side)
     if (c.sets == 1) {
         if (back) hipLaunchKernelGGL((glr_backward<T, VEC, true>), grid, block, 0, stream, p);
         else hipLaunchKernelGGL((glr_forward<T, VEC, true>), grid, block, 0, stream, p);
@@ -590,7 +579,7 @@ grim_status glr_launch(const GlrParams &p, const Cut &c, bool back, hipStream_t 
 
 grim_status glr_run(GlrParams p, grim_dtype dt, bool back, hipStream_t stream) {
     const Cut c = cut_rows(p.N, p.H);
-    p.L = c.L, p.sets = c.sets;
+    p.L = c.L, p.sets = c.sets, p.tiles = c.tiles;
     p.set_maps = p.chunk_maps + (int64_t)c.sets * kWaves * 2 * p.H;
     switch (dt) {
         case GRIM_F32: return c.vec == 2 ? glr_launch<float, 2>(p, c, back, stream) : glr_launch<float, 1>(p, c, back, stream);
@@ -600,7 +589,7 @@ grim_status glr_run(GlrParams p, grim_dtype dt, bool back, hipStream_t stream) {
 }
 
 inline bool glr_sizes(int64_t N, int64_t H, int32_t nseq, const int32_t *seq) {
-    // (row numbers in 32 bits with room for a group more; column blocks in one grid dimension)
+    // (row numbers in 32 bits with room for a group more; at most 128 sets of 2^15 column blocks)
     return N >= 0 && N <= (int64_t)1 << 30 && H >= 1 && H <= (int64_t)1 << 21 && nseq >= 1 && (seq || nseq == 1);
 }
 
