@@ -87,16 +87,35 @@ __device__ __forceinline__ void forget(Pack<T, V> &p) {
     for (int i = 0; i < p.W; ++i) asm volatile("" : "+v"(p.w[i]));
 }
 
+// The value of the lane that a pattern names: 0xb1, 0x4e: the neighbour, the neighbouring pair; 0x141, 0x140: mirrored in 8 and
+// in 16 lanes.
+template <int PATTERN>
+__device__ __forceinline__ float from_lane(float v) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), PATTERN, 0xf, 0xf, true));
+}
+
+// All lanes get join(v of all 64), each having joined the same pairs: first inside rows of 16 lanes, then across rows by exchanging
+// them.  (No trip through LDS: a reduction is some 30 cycles, not 600.)
+template <typename F>
+__device__ __forceinline__ float wave_join(float v, F join) {
+    v = join(v, from_lane<0xb1>(v));
+    v = join(v, from_lane<0x4e>(v));
+    v = join(v, from_lane<0x141>(v));
+    v = join(v, from_lane<0x140>(v));
+    const uint32_t r = __builtin_bit_cast(uint32_t, v);
+    const auto by16 = __builtin_amdgcn_permlane16_swap(r, r, false, false);
+    v = join(__builtin_bit_cast(float, (uint32_t)by16[0]), __builtin_bit_cast(float, (uint32_t)by16[1]));
+    const uint32_t q = __builtin_bit_cast(uint32_t, v);
+    const auto by32 = __builtin_amdgcn_permlane32_swap(q, q, false, false);
+    return join(__builtin_bit_cast(float, (uint32_t)by32[0]), __builtin_bit_cast(float, (uint32_t)by32[1]));
+}
+
 __device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d, 64);
-    return v;
+    return wave_join(v, [](float a, float b) { return a + b; });
 }
 
 __device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) v = fmaxf(v, __shfl_xor(v, d, 64));
-    return v;
+    return wave_join(v, [](float a, float b) { return fmaxf(a, b); });
 }
 
 // Sums over a workgroup of W waves, in the order of the waves; `room` holds W floats that nobody uses until the next barrier

@@ -240,8 +240,9 @@ struct Slice {
     }
 };
 
+// (kSliceWaves waves take the slice, one more the teacher's side meanwhile)
 template <typename T>
-__global__ void __launch_bounds__(64 * kSliceWaves) distill_slices(DistillParams p) {
+__global__ void __launch_bounds__(64 * (kSliceWaves + 1)) distill_slices(DistillParams p) {
     constexpr int V = piece<T>(), W = kSliceWaves;
     __shared__ Entries e;
     __shared__ float room[2][W];
@@ -249,8 +250,33 @@ __global__ void __launch_bounds__(64 * kSliceWaves) distill_slices(DistillParams
     if (p.weight && p.weight[n] == 0.f) return;
     const T *z = static_cast<const T *>(p.z) + n * p.ldz;
     const int64_t lo = s * slice_elements<T>(), hi = lo + slice_elements<T>() < p.V ? lo + slice_elements<T>() : p.V;
+    if (threadIdx.x >= 64 * W) {
+        const int lane = threadIdx.x & 63;
+        teacher(p, n, e);
+        __syncthreads();
+        __syncthreads();
+        float peak = -INFINITY, sum = 0.f;
+        for (int w = 0; w < W; ++w) peak = fmaxf(peak, room[0][w]), sum += room[1][w];
+        // (a slice of nothing but -infinity has the sum 0; one NaN makes the sum NaN)
+        const float base = peak == -INFINITY ? 0.f : peak;
+        // sum of p (log2 p - (z - peak) scale) over the words in this slice, and of p
+        float share = 0.f, there = 0.f;
+        for (int i = lane; i < p.k; i += 64) {
+            const int32_t id = e.id[i];
+            if (id >= lo && id < hi && e.p[i] != 0.f) {
+                share += e.p[i] * (e.log[i] - ((float)z[id] - base) * p.scale);
+                there += e.p[i];
+            }
+        }
+        share = wave_sum(share);
+        there = wave_sum(there);
+        if (lane == 0) {
+            float *part = p.part + (int64_t)blockIdx.x * 4;
+            part[0] = peak, part[1] = sum, part[2] = share, part[3] = there;
+        }
+        return;
+    }
     Slice<T> sl(z, lo, hi);
-    if (threadIdx.x < 64) teacher(p, n, e);
     float peak = -INFINITY, sum = 0.f;
 #pragma unroll
     for (int k = 0; k < kSlicePer; ++k) {
@@ -260,7 +286,6 @@ __global__ void __launch_bounds__(64 * kSliceWaves) distill_slices(DistillParams
         for (int j = 0; j < V; ++j) peak = fmaxf(peak, v[j]);
     }
     peak = group_max<W>(peak, room[0]);
-    // (a slice of nothing but -infinity has the sum 0; one NaN makes the sum NaN)
     const float base = peak == -INFINITY ? 0.f : peak;
 #pragma unroll
     for (int k = 0; k < kSlicePer; ++k) {
@@ -270,31 +295,14 @@ __global__ void __launch_bounds__(64 * kSliceWaves) distill_slices(DistillParams
 #pragma unroll
         for (int j = 0; j < V; ++j) sum += __builtin_amdgcn_exp2f((v[j] - base) * p.scale);
     }
-    sum = group_sum<W>(sum, room[1]);
-    if (threadIdx.x >= 64) return;
-    // sum of p (log2 p - (z - peak) scale) over the words in this slice, and of p
-    float share = 0.f, there = 0.f;
-    for (int i = threadIdx.x; i < p.k; i += 64) {
-        const int32_t id = e.id[i];
-        if (id >= lo && id < hi && e.p[i] != 0.f) {
-            share += e.p[i] * (e.log[i] - ((float)z[id] - base) * p.scale);
-            there += e.p[i];
-        }
-    }
-    share = wave_sum(share);
-    there = wave_sum(there);
-    if (threadIdx.x == 0) {
-        float *part = p.part + (int64_t)blockIdx.x * 4;
-        part[0] = peak, part[1] = sum, part[2] = share, part[3] = there;
-    }
+    group_sum<W>(sum, room[1]);
 }
 
 template <typename T>
-__global__ void __launch_bounds__(64 * kSliceWaves) distill_join(DistillParams p) {
-    constexpr int V = piece<T>();
+__global__ void __launch_bounds__(64 * (kSliceWaves + 1)) distill_join(DistillParams p) {
+    constexpr int V = piece<T>(), W = kSliceWaves;
     __shared__ Entries e;
     __shared__ float listed[kMostEntries];
-    __shared__ float joined[2];
     const int64_t n = blockIdx.x / p.slices, s = blockIdx.x % p.slices;
     const T *z = static_cast<const T *>(p.z) + n * p.ldz;
     T *dz = p.dz ? static_cast<T *>(p.dz) + n * p.lddz : nullptr;
@@ -305,24 +313,27 @@ __global__ void __launch_bounds__(64 * kSliceWaves) distill_join(DistillParams p
         if (dz) zero_row(dz, lo, hi);
         return;
     }
-    if (threadIdx.x < 64) {
-        const int lane = threadIdx.x;
+    const int lane = threadIdx.x & 63;
+    const bool aside = threadIdx.x >= 64 * W;
+    const Slice<T> sl(z, lo, aside ? lo : hi);
+    // the maximum and the sum of the whole row from its slices', by every wave for itself
+    const float *part = p.part + n * p.slices * 4;
+    float peak = -INFINITY, sum = 0.f;
+    for (int i = lane; i < p.slices; i += 64) peak = fmaxf(peak, part[4 * i]);
+    peak = wave_max(peak);
+    for (int i = lane; i < p.slices; i += 64) {
+        const float m = part[4 * i] == -INFINITY ? peak : part[4 * i];
+        sum += part[4 * i + 1] * __builtin_amdgcn_exp2f((m - peak) * p.scale);
+    }
+    sum = wave_sum(sum);
+    if (aside) {
         teacher(p, n, e);
         // (only of this slice: other slices' places may hold their gradient already, where dz is z)
         for (int i = lane; i < p.k; i += 64) listed[i] = e.id[i] >= lo && e.id[i] < hi ? (float)z[e.id[i]] : 0.f;
-        const float *part = p.part + n * p.slices * 4;
-        float peak = -INFINITY, sum = 0.f, share = 0.f;
-        for (int i = lane; i < p.slices; i += 64) peak = fmaxf(peak, part[4 * i]);
-        peak = wave_max(peak);
-        for (int i = lane; i < p.slices; i += 64) {
-            const float m = part[4 * i] == -INFINITY ? peak : part[4 * i];
-            sum += part[4 * i + 1] * __builtin_amdgcn_exp2f((m - peak) * p.scale);
-        }
-        sum = wave_sum(sum);
-        if (lane == 0) joined[0] = peak, joined[1] = sum;
         if (s == 0) {
             // log2 q = (z - base_i) scale + (base_i - peak) scale - log2 sum
             const float extra = log2f(sum) - log2f(e.total);
+            float share = 0.f;
             for (int i = lane; i < p.slices; i += 64) {
                 const float base = part[4 * i] == -INFINITY ? 0.f : part[4 * i], there = part[4 * i + 3];
                 if (there != 0.f) share += part[4 * i + 2] + there * ((peak - base) * p.scale + extra);
@@ -332,26 +343,33 @@ __global__ void __launch_bounds__(64 * kSliceWaves) distill_join(DistillParams p
         }
     }
     if (!dz) return;
-    __syncthreads();
-    const float total = e.total, peak = joined[0], rsum = 1.f / joined[1];
+    const float rsum = 1.f / sum;
+    float v[kSlicePer][V];
+#pragma unroll
+    for (int k = 0; k < kSlicePer; ++k) {
+        unpack(sl.raw[k], v[k]);
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[k][j] = rsum * __builtin_amdgcn_exp2f((v[k][j] - peak) * p.scale);
+    }
+    __syncthreads();                                        // (also: the words of this slice were read before it is written)
+    const float total = e.total;
     if (total == 0.f) {
         zero_row(dz, lo, hi);
         return;
     }
-    const float factor = weight * p.tau * (total / total), slope = factor * rsum;
-    const Slice<T> sl(z, lo, hi);
+    const float factor = weight * p.tau * (total / total);
+    if (!aside) {
 #pragma unroll
-    for (int k = 0; k < kSlicePer; ++k) {
-        float v[V], out[V];
-        unpack(sl.raw[k], v);
+        for (int k = 0; k < kSlicePer; ++k) {
 #pragma unroll
-        for (int j = 0; j < V; ++j) out[j] = slope * __builtin_amdgcn_exp2f((v[j] - peak) * p.scale);
-        T *to = dz + Slice<T>::at(lo, k);
-        if (sl.have[k] == V) store(to, out);
-        else
+            for (int j = 0; j < V; ++j) v[k][j] *= factor;
+            T *to = dz + Slice<T>::at(lo, k);
+            if (sl.have[k] == V) store(to, v[k]);
+            else
 #pragma unroll
-            for (int j = 0; j < V; ++j)
-                if (j < sl.have[k]) to[j] = (T)out[j];
+                for (int j = 0; j < V; ++j)
+                    if (j < sl.have[k]) to[j] = (T)v[k][j];
+        }
     }
     __syncthreads();
     write_listed(p, e, dz, listed, peak, rsum, factor, lo, hi);
@@ -385,7 +403,7 @@ grim_status distill_typed(DistillParams p, hipStream_t stream) {
     }
     p.slices = (int32_t)slices_of<T>(p.V);
     if (p.N > kMaxGrid / p.slices) return GRIM_ERR_SHAPE;
-    const dim3 g((unsigned)(p.N * p.slices)), b(64 * kSliceWaves);
+    const dim3 g((unsigned)(p.N * p.slices)), b(64 * (kSliceWaves + 1));
     hipLaunchKernelGGL(distill_slices<T>, g, b, 0, stream, p);
     const grim_status st = launched();
     if (st != GRIM_OK) return st;

@@ -33,48 +33,68 @@ struct CallerRules {
     }
 };
 
-// Words lo .. hi - 1 of caller b into count[(word - lo) << shift] and bias[...]; the whole workgroup, with barriers.
-__device__ __forceinline__ void gather_rules(const grim_logit_rules &r, int64_t b, int64_t lo, int64_t hi, uint32_t *count, float *bias,
-                                             int shift, int32_t *staged) {
-    const int span = (int)(hi - lo), first = (int)lo;
-    if (r.history && r.max_history > 0) {
-        const int32_t *h = r.history + b * r.ld_history;
-        const int len = r.history_len ? min(max(r.history_len[b], 0), r.max_history) : r.max_history;
-        const auto tally = [&](int32_t id) {
-            // (a word below lo wraps around to a large number; words of 2^31 and more do not exist)
-            const uint32_t at = (uint32_t)id - (uint32_t)first;
-            if (id >= 0 && at < (uint32_t)span) atomicAdd(&count[at << shift], 1u);
-        };
-        int i = threadIdx.x * 4;
-        for (; i + 4 <= len; i += blockDim.x * 4) {
-            const Pack<int32_t, 4> ids = load<4>(h + i);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) tally((int32_t)ids.w[j]);
-        }
-        for (; i < len; ++i) tally(h[i]);                       // the last, short piece is one thread's
+// A caller's history, walked by a team of `width` threads (this one is number t): its length and the first four words of each
+// thread are asked for before anything else (up to the most that a history may hold, so that they need not wait for the length).
+struct History {
+    const int32_t *h;
+    int most, len, t, width;
+    int32_t early[4];
+    __device__ __forceinline__ History(const grim_logit_rules &r, int64_t b, int t_, int width_) : t(t_), width(width_) {
+        most = r.history ? r.max_history : 0;
+        h = r.history + b * r.ld_history;
+        len = most > 0 && r.history_len ? min(max(r.history_len[b], 0), most) : most;
+        take(t * 4, early);
     }
-    if (!r.bias_ids || !r.bias_values || r.nbias <= 0) return;
-    const int32_t *ids = r.bias_ids + b * r.ld_bias;
+    __device__ __forceinline__ void take(int i, int32_t (&ids)[4]) const {
+        if (i + 4 <= most) {
+            const Pack<int32_t, 4> p = load<4>(h + i);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) ids[j] = (int32_t)p.w[j];
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) ids[j] = i + j < most ? h[i + j] : -1;
+        }
+    }
+    // Words lo .. lo + span - 1 into count[(word - lo) << shift].
+    __device__ __forceinline__ void tally(int lo, int span, uint32_t *count, int shift) {
+        int32_t ids[4] = {early[0], early[1], early[2], early[3]};
+        for (int i = t * 4; i < len; i += width * 4) {
+            if (i >= width * 4) take(i, ids);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                // (a word below lo wraps around to a large number; words of 2^31 and more do not exist)
+                const uint32_t at = (uint32_t)ids[j] - (uint32_t)lo;
+                if (i + j < len && ids[j] >= 0 && at < (uint32_t)span) atomicAdd(&count[at << shift], 1u);
+            }
+        }
+    }
+};
+
+// A caller's biases for words lo .. lo + span - 1 into bias[(word - lo) << shift], by thread t of `width`; `staged`: the list's words.
+__device__ __forceinline__ void add_biases(const grim_logit_rules &r, int64_t b, int lo, int span, const int32_t *staged, float *bias,
+                                           int shift, int t, int width) {
     const float *values = r.bias_values + b * r.ld_bias;
-    for (int i = threadIdx.x; i < r.nbias; i += blockDim.x) staged[i] = ids[i];
-    __syncthreads();
-    for (int i = threadIdx.x; i < r.nbias; i += blockDim.x) {
+    for (int i = t; i < r.nbias; i += width) {
         const int32_t id = staged[i];
-        const uint32_t at = (uint32_t)id - (uint32_t)first;
+        const uint32_t at = (uint32_t)id - (uint32_t)lo;
         if (id < 0 || at >= (uint32_t)span) continue;
-        // the first entry of a word adds up all of them, in the list's order
-        bool earlier = false;
-        for (int j = 0; j < i; ++j) earlier |= staged[j] == id;
-        if (earlier) continue;
+        int earlier = 0, alike = 0;
+#pragma unroll 8
+        for (int j = 0; j < r.nbias; ++j) {
+            const int same = staged[j] == id;
+            alike += same;
+            earlier += j < i ? same : 0;
+        }
+        if (earlier) continue;                                  // the first entry of a word adds up all, in the list's order
         float sum = values[i];
-        for (int j = i + 1; j < r.nbias; ++j)
-            if (staged[j] == id) sum += values[j];
+        if (alike > 1)
+            for (int j = i + 1; j < r.nbias; ++j)
+                if (staged[j] == id) sum += values[j];
         bias[at << shift] = sum;
     }
-    __syncthreads();                                            // (staged is free again)
 }
 
-// A row per caller: TILE words of one caller.
+// A row per caller: TILE words of one caller.  Everything that a tile reads is asked for at its start.
 template <typename T, int TILE, int THREADS>
 __global__ void __launch_bounds__(THREADS) rules_rows(RuleParams p, int tiles) {
     constexpr int V = 16 / (int)sizeof(T), PER = TILE / (THREADS * V);
@@ -86,7 +106,12 @@ __global__ void __launch_bounds__(THREADS) rules_rows(RuleParams p, int tiles) {
     const T *z = static_cast<const T *>(p.z) + b * p.ldz + lo;
     T *out = static_cast<T *>(p.out) + b * p.ldo + lo;
     const int span = (int)(hi - lo);
+    History history(p.r, b, threadIdx.x, THREADS);
+    for (int i = threadIdx.x; i < p.r.nbias; i += THREADS) staged[i] = p.r.bias_ids[b * p.r.ld_bias + i];
+    const CallerRules rules(p.r, b);
+    const uint32_t *allowed = p.r.allowed ? p.r.allowed + b * p.r.ld_allowed + lo / 32 : nullptr;
     Pack<T, V> raw[PER];
+    uint32_t bits[PER];
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
         const int c = (k * THREADS + threadIdx.x) * V;
@@ -94,21 +119,20 @@ __global__ void __launch_bounds__(THREADS) rules_rows(RuleParams p, int tiles) {
         else
 #pragma unroll
             for (int j = 0; j < V; ++j) put(raw[k], j, c + j < span ? z[c + j] : (T)0.f);
+        bits[k] = allowed && c < span ? allowed[c / 32] >> (c % 32) : 0xffffffffu;
     }
     for (int i = threadIdx.x; i < TILE; i += THREADS) count[i] = 0, bias[i] = 0.f;
     __syncthreads();
-    gather_rules(p.r, b, lo, hi, count, bias, 0, staged);
+    history.tally((int)lo, span, count, 0);
+    if (p.r.nbias > 0) add_biases(p.r, b, (int)lo, span, staged, bias, 0, threadIdx.x, THREADS);
     __syncthreads();
-    const CallerRules rules(p.r, b);
-    const uint32_t *allowed = p.r.allowed ? p.r.allowed + b * p.r.ld_allowed + lo / 32 : nullptr;
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
         const int c = (k * THREADS + threadIdx.x) * V;
         if (c >= span) continue;
-        const uint32_t bits = allowed ? allowed[c / 32] >> (c % 32) : 0xffffffffu;
         float v[V];
 #pragma unroll
-        for (int j = 0; j < V; ++j) v[j] = rules.apply(element(raw[k], j), count[c + j], bias[c + j], bits >> j & 1);
+        for (int j = 0; j < V; ++j) v[j] = rules.apply(element(raw[k], j), count[c + j], bias[c + j], bits[k] >> j & 1);
         if (c + V <= span) store(out + c, v);
         else
 #pragma unroll
@@ -120,29 +144,41 @@ __global__ void __launch_bounds__(THREADS) rules_rows(RuleParams p, int tiles) {
 // A column per caller: TILE >> shift words of up to 1 << shift callers.
 template <typename T, int TILE, int THREADS>
 __global__ void __launch_bounds__(THREADS) rules_columns(RuleParams p, int tiles, int shift) {
+    constexpr int PER = TILE / THREADS;
     __shared__ uint32_t count[TILE];
     __shared__ float bias[TILE];
-    __shared__ int32_t staged[kMostBias];
     const int words = TILE >> shift;
     const int64_t b0 = (int64_t)(blockIdx.x / tiles) << shift, lo = (int64_t)(blockIdx.x % tiles) * words;
     const int64_t hi = lo + words < p.V ? lo + words : p.V;
-    const int callers = (int)min((int64_t)1 << shift, p.batch - b0);
+    const int span = (int)(hi - lo), callers = (int)min((int64_t)1 << shift, p.batch - b0);
+    // (THREADS is a multiple of 1 << shift: a thread keeps its caller)
+    const int mine = min((int)threadIdx.x & ((1 << shift) - 1), callers - 1);
+    const bool live = ((int)threadIdx.x & ((1 << shift) - 1)) < callers;
+    const CallerRules rules(p.r, b0 + mine);
+    const uint32_t *allowed = p.r.allowed ? p.r.allowed + (b0 + mine) * p.r.ld_allowed : nullptr;
+    const T *z = static_cast<const T *>(p.z) + b0 + mine;
+    T *out = static_cast<T *>(p.out) + b0 + mine;
+    float v[PER];
+    uint32_t bits = 0;                                          // one for each of the thread's words
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        const int at = (k * THREADS + (int)threadIdx.x) >> shift;
+        const int64_t word = lo + min(at, span - 1);
+        v[k] = (float)z[word * p.ldz];
+        bits |= (allowed ? allowed[word / 32] >> (word % 32) & 1 : 1u) << k;
+    }
     for (int i = threadIdx.x; i < TILE; i += THREADS) count[i] = 0, bias[i] = 0.f;
     __syncthreads();
-    for (int b = 0; b < callers; ++b) gather_rules(p.r, b0 + b, lo, hi, count + b, bias + b, shift, staged);
+    const int lane = threadIdx.x & 63;
+    for (int b = threadIdx.x >> 6; b < callers; b += THREADS / 64) {          // a wave per caller
+        History(p.r, b0 + b, lane, 64).tally((int)lo, span, count + b, shift);
+        if (p.r.nbias > 0) add_biases(p.r, b0 + b, (int)lo, span, p.r.bias_ids + (b0 + b) * p.r.ld_bias, bias + b, shift, lane, 64);
+    }
     __syncthreads();
-    const int b = threadIdx.x & ((1 << shift) - 1);             // (THREADS is a multiple of 1 << shift: a thread keeps its caller)
-    if (b >= callers) return;
-    const CallerRules rules(p.r, b0 + b);
-    const uint32_t *allowed = p.r.allowed ? p.r.allowed + (b0 + b) * p.r.ld_allowed : nullptr;
-    const T *z = static_cast<const T *>(p.z) + b0 + b;
-    T *out = static_cast<T *>(p.out) + b0 + b;
-#pragma unroll 4
-    for (int i = threadIdx.x; i < TILE; i += THREADS) {
-        const int64_t word = lo + (i >> shift);
-        if (word >= hi) break;
-        const bool may = !allowed || (allowed[word / 32] >> (word % 32) & 1);
-        out[word * p.ldo] = (T)rules.apply((float)z[word * p.ldz], count[i], bias[i], may);
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        const int i = k * THREADS + (int)threadIdx.x, at = i >> shift;
+        if (live && at < span) out[(lo + at) * p.ldo] = (T)rules.apply(v[k], count[i], bias[i], bits >> k & 1);
     }
 }
 
@@ -162,6 +198,7 @@ grim_status rules_launch(const RuleParams &p, bool columns, hipStream_t stream) 
 // Tiles of 4096 words and callers; of 2048 where those would leave compute units without one.
 template <typename T>
 grim_status rules_typed(const RuleParams &p, bool columns, hipStream_t stream) {
+    if (p.batch == 1 && p.ldz == 1 && p.ldo == 1) columns = false;   // a single dense column is a row
     return p.V * p.batch >= (int64_t)4096 * kComputeUnits ? rules_launch<T, 4096, 512>(p, columns, stream)
                                                           : rules_launch<T, 2048, 256>(p, columns, stream);
 }
