@@ -139,9 +139,8 @@ typedef struct grim_logit_rules {
  *   z_dev, out_dev   element type dt; columns = 0: batch x V, a row per caller (ld >= V); columns = 1: V x batch, a column
  *                    per caller, as grim_bcr_spmv leaves logits (ld >= batch).  out_dev may be z_dev itself (same ld).
  * Arithmetic in fp32, rounded once.
- * Errors: NULL, SHAPE (V < 1, V >= 2^31, batch < 0, leading dimension too small, max_history or nbias negative,
- * max_history > 2^30), DTYPE,
- * DEVICE, UNSUPPORTED (nbias > 1024).
+ * Errors: NULL, SHAPE (V < 1, V >= 2^31, batch < 0, leading dimension too small, max_history or nbias negative), DTYPE,
+ * DEVICE, UNSUPPORTED (nbias > 1024, max_history > 2^20).
  */
 grim_status grim_apply_logit_rules(const void *z_dev, grim_dtype dt, int32_t columns, int64_t ldz, int64_t V, int32_t batch,
                                    const grim_logit_rules *rules, void *out_dev, int64_t ldo, void *hip_stream);

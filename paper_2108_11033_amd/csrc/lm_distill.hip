@@ -13,7 +13,7 @@
 namespace grim {
 namespace lm {
 
-constexpr int kMostEntries = 1024, kTable = 8192;
+constexpr int kMostEntries = 1024;
 constexpr float kLn2 = 0.69314718055994530942f;
 
 struct DistillParams {
@@ -28,20 +28,22 @@ struct DistillParams {
     float tau, scale;           // scale = log2(e) / tau
 };
 
-// The teacher's side of a row in LDS: words (-1: absent), probabilities, the sums of the probabilities of entries that list the
-// same word, and log2 p = (top - best) scale - log2(total) kept as its first part.
+// The teacher's side of a row in LDS, with room for E entries: words (-1: absent), probabilities, the sums of the probabilities of
+// entries that list the same word, the first part of log2 p = (top - best) scale - log2(total), and z at the words.
+template <int E>
 struct Entries {
-    int32_t id[kMostEntries];
-    float p[kMostEntries], sum[kMostEntries], log[kMostEntries];
-    uint16_t table[kTable];
+    static constexpr int kBits = E <= 64 ? 10 : 13;
+    int32_t id[E];
+    float p[E], sum[E], log[E], z[E];
+    uint16_t table[1 << kBits];
     float total;                // sum of exponentials (0: nothing is listed; NaN: a listed logit is)
+    // (multiplied, so that words in even steps spread)
+    static __device__ __forceinline__ int slot(int32_t id) { return (int)((uint32_t)id * 2654435761u >> (32 - kBits)); }
 };
 
-// (multiplied, so that words in even steps spread; 13 bits)
-__device__ __forceinline__ int slot(int32_t id) { return (int)((uint32_t)id * 2654435761u >> 19); }
-
-// Formed by one wave.
-__device__ __forceinline__ void teacher(const DistillParams &p, int64_t n, Entries &e) {
+// Formed by one wave.  z is read at the words lo .. hi - 1 (0 elsewhere).
+template <int E, typename T>
+__device__ __forceinline__ void teacher(const DistillParams &p, int64_t n, const T *z, int64_t lo, int64_t hi, Entries<E> &e) {
     const int lane = threadIdx.x & 63;
     const float *t = p.top + n * p.ldt;
     const int32_t *ids = p.ids + n * p.ldt;
@@ -49,8 +51,10 @@ __device__ __forceinline__ void teacher(const DistillParams &p, int64_t n, Entri
     bool nan = false;
     for (int i = lane; i < p.k; i += 64) {
         const int32_t id = ids[i];
+        const float listed = t[i];
         const bool there = id >= 0 && id < p.V;
-        const float v = there ? t[i] : -INFINITY;
+        const float v = there ? listed : -INFINITY;
+        e.z[i] = id >= lo && id < hi ? (float)z[id] : 0.f;
         e.id[i] = there ? id : -1;
         e.log[i] = v;
         nan |= v != v;
@@ -76,24 +80,24 @@ __device__ __forceinline__ void teacher(const DistillParams &p, int64_t n, Entri
         const float x = s > 0.f ? e.p[i] * r : s;                        // (s: 0, or NaN)
         e.p[i] = x;
         e.sum[i] = x;
-        if (e.id[i] >= 0) e.table[slot(e.id[i])] = (uint16_t)i;
+        if (e.id[i] >= 0) e.table[e.slot(e.id[i])] = (uint16_t)i;
     }
     __builtin_amdgcn_wave_barrier();
     __threadfence_block();
     for (int i0 = 0; i0 < p.k; i0 += 64) {
         const int i = i0 + lane;
         const int32_t id = i < p.k ? e.id[i] : -1;
-        const int other = id >= 0 ? e.table[slot(id)] : i;
+        const int other = id >= 0 ? e.table[e.slot(id)] : i;
         unsigned long long look = __ballot(id >= 0 && other != i);
         while (look) {
             const int l = __builtin_ctzll(look);
             look &= look - 1;
             const int32_t word = __shfl(id, l, 64);
             int alike = 0;
-            for (int j = lane; j < p.k; j += 64) alike += __popcll(__ballot(e.id[j] == word));
-            if (__builtin_amdgcn_readfirstlane(alike) == 1) continue;        // (lane 0 takes part in every step)
             float sum = 0.f;
-            for (int j = lane; j < p.k; j += 64) sum += e.id[j] == word ? e.p[j] : 0.f;
+            for (int j = lane; j < p.k; j += 64)
+                if (e.id[j] == word) sum += e.p[j], ++alike;
+            if (wave_sum((float)alike) == 1.f) continue;
             sum = wave_sum(sum);
             for (int j = lane; j < p.k; j += 64)
                 if (e.id[j] == word) e.sum[j] = sum;
@@ -115,24 +119,24 @@ __device__ __forceinline__ void zero_row(T *dz, int64_t lo, int64_t hi) {
     }
 }
 
-// weight tau (q_j - p_j) at the listed words, over what was streamed there.  zl: z at the entries' words.
-template <typename T>
-__device__ __forceinline__ void write_listed(const DistillParams &p, const Entries &e, T *dz, const float *zl, float peak, float rsum,
-                                             float factor, int64_t lo, int64_t hi) {
+// weight tau (q_j - p_j) at the listed words, over what was streamed there.
+template <int E, typename T>
+__device__ __forceinline__ void write_listed(const DistillParams &p, const Entries<E> &e, T *dz, float peak, float rsum, float factor,
+                                             int64_t lo, int64_t hi) {
     for (int i = threadIdx.x; i < p.k; i += blockDim.x) {
         const int32_t id = e.id[i];
-        if (id >= lo && id < hi) dz[id] = (T)(factor * (__builtin_amdgcn_exp2f((zl[i] - peak) * p.scale) * rsum - e.sum[i]));
+        if (id >= lo && id < hi) dz[id] = (T)(factor * (__builtin_amdgcn_exp2f((e.z[i] - peak) * p.scale) * rsum - e.sum[i]));
     }
 }
 
 // -------------------------------------------------------------------------------------------------- one workgroup per row
-// W waves, at most PER pieces of 16 bytes a thread: pieces k < full are whole for all threads, piece `full` for some, the
-// others are empty.  A piece that reaches past the row is moved back to end with it; what it shares counts in the other.
-template <typename T, int W, int PER>
-__global__ void __launch_bounds__(64 * W) distill_rows(DistillParams p) {
+// W waves hold the row, at most PER pieces of 16 bytes a thread: pieces k < full are whole for all threads, piece `full` for
+// some, the others are empty.  A piece that reaches past the row is moved back to end with it; what it shares counts in
+// the other.  One wave more forms the teacher's side meanwhile: its chain of loads and small reductions is as long as the row's own.
+template <typename T, int E, int W, int PER>
+__global__ void __launch_bounds__(64 * (W + 1)) distill_rows(DistillParams p) {
     constexpr int V = piece<T>(), TPR = 64 * W;
-    __shared__ Entries e;
-    __shared__ float listed[kMostEntries];                  // z at the listed words
+    __shared__ Entries<E> e;
     __shared__ float room[2][W];
     const int64_t n = blockIdx.x;
     const T *z = static_cast<const T *>(p.z) + n * p.ldz;
@@ -143,44 +147,47 @@ __global__ void __launch_bounds__(64 * W) distill_rows(DistillParams p) {
         if (dz) zero_row(dz, 0, p.V);
         return;
     }
+    const bool aside = threadIdx.x >= TPR;
     const int full = (int)(p.V / (TPR * V));
     const int mine = full * TPR * V + (int)threadIdx.x * V;   // where piece `full` would start
-    const bool some = mine < p.V;
+    const bool some = !aside && mine < p.V;
     const int tail = (int)min((int64_t)mine, p.V - V), first = mine - tail;
     Pack<T, V> raw[PER];
-#pragma unroll
-    for (int k = 0; k < PER; ++k) {
-        if (k < full) raw[k] = load<V>(z + k * TPR * V + (int)threadIdx.x * V);
-        else if (k == full && some) raw[k] = load<V>(z + tail);
-    }
-    if (threadIdx.x < 64) {
-        teacher(p, n, e);
-        for (int i = threadIdx.x; i < p.k; i += 64) listed[i] = e.id[i] >= 0 ? (float)z[e.id[i]] : 0.f;
-    }
-    // f(k, j, value) over the thread's own elements
-    auto own = [&](auto f) {
+    float peak = -INFINITY, sum = 0.f;
+    if (aside) {
+        teacher(p, n, z, 0, p.V, e);
+        __syncthreads();
+        __syncthreads();
+        for (int w = 0; w < W; ++w) peak = fmaxf(peak, room[0][w]), sum += room[1][w];
+    } else {
 #pragma unroll
         for (int k = 0; k < PER; ++k) {
-            if (k > full || (k == full && !some)) continue;
-            float v[V];
-            forget(raw[k]);
-            unpack(raw[k], v);
-            if (k < full) {
-#pragma unroll
-                for (int j = 0; j < V; ++j) f(v[j]);
-            } else {
-#pragma unroll
-                for (int j = 0; j < V; ++j)
-                    if (j >= first) f(v[j]);
-            }
+            if (k < full) raw[k] = load<V>(z + k * TPR * V + (int)threadIdx.x * V);
+            else if (k == full && some) raw[k] = load<V>(z + tail);
         }
-    };
-    float peak = -INFINITY, sum = 0.f;
-    own([&](float v) { peak = fmaxf(peak, v); });
-    peak = group_max<W>(peak, room[0]);
-    own([&](float v) { sum += __builtin_amdgcn_exp2f((v - peak) * p.scale); });
-    sum = group_sum<W>(sum, room[1]);                       // (its barrier also shows the teacher's side to all)
-    if (W == 1) __syncthreads();
+        // f(value) over the thread's own elements
+        auto own = [&](auto f) {
+#pragma unroll
+            for (int k = 0; k < PER; ++k) {
+                if (k > full || (k == full && !some)) continue;
+                float v[V];
+                forget(raw[k]);
+                unpack(raw[k], v);
+                if (k < full) {
+#pragma unroll
+                    for (int j = 0; j < V; ++j) f(v[j]);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < V; ++j)
+                        if (j >= first) f(v[j]);
+                }
+            }
+        };
+        own([&](float v) { peak = fmaxf(peak, v); });
+        peak = group_max<W>(peak, room[0]);
+        own([&](float v) { sum += __builtin_amdgcn_exp2f((v - peak) * p.scale); });
+        sum = group_sum<W>(sum, room[1]);                   // (its barrier also shows the teacher's side to all)
+    }
     const float total = e.total;
     if (total == 0.f) {
         if (threadIdx.x == 0) p.loss[n] = 0.f;
@@ -189,7 +196,14 @@ __global__ void __launch_bounds__(64 * W) distill_rows(DistillParams p) {
     }
     const float rsum = 1.f / sum;
     const float factor = weight * p.tau * (total / total);  // (a NaN of the teacher reaches the whole row)
-    if (dz) {
+    if (aside) {
+        const float lse = log2f(sum), ltotal = log2f(total);
+        float loss = 0.f;
+        for (int i = threadIdx.x & 63; i < p.k; i += 64)
+            if (e.p[i] != 0.f) loss += e.p[i] * ((e.log[i] - ltotal) - ((e.z[i] - peak) * p.scale - lse));
+        loss = wave_sum(loss);
+        if (threadIdx.x == TPR) p.loss[n] = weight * p.tau * p.tau * (kLn2 * loss);
+    } else if (dz) {
         const float slope = factor * rsum;
 #pragma unroll
         for (int k = 0; k < PER; ++k) {
@@ -201,17 +215,10 @@ __global__ void __launch_bounds__(64 * W) distill_rows(DistillParams p) {
             for (int j = 0; j < V; ++j) out[j] = slope * __builtin_amdgcn_exp2f((v[j] - peak) * p.scale);
             store(dz + (k < full ? k * TPR * V + (int)threadIdx.x * V : tail), out);
         }
-        __syncthreads();                                    // the listed words' places were written by other threads
-        write_listed(p, e, dz, listed, peak, rsum, factor, 0, p.V);
     }
-    if (threadIdx.x < 64) {
-        const float lse = log2f(sum), ltotal = log2f(total);
-        float loss = 0.f;
-        for (int i = threadIdx.x; i < p.k; i += 64)
-            if (e.p[i] != 0.f) loss += e.p[i] * ((e.log[i] - ltotal) - ((listed[i] - peak) * p.scale - lse));
-        loss = wave_sum(loss);
-        if (threadIdx.x == 0) p.loss[n] = weight * p.tau * p.tau * (kLn2 * loss);
-    }
+    if (!dz) return;
+    __syncthreads();                                        // the listed words' places were written by other threads
+    write_listed(p, e, dz, peak, rsum, factor, 0, p.V);
 }
 
 // -------------------------------------------------------------------------------------------------- slices of rows
@@ -241,10 +248,10 @@ struct Slice {
 };
 
 // (kSliceWaves waves take the slice, one more the teacher's side meanwhile)
-template <typename T>
+template <typename T, int E>
 __global__ void __launch_bounds__(64 * (kSliceWaves + 1)) distill_slices(DistillParams p) {
     constexpr int V = piece<T>(), W = kSliceWaves;
-    __shared__ Entries e;
+    __shared__ Entries<E> e;
     __shared__ float room[2][W];
     const int64_t n = blockIdx.x / p.slices, s = blockIdx.x % p.slices;
     if (p.weight && p.weight[n] == 0.f) return;
@@ -252,7 +259,7 @@ __global__ void __launch_bounds__(64 * (kSliceWaves + 1)) distill_slices(Distill
     const int64_t lo = s * slice_elements<T>(), hi = lo + slice_elements<T>() < p.V ? lo + slice_elements<T>() : p.V;
     if (threadIdx.x >= 64 * W) {
         const int lane = threadIdx.x & 63;
-        teacher(p, n, e);
+        teacher(p, n, z, lo, hi, e);
         __syncthreads();
         __syncthreads();
         float peak = -INFINITY, sum = 0.f;
@@ -264,7 +271,7 @@ __global__ void __launch_bounds__(64 * (kSliceWaves + 1)) distill_slices(Distill
         for (int i = lane; i < p.k; i += 64) {
             const int32_t id = e.id[i];
             if (id >= lo && id < hi && e.p[i] != 0.f) {
-                share += e.p[i] * (e.log[i] - ((float)z[id] - base) * p.scale);
+                share += e.p[i] * (e.log[i] - (e.z[i] - base) * p.scale);
                 there += e.p[i];
             }
         }
@@ -298,38 +305,38 @@ __global__ void __launch_bounds__(64 * (kSliceWaves + 1)) distill_slices(Distill
     group_sum<W>(sum, room[1]);
 }
 
-template <typename T>
+template <typename T, int E>
 __global__ void __launch_bounds__(64 * (kSliceWaves + 1)) distill_join(DistillParams p) {
     constexpr int V = piece<T>(), W = kSliceWaves;
-    __shared__ Entries e;
-    __shared__ float listed[kMostEntries];
+    __shared__ Entries<E> e;
     const int64_t n = blockIdx.x / p.slices, s = blockIdx.x % p.slices;
     const T *z = static_cast<const T *>(p.z) + n * p.ldz;
     T *dz = p.dz ? static_cast<T *>(p.dz) + n * p.lddz : nullptr;
     const int64_t lo = s * slice_elements<T>(), hi = lo + slice_elements<T>() < p.V ? lo + slice_elements<T>() : p.V;
     const float weight = p.weight ? p.weight[n] : 1.f;
-    if (weight == 0.f) {
-        if (threadIdx.x == 0 && s == 0) p.loss[n] = 0.f;
-        if (dz) zero_row(dz, lo, hi);
-        return;
-    }
     const int lane = threadIdx.x & 63;
     const bool aside = threadIdx.x >= 64 * W;
     const Slice<T> sl(z, lo, aside ? lo : hi);
     // the maximum and the sum of the whole row from its slices', by every wave for itself
     const float *part = p.part + n * p.slices * 4;
-    float peak = -INFINITY, sum = 0.f;
-    for (int i = lane; i < p.slices; i += 64) peak = fmaxf(peak, part[4 * i]);
-    peak = wave_max(peak);
+    float own = -INFINITY, sum = 0.f;
     for (int i = lane; i < p.slices; i += 64) {
-        const float m = part[4 * i] == -INFINITY ? peak : part[4 * i];
-        sum += part[4 * i + 1] * __builtin_amdgcn_exp2f((m - peak) * p.scale);
+        const float m = part[4 * i], x = part[4 * i + 1], high = fmaxf(own, m);
+        // (a slice without a maximum has the sum 0, or NaN)
+        sum = (own == -INFINITY ? sum : sum * __builtin_amdgcn_exp2f((own - high) * p.scale)) +
+              (m == -INFINITY ? x : x * __builtin_amdgcn_exp2f((m - high) * p.scale));
+        own = high;
     }
-    sum = wave_sum(sum);
+    const float peak = wave_max(own);
+    sum = wave_sum(own == -INFINITY && peak != -INFINITY ? sum : sum * __builtin_amdgcn_exp2f((own - peak) * p.scale));
+    if (weight == 0.f) {
+        if (threadIdx.x == 0 && s == 0) p.loss[n] = 0.f;
+        if (dz) zero_row(dz, lo, hi);
+        return;
+    }
     if (aside) {
-        teacher(p, n, e);
-        // (only of this slice: other slices' places may hold their gradient already, where dz is z)
-        for (int i = lane; i < p.k; i += 64) listed[i] = e.id[i] >= lo && e.id[i] < hi ? (float)z[e.id[i]] : 0.f;
+        // (z of this slice only: other slices' places may hold their gradient already, where dz is z)
+        teacher(p, n, z, lo, hi, e);
         if (s == 0) {
             // log2 q = (z - base_i) scale + (base_i - peak) scale - log2 sum
             const float extra = log2f(sum) - log2f(e.total);
@@ -372,43 +379,49 @@ __global__ void __launch_bounds__(64 * (kSliceWaves + 1)) distill_join(DistillPa
         }
     }
     __syncthreads();
-    write_listed(p, e, dz, listed, peak, rsum, factor, lo, hi);
+    write_listed(p, e, dz, peak, rsum, factor, lo, hi);
 }
 
 // -------------------------------------------------------------------------------------------------- launches
 template <typename T>
 int64_t slices_of(int64_t V) { return (V + slice_elements<T>() - 1) / slice_elements<T>(); }
 
-// A workgroup per row where its registers hold the row: 16 pieces a thread of 16 waves.
+// A workgroup per row where its registers hold the row: 18 pieces a thread of 15 waves.
 template <typename T>
-bool row_fits(int64_t V) { return V >= piece<T>() && V <= (int64_t)16 * 1024 * piece<T>(); }
+bool row_fits(int64_t V) { return V >= piece<T>() && V <= (int64_t)18 * 960 * piece<T>(); }
 
 template <typename T>
 bool by_rows(int64_t N, int64_t V) { return row_fits<T>(V) && (N >= 128 || slices_of<T>(V) <= 2); }
 
-template <typename T>
-grim_status distill_typed(DistillParams p, hipStream_t stream) {
+template <typename T, int E>
+grim_status distill_launch(DistillParams p, hipStream_t stream) {
     if (by_rows<T>(p.N, p.V)) {
         if (p.N > kMaxGrid) return GRIM_ERR_SHAPE;
         const dim3 g((unsigned)p.N);
         const int64_t pieces = (p.V + piece<T>() - 1) / piece<T>();
-        if (pieces <= 256) hipLaunchKernelGGL((distill_rows<T, 4, 1>), g, dim3(256), 0, stream, p);
-        else if (pieces <= 512) hipLaunchKernelGGL((distill_rows<T, 4, 2>), g, dim3(256), 0, stream, p);
-        else if (pieces <= 1024) hipLaunchKernelGGL((distill_rows<T, 4, 4>), g, dim3(256), 0, stream, p);
-        else if (pieces <= 2048) hipLaunchKernelGGL((distill_rows<T, 8, 4>), g, dim3(512), 0, stream, p);
-        else if (pieces <= 4096) hipLaunchKernelGGL((distill_rows<T, 8, 8>), g, dim3(512), 0, stream, p);
-        else if (pieces <= 8192) hipLaunchKernelGGL((distill_rows<T, 8, 16>), g, dim3(512), 0, stream, p);
-        else hipLaunchKernelGGL((distill_rows<T, 16, 16>), g, dim3(1024), 0, stream, p);
+        if (pieces <= 256) hipLaunchKernelGGL((distill_rows<T, E, 4, 1>), g, dim3(320), 0, stream, p);
+        else if (pieces <= 512) hipLaunchKernelGGL((distill_rows<T, E, 4, 2>), g, dim3(320), 0, stream, p);
+        else if (pieces <= 1024) hipLaunchKernelGGL((distill_rows<T, E, 4, 4>), g, dim3(320), 0, stream, p);
+        else if (pieces <= 2048) hipLaunchKernelGGL((distill_rows<T, E, 8, 4>), g, dim3(576), 0, stream, p);
+        else if (pieces <= 4096) hipLaunchKernelGGL((distill_rows<T, E, 8, 8>), g, dim3(576), 0, stream, p);
+        else if (pieces <= 8192) hipLaunchKernelGGL((distill_rows<T, E, 8, 16>), g, dim3(576), 0, stream, p);
+        else hipLaunchKernelGGL((distill_rows<T, E, 15, 18>), g, dim3(1024), 0, stream, p);
         return launched();
     }
     p.slices = (int32_t)slices_of<T>(p.V);
     if (p.N > kMaxGrid / p.slices) return GRIM_ERR_SHAPE;
     const dim3 g((unsigned)(p.N * p.slices)), b(64 * (kSliceWaves + 1));
-    hipLaunchKernelGGL(distill_slices<T>, g, b, 0, stream, p);
+    hipLaunchKernelGGL((distill_slices<T, E>), g, b, 0, stream, p);
     const grim_status st = launched();
     if (st != GRIM_OK) return st;
-    hipLaunchKernelGGL(distill_join<T>, g, b, 0, stream, p);
+    hipLaunchKernelGGL((distill_join<T, E>), g, b, 0, stream, p);
     return launched();
+}
+
+// (room for 64 entries where they suffice: it is what a short row's workgroups share a compute unit by)
+template <typename T>
+grim_status distill_typed(const DistillParams &p, hipStream_t stream) {
+    return p.k <= 64 ? distill_launch<T, 64>(p, stream) : distill_launch<T, kMostEntries>(p, stream);
 }
 
 }  // namespace lm

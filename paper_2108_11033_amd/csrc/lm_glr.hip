@@ -61,14 +61,20 @@ __device__ __forceinline__ void compose(float a0, float b0, float &a, float &b) 
 }
 
 // ---------------------------------------------------------------------------------------------- where sequences start
+// The starts of fewer than 64 sequences are kept in a register, one a lane.
 struct Starts {
     const int32_t *seq;
-    int32_t nseq, N;
-    __device__ __forceinline__ int at(int i) const { return seq ? seq[i] : i ? N : 0; }
+    int32_t nseq, N, held;
+    bool in_lanes;
+    __device__ __forceinline__ Starts(const GlrParams &p) : seq(p.seq), nseq(p.nseq), N((int32_t)p.N), held(0), in_lanes(p.nseq < 64) {
+        const int lane = threadIdx.x & 63;
+        if (in_lanes) held = seq ? seq[min(lane, nseq)] : lane ? N : 0;
+    }
+    __device__ __forceinline__ int at(int i) const { return in_lanes ? __builtin_amdgcn_readlane(held, i) : seq[i]; }
     // how many of the starts of sequences 0 .. nseq - 1 lie below `row`; the whole wave asks
     __device__ __forceinline__ int below(int row) const {
-        if (!seq) return row > 0 ? 1 : 0;
         const int lane = threadIdx.x & 63;
+        if (in_lanes) return __popcll(__ballot(lane < nseq && held < row));
         int lo = 0, n = nseq;
         while (n > 64) {
             const int step = (n + 63) / 64;
@@ -131,12 +137,11 @@ struct Rows {
 // ---------------------------------------------------------------------------------------------- maps of the chunks
 // What rows r0 .. r1 - 1 do to the state that enters in front of them.
 template <typename T, int VEC>
-__device__ __forceinline__ void forward_map(const GlrParams &p, const Units<VEC> &un, const Bias<VEC> &bias, int r0, int r1,
+__device__ __forceinline__ void forward_map(const GlrParams &p, const Starts &starts, const Units<VEC> &un, const Bias<VEC> &bias, int r0, int r1,
                                             float (&A)[VEC], float (&B)[VEC]) {
 #pragma unroll
     for (int j = 0; j < VEC; ++j) A[j] = 1.f, B[j] = 0.f;
     if (r0 >= r1) return;
-    const Starts starts{p.seq, p.nseq, (int32_t)p.N};
     int s = starts.below(r0) - 1, bound = starts.at(s + 1);
     for (int g = r0; g < r1; g += kGroup) {
         Rows<T, VEC> u, c;
@@ -171,12 +176,11 @@ __device__ __forceinline__ void forward_map(const GlrParams &p, const Units<VEC>
 
 // What rows r1 - 1 .. r0 do to the gradient R that enters behind them.
 template <typename T, int VEC>
-__device__ __forceinline__ void backward_map(const GlrParams &p, const Units<VEC> &un, const Bias<VEC> &bias, int r0, int r1,
+__device__ __forceinline__ void backward_map(const GlrParams &p, const Starts &starts, const Units<VEC> &un, const Bias<VEC> &bias, int r0, int r1,
                                              float (&A)[VEC], float (&B)[VEC]) {
 #pragma unroll
     for (int j = 0; j < VEC; ++j) A[j] = 1.f, B[j] = 0.f;
     if (r0 >= r1) return;
-    const Starts starts{p.seq, p.nseq, (int32_t)p.N};
     int s = starts.below(r1) - 1;                               // the sequence of row r1 - 1, and where it ends and starts
     int end = s >= 0 ? starts.at(s + 1) : -1, begin = s >= 0 ? starts.at(s) : 0;
     for (int g = r0 + (r1 - 1 - r0) / kGroup * kGroup; g >= r0; g -= kGroup) {
@@ -255,13 +259,14 @@ struct Chunk {
 template <typename T, int VEC, bool BACK>
 __global__ void __launch_bounds__(64 * kWaves, waves_forward<T>()) glr_maps(GlrParams p) {
     __shared__ float maps[kWaves][2][64 * VEC];
+    const Starts starts(p);
     const int set = blockIdx.x / p.tiles;
     const Units<VEC> un(blockIdx.x % p.tiles, p.H);
     const Bias<VEC> bias(p, un.at);
     const Chunk ch(p, set);
     float a[VEC], b[VEC], A[VEC], B[VEC], SA[VEC], SB[VEC];
-    if (BACK) backward_map<T, VEC>(p, un, bias, ch.r0, ch.r1, a, b);
-    else forward_map<T, VEC>(p, un, bias, ch.r0, ch.r1, a, b);
+    if (BACK) backward_map<T, VEC>(p, starts, un, bias, ch.r0, ch.r1, a, b);
+    else forward_map<T, VEC>(p, starts, un, bias, ch.r0, ch.r1, a, b);
     const int place = BACK ? kWaves - 1 - ch.wave : ch.wave;
     compose_chunks<VEC>(maps, place, a, b, A, B, SA, SB);
     if (!un.live) return;
@@ -311,15 +316,25 @@ __device__ __forceinline__ void entering(const GlrParams &p, float (*maps)[2][64
 template <typename T, int VEC, bool ALONE>
 __global__ void __launch_bounds__(64 * kWaves, waves_forward<T>()) glr_forward(GlrParams p) {
     __shared__ float maps[kWaves][2][64 * VEC];
+    const Starts starts(p);
     const int set = ALONE ? 0 : p.sets - 1 - (int)blockIdx.x / p.tiles;
     const Units<VEC> un(blockIdx.x % p.tiles, p.H);
     const Bias<VEC> bias(p, un.at);
     const Chunk ch(p, set);
-    const Starts starts{p.seq, p.nseq, (int32_t)p.N};
+    const int r0 = ch.r0, r1 = ch.r1;
+    Rows<T, VEC> u, c, v;
+    auto fetch = [&](int at) {
+        u.fetch(p.gates, p.ldg, un.at, at, r1 - at);
+        c.fetch(p.gates, p.ldg, p.H + un.at, at, r1 - at);
+        v.fetch(p.gates, p.ldg, 2 * p.H + un.at, at, r1 - at);
+    };
+    // With few rows the first group is on its way while the state is put together; with many, other waves are.
+    constexpr bool early = !ALONE && VEC == 1;
+    if (early && r0 < r1) fetch(r0);
     float h[VEC];
     if (ALONE) {
         float a[VEC], b[VEC], A[VEC], SA[VEC], SB[VEC];
-        forward_map<T, VEC>(p, un, bias, ch.r0, ch.r1, a, b);
+        forward_map<T, VEC>(p, starts, un, bias, ch.r0, ch.r1, a, b);
         compose_chunks<VEC>(maps, ch.wave, a, b, A, h, SA, SB);
     } else {
         entering<VEC>(p, maps, un, ch, set, 0, 1, set, h);
@@ -331,15 +346,11 @@ __global__ void __launch_bounds__(64 * kWaves, waves_forward<T>()) glr_forward(G
                 if (p.h0) take<VEC>(p.h0 + s * p.H + un.at, v);
                 store(p.h_last + s * p.H + un.at, v);
             }
-    const int r0 = ch.r0, r1 = ch.r1;
     if (r0 >= r1) return;
     int s = starts.below(r0) - 1, bound = starts.at(s + 1);
     T *y = static_cast<T *>(p.y) + un.at;
     for (int g = r0; g < r1; g += kGroup) {
-        Rows<T, VEC> u, c, v;
-        u.fetch(p.gates, p.ldg, un.at, g, r1 - g);
-        c.fetch(p.gates, p.ldg, p.H + un.at, g, r1 - g);
-        v.fetch(p.gates, p.ldg, 2 * p.H + un.at, g, r1 - g);
+        if (!early || g > r0) fetch(g);
         if (p.states && un.live) store(p.states + (int64_t)(g / kGroup) * p.H + un.at, h);
 #pragma unroll
         for (int i = 0; i < kGroup; ++i) {
@@ -379,15 +390,15 @@ template <typename T, int VEC, bool ALONE>
 __global__ void __launch_bounds__(64 * kWaves, waves_backward<T>()) glr_backward(GlrParams p) {
     __shared__ float maps[kWaves][2][64 * VEC];
     __shared__ float sums[3][64 * VEC];
+    const Starts starts(p);
     const int set = ALONE ? 0 : p.sets - 1 - (int)blockIdx.x / p.tiles;
     const Units<VEC> un(blockIdx.x % p.tiles, p.H);
     const Bias<VEC> bias(p, un.at);
     const Chunk ch(p, set);
-    const Starts starts{p.seq, p.nseq, (int32_t)p.N};
     float R[VEC];
     if (ALONE) {
         float a[VEC], b[VEC], A[VEC], SA[VEC], SB[VEC];
-        backward_map<T, VEC>(p, un, bias, ch.r0, ch.r1, a, b);
+        backward_map<T, VEC>(p, starts, un, bias, ch.r0, ch.r1, a, b);
         compose_chunks<VEC>(maps, kWaves - 1 - ch.wave, a, b, A, R, SA, SB);
     } else {
         entering<VEC>(p, maps, un, ch, set, p.sets - 1, -1, p.sets - 1 - set, R);

@@ -5,14 +5,16 @@
 //
 // One pass over the logits, bound by memory or, for a caller or two, by the launch.  A workgroup takes a tile of words and
 // callers, counts the histories' words that fall into it in LDS (whole-number atomics: the order cannot matter), and then
-// transforms the tile.  Every tile reads its callers' whole histories again (from L2), which costs less than a table of counts in memory, cleared,
-// filled and read by three launches.
+// transforms the tile.  Every tile reads its callers' whole histories again (from L2), which costs less than a table of counts in
+// memory, cleared, filled and read by three launches.  A word's place in LDS holds its count and, above it, the entry of the bias list
+// that adds to it: four bytes a word, so that a compute unit holds four tiles of 8192.
 #include "lm_common.hpp"
 
 namespace grim {
 namespace lm {
 
-constexpr int kMostBias = 1024;
+constexpr int kMostBias = 1024, kCountBits = 21;              // counts up to 2^21, entries 1 .. 1024
+constexpr int32_t kMostHistory = 1 << 20;
 
 struct RuleParams {
     const void *z;
@@ -23,13 +25,19 @@ struct RuleParams {
 };
 
 struct CallerRules {
-    float repetition, frequency, presence;
+    float repetition, inverse, frequency, presence;
     __device__ __forceinline__ CallerRules(const grim_logit_rules &r, int64_t b)
         : repetition(r.repetition ? r.repetition[b] : 1.f), frequency(r.frequency ? r.frequency[b] : 0.f),
-          presence(r.presence ? r.presence[b] : 0.f) {}
-    __device__ __forceinline__ float apply(float z, uint32_t count, float bias, bool allowed) const {
-        if (count) z = (z > 0.f ? z / repetition : z * repetition) - frequency * (float)count - presence;
-        return allowed ? z + bias : -INFINITY;
+          presence(r.presence ? r.presence[b] : 0.f) {
+        inverse = 1.f / repetition;             // (a product for a division: one rounding of 2^-24 more)
+    }
+    // place: the word's place in LDS; biases: the entries' values
+    __device__ __forceinline__ float apply(float z, uint32_t place, const float *biases, bool allowed) const {
+        const uint32_t count = place & ((1u << kCountBits) - 1), entry = place >> kCountBits;
+        const float said = z * (z > 0.f ? inverse : repetition) - frequency * (float)count - presence;
+        z = count ? said : z;
+        if (entry) z += biases[entry - 1];
+        return allowed ? z : -INFINITY;
     }
 };
 
@@ -55,8 +63,8 @@ struct History {
             for (int j = 0; j < 4; ++j) ids[j] = i + j < most ? h[i + j] : -1;
         }
     }
-    // Words lo .. lo + span - 1 into count[(word - lo) << shift].
-    __device__ __forceinline__ void tally(int lo, int span, uint32_t *count, int shift) {
+    // Counts words lo .. lo + span - 1 at places[(word - lo) << shift].
+    __device__ __forceinline__ void tally(int lo, int span, uint32_t *places, int shift) {
         int32_t ids[4] = {early[0], early[1], early[2], early[3]};
         for (int i = t * 4; i < len; i += width * 4) {
             if (i >= width * 4) take(i, ids);
@@ -64,33 +72,34 @@ struct History {
             for (int j = 0; j < 4; ++j) {
                 // (a word below lo wraps around to a large number; words of 2^31 and more do not exist)
                 const uint32_t at = (uint32_t)ids[j] - (uint32_t)lo;
-                if (i + j < len && ids[j] >= 0 && at < (uint32_t)span) atomicAdd(&count[at << shift], 1u);
+                if (i + j < len && ids[j] >= 0 && at < (uint32_t)span) atomicAdd(&places[at << shift], 1u);
             }
         }
     }
 };
 
-// A caller's biases for words lo .. lo + span - 1 into bias[(word - lo) << shift], by thread t of `width`; `staged`: the list's words.
-__device__ __forceinline__ void add_biases(const grim_logit_rules &r, int64_t b, int lo, int span, const int32_t *staged, float *bias,
-                                           int shift, int t, int width) {
-    const float *values = r.bias_values + b * r.ld_bias;
-    for (int i = t; i < r.nbias; i += width) {
-        const int32_t id = staged[i];
+// A caller's biases for words lo .. lo + span - 1, by thread t of `width`: the first entry of a word notes its number at the
+// word's place and adds up the values of all entries of the word, in the list's order, into sums[entry].
+__device__ __forceinline__ void add_biases(int32_t nbias, const int32_t *ids, const float *values, int lo, int span, uint32_t *places,
+                                           int shift, float *sums, int t, int width) {
+    for (int i = t; i < nbias; i += width) {
+        const int32_t id = ids[i];
         const uint32_t at = (uint32_t)id - (uint32_t)lo;
         if (id < 0 || at >= (uint32_t)span) continue;
         int earlier = 0, alike = 0;
 #pragma unroll 8
-        for (int j = 0; j < r.nbias; ++j) {
-            const int same = staged[j] == id;
+        for (int j = 0; j < nbias; ++j) {
+            const int same = ids[j] == id;
             alike += same;
             earlier += j < i ? same : 0;
         }
-        if (earlier) continue;                                  // the first entry of a word adds up all, in the list's order
+        if (earlier) continue;
         float sum = values[i];
         if (alike > 1)
-            for (int j = i + 1; j < r.nbias; ++j)
-                if (staged[j] == id) sum += values[j];
-        bias[at << shift] = sum;
+            for (int j = i + 1; j < nbias; ++j)
+                if (ids[j] == id) sum += values[j];
+        sums[i] = sum;
+        atomicAdd(&places[at << shift], (uint32_t)(i + 1) << kCountBits);
     }
 }
 
@@ -98,16 +107,15 @@ __device__ __forceinline__ void add_biases(const grim_logit_rules &r, int64_t b,
 template <typename T, int TILE, int THREADS>
 __global__ void __launch_bounds__(THREADS) rules_rows(RuleParams p, int tiles) {
     constexpr int V = 16 / (int)sizeof(T), PER = TILE / (THREADS * V);
-    __shared__ __attribute__((aligned(16))) uint32_t count[TILE];
-    __shared__ __attribute__((aligned(16))) float bias[TILE];
-    __shared__ int32_t staged[kMostBias];
+    __shared__ __attribute__((aligned(16))) uint32_t places[TILE];
+    __shared__ int32_t ids[kMostBias];
+    __shared__ float values[kMostBias];                         // becomes the sums: an entry's value is read for its own word only
     const int64_t b = blockIdx.x / tiles, lo = (int64_t)(blockIdx.x % tiles) * TILE;
     const int64_t hi = lo + TILE < p.V ? lo + TILE : p.V;
     const T *z = static_cast<const T *>(p.z) + b * p.ldz + lo;
     T *out = static_cast<T *>(p.out) + b * p.ldo + lo;
     const int span = (int)(hi - lo);
     History history(p.r, b, threadIdx.x, THREADS);
-    for (int i = threadIdx.x; i < p.r.nbias; i += THREADS) staged[i] = p.r.bias_ids[b * p.r.ld_bias + i];
     const CallerRules rules(p.r, b);
     const uint32_t *allowed = p.r.allowed ? p.r.allowed + b * p.r.ld_allowed + lo / 32 : nullptr;
     Pack<T, V> raw[PER];
@@ -121,10 +129,14 @@ __global__ void __launch_bounds__(THREADS) rules_rows(RuleParams p, int tiles) {
             for (int j = 0; j < V; ++j) put(raw[k], j, c + j < span ? z[c + j] : (T)0.f);
         bits[k] = allowed && c < span ? allowed[c / 32] >> (c % 32) : 0xffffffffu;
     }
-    for (int i = threadIdx.x; i < TILE; i += THREADS) count[i] = 0, bias[i] = 0.f;
+    for (int i = threadIdx.x; i < p.r.nbias; i += THREADS) {
+        ids[i] = p.r.bias_ids[b * p.r.ld_bias + i];
+        values[i] = p.r.bias_values[b * p.r.ld_bias + i];
+    }
+    for (int i = threadIdx.x; i < TILE / 4; i += THREADS) reinterpret_cast<uint4 *>(places)[i] = uint4{0, 0, 0, 0};
     __syncthreads();
-    history.tally((int)lo, span, count, 0);
-    if (p.r.nbias > 0) add_biases(p.r, b, (int)lo, span, staged, bias, 0, threadIdx.x, THREADS);
+    history.tally((int)lo, span, places, 0);
+    add_biases(p.r.nbias, ids, values, (int)lo, span, places, 0, values, threadIdx.x, THREADS);
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
@@ -132,7 +144,7 @@ __global__ void __launch_bounds__(THREADS) rules_rows(RuleParams p, int tiles) {
         if (c >= span) continue;
         float v[V];
 #pragma unroll
-        for (int j = 0; j < V; ++j) v[j] = rules.apply(element(raw[k], j), count[c + j], bias[c + j], bits[k] >> j & 1);
+        for (int j = 0; j < V; ++j) v[j] = rules.apply(element(raw[k], j), places[c + j], values, bits[k] >> j & 1);
         if (c + V <= span) store(out + c, v);
         else
 #pragma unroll
@@ -141,12 +153,14 @@ __global__ void __launch_bounds__(THREADS) rules_rows(RuleParams p, int tiles) {
     }
 }
 
-// A column per caller: TILE >> shift words of up to 1 << shift callers.
+// A column per caller: TILE >> shift words of up to 1 << shift (at most kMostCallers) callers.
+constexpr int kMostCallers = 8;
+
 template <typename T, int TILE, int THREADS>
 __global__ void __launch_bounds__(THREADS) rules_columns(RuleParams p, int tiles, int shift) {
     constexpr int PER = TILE / THREADS;
-    __shared__ uint32_t count[TILE];
-    __shared__ float bias[TILE];
+    __shared__ __attribute__((aligned(16))) uint32_t places[TILE];
+    __shared__ float sums[kMostCallers][kMostBias];
     const int words = TILE >> shift;
     const int64_t b0 = (int64_t)(blockIdx.x / tiles) << shift, lo = (int64_t)(blockIdx.x % tiles) * words;
     const int64_t hi = lo + words < p.V ? lo + words : p.V;
@@ -167,18 +181,19 @@ __global__ void __launch_bounds__(THREADS) rules_columns(RuleParams p, int tiles
         v[k] = (float)z[word * p.ldz];
         bits |= (allowed ? allowed[word / 32] >> (word % 32) & 1 : 1u) << k;
     }
-    for (int i = threadIdx.x; i < TILE; i += THREADS) count[i] = 0, bias[i] = 0.f;
+    for (int i = threadIdx.x; i < TILE / 4; i += THREADS) reinterpret_cast<uint4 *>(places)[i] = uint4{0, 0, 0, 0};
     __syncthreads();
     const int lane = threadIdx.x & 63;
     for (int b = threadIdx.x >> 6; b < callers; b += THREADS / 64) {          // a wave per caller
-        History(p.r, b0 + b, lane, 64).tally((int)lo, span, count + b, shift);
-        if (p.r.nbias > 0) add_biases(p.r, b0 + b, (int)lo, span, p.r.bias_ids + (b0 + b) * p.r.ld_bias, bias + b, shift, lane, 64);
+        History(p.r, b0 + b, lane, 64).tally((int)lo, span, places + b, shift);
+        const int64_t list = (b0 + b) * p.r.ld_bias;
+        add_biases(p.r.nbias, p.r.bias_ids + list, p.r.bias_values + list, (int)lo, span, places + b, shift, sums[b], lane, 64);
     }
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
         const int i = k * THREADS + (int)threadIdx.x, at = i >> shift;
-        if (live && at < span) out[(lo + at) * p.ldo] = (T)rules.apply(v[k], count[i], bias[i], bits >> k & 1);
+        if (live && at < span) out[(lo + at) * p.ldo] = (T)rules.apply(v[k], places[i], sums[mine], bits >> k & 1);
     }
 }
 
@@ -186,21 +201,28 @@ template <typename T, int TILE, int THREADS>
 grim_status rules_launch(const RuleParams &p, bool columns, hipStream_t stream) {
     int shift = 0;
     if (columns)
-        while (shift < 3 && (1 << shift) < p.batch) ++shift;    // up to 8 callers: 16 or 32 bytes of a row
+        while ((1 << shift) < kMostCallers && (1 << shift) < p.batch) ++shift;    // 16 or 32 bytes of a row
     const int64_t words = TILE >> shift, tiles = (p.V + words - 1) / words;
     const int64_t grid = tiles * ((p.batch + (1 << shift) - 1) >> shift);
     if (grid > kMaxGrid) return GRIM_ERR_SHAPE;
-    if (columns) hipLaunchKernelGGL((rules_columns<T, TILE, THREADS>), dim3((unsigned)grid), dim3(THREADS), 0, stream, p, (int)tiles, shift);
-    else hipLaunchKernelGGL((rules_rows<T, TILE, THREADS>), dim3((unsigned)grid), dim3(THREADS), 0, stream, p, (int)tiles);
+    if constexpr (TILE <= 4096) {
+        if (columns) {
+            hipLaunchKernelGGL((rules_columns<T, TILE, THREADS>), dim3((unsigned)grid), dim3(THREADS), 0, stream, p, (int)tiles, shift);
+            return launched();
+        }
+    }
+    if constexpr (TILE != 4096)
+        hipLaunchKernelGGL((rules_rows<T, TILE, THREADS>), dim3((unsigned)grid), dim3(THREADS), 0, stream, p, (int)tiles);
     return launched();
 }
 
-// Tiles of 4096 words and callers; of 2048 where those would leave compute units without one.
+// Tiles of 8192 places (4096 in columns, whose callers' sums take their share of LDS); of 2048 where those would leave compute
+// units without one.
 template <typename T>
 grim_status rules_typed(const RuleParams &p, bool columns, hipStream_t stream) {
     if (p.batch == 1 && p.ldz == 1 && p.ldo == 1) columns = false;   // a single dense column is a row
-    return p.V * p.batch >= (int64_t)4096 * kComputeUnits ? rules_launch<T, 4096, 512>(p, columns, stream)
-                                                          : rules_launch<T, 2048, 256>(p, columns, stream);
+    if (p.V * p.batch < (int64_t)4096 * kComputeUnits) return rules_launch<T, 2048, 256>(p, columns, stream);
+    return columns ? rules_launch<T, 4096, 512>(p, true, stream) : rules_launch<T, 8192, 512>(p, false, stream);
 }
 
 }  // namespace lm
@@ -211,14 +233,13 @@ extern "C" grim_status grim_apply_logit_rules(const void *z_dev, grim_dtype dt, 
     using namespace grim::lm;
     if (!rules) return GRIM_ERR_NULL;
     if (!known(dt)) return GRIM_ERR_DTYPE;
-    if (V < 1 || V >= (int64_t)1 << 31 || batch < 0 || rules->max_history < 0 || rules->max_history > 1 << 30 ||
-        rules->nbias < 0) return GRIM_ERR_SHAPE;
+    if (V < 1 || V >= (int64_t)1 << 31 || batch < 0 || rules->max_history < 0 || rules->nbias < 0) return GRIM_ERR_SHAPE;
     const int64_t width = columns ? batch : V, rows = columns ? V : batch;
     if (ldz < width || ldo < width || !fits(rows, ldz) || !fits(rows, ldo)) return GRIM_ERR_SHAPE;
     if (rules->history && (rules->ld_history < rules->max_history || !fits(batch, rules->ld_history))) return GRIM_ERR_SHAPE;
     if (rules->nbias > 0 && (rules->ld_bias < rules->nbias || !fits(batch, rules->ld_bias))) return GRIM_ERR_SHAPE;
     if (rules->allowed && (rules->ld_allowed < (V + 31) / 32 || !fits(batch, rules->ld_allowed))) return GRIM_ERR_SHAPE;
-    if (rules->nbias > kMostBias) return GRIM_ERR_UNSUPPORTED;
+    if (rules->nbias > kMostBias || (rules->history && rules->max_history > kMostHistory)) return GRIM_ERR_UNSUPPORTED;
     if (rules->nbias > 0 && (!rules->bias_ids || !rules->bias_values)) return GRIM_ERR_NULL;
     if (batch == 0) return GRIM_OK;
     if (!z_dev || !out_dev) return GRIM_ERR_NULL;

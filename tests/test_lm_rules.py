@@ -144,9 +144,10 @@ def test_refusals():
     assert name(z=None) == "GRIM_ERR_NULL" and name(out=None) == "GRIM_ERR_NULL"
     assert name(nbias=3, ld_bias=3) == "GRIM_ERR_NULL"
     for kw in [dict(ldz=63), dict(ldo=63), dict(V=0), dict(V=2 ** 31, ldz=2 ** 31, ldo=2 ** 31), dict(batch=-1), dict(columns=True, ldz=1),
-               dict(history=768, ld_history=4, max_history=5), dict(history=768, max_history=-1), dict(history=768, max_history=2 ** 30 + 1, ld_history=2 ** 31),
+               dict(history=768, ld_history=4, max_history=5), dict(history=768, max_history=-1),
                dict(nbias=-1), dict(nbias=4, ld_bias=3, bias_ids=768, bias_values=1024), dict(allowed=768, ld_allowed=1), dict(ldz=2 ** 60)]:
         assert name(**kw) == "GRIM_ERR_SHAPE", kw
     assert name(nbias=1025, ld_bias=1025, bias_ids=768, bias_values=1024) == "GRIM_ERR_UNSUPPORTED"
+    assert name(history=768, max_history=2 ** 20 + 1, ld_history=2 ** 21) == "GRIM_ERR_UNSUPPORTED"
     from paper_2108_11033_amd import lm
     assert lm._lib().grim_apply_logit_rules(256, 0, 0, 64, 64, 2, None, 512, 64, None) == 1              # GRIM_ERR_NULL: no rules
