@@ -41,8 +41,8 @@ struct Entries {
     static __device__ __forceinline__ int slot(int32_t id) { return (int)((uint32_t)id * 2654435761u >> (32 - kBits)); }
 };
 
-// Formed by one wave.  z is read at the words lo .. hi - 1 (0 elsewhere).
-template <int E, typename T>
+// Formed by one wave.  z is read at the words lo .. hi - 1 (0 elsewhere).  SUMS: words listed twice are looked for.
+template <bool SUMS, int E, typename T>
 __device__ __forceinline__ void teacher(const DistillParams &p, int64_t n, const T *z, int64_t lo, int64_t hi, Entries<E> &e) {
     const int lane = threadIdx.x & 63;
     const float *t = p.top + n * p.ldt;
@@ -79,9 +79,11 @@ __device__ __forceinline__ void teacher(const DistillParams &p, int64_t n, const
     for (int i = lane; i < p.k; i += 64) {
         const float x = s > 0.f ? e.p[i] * r : s;                        // (s: 0, or NaN)
         e.p[i] = x;
+        if (!SUMS) continue;
         e.sum[i] = x;
         if (e.id[i] >= 0) e.table[e.slot(e.id[i])] = (uint16_t)i;
     }
+    if (!SUMS) return;
     __builtin_amdgcn_wave_barrier();
     __threadfence_block();
     for (int i0 = 0; i0 < p.k; i0 += 64) {
@@ -155,7 +157,7 @@ __global__ void __launch_bounds__(64 * (W + 1)) distill_rows(DistillParams p) {
     Pack<T, V> raw[PER];
     float peak = -INFINITY, sum = 0.f;
     if (aside) {
-        teacher(p, n, z, 0, p.V, e);
+        teacher<true>(p, n, z, 0, p.V, e);
         __syncthreads();
         __syncthreads();
         for (int w = 0; w < W; ++w) peak = fmaxf(peak, room[0][w]), sum += room[1][w];
@@ -259,7 +261,7 @@ __global__ void __launch_bounds__(64 * (kSliceWaves + 1)) distill_slices(Distill
     const int64_t lo = s * slice_elements<T>(), hi = lo + slice_elements<T>() < p.V ? lo + slice_elements<T>() : p.V;
     if (threadIdx.x >= 64 * W) {
         const int lane = threadIdx.x & 63;
-        teacher(p, n, z, lo, hi, e);
+        teacher<false>(p, n, z, lo, hi, e);
         __syncthreads();
         __syncthreads();
         float peak = -INFINITY, sum = 0.f;
@@ -336,7 +338,7 @@ __global__ void __launch_bounds__(64 * (kSliceWaves + 1)) distill_join(DistillPa
     }
     if (aside) {
         // (z of this slice only: other slices' places may hold their gradient already, where dz is z)
-        teacher(p, n, z, lo, hi, e);
+        teacher<true>(p, n, z, lo, hi, e);
         if (s == 0) {
             // log2 q = (z - base_i) scale + (base_i - peak) scale - log2 sum
             const float extra = log2f(sum) - log2f(e.total);
@@ -399,12 +401,13 @@ grim_status distill_launch(DistillParams p, hipStream_t stream) {
         if (p.N > kMaxGrid) return GRIM_ERR_SHAPE;
         const dim3 g((unsigned)p.N);
         const int64_t pieces = (p.V + piece<T>() - 1) / piece<T>();
-        if (pieces <= 256) hipLaunchKernelGGL((distill_rows<T, E, 4, 1>), g, dim3(320), 0, stream, p);
-        else if (pieces <= 512) hipLaunchKernelGGL((distill_rows<T, E, 4, 2>), g, dim3(320), 0, stream, p);
-        else if (pieces <= 1024) hipLaunchKernelGGL((distill_rows<T, E, 4, 4>), g, dim3(320), 0, stream, p);
-        else if (pieces <= 2048) hipLaunchKernelGGL((distill_rows<T, E, 8, 4>), g, dim3(576), 0, stream, p);
-        else if (pieces <= 4096) hipLaunchKernelGGL((distill_rows<T, E, 8, 8>), g, dim3(576), 0, stream, p);
-        else if (pieces <= 8192) hipLaunchKernelGGL((distill_rows<T, E, 8, 16>), g, dim3(576), 0, stream, p);
+        // (4, 8 or 16 waves with the teacher's)
+        if (pieces <= 384) hipLaunchKernelGGL((distill_rows<T, E, 3, 2>), g, dim3(256), 0, stream, p);
+        else if (pieces <= 768) hipLaunchKernelGGL((distill_rows<T, E, 3, 4>), g, dim3(256), 0, stream, p);
+        else if (pieces <= 1792) hipLaunchKernelGGL((distill_rows<T, E, 7, 4>), g, dim3(512), 0, stream, p);
+        else if (pieces <= 2688) hipLaunchKernelGGL((distill_rows<T, E, 7, 6>), g, dim3(512), 0, stream, p);
+        else if (pieces <= 4480) hipLaunchKernelGGL((distill_rows<T, E, 7, 10>), g, dim3(512), 0, stream, p);
+        else if (pieces <= 8064) hipLaunchKernelGGL((distill_rows<T, E, 7, 18>), g, dim3(512), 0, stream, p);
         else hipLaunchKernelGGL((distill_rows<T, E, 15, 18>), g, dim3(1024), 0, stream, p);
         return launched();
     }

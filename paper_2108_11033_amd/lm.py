@@ -7,16 +7,12 @@ Argument marshalling only, as in binding.py: device buffers are anything with a 
 from __future__ import annotations
 
 import ctypes
+import struct
 
 from .binding import _DT_CODE, GrimError, _addr, _stream, load_library
 
-class LogitRules(ctypes.Structure):
-    _fields_ = [("history", ctypes.c_void_p), ("history_len", ctypes.c_void_p), ("ld_history", ctypes.c_int64),
-                ("max_history", ctypes.c_int32), ("nbias", ctypes.c_int32),
-                ("repetition", ctypes.c_void_p), ("frequency", ctypes.c_void_p), ("presence", ctypes.c_void_p),
-                ("bias_ids", ctypes.c_void_p), ("bias_values", ctypes.c_void_p), ("ld_bias", ctypes.c_int64),
-                ("allowed", ctypes.c_void_p), ("ld_allowed", ctypes.c_int64)]
-
+# struct grim_logit_rules
+_RULES = struct.Struct("@PPqiiPPPPPqPq")
 
 _I64, _I32, _P, _F = ctypes.c_int64, ctypes.c_int32, ctypes.c_void_p, ctypes.c_float
 ARGTYPES = {
@@ -30,7 +26,7 @@ ARGTYPES = {
     "grim_glr_step": [_P, _I64, _P, _P, _I64, _P, _I64, _P, _I32, _I64, _I64, _I32, _P],
     "grim_distill_topk_workspace": [_I64, _I64],
     "grim_distill_topk": [_P, _I32, _I64, _P, _P, _I32, _I64, _F, _P, _I64, _I64, _P, _P, _I64, _P, _I64, _P],
-    "grim_apply_logit_rules": [_P, _I32, _I32, _I64, _I64, _I32, ctypes.POINTER(LogitRules), _P, _I64, _P],
+    "grim_apply_logit_rules": [_P, _I32, _I32, _I64, _I64, _I32, _P, _P, _I64, _P],
 }
 
 
@@ -159,9 +155,9 @@ def logit_rules(z, dtype, ldz: int, V: int, batch: int, out, ldo: int, *, column
                 max_history: int = 0, history_len=None, repetition=None, frequency=None, presence=None, bias_ids=None,
                 bias_values=None, nbias: int = 0, ld_bias: int = 0, allowed=None, ld_allowed: int = 0, stream=None):
     """grim_apply_logit_rules: enqueue repetition, frequency and presence penalties, biases and the grammar's mask."""
-    rules = LogitRules(_at(history), _at(history_len), ld_history, max_history, nbias, _at(repetition), _at(frequency),
-                       _at(presence), _at(bias_ids), _at(bias_values), ld_bias, _at(allowed), ld_allowed)
-    status = _c.grim_apply_logit_rules(_at(z), _DT_CODE[dtype], int(bool(columns)), ldz, V, batch, ctypes.byref(rules), _at(out),
-                                       ldo, _on(stream))
+    rules = _RULES.pack(_at(history) or 0, _at(history_len) or 0, ld_history, max_history, nbias, _at(repetition) or 0,
+                        _at(frequency) or 0, _at(presence) or 0, _at(bias_ids) or 0, _at(bias_values) or 0, ld_bias,
+                        _at(allowed) or 0, ld_allowed)
+    status = _c.grim_apply_logit_rules(_at(z), _DT_CODE[dtype], 1 if columns else 0, ldz, V, batch, rules, _at(out), ldo, _on(stream))
     if status:
         raise GrimError(status, "grim_apply_logit_rules")
