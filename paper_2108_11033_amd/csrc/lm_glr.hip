@@ -21,10 +21,13 @@ namespace lm {
 
 constexpr int kWaves = 8;       // waves, and chunks, of a workgroup
 // Waves per SIMD that the kernels are held to: what the loads of a group of rows leave room for.  Waves that wait for each other's
-// loads hide more than a second group in flight per wave does (forward 125 against 112 us, backward 247 against 220, at
-// 65536 x 1024 bf16).
-template <typename T> constexpr int waves_forward() { return sizeof(T) == 2 ? 8 : 6; }
-template <typename T> constexpr int waves_backward() { return sizeof(T) == 2 ? 4 : 2; }
+// loads hide more than a second group in flight per wave does (at 65536 x 1024 bf16: forward 125 against 112 us, backward 247
+// against 212).
+template <int VEC> constexpr int waves_forward() { return VEC == 1 ? 8 : 6; }
+constexpr int kWavesBackward = 4;
+// Units of a lane where there are rows enough: 4 bytes, 256 of a row per wave.  (bf16, both directions: 65536 x 1024 555 us with one
+// unit, 479 with two, 490 with four; fp32: 896 with one, 903 with two.)
+template <typename T> constexpr int wide() { return sizeof(T) == 2 ? 2 : 1; }
 constexpr int kGroup = 8;       // rows whose loads are in flight together, and between two saved states
 constexpr float kLog2e = 1.44269504088896340736f;
 
@@ -257,7 +260,7 @@ struct Chunk {
 };
 
 template <typename T, int VEC, bool BACK>
-__global__ void __launch_bounds__(64 * kWaves, waves_forward<T>()) glr_maps(GlrParams p) {
+__global__ void __launch_bounds__(64 * kWaves, waves_forward<VEC>()) glr_maps(GlrParams p) {
     __shared__ float maps[kWaves][2][64 * VEC];
     const Starts starts(p);
     const int set = blockIdx.x / p.tiles;
@@ -293,7 +296,7 @@ __device__ __forceinline__ void entering(const GlrParams &p, float (*maps)[2][64
     for (int j = 0; j < VEC; ++j) a[j] = 1.f, b[j] = 0.f;
     const int per = (ahead + kWaves - 1) / kWaves;
     const int from = min(ch.wave * per, ahead), to = min(from + per, ahead);
-#pragma unroll 4
+#pragma unroll 8
     for (int i = from; i < to; ++i) {
         const float *m = p.set_maps + (int64_t)(first + dir * i) * 2 * p.H + un.at;
         float na[VEC], nb[VEC];
@@ -314,7 +317,7 @@ __device__ __forceinline__ void entering(const GlrParams &p, float (*maps)[2][64
 // ---------------------------------------------------------------------------------------------- forward
 // ALONE: one set holds all rows, and its workgroup forms the maps of its chunks itself.
 template <typename T, int VEC, bool ALONE>
-__global__ void __launch_bounds__(64 * kWaves, waves_forward<T>()) glr_forward(GlrParams p) {
+__global__ void __launch_bounds__(64 * kWaves, waves_forward<VEC>()) glr_forward(GlrParams p) {
     __shared__ float maps[kWaves][2][64 * VEC];
     const Starts starts(p);
     const int set = ALONE ? 0 : p.sets - 1 - (int)blockIdx.x / p.tiles;
@@ -387,7 +390,7 @@ __global__ void __launch_bounds__(64 * kWaves, waves_forward<T>()) glr_forward(G
 
 // ---------------------------------------------------------------------------------------------- backward
 template <typename T, int VEC, bool ALONE>
-__global__ void __launch_bounds__(64 * kWaves, waves_backward<T>()) glr_backward(GlrParams p) {
+__global__ void __launch_bounds__(64 * kWaves, kWavesBackward) glr_backward(GlrParams p) {
     __shared__ float maps[kWaves][2][64 * VEC];
     __shared__ float sums[3][64 * VEC];
     const Starts starts(p);
@@ -547,20 +550,22 @@ __global__ void __launch_bounds__(256) glr_step_kernel(GlrStepParams p) {
 }
 
 // ---------------------------------------------------------------------------------------------- launches
-// How the rows are cut.  Chunks as short as give some 1024 workgroups (four per compute unit, so that they even out), but
-// of no more than 128 sets, whose maps every workgroup reads, and no shorter than a group.
+// How the rows are cut.  Chunks as short as give some 1024 workgroups (four per compute unit, so that they even out), but no
+// shorter than keep the maps of the sets, all of which a workgroup may have to read, within its own rows' size (rows^2 = N / 64:
+// 64000 x 128 bf16, both directions, 80 us in 250 sets of 32 rows a wave, 92 in 500 and 97 in 125), nor than a group.
 struct Cut {
     int vec;
     int32_t L, sets, tiles;
 };
 
-inline Cut cut_rows(int64_t N, int64_t H) {
+inline Cut cut_rows(int64_t N, int64_t H, int wide) {
     Cut c;
-    // one unit a lane where two would leave compute units without a workgroup
-    c.vec = H >= 2 && N * H >= (int64_t)1 << 20 ? 2 : 1;
+    // one unit a lane where more would leave compute units without work (1024 x 1024 bf16 24 against 27 us, 2048 x 1024 31 against 30)
+    c.vec = H >= 256 && N * H >= (int64_t)1 << 21 ? wide : 1;
     c.tiles = (int32_t)((H + 64 * c.vec - 1) / (64 * c.vec));
-    const int64_t even = (N * c.tiles + kWaves * 1024 - 1) / (kWaves * 1024), few = (N + kWaves * 128 - 1) / (kWaves * 128);
-    int64_t L = even > few ? even : few;
+    const int64_t even = (N * c.tiles + kWaves * 1024 - 1) / (kWaves * 1024);
+    int64_t L = (int64_t)__builtin_sqrt((double)N / 64.0);
+    L = even > L ? even : L;
     if (N <= 2 * kWaves * kGroup) L = (N + kWaves - 1) / kWaves;          // one set, one launch
     L = (L + kGroup - 1) / kGroup * kGroup;
     c.L = (int32_t)(L < kGroup ? kGroup : L);
@@ -568,6 +573,8 @@ inline Cut cut_rows(int64_t N, int64_t H) {
     c.sets = N > 0 ? (int32_t)((N + rows - 1) / rows) : 1;
     return c;
 }
+
+inline int wide_of(grim_dtype dt) { return dt == GRIM_F32 ? wide<float>() : wide<f16>(); }
 
 inline int64_t map_floats(const Cut &c, int64_t H) { return ((int64_t)c.sets * (kWaves + 1)) * 2 * H; }
 
@@ -589,18 +596,18 @@ grim_status glr_launch(const GlrParams &p, const Cut &c, bool back, hipStream_t 
 }
 
 grim_status glr_run(GlrParams p, grim_dtype dt, bool back, hipStream_t stream) {
-    const Cut c = cut_rows(p.N, p.H);
+    const Cut c = cut_rows(p.N, p.H, wide_of(dt));
     p.L = c.L, p.sets = c.sets, p.tiles = c.tiles;
     p.set_maps = p.chunk_maps + (int64_t)c.sets * kWaves * 2 * p.H;
     switch (dt) {
-        case GRIM_F32: return c.vec == 2 ? glr_launch<float, 2>(p, c, back, stream) : glr_launch<float, 1>(p, c, back, stream);
-        case GRIM_F16: return c.vec == 2 ? glr_launch<f16, 2>(p, c, back, stream) : glr_launch<f16, 1>(p, c, back, stream);
-        default: return c.vec == 2 ? glr_launch<bf16, 2>(p, c, back, stream) : glr_launch<bf16, 1>(p, c, back, stream);
+        case GRIM_F32: return c.vec > 1 ? glr_launch<float, wide<float>()>(p, c, back, stream) : glr_launch<float, 1>(p, c, back, stream);
+        case GRIM_F16: return c.vec > 1 ? glr_launch<f16, wide<f16>()>(p, c, back, stream) : glr_launch<f16, 1>(p, c, back, stream);
+        default: return c.vec > 1 ? glr_launch<bf16, wide<bf16>()>(p, c, back, stream) : glr_launch<bf16, 1>(p, c, back, stream);
     }
 }
 
 inline bool glr_sizes(int64_t N, int64_t H, int32_t nseq, const int32_t *seq) {
-    // (row numbers in 32 bits with room for a group more; at most 128 sets of 2^15 column blocks)
+    // (row numbers in 32 bits with room for a group more; at most 2^15 sets of 2^15 column blocks)
     return N >= 0 && N <= (int64_t)1 << 30 && H >= 1 && H <= (int64_t)1 << 21 && nseq >= 1 && (seq || nseq == 1);
 }
 
@@ -617,8 +624,13 @@ int64_t grim_glr_states(int64_t N, int64_t H) {
 int64_t grim_glr_workspace(int64_t N, int64_t H) {
     using namespace grim::lm;
     if (!glr_sizes(N, H, 1, nullptr)) return 0;
-    const Cut c = cut_rows(N, H);
-    return (map_floats(c, H) + (int64_t)c.sets * 3 * H) * (int64_t)sizeof(float);
+    int64_t most = 0;                                           // (whichever type comes)
+    for (int w : {wide<float>(), wide<f16>()}) {
+        const Cut c = cut_rows(N, H, w);
+        const int64_t floats = map_floats(c, H) + (int64_t)c.sets * 3 * H;
+        most = floats > most ? floats : most;
+    }
+    return most * (int64_t)sizeof(float);
 }
 
 grim_status grim_glr_sequence(const void *gates_dev, grim_dtype dt, int64_t ldg, const float *bias_dev, const float *h0_dev,
@@ -650,7 +662,7 @@ grim_status grim_glr_sequence_backward(const void *gates_dev, grim_dtype dt, int
         return GRIM_ERR_SHAPE;
     if ((N > 0 && (!gates_dev || !states_dev || !dy_dev || !dgates_dev)) || !workspace) return GRIM_ERR_NULL;
     if (workspace_bytes < grim_glr_workspace(N, H)) return GRIM_ERR_SHAPE;
-    const Cut c = cut_rows(N, H);
+    const Cut c = cut_rows(N, H, wide_of(dt));
     GlrParams p{};
     p.gates = gates_dev, p.bias = bias_dev, p.h0 = h0_dev, p.seq = seq_start_dev, p.nseq = nseq;
     p.states = static_cast<float *>(const_cast<void *>(states_dev));
