@@ -31,27 +31,31 @@ struct CallerRules {
           presence(r.presence ? r.presence[b] : 0.f) {
         inverse = 1.f / repetition;             // (a product for a division: one rounding of 2^-24 more)
     }
-    // place: the word's place in LDS; biases: the entries' values
+    // place: the word's place in LDS; biases: the entries' values.  Most words are in no list: the arithmetic is skipped where that holds
+    // for all of a wave's.
     __device__ __forceinline__ float apply(float z, uint32_t place, const float *biases, bool allowed) const {
-        const uint32_t count = place & ((1u << kCountBits) - 1), entry = place >> kCountBits;
-        const float said = z * (z > 0.f ? inverse : repetition) - frequency * (float)count - presence;
-        z = count ? said : z;
-        if (entry) z += biases[entry - 1];
+        if (__any(place != 0)) {
+            const uint32_t count = place & ((1u << kCountBits) - 1), entry = place >> kCountBits;
+            const float said = z * (z > 0.f ? inverse : repetition) - frequency * (float)count - presence;
+            z = count ? said : z;
+            if (entry) z += biases[entry - 1];
+        }
         return allowed ? z : -INFINITY;
     }
 };
 
-// A caller's history, walked by a team of `width` threads (this one is number t): its length and the first four words of each
+// A caller's history, walked by a team of `width` threads (this one is number t): its length and the first eight words of each
 // thread are asked for before anything else (up to the most that a history may hold, so that they need not wait for the length).
 struct History {
     const int32_t *h;
     int most, len, t, width;
-    int32_t early[4];
+    int32_t early[2][4];
     __device__ __forceinline__ History(const grim_logit_rules &r, int64_t b, int t_, int width_) : t(t_), width(width_) {
         most = r.history ? r.max_history : 0;
         h = r.history + b * r.ld_history;
         len = most > 0 && r.history_len ? min(max(r.history_len[b], 0), most) : most;
-        take(t * 4, early);
+        take(t * 4, early[0]);
+        take((width + t) * 4, early[1]);
     }
     __device__ __forceinline__ void take(int i, int32_t (&ids)[4]) const {
         if (i + 4 <= most) {
@@ -65,15 +69,22 @@ struct History {
     }
     // Counts words lo .. lo + span - 1 at places[(word - lo) << shift].
     __device__ __forceinline__ void tally(int lo, int span, uint32_t *places, int shift) {
-        int32_t ids[4] = {early[0], early[1], early[2], early[3]};
-        for (int i = t * 4; i < len; i += width * 4) {
-            if (i >= width * 4) take(i, ids);
+        const auto count = [&](int i, const int32_t (&ids)[4]) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 // (a word below lo wraps around to a large number; words of 2^31 and more do not exist)
                 const uint32_t at = (uint32_t)ids[j] - (uint32_t)lo;
                 if (i + j < len && ids[j] >= 0 && at < (uint32_t)span) atomicAdd(&places[at << shift], 1u);
             }
+        };
+        count(t * 4, early[0]);
+        count((width + t) * 4, early[1]);
+        for (int i = (2 * width + t) * 4; i < len; i += 2 * width * 4) {
+            int32_t a[4], b[4];
+            take(i, a);
+            take(i + width * 4, b);
+            count(i, a);
+            count(i + width * 4, b);
         }
     }
 };
