@@ -1,0 +1,238 @@
+"""A small recurrent language model with pruned layers: retrained from its dense teacher's top logits, then served token by
+token -- the operators of include/grim_lm.h with the BCR products between them.
+
+    embedding -> [ layer norm -> gate product (3H x H) -> gated linear recurrence -> output product (H x H) -> + ] x layers
+              -> layer norm -> head product (V x H) -> logits
+
+Training keeps a dense copy of the weights under their masks (PyTorch's matrix products on rows of tokens); serving packs
+what the masks keep and runs everything in columns, one per caller, as grim_bcr_spmv leaves it.
+
+    python -m paper_2108_11033_amd.recurrent_lm            # a teacher, a student pruned 4x, 60 steps of distillation, some text
+"""
+from __future__ import annotations
+
+import numpy as np
+import torch
+
+from . import binding, lm
+
+EPS = 1e-5
+DTYPES = {torch.float32: "f32", torch.float16: "f16", torch.bfloat16: "bf16"}
+
+
+def _scratch(n: int, device) -> torch.Tensor:
+    return torch.empty((max(1, n),), dtype=torch.uint8, device=device)
+
+
+# ---------------------------------------------------------------------------------------------- training
+class LayerNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, gamma, beta):
+        x = x.contiguous()
+        N, C = x.shape
+        y, mean, rstd = torch.empty_like(x), x.new_empty(N, dtype=torch.float32), x.new_empty(N, dtype=torch.float32)
+        lm.layer_norm(x, DTYPES[x.dtype], C, gamma, beta, EPS, N, C, y, C, mean, rstd, torch.cuda.current_stream())
+        ctx.save_for_backward(x, gamma, mean, rstd)
+        return y
+
+    @staticmethod
+    def backward(ctx, dy):
+        x, gamma, mean, rstd = ctx.saved_tensors
+        N, C = x.shape
+        dx, dgamma, dbeta = torch.empty_like(x), torch.empty_like(gamma), torch.empty_like(gamma)
+        lm.layer_norm_backward(dy.contiguous(), C, x, C, DTYPES[x.dtype], gamma, mean, rstd, N, C, dx, C, dgamma, dbeta,
+                               _scratch(lm.layer_norm_workspace(N, C), x.device), torch.cuda.current_stream())
+        return dx, dgamma, dbeta
+
+
+class GatedRecurrence(torch.autograd.Function):
+    """(outputs, last states) of packed sequences; seq_start is an int32 tensor of their starts and the end."""
+
+    @staticmethod
+    def forward(ctx, gates, bias, h0, seq_start):
+        gates = gates.contiguous()
+        N, H = gates.shape[0], gates.shape[1] // 3
+        y, h_last = gates.new_empty(N, H), torch.empty_like(h0)
+        states = _scratch(lm.glr_states(N, H), gates.device)
+        lm.glr_sequence(gates, DTYPES[gates.dtype], 3 * H, bias, h0, seq_start, h0.shape[0], N, H, y, H, h_last, states,
+                        _scratch(lm.glr_workspace(N, H), gates.device), torch.cuda.current_stream())
+        ctx.save_for_backward(gates, bias, h0, seq_start, states)
+        return y, h_last
+
+    @staticmethod
+    def backward(ctx, dy, dh_last):
+        gates, bias, h0, seq_start, states = ctx.saved_tensors
+        N, H = gates.shape[0], gates.shape[1] // 3
+        dgates, dbias, dh0 = torch.empty_like(gates), torch.empty_like(bias), torch.empty_like(h0)
+        lm.glr_sequence_backward(gates, DTYPES[gates.dtype], 3 * H, bias, h0, seq_start, h0.shape[0], N, H, states, dy.contiguous(), H,
+                                 dh_last.contiguous(), dgates, 3 * H, dbias, dh0, _scratch(lm.glr_workspace(N, H), gates.device),
+                                 torch.cuda.current_stream())
+        return dgates, dbias, dh0, None
+
+
+class DistillTopK(torch.autograd.Function):
+    """The sum over rows of weight times the distillation loss.  The gradient is formed with the loss, in one pass over the logits."""
+
+    @staticmethod
+    def forward(ctx, logits, top_logits, top_ids, temperature, weight):
+        logits = logits.contiguous()
+        N, V = logits.shape
+        loss, dz = logits.new_empty(N, dtype=torch.float32), torch.empty_like(logits)
+        lm.distill_topk(logits, DTYPES[logits.dtype], V, top_logits, top_ids, top_ids.shape[1], top_ids.shape[1], temperature, weight, N, V,
+                        loss, dz, V, _scratch(lm.distill_topk_workspace(N, V), logits.device), torch.cuda.current_stream())
+        ctx.save_for_backward(dz)
+        return loss.sum()
+
+    @staticmethod
+    def backward(ctx, upstream):
+        return ctx.saved_tensors[0] * upstream, None, None, None, None
+
+
+class RecurrentLM(torch.nn.Module):
+    """Dense weights, each product's under a mask of ones and zeros (all ones until prune())."""
+
+    def __init__(self, vocabulary: int, units: int, layers: int, seed: int = 0):
+        super().__init__()
+        gen = torch.Generator().manual_seed(seed)
+        rand = lambda *shape: torch.nn.Parameter(torch.randn(shape, generator=gen) / shape[-1] ** 0.5)
+        self.units, self.layers = units, layers
+        self.embedding = torch.nn.Parameter(torch.randn((vocabulary, units), generator=gen))
+        self.gates = torch.nn.ParameterList([rand(3 * units, units) for _ in range(layers)])
+        self.outs = torch.nn.ParameterList([rand(units, units) for _ in range(layers)])
+        bias = torch.zeros(3 * units)
+        bias[:units] = 2.0                                     # forget gates start mostly open
+        self.biases = torch.nn.ParameterList([torch.nn.Parameter(bias.clone()) for _ in range(layers)])
+        self.gammas = torch.nn.ParameterList([torch.nn.Parameter(torch.ones(units)) for _ in range(layers + 1)])
+        self.betas = torch.nn.ParameterList([torch.nn.Parameter(torch.zeros(units)) for _ in range(layers + 1)])
+        self.head = rand(vocabulary, units)
+        self.blocks = {}                                       # name of a product -> (BR, BC, kept rows, kept columns) per block
+
+    def products(self):
+        return {**{f"gates{i}": w for i, w in enumerate(self.gates)}, **{f"outs{i}": w for i, w in enumerate(self.outs)}, "head": self.head}
+
+    def prune(self, BR: int, BC: int, kr: int, kc: int):
+        """Keeps, in every BR x BC block of every product, the kr rows and then the kc columns of the largest norms."""
+        for name, w in self.products().items():
+            M, K = w.shape
+            sq = w.detach().float().view(M // BR, BR, K // BC, BC).permute(0, 2, 1, 3).square()      # strip, column block, row, column
+            rows = sq.sum(3).topk(kr, dim=2).indices.sort(2).values
+            some = torch.zeros_like(sq[..., 0]).scatter_(2, rows, 1.0)
+            cols = (sq * some[..., None]).sum(2).topk(kc, dim=2).indices.sort(2).values
+            keep = some[..., None] * torch.zeros_like(sq[:, :, 0]).scatter_(2, cols, 1.0)[:, :, None]
+            mask = keep.permute(0, 2, 1, 3).reshape(M, K).to(w.dtype)
+            self.blocks[name] = (BR, BC, rows.cpu().numpy(), cols.cpu().numpy())
+            self.register_buffer("mask_" + name, mask)
+
+    def weight(self, name: str) -> torch.Tensor:
+        w = self.products()[name]
+        mask = getattr(self, "mask_" + name, None)
+        return w if mask is None else w * mask
+
+    def forward(self, tokens, seq_start, h0=None):
+        """Logits of packed sequences of tokens (N x V) and every layer's last states."""
+        x = self.embedding[tokens]
+        last = []
+        for i in range(self.layers):
+            state = h0[i] if h0 is not None else x.new_zeros((seq_start.numel() - 1, self.units), dtype=torch.float32)
+            n = LayerNorm.apply(x, self.gammas[i], self.betas[i])
+            y, h = GatedRecurrence.apply(n @ self.weight(f"gates{i}").t(), self.biases[i], state, seq_start)
+            x = x + y @ self.weight(f"outs{i}").t()
+            last.append(h)
+        return LayerNorm.apply(x, self.gammas[-1], self.betas[-1]) @ self.weight("head").t(), last
+
+
+def distill(student: RecurrentLM, teacher: RecurrentLM, batches, k: int = 16, temperature: float = 2.0, rate: float = 1e-2):
+    """One step of distillation per batch of (tokens, seq_start); the losses."""
+    optimizer = torch.optim.Adam(student.parameters(), lr=rate)
+    losses = []
+    for tokens, seq_start in batches:
+        with torch.no_grad():
+            top = teacher(tokens, seq_start)[0].topk(k, dim=1)
+        logits, _ = student(tokens, seq_start)
+        weight = torch.full((tokens.numel(),), 1.0 / tokens.numel(), device=tokens.device)
+        loss = DistillTopK.apply(logits, top.values.float().contiguous(), top.indices.int().contiguous(), temperature, weight)
+        optimizer.zero_grad()
+        loss.backward()
+        optimizer.step()
+        losses.append(float(loss.detach()))
+    return losses
+
+
+# ---------------------------------------------------------------------------------------------- serving
+class Server:
+    """A pruned model for `batch` callers, one token per step.  Products are BCR products in fp16; states stay in fp32."""
+
+    def __init__(self, model: RecurrentLM, batch: int):
+        self.model, self.batch = model, batch
+        self.packed = {name: self._pack(model, name) for name in model.products()}
+        dev = model.embedding.device
+        fp32, fp16 = (lambda *s: torch.empty(s, device=dev)), (lambda *s: torch.empty(s, dtype=torch.float16, device=dev))
+        H, V = model.units, model.head.shape[0]
+        self.h = [torch.zeros((H, batch), device=dev) for _ in range(model.layers)]
+        self.gates, self.y, self.out, self.norm, self.logits = fp32(3 * H, batch), fp16(H, batch), fp32(H, batch), fp32(batch, H), fp32(V, batch)
+
+    @staticmethod
+    def _pack(model, name):
+        BR, BC, rows, cols = model.blocks[name]
+        nb = rows.shape[0] * rows.shape[1]
+        ptr = lambda n: np.arange(nb + 1, dtype=np.int32) * n
+        w = model.weight(name).detach().half().cpu().numpy()
+        return binding.pack(w, "f16", BR, BC, ptr(rows.shape[2]), rows.astype(np.uint16).ravel(), ptr(cols.shape[2]),
+                            cols.astype(np.uint16).ravel())
+
+    def _norm(self, x, i, stream):
+        """Layer norm of the callers' rows, as the columns of the next product."""
+        lm.layer_norm(x, "f32", x.shape[1], self.model.gammas[i], self.model.betas[i], EPS, self.batch, x.shape[1], self.norm, x.shape[1],
+                      stream=stream)
+        return self.norm.t().to(torch.float16).contiguous()
+
+    @torch.no_grad()
+    def step(self, tokens: torch.Tensor, **rules) -> torch.Tensor:
+        """Takes one token of each caller; the logits of the next, V x batch, with the rules of lm.logit_rules applied."""
+        m, b, stream = self.model, self.batch, torch.cuda.current_stream()
+        H, V = m.units, self.logits.shape[0]
+        x = m.embedding[tokens].float()
+        for i in range(m.layers):
+            binding.spmm(self.packed[f"gates{i}"], self._norm(x, i, stream), b, b, self.gates, b, stream)
+            lm.glr_step(self.gates, b, m.biases[i], self.h[i], b, self.h[i], b, self.y, "f16", b, H, b, stream)
+            binding.spmm(self.packed[f"outs{i}"], self.y, b, b, self.out, b, stream)
+            x = x + self.out.t()
+        binding.spmm(self.packed["head"], self._norm(x, m.layers, stream), b, b, self.logits, b, stream)
+        if rules:
+            lm.logit_rules(self.logits, "f32", b, V, b, self.logits, b, columns=True, stream=stream, **rules)
+        return self.logits
+
+
+def generate(server: Server, prompt: torch.Tensor, steps: int, repetition: float = 1.3) -> torch.Tensor:
+    """The likeliest word after word for every caller, words said before made less likely (batch x (1 + steps))."""
+    b = server.batch
+    said = torch.zeros((b, steps + 1), dtype=torch.int32, device=prompt.device)
+    said[:, 0] = prompt
+    lens = torch.ones((b,), dtype=torch.int32, device=prompt.device)
+    strength = torch.full((b,), repetition, device=prompt.device)
+    for t in range(steps):
+        logits = server.step(said[:, t].long(), history=said, ld_history=steps + 1, max_history=steps + 1, history_len=lens,
+                             repetition=strength)
+        said[:, t + 1] = logits.argmax(0).int()
+        lens += 1
+    return said
+
+
+def main(vocabulary: int = 512, units: int = 256, layers: int = 2, steps: int = 60, seed: int = 0):
+    dev = torch.device("cuda:0")
+    teacher = RecurrentLM(vocabulary, units, layers, seed).to(dev)
+    student = RecurrentLM(vocabulary, units, layers, seed).to(dev)
+    student.prune(16, 32, 8, 16)
+    gen = torch.Generator().manual_seed(seed + 1)
+    lengths = [200, 1, 311, 0, 256, 256]                      # texts of different lengths, one after another
+    starts = torch.tensor([0] + np.cumsum(lengths).tolist(), dtype=torch.int32, device=dev)
+    batches = [(torch.randint(0, vocabulary, (sum(lengths),), generator=gen).to(dev), starts) for _ in range(steps)]
+    losses = distill(student, teacher, batches)
+    print(f"distillation loss {losses[0]:.4f} -> {losses[-1]:.4f} in {steps} steps of {sum(lengths)} tokens")
+    server = Server(student, batch=4)
+    print(generate(server, torch.arange(4, device=dev), 12).cpu().numpy())
+    return losses
+
+
+if __name__ == "__main__":
+    main()
