@@ -26,6 +26,7 @@ struct DistillParams {
     int64_t ldz, lddz, ldt, N, V;
     int32_t k, slices;
     float tau, scale;           // scale = log2(e) / tau
+    bool past;
 };
 
 // The teacher's side of a row in LDS, with room for E entries: words (-1: absent), probabilities, the sums of the probabilities of
@@ -207,16 +208,18 @@ __global__ void __launch_bounds__(64 * (W + 1)) distill_rows(DistillParams p) {
         if (threadIdx.x == TPR) p.loss[n] = weight * p.tau * p.tau * (kLn2 * loss);
     } else if (dz) {
         const float slope = factor * rsum;
+        store_rows(p.past, [&](auto past) {
 #pragma unroll
-        for (int k = 0; k < PER; ++k) {
-            if (k > full || (k == full && !some)) continue;
-            float v[V], out[V];
-            forget(raw[k]);
-            unpack(raw[k], v);
+            for (int k = 0; k < PER; ++k) {
+                if (k > full || (k == full && !some)) continue;
+                float v[V], out[V];
+                forget(raw[k]);
+                unpack(raw[k], v);
 #pragma unroll
-            for (int j = 0; j < V; ++j) out[j] = slope * __builtin_amdgcn_exp2f((v[j] - peak) * p.scale);
-            store(dz + (k < full ? k * TPR * V + (int)threadIdx.x * V : tail), out);
-        }
+                for (int j = 0; j < V; ++j) out[j] = slope * __builtin_amdgcn_exp2f((v[j] - peak) * p.scale);
+                store<past.value>(dz + (k < full ? k * TPR * V + (int)threadIdx.x * V : tail), out);
+            }
+        });
     }
     if (!dz) return;
     __syncthreads();                                        // the listed words' places were written by other threads
@@ -456,7 +459,8 @@ grim_status grim_distill_topk(const void *z_dev, grim_dtype dt, int64_t ldz, con
     if (!z_dev || !top_logits_dev || !top_ids_dev || !loss_dev || !workspace) return GRIM_ERR_NULL;
     if (workspace_bytes < grim_distill_topk_workspace(N, V)) return GRIM_ERR_SHAPE;
     const DistillParams p{z_dev, top_logits_dev, weight_dev, top_ids_dev, loss_dev, dz_dev, static_cast<float *>(workspace),
-                          ldz, lddz, ldt, N, V, k, 0, temperature, 1.44269504088896340736f / temperature};
+                          ldz, lddz, ldt, N, V, k, 0, temperature, 1.44269504088896340736f / temperature,
+                          past_caches(2 * N * V * bytes_of(dt))};
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     return dt == GRIM_F32   ? distill_typed<float>(p, stream)
            : dt == GRIM_F16 ? distill_typed<f16>(p, stream)

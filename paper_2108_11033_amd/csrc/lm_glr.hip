@@ -109,7 +109,7 @@ __device__ __forceinline__ void take(const float *from, float (&v)[VEC]) {
     unpack(load<VEC>(from), v);
 }
 
-// Scaled biases: the gates' exponents are one multiply-add each.
+// The biases, asked for early; scaled when the rows are in hand: the gates' exponents are one multiply-add each.
 template <int VEC>
 struct Bias {
     float u[VEC], c[VEC], v[VEC];
@@ -120,9 +120,11 @@ struct Bias {
             take<VEC>(p.bias + at, u);
             take<VEC>(p.bias + p.H + at, c);
             take<VEC>(p.bias + 2 * p.H + at, v);
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) u[j] *= -kLog2e, v[j] *= -kLog2e;
         }
+    }
+    __device__ __forceinline__ void scale() {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) u[j] *= -kLog2e, v[j] *= -kLog2e;
     }
 };
 
@@ -140,16 +142,21 @@ struct Rows {
 // ---------------------------------------------------------------------------------------------- maps of the chunks
 // What rows r0 .. r1 - 1 do to the state that enters in front of them.
 template <typename T, int VEC>
-__device__ __forceinline__ void forward_map(const GlrParams &p, const Starts &starts, const Units<VEC> &un, const Bias<VEC> &bias, int r0, int r1,
+__device__ __forceinline__ void forward_map(const GlrParams &p, const Starts &starts, const Units<VEC> &un, Bias<VEC> &bias, int r0, int r1,
                                             float (&A)[VEC], float (&B)[VEC]) {
 #pragma unroll
     for (int j = 0; j < VEC; ++j) A[j] = 1.f, B[j] = 0.f;
+    Rows<T, VEC> u, c;
+    auto fetch = [&](int at) {
+        u.fetch(p.gates, p.ldg, un.at, at, r1 - at);
+        c.fetch(p.gates, p.ldg, p.H + un.at, at, r1 - at);
+    };
+    if (r0 < r1) fetch(r0);
+    bias.scale();
     if (r0 >= r1) return;
     int s = starts.below(r0) - 1, bound = starts.at(s + 1);
     for (int g = r0; g < r1; g += kGroup) {
-        Rows<T, VEC> u, c;
-        u.fetch(p.gates, p.ldg, un.at, g, r1 - g);
-        c.fetch(p.gates, p.ldg, p.H + un.at, g, r1 - g);
+        if (g > r0) fetch(g);
 #pragma unroll
         for (int i = 0; i < kGroup; ++i) {
             const int r = g + i;
@@ -179,18 +186,24 @@ __device__ __forceinline__ void forward_map(const GlrParams &p, const Starts &st
 
 // What rows r1 - 1 .. r0 do to the gradient R that enters behind them.
 template <typename T, int VEC>
-__device__ __forceinline__ void backward_map(const GlrParams &p, const Starts &starts, const Units<VEC> &un, const Bias<VEC> &bias, int r0, int r1,
+__device__ __forceinline__ void backward_map(const GlrParams &p, const Starts &starts, const Units<VEC> &un, Bias<VEC> &bias, int r0, int r1,
                                              float (&A)[VEC], float (&B)[VEC]) {
 #pragma unroll
     for (int j = 0; j < VEC; ++j) A[j] = 1.f, B[j] = 0.f;
+    const int last = r0 + (r1 - 1 - r0) / kGroup * kGroup;
+    Rows<T, VEC> u, v, d;
+    auto fetch = [&](int at) {
+        u.fetch(p.gates, p.ldg, un.at, at, r1 - at);
+        v.fetch(p.gates, p.ldg, 2 * p.H + un.at, at, r1 - at);
+        d.fetch(p.dy, p.lddy, un.at, at, r1 - at);
+    };
+    if (r0 < r1) fetch(last);
+    bias.scale();
     if (r0 >= r1) return;
     int s = starts.below(r1) - 1;                               // the sequence of row r1 - 1, and where it ends and starts
     int end = s >= 0 ? starts.at(s + 1) : -1, begin = s >= 0 ? starts.at(s) : 0;
-    for (int g = r0 + (r1 - 1 - r0) / kGroup * kGroup; g >= r0; g -= kGroup) {
-        Rows<T, VEC> u, v, d;
-        u.fetch(p.gates, p.ldg, un.at, g, r1 - g);
-        v.fetch(p.gates, p.ldg, 2 * p.H + un.at, g, r1 - g);
-        d.fetch(p.dy, p.lddy, un.at, g, r1 - g);
+    for (int g = last; g >= r0; g -= kGroup) {
+        if (g < last) fetch(g);
 #pragma unroll
         for (int i = kGroup - 1; i >= 0; --i) {
             const int r = g + i;
@@ -265,7 +278,7 @@ __global__ void __launch_bounds__(64 * kWaves, waves_forward<VEC>()) glr_maps(Gl
     const Starts starts(p);
     const int set = blockIdx.x / p.tiles;
     const Units<VEC> un(blockIdx.x % p.tiles, p.H);
-    const Bias<VEC> bias(p, un.at);
+    Bias<VEC> bias(p, un.at);
     const Chunk ch(p, set);
     float a[VEC], b[VEC], A[VEC], B[VEC], SA[VEC], SB[VEC];
     if (BACK) backward_map<T, VEC>(p, starts, un, bias, ch.r0, ch.r1, a, b);
@@ -316,13 +329,13 @@ __device__ __forceinline__ void entering(const GlrParams &p, float (*maps)[2][64
 
 // ---------------------------------------------------------------------------------------------- forward
 // ALONE: one set holds all rows, and its workgroup forms the maps of its chunks itself.
-template <typename T, int VEC, bool ALONE>
+template <typename T, int VEC, bool ALONE, bool PAST>
 __global__ void __launch_bounds__(64 * kWaves, waves_forward<VEC>()) glr_forward(GlrParams p) {
     __shared__ float maps[kWaves][2][64 * VEC];
     const Starts starts(p);
     const int set = ALONE ? 0 : p.sets - 1 - (int)blockIdx.x / p.tiles;
     const Units<VEC> un(blockIdx.x % p.tiles, p.H);
-    const Bias<VEC> bias(p, un.at);
+    Bias<VEC> bias(p, un.at);
     const Chunk ch(p, set);
     const int r0 = ch.r0, r1 = ch.r1;
     Rows<T, VEC> u, c, v;
@@ -341,6 +354,7 @@ __global__ void __launch_bounds__(64 * kWaves, waves_forward<VEC>()) glr_forward
         compose_chunks<VEC>(maps, ch.wave, a, b, A, h, SA, SB);
     } else {
         entering<VEC>(p, maps, un, ch, set, 0, 1, set, h);
+        bias.scale();
     }
     if (p.h_last)                                               // sequences without a token keep their state
         for (int s = ch.index; s < p.nseq; s += p.sets * kWaves)
@@ -380,7 +394,7 @@ __global__ void __launch_bounds__(64 * kWaves, waves_forward<VEC>()) glr_forward
                     out[j] = o * h[j];
                 }
                 if (un.live) {
-                    store(y + (int64_t)r * p.ldy, out);
+                    store<PAST>(y + (int64_t)r * p.ldy, out);
                     if (p.h_last && s >= 0 && r + 1 == bound) store(p.h_last + s * p.H + un.at, h);
                 }
             }
@@ -389,14 +403,14 @@ __global__ void __launch_bounds__(64 * kWaves, waves_forward<VEC>()) glr_forward
 }
 
 // ---------------------------------------------------------------------------------------------- backward
-template <typename T, int VEC, bool ALONE>
+template <typename T, int VEC, bool ALONE, bool PAST>
 __global__ void __launch_bounds__(64 * kWaves, kWavesBackward) glr_backward(GlrParams p) {
     __shared__ float maps[kWaves][2][64 * VEC];
     __shared__ float sums[3][64 * VEC];
     const Starts starts(p);
     const int set = ALONE ? 0 : p.sets - 1 - (int)blockIdx.x / p.tiles;
     const Units<VEC> un(blockIdx.x % p.tiles, p.H);
-    const Bias<VEC> bias(p, un.at);
+    Bias<VEC> bias(p, un.at);
     const Chunk ch(p, set);
     float R[VEC];
     if (ALONE) {
@@ -405,6 +419,7 @@ __global__ void __launch_bounds__(64 * kWaves, kWavesBackward) glr_backward(GlrP
         compose_chunks<VEC>(maps, kWaves - 1 - ch.wave, a, b, A, R, SA, SB);
     } else {
         entering<VEC>(p, maps, un, ch, set, p.sets - 1, -1, p.sets - 1 - set, R);
+        bias.scale();
     }
     if (p.dh0)
         for (int s = ch.index; s < p.nseq; s += p.sets * kWaves)
@@ -493,9 +508,9 @@ __global__ void __launch_bounds__(64 * kWaves, kWavesBackward) glr_backward(GlrP
                     }
                     if (un.live) {
                         T *out = static_cast<T *>(p.dgates) + (int64_t)r * p.lddg + un.at;
-                        store(out, du);
-                        store(out + p.H, dc);
-                        store(out + 2 * p.H, dv);
+                        store<PAST>(out, du);
+                        store<PAST>(out + p.H, dc);
+                        store<PAST>(out + 2 * p.H, dv);
                         if (p.dh0 && s >= 0 && (first >> i & 1)) store(p.dh0 + s * p.H + un.at, R);
                     }
                 }
@@ -582,16 +597,21 @@ template <typename T, int VEC>
 grim_status glr_launch(const GlrParams &p, const Cut &c, bool back, hipStream_t stream) {
     const dim3 grid((unsigned)c.sets * c.tiles), block(64 * kWaves);      // (the column blocks of a set's rows side by side)
     if (c.sets == 1) {
-        if (back) hipLaunchKernelGGL((glr_backward<T, VEC, true>), grid, block, 0, stream, p);
-        else hipLaunchKernelGGL((glr_forward<T, VEC, true>), grid, block, 0, stream, p);
+        if (back) hipLaunchKernelGGL((glr_backward<T, VEC, true, false>), grid, block, 0, stream, p);
+        else hipLaunchKernelGGL((glr_forward<T, VEC, true, false>), grid, block, 0, stream, p);
         return launched();
     }
     if (back) hipLaunchKernelGGL((glr_maps<T, VEC, true>), grid, block, 0, stream, p);
     else hipLaunchKernelGGL((glr_maps<T, VEC, false>), grid, block, 0, stream, p);
     const grim_status st = launched();
     if (st != GRIM_OK) return st;
-    if (back) hipLaunchKernelGGL((glr_backward<T, VEC, false>), grid, block, 0, stream, p);
-    else hipLaunchKernelGGL((glr_forward<T, VEC, false>), grid, block, 0, stream, p);
+    if (past_caches((back ? 7 : 4) * p.N * p.H * (int64_t)sizeof(T))) {
+        if (back) hipLaunchKernelGGL((glr_backward<T, VEC, false, true>), grid, block, 0, stream, p);
+        else hipLaunchKernelGGL((glr_forward<T, VEC, false, true>), grid, block, 0, stream, p);
+    } else {
+        if (back) hipLaunchKernelGGL((glr_backward<T, VEC, false, false>), grid, block, 0, stream, p);
+        else hipLaunchKernelGGL((glr_forward<T, VEC, false, false>), grid, block, 0, stream, p);
+    }
     return launched();
 }
 

@@ -44,6 +44,7 @@ struct NormParams {
     float *mean, *rstd;
     int64_t ldx, ldy, N, C;
     float eps;
+    bool past;
 };
 
 // TPR threads (one wave, or a workgroup of 4 or 16) per row.
@@ -73,17 +74,19 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_rows(NormParams p)
         if (p.rstd) p.rstd[n] = s;
     }
     T *y = static_cast<T *>(p.y) + n * p.ldy;
+    store_rows(p.past, [&](auto past) {
 #pragma unroll
-    for (int k = 0; k < PER; ++k) {
-        float g[V], b[V], out[V];
+        for (int k = 0; k < PER; ++k) {
+            float g[V], b[V], out[V];
 #pragma unroll
-        for (int j = 0; j < V; ++j) g[j] = 1.f, b[j] = 0.f;
-        if (p.gamma) unpack(load<V>(p.gamma + cut.at[k]), g);
-        if (p.beta) unpack(load<V>(p.beta + cut.at[k]), b);
+            for (int j = 0; j < V; ++j) g[j] = 1.f, b[j] = 0.f;
+            if (p.gamma) unpack(load<V>(p.gamma + cut.at[k]), g);
+            if (p.beta) unpack(load<V>(p.beta + cut.at[k]), b);
 #pragma unroll
-        for (int j = 0; j < V; ++j) out[j] = __builtin_fmaf((v[k][j] - m) * s, g[j], b[j]);
-        if (k < PER - 1 || cut.first < V) store(y + cut.at[k], out);
-    }
+            for (int j = 0; j < V; ++j) out[j] = __builtin_fmaf((v[k][j] - m) * s, g[j], b[j]);
+            if (k < PER - 1 || cut.first < V) store<past.value>(y + cut.at[k], out);
+        }
+    });
 }
 
 // Rows narrower than one piece, or too wide for registers: a workgroup walks the row three times, an element a thread.
@@ -115,6 +118,7 @@ struct NormBackParams {
     void *dx;
     float *part;            // [workgroup][dgamma | dbeta][C], or NULL
     int64_t lddy, ldx, lddx, N, C;
+    bool past;
 };
 
 constexpr int kBackWaves = 4;           // waves of a workgroup whose waves take rows of their own
@@ -186,17 +190,19 @@ __global__ void __launch_bounds__(TPR < 256 ? 64 * kBackWaves : TPR) norm_back_r
         }
         const float c1 = s1 * inv, c2 = s2 * inv;
         T *dx = static_cast<T *>(p.dx) + n * p.lddx;
+        store_rows(p.past, [&](auto past) {
 #pragma unroll
-        for (int k = 0; k < PER; ++k) {
-            float xh[V], d[V], out[V];
-            forget(xr[k]);
-            forget(dr[k]);
-            unpack(xr[k], xh);
-            unpack(dr[k], d);
+            for (int k = 0; k < PER; ++k) {
+                float xh[V], d[V], out[V];
+                forget(xr[k]);
+                forget(dr[k]);
+                unpack(xr[k], xh);
+                unpack(dr[k], d);
 #pragma unroll
-            for (int j = 0; j < V; ++j) out[j] = s * (d[j] * g[k][j] - c1 - (xh[j] - m) * s * c2);
-            if (k < PER - 1 || cut.first < V) store(dx + cut.at[k], out);
-        }
+                for (int j = 0; j < V; ++j) out[j] = s * (d[j] * g[k][j] - c1 - (xh[j] - m) * s * c2);
+                if (k < PER - 1 || cut.first < V) store<past.value>(dx + cut.at[k], out);
+            }
+        });
     }
     if (!p.part) return;
     float *part = p.part + (int64_t)blockIdx.x * 2 * p.C;
@@ -265,7 +271,7 @@ __global__ void __launch_bounds__(1024) join_columns_kernel(const float *part, i
     const int64_t c = (int64_t)blockIdx.x * 64 + lane, width = C0 + C1;
     float s = 0.f;
     if (c < width) {
-#pragma unroll 8
+#pragma unroll 32
         for (int64_t i = w; i < groups; i += 16) s += part[i * width + c];
     }
     sums[w][lane] = s;
@@ -396,7 +402,8 @@ grim_status grim_layer_norm(const void *x_dev, grim_dtype dt, int64_t ldx, const
     if (N < 0 || C < 1 || ldx < C || ldy < C || !fits(N, ldx) || !fits(N, ldy) || !(eps >= 0.f) || eps > 3.4e38f) return GRIM_ERR_SHAPE;
     if (N == 0) return GRIM_OK;
     if (!x_dev || !y_dev) return GRIM_ERR_NULL;
-    const NormParams p{x_dev, gamma_dev, beta_dev, y_dev, mean_dev, rstd_dev, ldx, ldy, N, C, eps};
+    const NormParams p{x_dev, gamma_dev, beta_dev, y_dev, mean_dev, rstd_dev, ldx, ldy, N, C, eps,
+                       past_caches(2 * N * C * bytes_of(dt))};
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     return dt == GRIM_F32 ? norm_typed<float>(p, stream) : dt == GRIM_F16 ? norm_typed<f16>(p, stream) : norm_typed<bf16>(p, stream);
 }
@@ -424,7 +431,7 @@ grim_status grim_layer_norm_backward(const void *dy_dev, int64_t lddy, const voi
     if (sums && workspace_bytes < grim_layer_norm_workspace(N, C)) return GRIM_ERR_SHAPE;
     if (!sums && (!dx_dev || N == 0)) return GRIM_OK;
     const NormBackParams p{dy_dev, x_dev, gamma_dev, mean_dev, rstd_dev, dx_dev, sums ? static_cast<float *>(workspace) : nullptr,
-                           lddy, ldx, lddx, N, C};
+                           lddy, ldx, lddx, N, C, past_caches(3 * N * C * bytes_of(dt))};
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     return dt == GRIM_F32   ? norm_back_typed<float>(p, dgamma_dev, dbeta_dev, stream)
            : dt == GRIM_F16 ? norm_back_typed<f16>(p, dgamma_dev, dbeta_dev, stream)
