@@ -23,8 +23,8 @@ constexpr int kWaves = 8;       // waves, and chunks, of a workgroup
 // Waves per SIMD that the kernels are held to: what the loads of a group of rows leave room for.  Waves that wait for each other's
 // loads hide more than a second group in flight per wave does (at 65536 x 1024 bf16: forward 125 against 112 us, backward 247
 // against 212).
-template <int VEC> constexpr int waves_forward() { return VEC == 1 ? 8 : 6; }
-constexpr int kWavesBackward = 4;
+template <int VEC> constexpr int waves_forward() { return VEC == 1 ? 8 : VEC == 2 ? 6 : 4; }
+template <int VEC> constexpr int waves_backward() { return VEC <= 2 ? 4 : 2; }
 // Units of a lane where there are rows enough: 4 bytes, 256 of a row per wave.  (bf16, both directions: 65536 x 1024 555 us with one
 // unit, 479 with two, 490 with four; fp32: 896 with one, 903 with two.)
 template <typename T> constexpr int wide() { return sizeof(T) == 2 ? 2 : 1; }
@@ -404,7 +404,7 @@ __global__ void __launch_bounds__(64 * kWaves, waves_forward<VEC>()) glr_forward
 
 // ---------------------------------------------------------------------------------------------- backward
 template <typename T, int VEC, bool ALONE, bool PAST>
-__global__ void __launch_bounds__(64 * kWaves, kWavesBackward) glr_backward(GlrParams p) {
+__global__ void __launch_bounds__(64 * kWaves, waves_backward<VEC>()) glr_backward(GlrParams p) {
     __shared__ float maps[kWaves][2][64 * VEC];
     __shared__ float sums[3][64 * VEC];
     const Starts starts(p);
@@ -606,8 +606,12 @@ grim_status glr_launch(const GlrParams &p, const Cut &c, bool back, hipStream_t 
     const grim_status st = launched();
     if (st != GRIM_OK) return st;
     if (past_caches((back ? 7 : 4) * p.N * p.H * (int64_t)sizeof(T))) {
-        if (back) hipLaunchKernelGGL((glr_backward<T, VEC, false, true>), grid, block, 0, stream, p);
-        else hipLaunchKernelGGL((glr_forward<T, VEC, false, true>), grid, block, 0, stream, p);
+        constexpr int W = VEC == 2 ? 4 : VEC;
+        GlrParams q = p;
+        q.tiles = (int32_t)((p.H + 64 * W - 1) / (64 * W));
+        const dim3 wider((unsigned)c.sets * q.tiles);
+        if (back) hipLaunchKernelGGL((glr_backward<T, W, false, true>), wider, block, 0, stream, q);
+        else hipLaunchKernelGGL((glr_forward<T, W, false, true>), wider, block, 0, stream, q);
     } else {
         if (back) hipLaunchKernelGGL((glr_backward<T, VEC, false, false>), grid, block, 0, stream, p);
         else hipLaunchKernelGGL((glr_forward<T, VEC, false, false>), grid, block, 0, stream, p);
