@@ -23,6 +23,7 @@ constexpr int kWaves = 8;       // waves, and chunks, of a workgroup
 // Waves per SIMD that the kernels are held to: what the loads of a group of rows leave room for.  Waves that wait for each other's
 // loads hide more than a second group in flight per wave does (at 65536 x 1024 bf16: forward 125 against 112 us, backward 247
 // against 212).
+constexpr int kWavesMaps = 8;
 template <int VEC> constexpr int waves_forward() { return VEC == 1 ? 8 : VEC == 2 ? 6 : 4; }
 template <int VEC> constexpr int waves_backward() { return VEC <= 2 ? 4 : 2; }
 // Units of a lane where there are rows enough: 4 bytes, 256 of a row per wave.  (bf16, both directions: 65536 x 1024 555 us with one
@@ -273,7 +274,7 @@ struct Chunk {
 };
 
 template <typename T, int VEC, bool BACK>
-__global__ void __launch_bounds__(64 * kWaves, waves_forward<VEC>()) glr_maps(GlrParams p) {
+__global__ void __launch_bounds__(64 * kWaves, kWavesMaps) glr_maps(GlrParams p) {
     __shared__ float maps[kWaves][2][64 * VEC];
     const Starts starts(p);
     const int set = blockIdx.x / p.tiles;
@@ -309,17 +310,25 @@ __device__ __forceinline__ void entering(const GlrParams &p, float (*maps)[2][64
     for (int j = 0; j < VEC; ++j) a[j] = 1.f, b[j] = 0.f;
     const int per = (ahead + kWaves - 1) / kWaves;
     const int from = min(ch.wave * per, ahead), to = min(from + per, ahead);
-#pragma unroll 8
-    for (int i = from; i < to; ++i) {
-        const float *m = p.set_maps + (int64_t)(first + dir * i) * 2 * p.H + un.at;
-        float na[VEC], nb[VEC];
-        take<VEC>(m, na);
-        take<VEC>(m + p.H, nb);
+    constexpr int kBatch = 8;                                   // maps on their way together
+    for (int i = from; i < to; i += kBatch) {
+        Pack<float, VEC> na[kBatch], nb[kBatch];
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-            compose(a[j], b[j], na[j], nb[j]);
-            a[j] = na[j], b[j] = nb[j];
+        for (int k = 0; k < kBatch; ++k) {
+            const float *m = p.set_maps + (int64_t)(first + dir * min(i + k, to - 1)) * 2 * p.H + un.at;
+            na[k] = load<VEC>(m);
+            nb[k] = load<VEC>(m + p.H);
         }
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k)
+            if (i + k < to) {
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    float ka = element(na[k], j), kb = element(nb[k], j);
+                    compose(a[j], b[j], ka, kb);
+                    a[j] = ka, b[j] = kb;
+                }
+            }
     }
     float A[VEC], B[VEC], SA[VEC], SB[VEC];
     compose_chunks<VEC>(maps, ch.wave, a, b, A, B, SA, SB);
@@ -565,22 +574,31 @@ __global__ void __launch_bounds__(256) glr_step_kernel(GlrStepParams p) {
 }
 
 // ---------------------------------------------------------------------------------------------- launches
-// How the rows are cut.  Chunks as short as give some 1024 workgroups (four per compute unit, so that they even out), but no
-// shorter than keep the maps of the sets, all of which a workgroup may have to read, within its own rows' size (rows^2 = N / 64:
-// 64000 x 128 bf16, both directions, 80 us in 250 sets of 32 rows a wave, 92 in 500 and 97 in 125), nor than a group.
+// How the rows are cut.
 struct Cut {
-    int vec;
+    int vec, last;              // units of a lane, and in the second launch
+    bool past;
     int32_t L, sets, tiles;
 };
 
-inline Cut cut_rows(int64_t N, int64_t H, int wide) {
+inline Cut cut_rows(int64_t N, int64_t H, bool fp32, bool back) {
     Cut c;
+    const int wide_one = fp32 ? wide<float>() : wide<f16>();
     // one unit a lane where more would leave compute units without work (1024 x 1024 bf16 24 against 27 us, 2048 x 1024 31 against 30)
-    c.vec = H >= 256 && N * H >= (int64_t)1 << 21 ? wide : 1;
+    c.vec = H >= 256 && N * H >= (int64_t)1 << 21 ? wide_one : 1;
+    c.past = past_caches((back ? 7 : 4) * N * H * (fp32 ? 4 : 2));
+    // eight bytes of a row where the outputs go past the caches, if three or more column blocks remain (24007 x 1000 fp16 193 against 209
+    // us; 32768 x 512 139 against 119)
+    c.last = c.past && c.vec == 2 && H >= 768 ? 4 : c.vec;
     c.tiles = (int32_t)((H + 64 * c.vec - 1) / (64 * c.vec));
-    const int64_t even = (N * c.tiles + kWaves * 1024 - 1) / (kWaves * 1024);
-    int64_t L = (int64_t)__builtin_sqrt((double)N / 64.0);
-    L = even > L ? even : L;
+    // Chunks so short that the workgroups fill the compute units once (the second launch of the backward pass has room for 512,
+    // the others for 1024), but no shorter than keep the maps of the sets, all of which a workgroup may have to read, within its own
+    // rows' size: rows^2 = N / 64.  (bf16, both directions: 64000 x 128 81 us in 250 sets of 32 rows a wave, 94 in 334, 97
+    // in 125; 20863 x 192 52 in 163 sets of 16, 61 in 109, 65 in 327.)
+    const int64_t room = kWaves * (back && c.last < 4 ? 512 : 1024);
+    const int64_t even = (N * c.tiles + room - 1) / room;
+    const int64_t square = ((int64_t)__builtin_sqrt((double)N / 64.0) + kGroup / 2) / kGroup * kGroup;
+    int64_t L = even > square ? even : square;
     if (N <= 2 * kWaves * kGroup) L = (N + kWaves - 1) / kWaves;          // one set, one launch
     L = (L + kGroup - 1) / kGroup * kGroup;
     c.L = (int32_t)(L < kGroup ? kGroup : L);
@@ -588,8 +606,6 @@ inline Cut cut_rows(int64_t N, int64_t H, int wide) {
     c.sets = N > 0 ? (int32_t)((N + rows - 1) / rows) : 1;
     return c;
 }
-
-inline int wide_of(grim_dtype dt) { return dt == GRIM_F32 ? wide<float>() : wide<f16>(); }
 
 inline int64_t map_floats(const Cut &c, int64_t H) { return ((int64_t)c.sets * (kWaves + 1)) * 2 * H; }
 
@@ -605,22 +621,25 @@ grim_status glr_launch(const GlrParams &p, const Cut &c, bool back, hipStream_t 
     else hipLaunchKernelGGL((glr_maps<T, VEC, false>), grid, block, 0, stream, p);
     const grim_status st = launched();
     if (st != GRIM_OK) return st;
-    if (past_caches((back ? 7 : 4) * p.N * p.H * (int64_t)sizeof(T))) {
-        constexpr int W = VEC == 2 ? 4 : VEC;
-        GlrParams q = p;
-        q.tiles = (int32_t)((p.H + 64 * W - 1) / (64 * W));
-        const dim3 wider((unsigned)c.sets * q.tiles);
-        if (back) hipLaunchKernelGGL((glr_backward<T, W, false, true>), wider, block, 0, stream, q);
-        else hipLaunchKernelGGL((glr_forward<T, W, false, true>), wider, block, 0, stream, q);
+    constexpr int W = VEC == 2 ? 4 : VEC;
+    GlrParams q = p;
+    q.tiles = (int32_t)((p.H + 64 * c.last - 1) / (64 * c.last));
+    const dim3 last((unsigned)c.sets * q.tiles);
+    if (c.last == 4) {
+        if (back) hipLaunchKernelGGL((glr_backward<T, W, false, true>), last, block, 0, stream, q);
+        else hipLaunchKernelGGL((glr_forward<T, W, false, true>), last, block, 0, stream, q);
+    } else if (c.past) {
+        if (back) hipLaunchKernelGGL((glr_backward<T, VEC, false, true>), last, block, 0, stream, q);
+        else hipLaunchKernelGGL((glr_forward<T, VEC, false, true>), last, block, 0, stream, q);
     } else {
-        if (back) hipLaunchKernelGGL((glr_backward<T, VEC, false, false>), grid, block, 0, stream, p);
-        else hipLaunchKernelGGL((glr_forward<T, VEC, false, false>), grid, block, 0, stream, p);
+        if (back) hipLaunchKernelGGL((glr_backward<T, VEC, false, false>), last, block, 0, stream, q);
+        else hipLaunchKernelGGL((glr_forward<T, VEC, false, false>), last, block, 0, stream, q);
     }
     return launched();
 }
 
 grim_status glr_run(GlrParams p, grim_dtype dt, bool back, hipStream_t stream) {
-    const Cut c = cut_rows(p.N, p.H, wide_of(dt));
+    const Cut c = cut_rows(p.N, p.H, dt == GRIM_F32, back);
     p.L = c.L, p.sets = c.sets, p.tiles = c.tiles;
     p.set_maps = p.chunk_maps + (int64_t)c.sets * kWaves * 2 * p.H;
     switch (dt) {
@@ -648,9 +667,9 @@ int64_t grim_glr_states(int64_t N, int64_t H) {
 int64_t grim_glr_workspace(int64_t N, int64_t H) {
     using namespace grim::lm;
     if (!glr_sizes(N, H, 1, nullptr)) return 0;
-    int64_t most = 0;                                           // (whichever type comes)
-    for (int w : {wide<float>(), wide<f16>()}) {
-        const Cut c = cut_rows(N, H, w);
+    int64_t most = 0;                                           // (whichever type and direction come)
+    for (int way = 0; way < 4; ++way) {
+        const Cut c = cut_rows(N, H, way & 1, way & 2);
         const int64_t floats = map_floats(c, H) + (int64_t)c.sets * 3 * H;
         most = floats > most ? floats : most;
     }
@@ -686,7 +705,7 @@ grim_status grim_glr_sequence_backward(const void *gates_dev, grim_dtype dt, int
         return GRIM_ERR_SHAPE;
     if ((N > 0 && (!gates_dev || !states_dev || !dy_dev || !dgates_dev)) || !workspace) return GRIM_ERR_NULL;
     if (workspace_bytes < grim_glr_workspace(N, H)) return GRIM_ERR_SHAPE;
-    const Cut c = cut_rows(N, H, wide_of(dt));
+    const Cut c = cut_rows(N, H, dt == GRIM_F32, true);
     GlrParams p{};
     p.gates = gates_dev, p.bias = bias_dev, p.h0 = h0_dev, p.seq = seq_start_dev, p.nseq = nseq;
     p.states = static_cast<float *>(const_cast<void *>(states_dev));
