@@ -117,11 +117,15 @@ __device__ __forceinline__ float from_lane(float v) {
 // All lanes get join(v of all 64), each having joined the same pairs: first inside rows of 16 lanes, then across rows by exchanging
 // them.  (No trip through LDS: a reduction is some 30 cycles, not 600.)
 template <typename F>
-__device__ __forceinline__ float wave_join(float v, F join) {
+__device__ __forceinline__ float row_join(float v, F join) {
     v = join(v, from_lane<0xb1>(v));
     v = join(v, from_lane<0x4e>(v));
     v = join(v, from_lane<0x141>(v));
-    v = join(v, from_lane<0x140>(v));
+    return join(v, from_lane<0x140>(v));
+}
+
+template <typename F>
+__device__ __forceinline__ float across_rows(float v, F join) {
     const uint32_t r = __builtin_bit_cast(uint32_t, v);
     const auto by16 = __builtin_amdgcn_permlane16_swap(r, r, false, false);
     v = join(__builtin_bit_cast(float, (uint32_t)by16[0]), __builtin_bit_cast(float, (uint32_t)by16[1]));
@@ -130,13 +134,15 @@ __device__ __forceinline__ float wave_join(float v, F join) {
     return join(__builtin_bit_cast(float, (uint32_t)by32[0]), __builtin_bit_cast(float, (uint32_t)by32[1]));
 }
 
-__device__ __forceinline__ float wave_sum(float v) {
-    return wave_join(v, [](float a, float b) { return a + b; });
-}
+struct Add {
+    __device__ __forceinline__ float operator()(float a, float b) const { return a + b; }
+};
+struct Max {
+    __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }
+};
 
-__device__ __forceinline__ float wave_max(float v) {
-    return wave_join(v, [](float a, float b) { return fmaxf(a, b); });
-}
+__device__ __forceinline__ float wave_sum(float v) { return across_rows(row_join(v, Add()), Add()); }
+__device__ __forceinline__ float wave_max(float v) { return across_rows(row_join(v, Max()), Max()); }
 
 // Sums over a workgroup of W waves, in the order of the waves; `room` holds W floats that nobody uses until the next barrier
 // of the caller.
@@ -150,6 +156,13 @@ __device__ __forceinline__ float group_sum(float v, float *room) {
 #pragma unroll
     for (int w = 0; w < W; ++w) s += room[w];
     return s;
+}
+
+// The same over teams of TPR threads: a row of 16 lanes, a wave, a workgroup of TPR / 64 waves.
+template <int TPR>
+__device__ __forceinline__ float team_sum(float v, float *room) {
+    if constexpr (TPR == 16) return row_join(v, Add());
+    else return group_sum<TPR / 64>(v, room);
 }
 
 template <int W>

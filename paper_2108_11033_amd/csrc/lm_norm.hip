@@ -47,14 +47,14 @@ struct NormParams {
     bool past;
 };
 
-// TPR threads (one wave, or a workgroup of 4 or 16) per row.
+// TPR threads (16 lanes, one wave, or a workgroup of 4 or 16) per row.
 template <typename T, int TPR, int PER>
 __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_rows(NormParams p) {
-    constexpr int V = vec_of<T>(), W = TPR / 64, RPG = TPR < 256 ? 256 / TPR : 1;
-    __shared__ float room[2][W];
+    constexpr int V = vec_of<T>(), RPG = TPR < 256 ? 256 / TPR : 1;
+    __shared__ float room[2][TPR < 64 ? 1 : TPR / 64];
     const int t = threadIdx.x % TPR;
     const int64_t n = (int64_t)blockIdx.x * RPG + threadIdx.x / TPR;
-    if (TPR < 256 && n >= p.N) return;                     // (a wave of its own: no barrier follows)
+    if (TPR < 256 && n >= p.N) return;                     // (a team inside a wave: no barrier follows)
     const RowCut<V, TPR, PER> cut(t, p.C);
     const T *x = static_cast<const T *>(p.x) + n * p.ldx;
     Pack<T, V> raw[PER];
@@ -65,10 +65,10 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_rows(NormParams p)
     for (int k = 0; k < PER; ++k) unpack(raw[k], v[k]);
     float sum = 0.f;
     cut.own([&](int k, int j) { sum += v[k][j]; });
-    const float m = group_sum<W>(sum, room[0]) / (float)p.C;
+    const float m = team_sum<TPR>(sum, room[0]) / (float)p.C;
     float sq = 0.f;
     cut.own([&](int k, int j) { const float d = v[k][j] - m; sq = __builtin_fmaf(d, d, sq); });
-    const float s = 1.0f / sqrtf(group_sum<W>(sq, room[1]) / (float)p.C + p.eps);
+    const float s = 1.0f / sqrtf(team_sum<TPR>(sq, room[1]) / (float)p.C + p.eps);
     if (t == 0) {
         if (p.mean) p.mean[n] = m;
         if (p.rstd) p.rstd[n] = s;
@@ -123,12 +123,12 @@ struct NormBackParams {
 
 constexpr int kBackWaves = 4;           // waves of a workgroup whose waves take rows of their own
 
-// A workgroup walks over rows blockIdx.x * RPG, + gridDim.x * RPG, ...; each thread keeps the sums of dgamma and dbeta for its
+// A workgroup walks over rows blockIdx.x * RPG, + gridDim.x * RPG, ... (RPG teams of TPR threads); each thread keeps the sums of dgamma and dbeta for its
 // columns in registers over all of them, so x and dy are read once for all three gradients.  The next row is asked for
 // before the present one is summed.
 template <typename T, int TPR, int PER>
 __global__ void __launch_bounds__(TPR < 256 ? 64 * kBackWaves : TPR) norm_back_rows(NormBackParams p) {
-    constexpr int V = vec_of<T>(), W = TPR / 64, RPG = TPR < 256 ? kBackWaves : 1;
+    constexpr int V = vec_of<T>(), W = TPR < 64 ? 1 : TPR / 64, RPG = TPR < 256 ? 64 * kBackWaves / TPR : 1;
     __shared__ float room[2][2][W];
     extern __shared__ float sums[];                         // one wave per row: [dgamma | dbeta][C]
     const int t = threadIdx.x % TPR, team = threadIdx.x / TPR;
@@ -179,8 +179,9 @@ __global__ void __launch_bounds__(TPR < 256 ? 64 * kBackWaves : TPR) norm_back_r
         }
         if (!p.dx) continue;
         // (two sets of words in turn: a wave may be one row ahead of another)
-        s1 = wave_sum(s1);
-        s2 = wave_sum(s2);
+        s1 = row_join(s1, Add());
+        s2 = row_join(s2, Add());
+        if (TPR >= 64) s1 = across_rows(s1, Add()), s2 = across_rows(s2, Add());
         if (W > 1) {
             if ((threadIdx.x & 63) == 0) room[turn][0][threadIdx.x >> 6] = s1, room[turn][1][threadIdx.x >> 6] = s2;
             __syncthreads();
@@ -213,8 +214,13 @@ __global__ void __launch_bounds__(TPR < 256 ? 64 * kBackWaves : TPR) norm_back_r
         });
         return;
     }
-    for (int w = 0; w < RPG; ++w) {                         // the waves' sums, in the order of the waves
-        if (team == w)
+    if (TPR < 64)
+#pragma unroll
+        for (int k = 0; k < PER; ++k)
+#pragma unroll
+            for (int j = 0; j < V; ++j) ag[k][j] = across_rows(ag[k][j], Add()), ab[k][j] = across_rows(ab[k][j], Add());
+    for (int w = 0; w < kBackWaves; ++w) {                  // the waves' sums, in the order of the waves
+        if ((int)threadIdx.x / 64 == w && threadIdx.x % 64 < TPR)
             cut.own([&](int k, int j) {
                 const int64_t c = cut.at[k] + j;
                 sums[c] = w ? sums[c] + ag[k][j] : ag[k][j];
@@ -263,40 +269,49 @@ __global__ void __launch_bounds__(256) norm_back_columns(NormBackParams p, int64
     part[p.C + c] = ab;
 }
 
-// Sums of the workgroups' columns, in a fixed order: 64 columns by 16 waves, each wave every 16th workgroup's.
+// Sums of the workgroups' columns, in a fixed order: 16 columns by 64 threads, each every 64th workgroup's, then four sums of 16
+// and theirs.  (Short runs of columns: what it takes is the loads that follow each other in a thread.)
 __global__ void __launch_bounds__(1024) join_columns_kernel(const float *part, int64_t groups, int64_t C0, float *out0, int64_t C1,
                                                             float *out1) {
-    __shared__ float sums[16][64];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int64_t c = (int64_t)blockIdx.x * 64 + lane, width = C0 + C1;
+    __shared__ float sums[64][17];
+    const int col = threadIdx.x & 15, w = threadIdx.x >> 4;
+    const int64_t c = (int64_t)blockIdx.x * 16 + col, width = C0 + C1;
     float s = 0.f;
     if (c < width) {
-#pragma unroll 32
-        for (int64_t i = w; i < groups; i += 16) s += part[i * width + c];
+#pragma unroll 16
+        for (int64_t i = w; i < groups; i += 64) s += part[i * width + c];
     }
-    sums[w][lane] = s;
+    sums[w][col] = s;
+    __syncthreads();
+    if (w < 4) {
+        s = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s += sums[16 * w + i][col];
+    }
+    __syncthreads();
+    if (w < 4) sums[w][col] = s;
     __syncthreads();
     if (w || c >= width) return;
-    s = 0.f;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) s += sums[i][lane];
+    s = (sums[0][col] + sums[1][col]) + (sums[2][col] + sums[3][col]);
     if (c < C0) {
         if (out0) out0[c] = s;
     } else if (out1) out1[c - C0] = s;
 }
 
 grim_status join_columns(const float *part, int64_t groups, int64_t C0, float *out0, int64_t C1, float *out1, hipStream_t stream) {
-    const int64_t grid = (C0 + C1 + 63) / 64;
+    const int64_t grid = (C0 + C1 + 15) / 16;
     if (grid > kMaxGrid) return GRIM_ERR_SHAPE;
     hipLaunchKernelGGL(join_columns_kernel, dim3((unsigned)grid), dim3(1024), 0, stream, part, groups, C0, out0, C1, out1);
     return launched();
 }
 
-// Threads per row: one wave while four pieces a thread hold the row, then 4 waves, then 16; 0: the walking kernels.
+// Threads per row: as few (16, a wave, 4 waves, 16) as hold the row in four pieces each; 0: the walking kernels.
 template <typename T>
 int threads_per_row(int64_t C) {
     const int64_t V = vec_of<T>();
-    return C < V ? 0 : C <= 256 * V ? 64 : C <= 1024 * V ? 256 : C <= 4096 * V ? 1024 : 0;
+    for (int tpr : {16, 64, 256, 1024})
+        if (C >= V && C <= 4 * tpr * V) return tpr;
+    return 0;
 }
 
 // The same for the backward pass, whose threads hold five values per element: as many as leave no register spilled.
@@ -305,7 +320,7 @@ constexpr int back_pieces(int tpr) { return (tpr == 1024 ? 8 : tpr == 256 && siz
 template <typename T>
 int back_threads_per_row(int64_t C) {
     const int64_t V = vec_of<T>();
-    for (int tpr : {64, 256, 1024})
+    for (int tpr : {16, 64, 256, 1024})
         if (C >= V && C <= back_pieces<T>(tpr) * tpr * V) return tpr;
     return 0;
 }
@@ -321,7 +336,7 @@ inline int64_t back_groups(int64_t N, int rows_at_once) {
 template <typename T>
 int64_t back_groups_of(int64_t N, int64_t C) {
     const int tpr = back_threads_per_row<T>(C);
-    return back_groups(N, tpr == 64 ? kBackWaves : 1);
+    return back_groups(N, tpr == 16 || tpr == 64 ? 64 * kBackWaves / tpr : 1);
 }
 
 template <typename T, int TPR>
@@ -342,6 +357,7 @@ grim_status norm_launch(const NormParams &p, hipStream_t stream) {
 template <typename T>
 grim_status norm_typed(const NormParams &p, hipStream_t stream) {
     switch (threads_per_row<T>(p.C)) {
+        case 16: return norm_launch<T, 16>(p, stream);
         case 64: return norm_launch<T, 64>(p, stream);
         case 256: return norm_launch<T, 256>(p, stream);
         case 1024: return norm_launch<T, 1024>(p, stream);
@@ -371,6 +387,7 @@ grim_status norm_back_typed(const NormBackParams &p, float *dgamma, float *dbeta
     grim_status st = GRIM_OK;
     if (p.N > 0) {
         switch (back_threads_per_row<T>(p.C)) {
+            case 16: st = norm_back_launch<T, 16>(p, groups, stream); break;
             case 64: st = norm_back_launch<T, 64>(p, groups, stream); break;
             case 256: st = norm_back_launch<T, 256>(p, groups, stream); break;
             case 1024: st = norm_back_launch<T, 1024>(p, groups, stream); break;
