@@ -79,12 +79,13 @@ struct History {
         };
         count(t * 4, early[0]);
         count((width + t) * 4, early[1]);
-        for (int i = (2 * width + t) * 4; i < len; i += 2 * width * 4) {
-            int32_t a[4], b[4];
-            take(i, a);
-            take(i + width * 4, b);
-            count(i, a);
-            count(i + width * 4, b);
+        constexpr int kAhead = 4;                               // loads on their way together: a long history is a chain of them
+        for (int i = (2 * width + t) * 4; i < len; i += kAhead * width * 4) {
+            int32_t ids[kAhead][4];
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) take(i + k * width * 4, ids[k]);
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) count(i + k * width * 4, ids[k]);
         }
     }
 };
@@ -167,11 +168,11 @@ __global__ void __launch_bounds__(THREADS) rules_rows(RuleParams p, int tiles) {
 // A column per caller: TILE >> shift words of up to 1 << shift (at most kMostCallers) callers.
 constexpr int kMostCallers = 8;
 
-template <typename T, int TILE, int THREADS>
+template <typename T, int TILE, int THREADS, int BIAS>
 __global__ void __launch_bounds__(THREADS) rules_columns(RuleParams p, int tiles, int shift) {
     constexpr int PER = TILE / THREADS;
     __shared__ __attribute__((aligned(16))) uint32_t places[TILE];
-    __shared__ float sums[kMostCallers][kMostBias];
+    __shared__ float sums[kMostCallers][BIAS];
     const int words = TILE >> shift;
     const int64_t b0 = (int64_t)(blockIdx.x / tiles) << shift, lo = (int64_t)(blockIdx.x % tiles) * words;
     const int64_t hi = lo + words < p.V ? lo + words : p.V;
@@ -183,57 +184,65 @@ __global__ void __launch_bounds__(THREADS) rules_columns(RuleParams p, int tiles
     const uint32_t *allowed = p.r.allowed ? p.r.allowed + (b0 + mine) * p.r.ld_allowed : nullptr;
     const T *z = static_cast<const T *>(p.z) + b0 + mine;
     T *out = static_cast<T *>(p.out) + b0 + mine;
-    float v[PER];
-    uint32_t bits = 0;                                          // one for each of the thread's words
+    // a few words a thread are asked for at the start; more would keep other workgroups from the compute unit
+    constexpr bool early = PER <= 4;
+    constexpr int STEP = early ? PER : 4;
+    float v[STEP];
+    uint32_t bits[STEP];
+    auto fetch = [&](int k0) {
 #pragma unroll
-    for (int k = 0; k < PER; ++k) {
-        const int at = (k * THREADS + (int)threadIdx.x) >> shift;
-        const int64_t word = lo + min(at, span - 1);
-        v[k] = (float)z[word * p.ldz];
-        bits |= (allowed ? allowed[word / 32] >> (word % 32) & 1 : 1u) << k;
-    }
+        for (int k = 0; k < STEP; ++k) {
+            const int at = ((k0 + k) * THREADS + (int)threadIdx.x) >> shift;
+            const int64_t word = lo + min(at, span - 1);
+            v[k] = (float)z[word * p.ldz];
+            bits[k] = allowed ? allowed[word / 32] >> (word % 32) : 1u;
+        }
+    };
+    if (early) fetch(0);
     for (int i = threadIdx.x; i < TILE / 4; i += THREADS) reinterpret_cast<uint4 *>(places)[i] = uint4{0, 0, 0, 0};
     __syncthreads();
-    const int lane = threadIdx.x & 63;
-    for (int b = threadIdx.x >> 6; b < callers; b += THREADS / 64) {          // a wave per caller
-        History(p.r, b0 + b, lane, 64).tally((int)lo, span, places + b, shift);
+    // as many waves per caller as there are
+    const int each = max(THREADS / 64 >> shift, 1), wave = threadIdx.x >> 6;
+    const int t = (wave % each) * 64 + (threadIdx.x & 63), width = each * 64;
+    for (int b = wave / each; b < callers; b += THREADS / 64 / each) {
+        History(p.r, b0 + b, t, width).tally((int)lo, span, places + b, shift);
         const int64_t list = (b0 + b) * p.r.ld_bias;
-        add_biases(p.r.nbias, p.r.bias_ids + list, p.r.bias_values + list, (int)lo, span, places + b, shift, sums[b], lane, 64);
+        add_biases(p.r.nbias, p.r.bias_ids + list, p.r.bias_values + list, (int)lo, span, places + b, shift, sums[b], t, width);
     }
     __syncthreads();
+    for (int k0 = 0; k0 < PER; k0 += STEP) {
+        if (!early) fetch(k0);
 #pragma unroll
-    for (int k = 0; k < PER; ++k) {
-        const int i = k * THREADS + (int)threadIdx.x, at = i >> shift;
-        if (live && at < span) out[(lo + at) * p.ldo] = (T)rules.apply(v[k], places[i], sums[mine], bits >> k & 1);
+        for (int k = 0; k < STEP; ++k) {
+            const int i = (k0 + k) * THREADS + (int)threadIdx.x, at = i >> shift;
+            if (live && at < span) out[(lo + at) * p.ldo] = (T)rules.apply(v[k], places[i], sums[mine], bits[k] & 1);
+        }
     }
 }
 
-template <typename T, int TILE, int THREADS>
-grim_status rules_launch(const RuleParams &p, bool columns, hipStream_t stream) {
+template <typename T, int TILE, int THREADS, bool COLUMNS>
+grim_status rules_launch(const RuleParams &p, hipStream_t stream) {
     int shift = 0;
-    if (columns)
+    if (COLUMNS)
         while ((1 << shift) < kMostCallers && (1 << shift) < p.batch) ++shift;    // 16 or 32 bytes of a row
     const int64_t words = TILE >> shift, tiles = (p.V + words - 1) / words;
     const int64_t grid = tiles * ((p.batch + (1 << shift) - 1) >> shift);
     if (grid > kMaxGrid) return GRIM_ERR_SHAPE;
-    if constexpr (TILE <= 4096) {
-        if (columns) {
-            hipLaunchKernelGGL((rules_columns<T, TILE, THREADS>), dim3((unsigned)grid), dim3(THREADS), 0, stream, p, (int)tiles, shift);
-            return launched();
-        }
-    }
-    if constexpr (TILE != 4096)
-        hipLaunchKernelGGL((rules_rows<T, TILE, THREADS>), dim3((unsigned)grid), dim3(THREADS), 0, stream, p, (int)tiles);
+    const dim3 g((unsigned)grid), b(THREADS);
+    if constexpr (!COLUMNS) hipLaunchKernelGGL((rules_rows<T, TILE, THREADS>), g, b, 0, stream, p, (int)tiles);
+    else if (p.r.nbias <= 128) hipLaunchKernelGGL((rules_columns<T, TILE, THREADS, 128>), g, b, 0, stream, p, (int)tiles, shift);
+    else hipLaunchKernelGGL((rules_columns<T, TILE, THREADS, kMostBias>), g, b, 0, stream, p, (int)tiles, shift);
     return launched();
 }
 
-// Tiles of 8192 places (4096 in columns, whose callers' sums take their share of LDS); of 2048 where those would leave compute
-// units without one.
+// Tiles of 8192 places, of 2048 where those would leave compute units without one.  (64 callers x 131072 words bf16: 13.5 us with
+// 8192 places and 512 threads, 14.9 with 256 threads, 16.3 with 1024; 16384 places 14.4, 2048 places and 256 threads 15.5.)
 template <typename T>
 grim_status rules_typed(const RuleParams &p, bool columns, hipStream_t stream) {
     if (p.batch == 1 && p.ldz == 1 && p.ldo == 1) columns = false;   // a single dense column is a row
-    if (p.V * p.batch < (int64_t)4096 * kComputeUnits) return rules_launch<T, 2048, 256>(p, columns, stream);
-    return columns ? rules_launch<T, 4096, 512>(p, true, stream) : rules_launch<T, 8192, 512>(p, false, stream);
+    if (p.V * p.batch >= (int64_t)4096 * kComputeUnits)
+        return columns ? rules_launch<T, 8192, 512, true>(p, stream) : rules_launch<T, 8192, 512, false>(p, stream);
+    return columns ? rules_launch<T, 2048, 512, true>(p, stream) : rules_launch<T, 2048, 256, false>(p, stream);
 }
 
 }  // namespace lm
