@@ -395,8 +395,10 @@ int64_t slices_of(int64_t V) { return (V + slice_elements<T>() - 1) / slice_elem
 template <typename T>
 bool row_fits(int64_t V) { return V >= piece<T>() && V <= (int64_t)18 * 960 * piece<T>(); }
 
+// Rows of up to 128 KB do so however few they are (100 x 32768 fp32 16.9 us against 20.1 in slices, 64 x 9000 7.0 against 10.1), longer ones
+// if half of the compute units have one (62 x 90880 bf16 18.6 us against 14.5 in slices, 100 x 131072 28 against 22.5).
 template <typename T>
-bool by_rows(int64_t N, int64_t V) { return row_fits<T>(V) && (N >= 128 || slices_of<T>(V) <= 2); }
+bool by_rows(int64_t N, int64_t V) { return row_fits<T>(V) && (N >= 128 || V * (int64_t)sizeof(T) <= 128 * 1024); }
 
 template <typename T, int E>
 grim_status distill_launch(DistillParams p, hipStream_t stream) {
@@ -404,10 +406,14 @@ grim_status distill_launch(DistillParams p, hipStream_t stream) {
         if (p.N > kMaxGrid) return GRIM_ERR_SHAPE;
         const dim3 g((unsigned)p.N);
         const int64_t pieces = (p.V + piece<T>() - 1) / piece<T>();
-        // (4, 8 or 16 waves with the teacher's)
+        // 4, 8 or 16 waves with the teacher's.  Long rows take 16 where a compute unit has one row, very long ones where it has two:
+        // (300 x 32768 fp32 19.3 us against 26.7 with 8, 269 x 19445 bf16 12.8 against 11.5, 512 x 32768 bf16 24.4 against 22.5).
+        const bool many = p.N > (pieces > 4480 ? 2 : 1) * kComputeUnits;
         if (pieces <= 384) hipLaunchKernelGGL((distill_rows<T, E, 3, 2>), g, dim3(256), 0, stream, p);
         else if (pieces <= 768) hipLaunchKernelGGL((distill_rows<T, E, 3, 4>), g, dim3(256), 0, stream, p);
         else if (pieces <= 1792) hipLaunchKernelGGL((distill_rows<T, E, 7, 4>), g, dim3(512), 0, stream, p);
+        else if (!many && pieces <= 3840) hipLaunchKernelGGL((distill_rows<T, E, 15, 4>), g, dim3(1024), 0, stream, p);
+        else if (!many && pieces <= 9600) hipLaunchKernelGGL((distill_rows<T, E, 15, 10>), g, dim3(1024), 0, stream, p);
         else if (pieces <= 2688) hipLaunchKernelGGL((distill_rows<T, E, 7, 6>), g, dim3(512), 0, stream, p);
         else if (pieces <= 4480) hipLaunchKernelGGL((distill_rows<T, E, 7, 10>), g, dim3(512), 0, stream, p);
         else if (pieces <= 8064) hipLaunchKernelGGL((distill_rows<T, E, 7, 18>), g, dim3(512), 0, stream, p);
