@@ -26,20 +26,25 @@ struct DistillParams {
     int64_t ldz, lddz, ldt, N, V;
     int32_t k, slices;
     float tau, scale;           // scale = log2(e) / tau
-    bool past;
+    bool past;                  // (not with many listed words, which are written a second time: 4000 x 32768 bf16 with 256 of
+                                // them 133 us past the caches and 129 through them, with 65 112 and 116)
 };
 
 // The teacher's side of a row in LDS, with room for E entries: words (-1: absent), probabilities, the sums of the probabilities of
 // entries that list the same word, the first part of log2 p = (top - best) scale - log2(total), and z at the words.
 template <int E>
 struct Entries {
-    static constexpr int kBits = E <= 64 ? 10 : 13;
+    static constexpr int kBits = E <= 64 ? 11 : 13;
     int32_t id[E];
     float p[E], sum[E], log[E], z[E];
     uint16_t table[1 << kBits];
     float total;                // sum of exponentials (0: nothing is listed; NaN: a listed logit is)
-    // (multiplied, so that words in even steps spread)
-    static __device__ __forceinline__ int slot(int32_t id) { return (int)((uint32_t)id * 2654435761u >> (32 - kBits)); }
+    // (two multiplications with a shift between them: words in even steps spread, whatever the step)
+    static __device__ __forceinline__ int slot(int32_t id, uint32_t turn) {
+        uint32_t h = ((uint32_t)id + turn) * 2654435761u;
+        h = (h ^ h >> 15) * 0xa3d95fa7u;
+        return (int)((h ^ h >> 14) >> (32 - kBits));
+    }
 };
 
 // Formed by one wave.  z is read at the words lo .. hi - 1 (0 elsewhere).  SUMS: words listed twice are looked for.
@@ -74,33 +79,45 @@ __device__ __forceinline__ void teacher(const DistillParams &p, int64_t n, const
     }
     s = wave_sum(s);
     if (lane == 0) e.total = s;
-    // Words listed twice.  Every entry leaves its number in a table at its word's hash; one that finds another's there
-    // either lists the same word (both have company) or has to look.  Those few are looked up by the whole wave.
     const float r = 1.f / s;
     for (int i = lane; i < p.k; i += 64) {
         const float x = s > 0.f ? e.p[i] * r : s;                        // (s: 0, or NaN)
         e.p[i] = x;
-        if (!SUMS) continue;
-        e.sum[i] = x;
-        if (e.id[i] >= 0) e.table[e.slot(e.id[i])] = (uint16_t)i;
+        if (SUMS) e.sum[i] = x;
     }
     if (!SUMS) return;
+    // Words listed twice.  Every entry leaves its number in a table at its word's hash; one that finds another's there either
+    // lists the same word, or takes part in a second turn with another hash.  Who then finds another's number once more, or has
+    // found its own word, is looked up by the whole wave.  (Entries that list one word meet in the turn that they reach together.)
+    const auto leave = [&](uint32_t turn, uint32_t who) {
+        for (int i = lane, c = 0; i < p.k; i += 64, ++c)
+            if (who >> c & 1 && e.id[i] >= 0) e.table[e.slot(e.id[i], turn)] = (uint16_t)i;
+        __builtin_amdgcn_wave_barrier();
+        __threadfence_block();
+    };
+    uint32_t again = 0, look = 0;                           // bit c: the lane's entry lane + 64 c
+    leave(0, ~0u);
+    for (int i = lane, c = 0; i < p.k; i += 64, ++c) {
+        const int32_t id = e.id[i];
+        const int other = id >= 0 ? e.table[e.slot(id, 0)] : i;
+        if (other != i) (e.id[other] == id ? look : again) |= 1u << c;
+    }
     __builtin_amdgcn_wave_barrier();
     __threadfence_block();
-    for (int i0 = 0; i0 < p.k; i0 += 64) {
-        const int i = i0 + lane;
-        const int32_t id = i < p.k ? e.id[i] : -1;
-        const int other = id >= 0 ? e.table[e.slot(id)] : i;
-        unsigned long long look = __ballot(id >= 0 && other != i);
-        while (look) {
-            const int l = __builtin_ctzll(look);
-            look &= look - 1;
+    if (__any(again != 0)) {
+        leave(1, again);
+        for (int i = lane, c = 0; i < p.k; i += 64, ++c)
+            if (again >> c & 1 && e.table[e.slot(e.id[i], 1)] != i) look |= 1u << c;
+    }
+    for (int i0 = 0, c = 0; i0 < p.k; i0 += 64, ++c) {
+        const int32_t id = i0 + lane < p.k ? e.id[i0 + lane] : -1;
+        unsigned long long left = __ballot(look >> c & 1);
+        while (left) {
+            const int l = __builtin_ctzll(left);
+            left &= left - 1;
             const int32_t word = __shfl(id, l, 64);
-            int alike = 0;
             float sum = 0.f;
-            for (int j = lane; j < p.k; j += 64)
-                if (e.id[j] == word) sum += e.p[j], ++alike;
-            if (wave_sum((float)alike) == 1.f) continue;
+            for (int j = lane; j < p.k; j += 64) sum += e.id[j] == word ? e.p[j] : 0.f;
             sum = wave_sum(sum);
             for (int j = lane; j < p.k; j += 64)
                 if (e.id[j] == word) e.sum[j] = sum;
@@ -430,7 +447,7 @@ grim_status distill_launch(DistillParams p, hipStream_t stream) {
     return launched();
 }
 
-// (room for 64 entries where they suffice: it is what a short row's workgroups share a compute unit by)
+// (room for 64 entries where they suffice: workgroups share a compute unit by their LDS)
 template <typename T>
 grim_status distill_typed(const DistillParams &p, hipStream_t stream) {
     return p.k <= 64 ? distill_launch<T, 64>(p, stream) : distill_launch<T, kMostEntries>(p, stream);
@@ -466,7 +483,7 @@ grim_status grim_distill_topk(const void *z_dev, grim_dtype dt, int64_t ldz, con
     if (workspace_bytes < grim_distill_topk_workspace(N, V)) return GRIM_ERR_SHAPE;
     const DistillParams p{z_dev, top_logits_dev, weight_dev, top_ids_dev, loss_dev, dz_dev, static_cast<float *>(workspace),
                           ldz, lddz, ldt, N, V, k, 0, temperature, 1.44269504088896340736f / temperature,
-                          past_caches(2 * N * V * bytes_of(dt))};
+                          k <= 128 && past_caches(2 * N * V * bytes_of(dt))};
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     return dt == GRIM_F32   ? distill_typed<float>(p, stream)
            : dt == GRIM_F16 ? distill_typed<f16>(p, stream)

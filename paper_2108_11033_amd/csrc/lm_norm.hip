@@ -325,18 +325,22 @@ int back_threads_per_row(int64_t C) {
     return 0;
 }
 
-// Workgroups of the backward pass.  A workgroup's column sums cost 8 C bytes written and read again, so it should have some
-// 64 rows (2 % of 6 C bytes each in 16 bits); but where there are fewer rows than that for 256 workgroups, filling the
-// compute units counts for more.
-inline int64_t back_groups(int64_t N, int rows_at_once) {
-    const int64_t all = (N + rows_at_once - 1) / rows_at_once, lean = N / 64;
-    return all < 256 ? all : lean < 256 ? 256 : lean < 1024 ? lean : 1024;
-}
-
+// Workgroups of the backward pass.  A workgroup's column sums cost 8 C bytes written and read again.  Several rows at a time (teams of
+// a wave or less): 64 rows each, 2 % of 6 C bytes a row in 16 bits, but at least 256 workgroups and at most 1024.  One row at a time: as
+// many as have some 32 KB of rows on their way to a compute unit, up to 1024 with 8 rows or more each (12142 x 1038 fp16: 256
+// workgroups 47 us, 1024 28), but no fewer than 256.
 template <typename T>
 int64_t back_groups_of(int64_t N, int64_t C) {
     const int tpr = back_threads_per_row<T>(C);
-    return back_groups(N, tpr == 16 || tpr == 64 ? 64 * kBackWaves / tpr : 1);
+    const int at_once = tpr == 16 || tpr == 64 ? 64 * kBackWaves / tpr : 1;
+    const int64_t all = (N + at_once - 1) / at_once;
+    int64_t groups = N / 64;
+    if (at_once == 1) {
+        const int64_t each = 32768 / (2 * C * (int64_t)sizeof(T)), room = (each < 1 ? 1 : each) * kComputeUnits;
+        groups = N / 8 < room ? N / 8 : room;
+    }
+    groups = groups < kComputeUnits ? kComputeUnits : groups > 4 * kComputeUnits ? 4 * kComputeUnits : groups;
+    return all < groups ? all : groups;
 }
 
 template <typename T, int TPR>
