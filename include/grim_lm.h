@@ -102,8 +102,8 @@ grim_status grim_glr_step(const float *gates_dev, int64_t ldg, const float *bias
  *   dz_dev         N x V of element type dt, rows of lddz, may be z_dev itself (same ld); NULL: the loss alone
  *   workspace      grim_distill_topk_workspace(N, V) bytes
  * z may hold -infinity (words that cannot come: q = 0); a row that holds nothing else, or +infinity or NaN, gives NaN.
- * Errors: NULL, SHAPE (N < 0, V < 1, V >= 2^31, k < 1, leading dimension too small, tau not positive and finite, workspace
- * too small), DTYPE, DEVICE, UNSUPPORTED (k > 1024).
+ * Errors: NULL, SHAPE (N < 0, V < 1, V >= 2^31, k < 1, leading dimension too small, tau outside 1e-30 .. 1e30,
+ * workspace too small), DTYPE, DEVICE, UNSUPPORTED (k > 1024).
  */
 int64_t grim_distill_topk_workspace(int64_t N, int64_t V);
 grim_status grim_distill_topk(const void *z_dev, grim_dtype dt, int64_t ldz, const float *top_logits_dev,

@@ -475,7 +475,7 @@ grim_status grim_distill_topk(const void *z_dev, grim_dtype dt, int64_t ldz, con
     using namespace grim::lm;
     if (!known(dt)) return GRIM_ERR_DTYPE;
     if (N < 0 || V < 1 || V >= (int64_t)1 << 31 || k < 1 || ldz < V || ldt < k || (dz_dev && lddz < V) || !fits(N, ldz) ||
-        !fits(N, ldt) || (dz_dev && !fits(N, lddz)) || !(temperature > 0.f) || temperature > 3.4e38f)
+        !fits(N, ldt) || (dz_dev && !fits(N, lddz)) || !(temperature >= 1e-30f) || temperature > 1e30f)
         return GRIM_ERR_SHAPE;
     if (k > kMostEntries) return GRIM_ERR_UNSUPPORTED;
     if (N == 0) return GRIM_OK;

@@ -599,6 +599,7 @@ inline Cut cut_rows(int64_t N, int64_t H, bool fp32, bool back) {
     const int64_t even = (N * c.tiles + room - 1) / room;
     const int64_t square = ((int64_t)__builtin_sqrt((double)N / 64.0) + kGroup / 2) / kGroup * kGroup;
     int64_t L = even > square ? even : square;
+    L = L < N ? L : N;
     L = (L + kGroup - 1) / kGroup * kGroup;                     // (up to 64 rows: one set, one launch)
     c.L = (int32_t)(L < kGroup ? kGroup : L);
     const int64_t rows = (int64_t)c.L * kWaves;

@@ -397,12 +397,12 @@ grim_status norm_back_typed(const NormBackParams &p, float *dgamma, float *dbeta
             case 1024: st = norm_back_launch<T, 1024>(p, groups, stream); break;
             default:
                 if (p.N > kMaxGrid || (p.C + 255) / 256 > 65535) return GRIM_ERR_SHAPE;
-                if (p.dx) hipLaunchKernelGGL(norm_back_any<T>, dim3((unsigned)p.N), dim3(256), 0, stream, p);
-                if (p.part) {
+                if (p.part) {                                               // first: dx may take dy's place
                     const int64_t slab = (p.N + groups - 1) / groups;
                     hipLaunchKernelGGL(norm_back_columns<T>, dim3((unsigned)groups, (unsigned)((p.C + 255) / 256)), dim3(256), 0,
                                        stream, p, slab);
                 }
+                if (p.dx) hipLaunchKernelGGL(norm_back_any<T>, dim3((unsigned)p.N), dim3(256), 0, stream, p);
                 st = launched();
         }
     }

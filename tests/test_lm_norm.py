@@ -122,8 +122,12 @@ def test_in_place_and_partial_outputs(dtype, C):
     assert torch.equal(only, dbeta)
     g.layer_norm_backward(dy, C, *args, None, 0, only, None, ws)
     assert torch.equal(only, dgamma)
-    g.layer_norm_backward(dy, C, *args, dy, C, None, None, None)             # dx over dy, no column sums, no workspace
-    assert torch.equal(dy, dx)
+    mine = dy.clone()
+    g.layer_norm_backward(mine, C, *args, mine, C, None, None, None)         # dx over dy, no column sums, no workspace
+    assert torch.equal(mine, dx)
+    again = [torch.empty(C, device="cuda") for _ in range(2)]
+    g.layer_norm_backward(dy, C, *args, dy, C, *again, ws)                   # dx over dy, which the column sums read too
+    assert torch.equal(dy, dx) and torch.equal(again[0], dgamma) and torch.equal(again[1], dbeta)
 
 
 @pytest.mark.gpu
