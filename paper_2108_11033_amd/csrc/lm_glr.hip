@@ -56,6 +56,9 @@ __device__ __forceinline__ void gate(float t, float &f, float &k) {
     k = e * f;
 }
 
+// sigmoid(z) alone needs no bound: the reciprocal of infinity is 0
+__device__ __forceinline__ float open(float t) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(t)); }
+
 __device__ __forceinline__ bool forgets(float a) { return __builtin_bit_cast(unsigned, a) == 0x80000000u; }
 __device__ __forceinline__ float apply(float a, float b, float s) { return forgets(a) ? b : __builtin_fmaf(a, s, b); }
 // (a, b) after (a0, b0)
@@ -225,9 +228,7 @@ __device__ __forceinline__ void backward_map(const GlrParams &p, const Starts &s
                 unpack(d.r[i], dy);
 #pragma unroll
                 for (int j = 0; j < VEC; ++j) {
-                    float f, k, o, ko;
-                    gate(__builtin_fmaf(zu[j], -kLog2e, bias.u[j]), f, k);
-                    gate(__builtin_fmaf(zv[j], -kLog2e, bias.v[j]), o, ko);
+                    const float f = open(__builtin_fmaf(zu[j], -kLog2e, bias.u[j])), o = open(__builtin_fmaf(zv[j], -kLog2e, bias.v[j]));
                     A[j] *= f;
                     B[j] = f * __builtin_fmaf(dy[j], o, B[j]);
                 }
@@ -396,11 +397,10 @@ __global__ void __launch_bounds__(64 * kWaves, waves_forward<VEC>()) glr_forward
                 unpack(v.r[i], zv);
 #pragma unroll
                 for (int j = 0; j < VEC; ++j) {
-                    float f, k, o, ko;
+                    float f, k;
                     gate(__builtin_fmaf(zu[j], -kLog2e, bias.u[j]), f, k);
-                    gate(__builtin_fmaf(zv[j], -kLog2e, bias.v[j]), o, ko);
                     h[j] = __builtin_fmaf(f, h[j], k * (zc[j] + bias.c[j]));
-                    out[j] = o * h[j];
+                    out[j] = open(__builtin_fmaf(zv[j], -kLog2e, bias.v[j])) * h[j];
                 }
                 if (un.live) {
                     store<PAST>(y + (int64_t)r * p.ldy, out);
@@ -565,12 +565,11 @@ __global__ void __launch_bounds__(256) glr_step_kernel(GlrStepParams p) {
     const int64_t b = e - r * p.batch;
     float zu = p.gates[r * p.ldg + b], zc = p.gates[(p.H + r) * p.ldg + b], zv = p.gates[(2 * p.H + r) * p.ldg + b];
     if (p.bias) zu += p.bias[r], zc += p.bias[p.H + r], zv += p.bias[2 * p.H + r];
-    float f, k, o, ko;
+    float f, k;
     gate(zu * -kLog2e, f, k);
-    gate(zv * -kLog2e, o, ko);
     const float h = __builtin_fmaf(f, p.h[r * p.ldh + b], k * zc);
     p.h_new[r * p.ldh_new + b] = h;
-    if (p.y) static_cast<T *>(p.y)[r * p.ldy + b] = (T)(o * h);
+    if (p.y) static_cast<T *>(p.y)[r * p.ldy + b] = (T)(open(zv * -kLog2e) * h);
 }
 
 // ---------------------------------------------------------------------------------------------- launches
