@@ -5,12 +5,15 @@
 //     du = G f (1 - f) (h_(t-1) - c)    dc = G (1 - f)    dv = dy h sigmoid(v) (1 - sigmoid(v))    dh0 = f_0 G_0
 //
 // Both directions are linear in the state that is handed on: what a run of tokens does to it is a map S -> A S + B per unit, and
-// maps compose.  The rows of all sequences are cut alike, whatever their lengths, into chunks (one wave, 64 or 128 units)
+// maps compose.  The rows of all sequences are cut alike, whatever their lengths, into chunks (one wave, 64 to 256 units)
 // and sets of kWaves chunks (one workgroup).  A first launch forms the maps of the chunks and sets; the second composes the maps of the
 // sets in front of its own, which gives every wave its state, and walks its rows again.  That reads u and c (backward: u, v
 // and dy) twice, the price of the parallelism along the sequence; the sets are walked in the opposite order so that what was
 // read last is still in the last-level cache.  A sequence that starts inside a run makes the map forget what came before: A = -0, told
 // apart from a product of gates that has underflowed, so that an infinity or NaN crosses underflow but no start.
+//
+// What it measured (both directions, bf16): 65536 x 1024 459 us, of which maps 55 + 79, forward 110, backward 202, at 4.4 to 5.2 TB/s each
+// of what they read and write; 512 x 1024 23.7 us, where launches and the chain starts -> rows -> maps through LDS count.
 //
 // The backward pass needs h_(t-1).  The forward pass leaves the state in front of every kGroup-th row (fp32: 4 bytes for 8 rows of
 // 2 to 4 bytes each), from which a group's states are formed again in registers.
