@@ -48,6 +48,7 @@ struct GlrParams {
     float *chunk_maps, *set_maps;   // [chunk or set][A | B][H]
     int64_t ldg, ldy, lddy, lddg, N, H;
     int32_t nseq, L, sets, tiles;   // rows of a chunk (a multiple of kGroup), sets of kWaves chunks, column blocks
+    bool torn;                      // rows that are not whole cache lines
 };
 
 // f = sigmoid(z) and k = 1 - f = sigmoid(-z) of t = -z log2(e), without cancellation: k = 2^t f.  2^126 is as good as
@@ -266,6 +267,26 @@ __device__ __forceinline__ void compose_chunks(float (*maps)[2][64 * VEC], int p
     }
 }
 
+// The set and column block of a workgroup.  Workgroups are dealt to the eight XCDs in turn.  Where rows are whole cache lines, the column blocks of a
+// set are: one XCD reads the same units of all sets, and its L2 still holds their maps in the second launch.  Where lines are torn
+// between column blocks, all blocks of a set go to one XCD, whose L2 reads a line once for both (24007 x 1000 fp16, both directions, 193 against
+// 173 us; 65536 x 1024 bf16, whole lines, 458 against 460, fp32 2048 x 1024 33.6 against 35.2).  LAST: the sets in descending order.
+template <bool LAST>
+struct Place {
+    int set, tile;
+    __device__ __forceinline__ Place(const GlrParams &p) {
+        const int b = blockIdx.x;
+        if (p.torn) {
+            set = b % 8 + 8 * (LAST ? (p.sets + 7) / 8 - 1 - b / 8 / p.tiles : b / 8 / p.tiles);      // (set may be one of up to 7 too many)
+            tile = b / 8 % p.tiles;
+        } else {
+            set = LAST ? p.sets - 1 - b / p.tiles : b / p.tiles;
+            tile = b % p.tiles;
+        }
+    }
+};
+inline unsigned workgroups(const GlrParams &p) { return (unsigned)(p.torn ? (p.sets + 7) / 8 * 8 : p.sets) * p.tiles; }
+
 // Rows of this wave's chunk.
 struct Chunk {
     int wave, index, r0, r1;
@@ -281,8 +302,10 @@ template <typename T, int VEC, bool BACK>
 __global__ void __launch_bounds__(64 * kWaves, kWavesMaps) glr_maps(GlrParams p) {
     __shared__ float maps[kWaves][2][64 * VEC];
     const Starts starts(p);
-    const int set = blockIdx.x / p.tiles;
-    const Units<VEC> un(blockIdx.x % p.tiles, p.H);
+    const Place<false> here(p);
+    const int set = here.set;
+    if (set >= p.sets) return;
+    const Units<VEC> un(here.tile, p.H);
     Bias<VEC> bias(p, un.at);
     const Chunk ch(p, set);
     float a[VEC], b[VEC], A[VEC], B[VEC], SA[VEC], SB[VEC];
@@ -346,8 +369,10 @@ template <typename T, int VEC, bool ALONE, bool PAST>
 __global__ void __launch_bounds__(64 * kWaves, waves_forward<VEC>()) glr_forward(GlrParams p) {
     __shared__ float maps[kWaves][2][64 * VEC];
     const Starts starts(p);
-    const int set = ALONE ? 0 : p.sets - 1 - (int)blockIdx.x / p.tiles;
-    const Units<VEC> un(blockIdx.x % p.tiles, p.H);
+    const Place<true> here(p);
+    const int set = ALONE ? 0 : here.set;
+    if (set >= p.sets) return;
+    const Units<VEC> un(ALONE ? (int)blockIdx.x : here.tile, p.H);
     Bias<VEC> bias(p, un.at);
     const Chunk ch(p, set);
     const int r0 = ch.r0, r1 = ch.r1;
@@ -420,8 +445,10 @@ __global__ void __launch_bounds__(64 * kWaves, waves_backward<VEC>()) glr_backwa
     __shared__ float maps[kWaves][2][64 * VEC];
     __shared__ float sums[3][64 * VEC];
     const Starts starts(p);
-    const int set = ALONE ? 0 : p.sets - 1 - (int)blockIdx.x / p.tiles;
-    const Units<VEC> un(blockIdx.x % p.tiles, p.H);
+    const Place<true> here(p);
+    const int set = ALONE ? 0 : here.set;
+    if (set >= p.sets) return;
+    const Units<VEC> un(ALONE ? (int)blockIdx.x : here.tile, p.H);
     Bias<VEC> bias(p, un.at);
     const Chunk ch(p, set);
     float R[VEC];
@@ -589,9 +616,10 @@ inline Cut cut_rows(int64_t N, int64_t H, bool fp32, bool back) {
     // one unit a lane where more would leave compute units without work (1024 x 1024 bf16 24 against 27 us, 2048 x 1024 31 against 30)
     c.vec = H >= 256 && N * H >= (int64_t)1 << 21 ? wide_one : 1;
     c.past = past_caches((back ? 7 : 4) * N * H * (fp32 ? 4 : 2));
-    // eight bytes of a row where the outputs go past the caches, if three or more column blocks remain (24007 x 1000 fp16 193 against 209
-    // us; 32768 x 512 139 against 119)
-    c.last = c.past && c.vec == 2 && H >= 768 ? 4 : c.vec;
+    // Eight bytes of a row where the outputs go past the caches, if three or more column blocks remain (bf16 forward 65536 x 1000 183 against
+    // 194 us, as long with H = 1024); backward, where a compute unit then holds one workgroup instead of two, only with more than one
+    // round of them (26 M units: 65536 x 1000 322 against 377 us, 65536 x 1024 285 against 297; 16384 x 1024 74 against 66).
+    c.last = c.past && c.vec == 2 && H >= 768 && (!back || N * H >= (int64_t)26 << 20) ? 4 : c.vec;
     c.tiles = (int32_t)((H + 64 * c.vec - 1) / (64 * c.vec));
     // Chunks so short that the workgroups fill the compute units once (the second launch of the backward pass has room for 512,
     // the others for 1024), but no shorter than keep the maps of the sets, all of which a workgroup may have to read, within its own
@@ -613,7 +641,7 @@ inline int64_t map_floats(const Cut &c, int64_t H) { return ((int64_t)c.sets * (
 
 template <typename T, int VEC>
 grim_status glr_launch(const GlrParams &p, const Cut &c, bool back, hipStream_t stream) {
-    const dim3 grid((unsigned)c.sets * c.tiles), block(64 * kWaves);      // (the column blocks of a set's rows side by side)
+    const dim3 grid(c.sets == 1 ? (unsigned)p.tiles : workgroups(p)), block(64 * kWaves);
     if (c.sets == 1) {
         if (back) hipLaunchKernelGGL((glr_backward<T, VEC, true, false>), grid, block, 0, stream, p);
         else hipLaunchKernelGGL((glr_forward<T, VEC, true, false>), grid, block, 0, stream, p);
@@ -626,7 +654,7 @@ grim_status glr_launch(const GlrParams &p, const Cut &c, bool back, hipStream_t 
     constexpr int W = VEC == 2 ? 4 : VEC;
     GlrParams q = p;
     q.tiles = (int32_t)((p.H + 64 * c.last - 1) / (64 * c.last));
-    const dim3 last((unsigned)c.sets * q.tiles);
+    const dim3 last(workgroups(q));
     if (c.last == 4) {
         if (back) hipLaunchKernelGGL((glr_backward<T, W, false, true>), last, block, 0, stream, q);
         else hipLaunchKernelGGL((glr_forward<T, W, false, true>), last, block, 0, stream, q);
@@ -643,6 +671,9 @@ grim_status glr_launch(const GlrParams &p, const Cut &c, bool back, hipStream_t 
 grim_status glr_run(GlrParams p, grim_dtype dt, bool back, hipStream_t stream) {
     const Cut c = cut_rows(p.N, p.H, dt == GRIM_F32, back);
     p.L = c.L, p.sets = c.sets, p.tiles = c.tiles;
+    const int64_t e = bytes_of(dt);
+    const auto whole = [&](const void *at, int64_t ld) { return !at || ((uintptr_t)at | (uintptr_t)(ld * e)) % 128 == 0; };
+    p.torn = !(p.H * e % 128 == 0 && whole(p.gates, p.ldg) && whole(p.y, p.ldy) && whole(p.dy, p.lddy) && whole(p.dgates, p.lddg));
     p.set_maps = p.chunk_maps + (int64_t)c.sets * kWaves * 2 * p.H;
     switch (dt) {
         case GRIM_F32: return c.vec > 1 ? glr_launch<float, wide<float>()>(p, c, back, stream) : glr_launch<float, 1>(p, c, back, stream);

@@ -129,6 +129,20 @@ def test_forward_and_backward(dtype, N, H, starts):
     assert all(torch.equal(a, b) for a, b in zip(got, again)), "a second call gave other bits"
 
 
+# Several units of a lane (from 2 M units), operands of more than 128 MiB, rows of whole cache lines and others.
+WIDE = [("bf16", 2100, 1024, 0), ("f16", 2310, 1001, 3), ("f32", 5000, 1000, 1), ("bf16", 20000, 512, 0), ("f16", 17000, 1000, 0), ("bf16", 27400, 1000, 0), ("f16", 26700, 1024, 0)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,N,H,pad", WIDE)
+def test_wide_and_large(dtype, N, H, pad):
+    starts = _cuts(H, N, 7)
+    gates, bias, h0, dy, dh_last = _operands(dtype, N, H, 7, pad, pad, 80)
+    seq = torch.tensor(starts, dtype=torch.int32, device="cuda")
+    got = _train(dtype, gates, bias, h0, seq, 7, N, H, dy, dh_last, pad, pad)
+    _check(got, *reference(gates, bias, h0, starts, dy, dh_last), dtype)
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("N", [0, 1, 100, 700])
 def test_left_out_operands(N):
