@@ -88,6 +88,13 @@ def test_loss_and_gradient(dtype, N, V, k):
     assert torch.equal(mine, first) and torch.equal(again, loss) and untouched(mine, mbuf)
 
 
+# logits and gradients of more than 128 MiB, written past the caches up to 128 listed words
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,N,V,k", [("bf16", 9001, 4100, 64), ("f16", 1100, 32771, 129), ("f32", 600, 30000, 32)])
+def test_operands_beyond_the_caches(dtype, N, V, k):
+    test_loss_and_gradient(dtype, N, V, k)
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("N,V", [(4, 50000), (200, 5000)])
 def test_masked_words(N, V):

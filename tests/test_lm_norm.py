@@ -76,6 +76,14 @@ def test_backward(dtype, N, C):
         assert all(torch.equal(a, b) for a, b in zip(first, (dx, dgamma, dbeta))), "a second call gave other bits"
 
 
+# operands of more than 128 MiB, which are written past the caches: rows in registers and rows that are walked
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,N,C", [("f16", 35001, 1001), ("bf16", 36000, 1024), ("f32", 4200, 4100), ("bf16", 900, 40001)])
+def test_operands_beyond_the_caches(dtype, N, C):
+    test_forward(dtype, N, C)
+    test_backward(dtype, N, C)
+
+
 @pytest.mark.gpu
 def test_backward_against_differences():
     """sum(dy y) along a direction, both ways, of the fp32 kernel itself: the difference quotient at h = 1/64 is off by
