@@ -48,7 +48,7 @@ struct Entries {
     }
 };
 
-// Formed by one wave.  z is read at the words lo .. hi - 1 (0 elsewhere).  SUMS: words listed twice are looked for.
+// Formed by one wave.  The words lo .. hi - 1 get their z, others the word -1.  SUMS: words listed twice are looked for.
 template <bool SUMS, int E, typename T>
 __device__ __forceinline__ void teacher(const DistillParams &p, int64_t n, const T *z, int64_t lo, int64_t hi, Entries<E> &e) {
     const int lane = threadIdx.x & 63;
@@ -56,16 +56,31 @@ __device__ __forceinline__ void teacher(const DistillParams &p, int64_t n, const
     const int32_t *ids = p.ids + n * p.ldt;
     float m = -INFINITY;
     bool nan = false;
-    for (int i = lane; i < p.k; i += 64) {
-        const int32_t id = ids[i];
-        const float listed = t[i];
-        const bool there = id >= 0 && id < p.V;
-        const float v = there ? listed : -INFINITY;
-        e.z[i] = id >= lo && id < hi ? (float)z[id] : 0.f;
-        e.id[i] = there ? id : -1;
-        e.log[i] = v;
-        nan |= v != v;
-        m = fmaxf(m, v);
+    // (up to 256 entries asked for at once, then their words: two waits for memory.  24 x 131075 fp16 in slices, 1000 listed words 32.9 us
+    // against 34.7 one by one, and 28.2 since a slice leaves out the others' words here)
+    constexpr int B = E < 256 ? E / 64 : 4;
+    for (int i0 = lane; i0 < p.k; i0 += 64 * B) {
+        int32_t id[B];
+        float listed[B], z_at[B];
+#pragma unroll
+        for (int b = 0; b < B; ++b) {
+            const int i = i0 + 64 * b < p.k ? i0 + 64 * b : 0;
+            id[b] = ids[i], listed[b] = t[i];
+        }
+#pragma unroll
+        for (int b = 0; b < B; ++b) z_at[b] = (float)z[id[b] >= lo && id[b] < hi ? id[b] : lo];
+#pragma unroll
+        for (int b = 0; b < B; ++b) {
+            const int i = i0 + 64 * b;
+            if (i >= p.k) break;
+            const bool here = id[b] >= lo && id[b] < hi;
+            const float v = id[b] >= 0 && id[b] < p.V ? listed[b] : -INFINITY;
+            e.z[i] = here ? z_at[b] : 0.f;
+            e.id[i] = here ? id[b] : -1;
+            e.log[i] = v;
+            nan |= v != v;
+            m = fmaxf(m, v);
+        }
     }
     m = wave_max(m);
     if (__any(nan)) m = NAN;
