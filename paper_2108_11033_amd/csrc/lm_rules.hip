@@ -7,7 +7,7 @@
 // callers, counts the histories' words that fall into it in LDS (whole-number atomics: the order cannot matter), and then
 // transforms the tile.  Every tile reads its callers' whole histories again (from L2), which costs less than a table of counts in
 // memory, cleared, filled and read by three launches.  A word's place in LDS holds its count and, above it, the entry of the bias list
-// that adds to it: four bytes a word, so that a compute unit holds four tiles of 8192.  Measured: 64 callers x 131072 words bf16 13.5 us (9.7
+// that adds to it: four bytes a word, so that a compute unit holds four tiles of 8192.  Measured: 64 callers x 131072 words bf16 12.6 us (9.7
 // without any rule, a copy 5.9: the phases of one round of workgroups follow each other), one caller x 32768 words 4.5 us of kernel.
 #include "lm_common.hpp"
 
@@ -32,14 +32,14 @@ struct CallerRules {
           presence(r.presence ? r.presence[b] : 0.f) {
         inverse = 1.f / repetition;             // (a product for a division: one rounding of 2^-24 more)
     }
-    // place: the word's place in LDS; biases: the entries' values.  Most words are in no list: the arithmetic is skipped where that holds
+    // place: the word's place in LDS; biases: the end of the entries' sums.  Most words are in no list: the arithmetic is skipped where that holds
     // for all of a wave's.
     __device__ __forceinline__ float apply(float z, uint32_t place, const float *biases, bool allowed) const {
         if (__any(place != 0)) {
             const uint32_t count = place & ((1u << kCountBits) - 1), entry = place >> kCountBits;
             const float said = z * (z > 0.f ? inverse : repetition) - frequency * (float)count - presence;
             z = count ? said : z;
-            if (entry) z += biases[entry - 1];
+            if (entry) z += biases[-(int)entry];
         }
         return allowed ? z : -INFINITY;
     }
@@ -91,44 +91,66 @@ struct History {
     }
 };
 
-// A caller's biases for words lo .. lo + span - 1, by thread t of `width`: the first entry of a word notes its number at the
-// word's place and adds up the values of all entries of the word, in the list's order, into sums[entry].
-__device__ __forceinline__ void add_biases(int32_t nbias, const int32_t *ids, const float *values, int lo, int span, uint32_t *places,
-                                           int shift, float *sums, int t, int width) {
-    for (int i = t; i < nbias; i += width) {
-        const int32_t id = ids[i];
-        const uint32_t at = (uint32_t)id - (uint32_t)lo;
-        if (id < 0 || at >= (uint32_t)span) continue;
-        int earlier = 0, alike = 0;
-#pragma unroll 8
-        for (int j = 0; j < nbias; ++j) {
-            const int same = ids[j] == id;
-            alike += same;
-            earlier += j < i ? same : 0;
+// A caller's biases, by thread t of `width`; the first two entries of each thread are asked for early.  Two steps, each behind a
+// barrier: a place gets nbias - i for the first entry i of its word, by a maximum, before anything is counted there, and sums[i] the
+// entry's value; and where `twice` says that a word of the tile is listed again, first entries add up their words' in the list's order.
+// (43 callers x 18112 words fp32 in columns with 126 entries 8.5 us; 15.9 with every entry held against the whole list.)
+struct Biases {
+    const int32_t *ids;
+    const float *values;
+    int n, t, width;
+    int32_t id[2];
+    float value[2];
+    __device__ __forceinline__ Biases(const grim_logit_rules &r, int64_t b, int t_, int width_)
+        : ids(r.bias_ids + b * r.ld_bias), values(r.bias_values + b * r.ld_bias), n(r.nbias), t(t_), width(width_) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int i = t + k * width;
+            id[k] = i < n ? ids[i] : -1;
+            value[k] = i < n ? values[i] : 0.f;
         }
-        if (earlier) continue;
-        float sum = values[i];
-        if (alike > 1)
-            for (int j = i + 1; j < nbias; ++j)
-                if (ids[j] == id) sum += values[j];
-        sums[i] = sum;
-        atomicAdd(&places[at << shift], (uint32_t)(i + 1) << kCountBits);
     }
-}
+    // f(entry, which of the thread's it is, word, its distance from lo) for the entries of words lo .. lo + span - 1
+    template <typename F>
+    __device__ __forceinline__ void each(int lo, int span, F f) const {
+        for (int i = t, k = 0; i < n; i += width, ++k) {
+            const int32_t word = k == 0 ? id[0] : k == 1 ? id[1] : ids[i];
+            const uint32_t at = (uint32_t)word - (uint32_t)lo;
+            if (word >= 0 && at < (uint32_t)span) f(i, k, word, at);
+        }
+    }
+    __device__ __forceinline__ void place(int lo, int span, uint32_t *places, int shift, float *sums, int *twice) const {
+        each(lo, span, [&](int i, int k, int32_t, uint32_t at) {
+            sums[i] = k == 0 ? value[0] : k == 1 ? value[1] : values[i];
+            if (atomicMax(&places[at << shift], (uint32_t)(n - i) << kCountBits)) *twice = 1;
+        });
+    }
+    __device__ __forceinline__ void join(int lo, int span, const uint32_t *places, int shift, float *sums) const {
+        each(lo, span, [&](int i, int, int32_t word, uint32_t at) {
+            if (places[at << shift] >> kCountBits != (uint32_t)(n - i)) return;
+            float sum = values[i];
+#pragma unroll 8
+            for (int j = i + 1; j < n; ++j)
+                if (ids[j] == word) sum += values[j];
+            sums[i] = sum;
+        });
+    }
+};
 
 // A row per caller: TILE words of one caller.  Everything that a tile reads is asked for at its start.
 template <typename T, int TILE, int THREADS>
 __global__ void __launch_bounds__(THREADS) rules_rows(RuleParams p, int tiles) {
     constexpr int V = 16 / (int)sizeof(T), PER = TILE / (THREADS * V);
     __shared__ __attribute__((aligned(16))) uint32_t places[TILE];
-    __shared__ int32_t ids[kMostBias];
-    __shared__ float values[kMostBias];                         // becomes the sums: an entry's value is read for its own word only
+    __shared__ float sums[kMostBias];
+    __shared__ int twice;
     const int64_t b = blockIdx.x / tiles, lo = (int64_t)(blockIdx.x % tiles) * TILE;
     const int64_t hi = lo + TILE < p.V ? lo + TILE : p.V;
     const T *z = static_cast<const T *>(p.z) + b * p.ldz + lo;
     T *out = static_cast<T *>(p.out) + b * p.ldo + lo;
     const int span = (int)(hi - lo);
     History history(p.r, b, threadIdx.x, THREADS);
+    const Biases biases(p.r, b, threadIdx.x, THREADS);
     const CallerRules rules(p.r, b);
     const uint32_t *allowed = p.r.allowed ? p.r.allowed + b * p.r.ld_allowed + lo / 32 : nullptr;
     Pack<T, V> raw[PER];
@@ -142,16 +164,17 @@ __global__ void __launch_bounds__(THREADS) rules_rows(RuleParams p, int tiles) {
             for (int j = 0; j < V; ++j) put(raw[k], j, c + j < span ? z[c + j] : (T)0.f);
         bits[k] = allowed && c < span ? allowed[c / 32] >> (c % 32) : 0xffffffffu;
     }
-    for (int i = threadIdx.x; i < p.r.nbias; i += THREADS) {
-        ids[i] = p.r.bias_ids[b * p.r.ld_bias + i];
-        values[i] = p.r.bias_values[b * p.r.ld_bias + i];
-    }
     const bool lists = history.most > 0 || p.r.nbias > 0;       // (a mask alone needs no places)
     if (lists) {
         for (int i = threadIdx.x; i < TILE / 4; i += THREADS) reinterpret_cast<uint4 *>(places)[i] = uint4{0, 0, 0, 0};
+        if (threadIdx.x == 0) twice = 0;
         __syncthreads();
+        if (p.r.nbias > 0) {
+            biases.place((int)lo, span, places, 0, sums, &twice);
+            __syncthreads();
+            if (twice) biases.join((int)lo, span, places, 0, sums);
+        }
         history.tally((int)lo, span, places, 0);
-        add_biases(p.r.nbias, ids, values, (int)lo, span, places, 0, values, threadIdx.x, THREADS);
         __syncthreads();
     }
 #pragma unroll
@@ -160,7 +183,7 @@ __global__ void __launch_bounds__(THREADS) rules_rows(RuleParams p, int tiles) {
         if (c >= span) continue;
         float v[V];
 #pragma unroll
-        for (int j = 0; j < V; ++j) v[j] = rules.apply(element(raw[k], j), lists ? places[c + j] : 0, values, bits[k] >> j & 1);
+        for (int j = 0; j < V; ++j) v[j] = rules.apply(element(raw[k], j), lists ? places[c + j] : 0, sums + p.r.nbias, bits[k] >> j & 1);
         if (c + V <= span) store(out + c, v);
         else
 #pragma unroll
@@ -177,6 +200,7 @@ __global__ void __launch_bounds__(THREADS) rules_columns(RuleParams p, int tiles
     constexpr int PER = TILE / THREADS;
     __shared__ __attribute__((aligned(16))) uint32_t places[TILE];
     __shared__ float sums[kMostCallers][BIAS];
+    __shared__ int twice[kMostCallers];
     const int words = TILE >> shift;
     const int64_t b0 = (int64_t)(blockIdx.x / tiles) << shift, lo = (int64_t)(blockIdx.x % tiles) * words;
     const int64_t hi = lo + words < p.V ? lo + words : p.V;
@@ -202,24 +226,31 @@ __global__ void __launch_bounds__(THREADS) rules_columns(RuleParams p, int tiles
             bits[k] = allowed ? allowed[word / 32] >> (word % 32) : 1u;
         }
     };
+    // as many waves per caller as there are
+    static_assert(THREADS / 64 >= kMostCallers, "a wave per caller");
+    const int each = THREADS / 64 >> shift, wave = threadIdx.x >> 6, b = wave / each;
+    const int t = (wave % each) * 64 + (threadIdx.x & 63), width = each * 64;
+    const bool lists = b < callers;
+    const int64_t own = b0 + (lists ? b : 0);
+    History history(p.r, own, t, width);
+    const Biases biases(p.r, own, t, width);
     if (early) fetch(0);
     for (int i = threadIdx.x; i < TILE / 4; i += THREADS) reinterpret_cast<uint4 *>(places)[i] = uint4{0, 0, 0, 0};
+    if (threadIdx.x < kMostCallers) twice[threadIdx.x] = 0;
     __syncthreads();
-    // as many waves per caller as there are
-    const int each = max(THREADS / 64 >> shift, 1), wave = threadIdx.x >> 6;
-    const int t = (wave % each) * 64 + (threadIdx.x & 63), width = each * 64;
-    for (int b = wave / each; b < callers; b += THREADS / 64 / each) {
-        History(p.r, b0 + b, t, width).tally((int)lo, span, places + b, shift);
-        const int64_t list = (b0 + b) * p.r.ld_bias;
-        add_biases(p.r.nbias, p.r.bias_ids + list, p.r.bias_values + list, (int)lo, span, places + b, shift, sums[b], t, width);
+    if (p.r.nbias > 0) {
+        if (lists) biases.place((int)lo, span, places + b, shift, sums[b], &twice[b]);
+        __syncthreads();
+        if (lists && twice[b]) biases.join((int)lo, span, places + b, shift, sums[b]);
     }
+    if (lists) history.tally((int)lo, span, places + b, shift);
     __syncthreads();
     for (int k0 = 0; k0 < PER; k0 += STEP) {
         if (!early) fetch(k0);
 #pragma unroll
         for (int k = 0; k < STEP; ++k) {
             const int i = (k0 + k) * THREADS + (int)threadIdx.x, at = i >> shift;
-            if (live && at < span) out[(lo + at) * p.ldo] = (T)rules.apply(v[k], places[i], sums[mine], bits[k] & 1);
+            if (live && at < span) out[(lo + at) * p.ldo] = (T)rules.apply(v[k], places[i], sums[mine] + p.r.nbias, bits[k] & 1);
         }
     }
 }

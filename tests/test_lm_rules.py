@@ -113,6 +113,22 @@ def test_grammar_that_allows_nothing_and_nan():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("columns", [False, True])
+def test_longest_lists_of_one_word(columns):
+    """A word's count and its entry of the bias list at their most, together: a history of 2^20 times one word, that word first and last of 1024."""
+    V, batch, L, nb = 1500, 2, 2 ** 20, 1024
+    ids = torch.arange(100, 100 + nb, device="cuda", dtype=torch.int32).repeat(batch, 1)
+    ids[:, 0] = ids[:, nb - 1] = 7
+    r = dict(history=torch.full((batch, L), 7, device="cuda", dtype=torch.int32), ld_history=L, max_history=L, frequency=torch.full((batch,), 0.25, device="cuda"),
+             bias_ids=ids, bias_values=randn(3, batch, nb), nbias=nb, ld_bias=nb)
+    buf, view = _logits("f32", V, batch, columns, 0, 4)
+    out, oview = _logits("f32", V, batch, columns, 0, 1)
+    g.logit_rules(buf, "f32", buf.stride(0), V, batch, out, out.stride(0), columns=columns, **r)
+    want, slack = reference(view.double(), r, batch, V)
+    close(oview, want, slack, "f32", "logits")
+
+
+@pytest.mark.gpu
 def test_same_bits_again_and_no_callers():
     V, batch = 40000, 17
     r = _rules(V, batch, 3000, 200, 8)
