@@ -270,12 +270,14 @@ grim_status rules_launch(const RuleParams &p, hipStream_t stream) {
     return launched();
 }
 
-// Tiles of 8192 places, of 2048 where those would leave compute units without one.  (64 callers x 131072 words bf16: 13.5 us with
-// 8192 places and 512 threads, 14.9 with 256 threads, 16.3 with 1024; 16384 places 14.4, 2048 places and 256 threads 15.5.)
+// Tiles of 8192 places, of 2048 where those would leave compute units without one, or in columns, where a tile's chain is longer, with
+// less than two.  (64 callers x 131072 words bf16, masks too, 12.6 us with 8192 places and 512 threads, 14.5 with 256 threads; 4096
+// places 11.9, but 128 callers 19.9 against 18.3; 2048 places 14.0.  Columns bf16: 32 x 32768 9.1 us with 8192 places, 5.6 with 2048; 64 x 50000
+// 17.0 and 13.7; 32 x 131072 13.1 and 13.3, 64 x 131072 18.2 and 27.)
 template <typename T>
 grim_status rules_typed(const RuleParams &p, bool columns, hipStream_t stream) {
     if (p.batch == 1 && p.ldz == 1 && p.ldo == 1) columns = false;   // a single dense column is a row
-    if (p.V * p.batch >= (int64_t)4096 * kComputeUnits)
+    if (p.V * p.batch >= (int64_t)(columns ? 16384 : 4096) * kComputeUnits)
         return columns ? rules_launch<T, 8192, 512, true>(p, stream) : rules_launch<T, 8192, 512, false>(p, stream);
     return columns ? rules_launch<T, 2048, 512, true>(p, stream) : rules_launch<T, 2048, 256, false>(p, stream);
 }
