@@ -210,10 +210,17 @@ __global__ void __launch_bounds__(TPR < 256 ? 64 * kBackWaves : TPR) norm_back_r
     if (!p.part) return;
     float *part = p.part + (int64_t)blockIdx.x * 2 * p.C;
     if (TPR >= 256) {
-        cut.own([&](int k, int j) {
-            part[cut.at[k] + j] = ag[k][j];
-            part[p.C + cut.at[k] + j] = ab[k][j];
-        });
+        // (whole pieces at a time: 300 x 8192 fp16 16 us, 25 element by element)
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            if (k < PER - 1 || cut.first == 0) {
+                store(part + cut.at[k], ag[k]);
+                store(part + p.C + cut.at[k], ab[k]);
+            } else
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    if (j >= cut.first) part[cut.at[k] + j] = ag[k][j], part[p.C + cut.at[k] + j] = ab[k][j];
+        }
         return;
     }
     if (TPR < 64)
@@ -329,8 +336,8 @@ int back_threads_per_row(int64_t C) {
 
 // Workgroups of the backward pass.  A workgroup's column sums cost 8 C bytes written and read again.  Several rows at a time (teams of
 // a wave or less): 64 rows each, 2 % of 6 C bytes a row in 16 bits, but at least 256 workgroups and at most 1024.  One row at a time: as
-// many as have some 32 KB of rows on their way to a compute unit, up to 1024 with 8 rows or more each (12142 x 1038 fp16: 256
-// workgroups 47 us, 1024 28), but no fewer than 256.
+// many as have some 32 KB of rows on their way to a compute unit, up to 1024 with 8 rows or more each (12142 x 1038 bf16: 256
+// workgroups 47 us, 1024 24), but no fewer than 256.
 template <typename T>
 int64_t back_groups_of(int64_t N, int64_t C) {
     const int tpr = back_threads_per_row<T>(C);
