@@ -193,7 +193,7 @@ __global__ void __launch_bounds__(64 * (W + 1)) distill_rows(DistillParams p) {
     if (aside) {
         teacher<true>(p, n, z, 0, p.V, e);
         __syncthreads();
-        __syncthreads();
+        if (W > 1) __syncthreads();
         for (int w = 0; w < W; ++w) peak = fmaxf(peak, room[0][w]), sum += room[1][w];
     } else {
 #pragma unroll
@@ -223,6 +223,10 @@ __global__ void __launch_bounds__(64 * (W + 1)) distill_rows(DistillParams p) {
         peak = group_max<W>(peak, room[0]);
         own([&](float v) { sum += __builtin_amdgcn_exp2f((v - peak) * p.scale); });
         sum = group_sum<W>(sum, room[1]);                   // (its barrier also shows the teacher's side to all)
+        if (W == 1) {                                       // (one wave: no barrier in either)
+            room[0][0] = peak, room[1][0] = sum;
+            __syncthreads();
+        }
     }
     const float total = e.total;
     if (total == 0.f) {
@@ -439,10 +443,11 @@ grim_status distill_launch(DistillParams p, hipStream_t stream) {
         if (p.N > kMaxGrid) return GRIM_ERR_SHAPE;
         const dim3 g((unsigned)p.N);
         const int64_t pieces = (p.V + piece<T>() - 1) / piece<T>();
-        // 4, 8 or 16 waves with the teacher's.  Long rows take 16 where a compute unit has one row, very long ones where it has two:
+        // 2, 4, 8 or 16 waves with the teacher's (7180 x 512 bf16 8.5 us with 2, 14.0 with 4; 20000 x 1000 fp16 23.8 and 36.5).  Long rows take 16 where a compute unit has one row, very long ones where it has two:
         // (300 x 32768 fp32 19.3 us against 26.7 with 8, 269 x 19445 bf16 12.8 against 11.5, 512 x 32768 bf16 24.4 against 22.5).
         const bool many = p.N > (pieces > 4480 ? 2 : 1) * kComputeUnits;
-        if (pieces <= 384) hipLaunchKernelGGL((distill_rows<T, E, 3, 2>), g, dim3(256), 0, stream, p);
+        if (pieces <= 128) hipLaunchKernelGGL((distill_rows<T, E, 1, 2>), g, dim3(128), 0, stream, p);
+        else if (pieces <= 384) hipLaunchKernelGGL((distill_rows<T, E, 3, 2>), g, dim3(256), 0, stream, p);
         else if (pieces <= 768) hipLaunchKernelGGL((distill_rows<T, E, 3, 4>), g, dim3(256), 0, stream, p);
         else if (pieces <= 1792) hipLaunchKernelGGL((distill_rows<T, E, 7, 4>), g, dim3(512), 0, stream, p);
         else if (!many && pieces <= 3840) hipLaunchKernelGGL((distill_rows<T, E, 15, 4>), g, dim3(1024), 0, stream, p);
