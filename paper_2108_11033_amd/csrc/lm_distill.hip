@@ -8,7 +8,7 @@
 // leaves every slice's maximum, sum and share of the loss, and the second joins them and writes the gradient from a second
 // read of z, which a few rows leave in the caches.  Exponents are taken of differences from the maximum, (z - max) / tau, so that
 // masks of the type's lowest value do not overflow on the way.  Measured: 8192 x 32768 bf16 with 64 listed words 216 us (5.0 TB/s, a copy's
-// rate), 24 x 131075 fp16 in slices 12 (two launches), 1024 x 1000 fp32 5.3.
+// rate), 24 x 131075 fp16 in slices 12 (two launches), 1024 x 1000 fp32 5.6.
 #include "lm_common.hpp"
 
 namespace grim {
@@ -443,10 +443,12 @@ grim_status distill_launch(DistillParams p, hipStream_t stream) {
         if (p.N > kMaxGrid) return GRIM_ERR_SHAPE;
         const dim3 g((unsigned)p.N);
         const int64_t pieces = (p.V + piece<T>() - 1) / piece<T>();
-        // 2, 4, 8 or 16 waves with the teacher's (7180 x 512 bf16 8.5 us with 2, 14.0 with 4; 20000 x 1000 fp16 23.8 and 36.5).  Long rows take 16 where a compute unit has one row, very long ones where it has two:
-        // (300 x 32768 fp32 19.3 us against 26.7 with 8, 269 x 19445 bf16 12.8 against 11.5, 512 x 32768 bf16 24.4 against 22.5).
+        // 2, 4, 8 or 16 waves with the teacher's.  Short rows are bound by their workgroups' waves: 7180 x 512 bf16 8.5 us with 2 waves, 14.0
+        // with 4; 20000 x 1000 fp32 30.4 and 38.6, 256 x 2000 bf16 6.8 and 6.6.  Long rows take 16 where a compute unit has one row, very long
+        // ones where it has two (300 x 32768 fp32 19.3 us against 26.7 with 8, 269 x 19445 bf16 12.8 against 11.5, 512 x 32768 bf16 24.4 against 22.5).
         const bool many = p.N > (pieces > 4480 ? 2 : 1) * kComputeUnits;
         if (pieces <= 128) hipLaunchKernelGGL((distill_rows<T, E, 1, 2>), g, dim3(128), 0, stream, p);
+        else if (pieces <= 256) hipLaunchKernelGGL((distill_rows<T, E, 1, 4>), g, dim3(128), 0, stream, p);
         else if (pieces <= 384) hipLaunchKernelGGL((distill_rows<T, E, 3, 2>), g, dim3(256), 0, stream, p);
         else if (pieces <= 768) hipLaunchKernelGGL((distill_rows<T, E, 3, 4>), g, dim3(256), 0, stream, p);
         else if (pieces <= 1792) hipLaunchKernelGGL((distill_rows<T, E, 7, 4>), g, dim3(512), 0, stream, p);
