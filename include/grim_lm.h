@@ -34,7 +34,8 @@ extern "C" {
  *   dx_dev                element type dt, or NULL; may be dy_dev itself (same ld) but must not overlap x_dev otherwise
  *   dgamma_dev, dbeta_dev C fp32, overwritten (zeros for N = 0), or NULL
  *   workspace             grim_layer_norm_workspace(N, C) bytes, or NULL if neither dgamma nor dbeta is asked for
- * Errors: NULL, SHAPE (N < 0, C < 1, leading dimension too small, eps negative or not finite, workspace too small), DTYPE, DEVICE.
+ * Errors: NULL, SHAPE (N < 0, N >= 2^31, C < 1, C > 16776960 in the backward pass, leading dimension too small, eps negative or not
+ * finite, workspace too small), DTYPE, DEVICE.
  */
 grim_status grim_layer_norm(const void *x_dev, grim_dtype dt, int64_t ldx, const float *gamma_dev, const float *beta_dev,
                             float eps, int64_t N, int64_t C, void *y_dev, int64_t ldy, float *mean_dev, float *rstd_dev,
@@ -71,7 +72,8 @@ grim_status grim_layer_norm_backward(const void *dy_dev, int64_t lddy, const voi
  * grim_glr_step is one token for `batch` callers at once, in the layout of grim_lstm_cell: gates 3H x batch fp32 as
  * grim_bcr_spmv leaves them (ldg >= batch), states H x batch fp32 (h_new_dev may be h_dev itself), y H x batch of element
  * type dt (what the next product reads), or NULL.
- * Errors: NULL, SHAPE (N < 0, N > 2^30, H < 1, H > 2^21, nseq < 1, nseq > 1 without starts, leading dimension or a buffer too small), DTYPE, DEVICE.
+ * Errors: NULL, SHAPE (N < 0, N > 2^30, H < 1, H > 2^21, nseq < 1, nseq > 1 without starts, leading dimension or a buffer too small; of
+ * the step: H < 1, batch < 0, H * batch > 2^32 - 256, leading dimension too small), DTYPE, DEVICE.
  */
 int64_t grim_glr_states(int64_t N, int64_t H);
 int64_t grim_glr_workspace(int64_t N, int64_t H);
@@ -102,7 +104,7 @@ grim_status grim_glr_step(const float *gates_dev, int64_t ldg, const float *bias
  *   dz_dev         N x V of element type dt, rows of lddz, may be z_dev itself (same ld); NULL: the loss alone
  *   workspace      grim_distill_topk_workspace(N, V) bytes
  * z may hold -infinity (words that cannot come: q = 0); a row that holds nothing else, or +infinity or NaN, gives NaN.
- * Errors: NULL, SHAPE (N < 0, V < 1, V >= 2^31, k < 1, leading dimension too small, tau outside 1e-30 .. 1e30,
+ * Errors: NULL, SHAPE (N < 0, N >= 2^31, V < 1, V >= 2^31, k < 1, leading dimension too small, tau outside 1e-30 .. 1e30,
  * workspace too small), DTYPE, DEVICE, UNSUPPORTED (k > 1024).
  */
 int64_t grim_distill_topk_workspace(int64_t N, int64_t V);

@@ -14,7 +14,7 @@ using bf16 = __bf16;
 using f16 = _Float16;
 
 constexpr int kComputeUnits = 256;
-constexpr int kMaxGrid = 0x7fffffff;
+constexpr int64_t kMostRows = 0x7fffffff;       // of a layer norm, a distillation
 
 // V elements of T as they lie in memory, in words: what waits in registers keeps two 16-bit elements in each.  They are read
 // and written at any address that an element may have: rows may start anywhere (odd widths, leading dimensions and offsets), the
@@ -183,6 +183,23 @@ grim_status join_columns(const float *part, int64_t groups, int64_t C0, float *o
 inline bool known(grim_dtype dt) { return dt == GRIM_F32 || dt == GRIM_F16 || dt == GRIM_BF16; }
 inline int bytes_of(grim_dtype dt) { return dt == GRIM_F32 ? 4 : 2; }
 inline grim_status launched() { return hipGetLastError() == hipSuccess ? GRIM_OK : GRIM_ERR_DEVICE; }
+
+// A launch has fewer than 2^32 threads; one of more starts what is left of their number in 32 bits, without an error.  So many
+// workgroups are a launch's most:
+constexpr int64_t most_groups(int threads) { return 0xffffffffll / threads; }
+
+// f(first, count) for runs of at most `most` out of `all`, one launch each.
+template <typename F>
+grim_status in_runs(int64_t all, int64_t most, F f) {
+    for (int64_t first = 0; first < all; first += most) {
+        const grim_status st = f(first, all - first < most ? all - first : most);
+        if (st != GRIM_OK) return st;
+    }
+    return GRIM_OK;
+}
+
+template <typename T>
+T *ahead(T *p, int64_t elements) { return p ? p + elements : p; }
 
 // rows x ld elements stay far below what a 64-bit byte offset holds
 inline bool fits(int64_t rows, int64_t ld) { return ld >= 0 && ld <= (int64_t(1) << 40) && (rows <= 1 || ld <= (int64_t(1) << 56) / rows); }

@@ -437,37 +437,56 @@ bool row_fits(int64_t V) { return V >= piece<T>() && V <= (int64_t)18 * 960 * pi
 template <typename T>
 bool by_rows(int64_t N, int64_t V) { return row_fits<T>(V) && (N >= 128 || V * (int64_t)sizeof(T) <= 128 * 1024); }
 
+// Rows first .. first + count - 1 of a call.
+template <typename T>
+DistillParams rows_of(DistillParams p, int64_t first, int64_t count) {
+    p.z = static_cast<const T *>(p.z) + first * p.ldz;
+    p.top += first * p.ldt, p.ids += first * p.ldt;
+    p.weight = ahead(p.weight, first);
+    p.loss += first;
+    p.dz = ahead(static_cast<T *>(p.dz), first * p.lddz);
+    p.part += first * p.slices * 4;
+    p.N = count;
+    return p;
+}
+
 template <typename T, int E>
-grim_status distill_launch(DistillParams p, hipStream_t stream) {
-    if (by_rows<T>(p.N, p.V)) {
-        if (p.N > kMaxGrid) return GRIM_ERR_SHAPE;
-        const dim3 g((unsigned)p.N);
-        const int64_t pieces = (p.V + piece<T>() - 1) / piece<T>();
+grim_status distill_launch(DistillParams call, hipStream_t stream) {
+    if (by_rows<T>(call.N, call.V)) {
+        const int64_t pieces = (call.V + piece<T>() - 1) / piece<T>();
         // 2, 4, 8 or 16 waves with the teacher's.  Short rows are bound by their workgroups' waves: 7180 x 512 bf16 8.5 us with 2 waves, 14.0
         // with 4; 20000 x 1000 fp32 30.4 and 38.6, 256 x 2000 bf16 6.8 and 6.6.  Long rows take 16 where a compute unit has one row, very long
         // ones where it has two (300 x 32768 fp32 19.3 us against 26.7 with 8, 269 x 19445 bf16 12.8 against 11.5, 512 x 32768 bf16 24.4 against 22.5).
-        const bool many = p.N > (pieces > 4480 ? 2 : 1) * kComputeUnits;
-        if (pieces <= 128) hipLaunchKernelGGL((distill_rows<T, E, 1, 2>), g, dim3(128), 0, stream, p);
-        else if (pieces <= 256) hipLaunchKernelGGL((distill_rows<T, E, 1, 4>), g, dim3(128), 0, stream, p);
-        else if (pieces <= 384) hipLaunchKernelGGL((distill_rows<T, E, 3, 2>), g, dim3(256), 0, stream, p);
-        else if (pieces <= 768) hipLaunchKernelGGL((distill_rows<T, E, 3, 4>), g, dim3(256), 0, stream, p);
-        else if (pieces <= 1792) hipLaunchKernelGGL((distill_rows<T, E, 7, 4>), g, dim3(512), 0, stream, p);
-        else if (!many && pieces <= 3840) hipLaunchKernelGGL((distill_rows<T, E, 15, 4>), g, dim3(1024), 0, stream, p);
-        else if (!many && pieces <= 9600) hipLaunchKernelGGL((distill_rows<T, E, 15, 10>), g, dim3(1024), 0, stream, p);
-        else if (pieces <= 2688) hipLaunchKernelGGL((distill_rows<T, E, 7, 6>), g, dim3(512), 0, stream, p);
-        else if (pieces <= 4480) hipLaunchKernelGGL((distill_rows<T, E, 7, 10>), g, dim3(512), 0, stream, p);
-        else if (pieces <= 8064) hipLaunchKernelGGL((distill_rows<T, E, 7, 18>), g, dim3(512), 0, stream, p);
-        else hipLaunchKernelGGL((distill_rows<T, E, 15, 18>), g, dim3(1024), 0, stream, p);
-        return launched();
+        const bool many = call.N > (pieces > 4480 ? 2 : 1) * kComputeUnits;
+        const auto launch = [&](auto kernel, int threads) {
+            return in_runs(call.N, most_groups(threads), [&](int64_t first, int64_t count) {
+                hipLaunchKernelGGL(kernel, dim3((unsigned)count), dim3(threads), 0, stream, rows_of<T>(call, first, count));
+                return launched();
+            });
+        };
+        if (pieces <= 128) return launch(distill_rows<T, E, 1, 2>, 128);
+        if (pieces <= 256) return launch(distill_rows<T, E, 1, 4>, 128);
+        if (pieces <= 384) return launch(distill_rows<T, E, 3, 2>, 256);
+        if (pieces <= 768) return launch(distill_rows<T, E, 3, 4>, 256);
+        if (pieces <= 1792) return launch(distill_rows<T, E, 7, 4>, 512);
+        if (!many && pieces <= 3840) return launch(distill_rows<T, E, 15, 4>, 1024);
+        if (!many && pieces <= 9600) return launch(distill_rows<T, E, 15, 10>, 1024);
+        if (pieces <= 2688) return launch(distill_rows<T, E, 7, 6>, 512);
+        if (pieces <= 4480) return launch(distill_rows<T, E, 7, 10>, 512);
+        if (pieces <= 8064) return launch(distill_rows<T, E, 7, 18>, 512);
+        return launch(distill_rows<T, E, 15, 18>, 1024);
     }
-    p.slices = (int32_t)slices_of<T>(p.V);
-    if (p.N > kMaxGrid / p.slices) return GRIM_ERR_SHAPE;
-    const dim3 g((unsigned)(p.N * p.slices)), b(64 * (kSliceWaves + 1));
-    hipLaunchKernelGGL((distill_slices<T, E>), g, b, 0, stream, p);
-    const grim_status st = launched();
-    if (st != GRIM_OK) return st;
-    hipLaunchKernelGGL((distill_join<T, E>), g, b, 0, stream, p);
-    return launched();
+    call.slices = (int32_t)slices_of<T>(call.V);
+    constexpr int threads = 64 * (kSliceWaves + 1);
+    return in_runs(call.N, most_groups(threads) / call.slices, [&](int64_t first, int64_t count) {
+        const DistillParams p = rows_of<T>(call, first, count);
+        const dim3 g((unsigned)(p.N * p.slices)), b(threads);
+        hipLaunchKernelGGL((distill_slices<T, E>), g, b, 0, stream, p);
+        const grim_status st = launched();
+        if (st != GRIM_OK) return st;
+        hipLaunchKernelGGL((distill_join<T, E>), g, b, 0, stream, p);
+        return launched();
+    });
 }
 
 // (room for 64 entries where they suffice: workgroups share a compute unit by their LDS)
@@ -497,7 +516,7 @@ grim_status grim_distill_topk(const void *z_dev, grim_dtype dt, int64_t ldz, con
                               void *workspace, int64_t workspace_bytes, void *hip_stream) {
     using namespace grim::lm;
     if (!known(dt)) return GRIM_ERR_DTYPE;
-    if (N < 0 || V < 1 || V >= (int64_t)1 << 31 || k < 1 || ldz < V || ldt < k || (dz_dev && lddz < V) || !fits(N, ldz) ||
+    if (N < 0 || N > kMostRows || V < 1 || V >= (int64_t)1 << 31 || k < 1 || ldz < V || ldt < k || (dz_dev && lddz < V) || !fits(N, ldz) ||
         !fits(N, ldt) || (dz_dev && !fits(N, lddz)) || !(temperature >= 1e-30f) || temperature > 1e30f)
         return GRIM_ERR_SHAPE;
     if (k > kMostEntries) return GRIM_ERR_UNSUPPORTED;

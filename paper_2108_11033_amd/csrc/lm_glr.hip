@@ -589,10 +589,9 @@ struct GlrStepParams {
 
 template <typename T>
 __global__ void __launch_bounds__(256) glr_step_kernel(GlrStepParams p) {
-    const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const uint32_t e = blockIdx.x * 256 + threadIdx.x;          // (all of a launch's threads count in 32 bits)
     if (e >= p.H * p.batch) return;
-    const int64_t r = e >> 32 ? e / p.batch : (int64_t)((uint32_t)e / (uint32_t)p.batch);
-    const int64_t b = e - r * p.batch;
+    const int64_t r = e / (uint32_t)p.batch, b = e % (uint32_t)p.batch;
     float zu = p.gates[r * p.ldg + b], zc = p.gates[(p.H + r) * p.ldg + b], zv = p.gates[(2 * p.H + r) * p.ldg + b];
     if (p.bias) zu += p.bias[r], zc += p.bias[p.H + r], zv += p.bias[2 * p.H + r];
     float f, k;
@@ -683,7 +682,8 @@ grim_status glr_run(GlrParams p, grim_dtype dt, bool back, hipStream_t stream) {
 }
 
 inline bool glr_sizes(int64_t N, int64_t H, int32_t nseq, const int32_t *seq) {
-    // (row numbers in 32 bits with room for a group more; at most 2^15 sets of 2^15 column blocks)
+    // (row numbers in 32 bits with room for a group more; cut_rows leaves some 1024 workgroups, or eight rows of up to 2^15 column blocks:
+    // few enough threads for a launch)
     return N >= 0 && N <= (int64_t)1 << 30 && H >= 1 && H <= (int64_t)1 << 21 && nseq >= 1 && (seq || nseq == 1);
 }
 
@@ -762,7 +762,7 @@ grim_status grim_glr_step(const float *gates_dev, int64_t ldg, const float *bias
         return GRIM_ERR_SHAPE;
     if (batch == 0) return GRIM_OK;
     if (!gates_dev || !h_dev || !h_new_dev) return GRIM_ERR_NULL;
-    if (H > (int64_t)kMaxGrid * 256 / batch) return GRIM_ERR_SHAPE;
+    if (H > most_groups(256) * 256 / batch) return GRIM_ERR_SHAPE;
     const GlrStepParams p{gates_dev, bias_dev, h_dev, h_new_dev, y_dev, ldg, ldh, ldh_new, ldy, H, batch};
     const dim3 grid((unsigned)((H * batch + 255) / 256)), block(256);
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);

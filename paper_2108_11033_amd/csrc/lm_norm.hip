@@ -308,8 +308,7 @@ __global__ void __launch_bounds__(1024) join_columns_kernel(const float *part, i
 }
 
 grim_status join_columns(const float *part, int64_t groups, int64_t C0, float *out0, int64_t C1, float *out1, hipStream_t stream) {
-    const int64_t grid = (C0 + C1 + 15) / 16;
-    if (grid > kMaxGrid) return GRIM_ERR_SHAPE;
+    const int64_t grid = (C0 + C1 + 15) / 16;                   // (C0 + C1 below 2^26 in all calls)
     hipLaunchKernelGGL(join_columns_kernel, dim3((unsigned)grid), dim3(1024), 0, stream, part, groups, C0, out0, C1, out1);
     return launched();
 }
@@ -352,19 +351,30 @@ int64_t back_groups_of(int64_t N, int64_t C) {
     return all < groups ? all : groups;
 }
 
+// Rows first .. first + count - 1 of a call.
+template <typename T>
+NormParams rows_of(NormParams p, int64_t first, int64_t count) {
+    p.x = static_cast<const T *>(p.x) + first * p.ldx;
+    p.y = static_cast<T *>(p.y) + first * p.ldy;
+    p.mean = ahead(p.mean, first), p.rstd = ahead(p.rstd, first);
+    p.N = count;
+    return p;
+}
+
 template <typename T, int TPR>
-grim_status norm_launch(const NormParams &p, hipStream_t stream) {
-    constexpr int RPG = TPR < 256 ? 256 / TPR : 1;
-    const int64_t grid = (p.N + RPG - 1) / RPG;
-    if (grid > kMaxGrid) return GRIM_ERR_SHAPE;
-    const dim3 g((unsigned)grid), b(TPR < 256 ? 256 : TPR);
-    switch ((p.C + TPR * vec_of<T>() - 1) / (TPR * vec_of<T>())) {
-        case 1: hipLaunchKernelGGL((norm_rows<T, TPR, 1>), g, b, 0, stream, p); break;
-        case 2: hipLaunchKernelGGL((norm_rows<T, TPR, 2>), g, b, 0, stream, p); break;
-        case 3: hipLaunchKernelGGL((norm_rows<T, TPR, 3>), g, b, 0, stream, p); break;
-        default: hipLaunchKernelGGL((norm_rows<T, TPR, 4>), g, b, 0, stream, p); break;
-    }
-    return launched();
+grim_status norm_launch(const NormParams &call, hipStream_t stream) {
+    constexpr int RPG = TPR < 256 ? 256 / TPR : 1, threads = TPR < 256 ? 256 : TPR;
+    return in_runs(call.N, most_groups(threads) * RPG, [&](int64_t first, int64_t count) {
+        const NormParams p = rows_of<T>(call, first, count);
+        const dim3 g((unsigned)((p.N + RPG - 1) / RPG)), b(threads);
+        switch ((p.C + TPR * vec_of<T>() - 1) / (TPR * vec_of<T>())) {
+            case 1: hipLaunchKernelGGL((norm_rows<T, TPR, 1>), g, b, 0, stream, p); break;
+            case 2: hipLaunchKernelGGL((norm_rows<T, TPR, 2>), g, b, 0, stream, p); break;
+            case 3: hipLaunchKernelGGL((norm_rows<T, TPR, 3>), g, b, 0, stream, p); break;
+            default: hipLaunchKernelGGL((norm_rows<T, TPR, 4>), g, b, 0, stream, p); break;
+        }
+        return launched();
+    });
 }
 
 template <typename T>
@@ -375,9 +385,10 @@ grim_status norm_typed(const NormParams &p, hipStream_t stream) {
         case 256: return norm_launch<T, 256>(p, stream);
         case 1024: return norm_launch<T, 1024>(p, stream);
     }
-    if (p.N > kMaxGrid) return GRIM_ERR_SHAPE;
-    hipLaunchKernelGGL(norm_rows_any<T>, dim3((unsigned)p.N), dim3(256), 0, stream, p);
-    return launched();
+    return in_runs(p.N, most_groups(256), [&](int64_t first, int64_t count) {
+        hipLaunchKernelGGL(norm_rows_any<T>, dim3((unsigned)count), dim3(256), 0, stream, rows_of<T>(p, first, count));
+        return launched();
+    });
 }
 
 template <typename T, int TPR>
@@ -395,6 +406,18 @@ grim_status norm_back_launch(const NormBackParams &p, int64_t groups, hipStream_
 }
 
 template <typename T>
+NormBackParams rows_of(NormBackParams p, int64_t first, int64_t count) {
+    p.dy = static_cast<const T *>(p.dy) + first * p.lddy;
+    p.x = static_cast<const T *>(p.x) + first * p.ldx;
+    p.dx = static_cast<T *>(p.dx) + first * p.lddx;
+    p.mean += first, p.rstd += first;
+    p.N = count;
+    return p;
+}
+
+constexpr int64_t kMostFeatures = 65535 * 256;              // of the backward pass: norm_back_columns has so many blocks of columns
+
+template <typename T>
 grim_status norm_back_typed(const NormBackParams &p, float *dgamma, float *dbeta, hipStream_t stream) {
     const int64_t groups = back_groups_of<T>(p.N, p.C);
     grim_status st = GRIM_OK;
@@ -405,14 +428,17 @@ grim_status norm_back_typed(const NormBackParams &p, float *dgamma, float *dbeta
             case 256: st = norm_back_launch<T, 256>(p, groups, stream); break;
             case 1024: st = norm_back_launch<T, 1024>(p, groups, stream); break;
             default:
-                if (p.N > kMaxGrid || (p.C + 255) / 256 > 65535) return GRIM_ERR_SHAPE;
                 if (p.part) {                                               // first: dx may take dy's place
                     const int64_t slab = (p.N + groups - 1) / groups;
                     hipLaunchKernelGGL(norm_back_columns<T>, dim3((unsigned)groups, (unsigned)((p.C + 255) / 256)), dim3(256), 0,
                                        stream, p, slab);
+                    st = launched();
                 }
-                if (p.dx) hipLaunchKernelGGL(norm_back_any<T>, dim3((unsigned)p.N), dim3(256), 0, stream, p);
-                st = launched();
+                if (p.dx && st == GRIM_OK)
+                    st = in_runs(p.N, most_groups(256), [&](int64_t first, int64_t count) {
+                        hipLaunchKernelGGL(norm_back_any<T>, dim3((unsigned)count), dim3(256), 0, stream, rows_of<T>(p, first, count));
+                        return launched();
+                    });
         }
     }
     if (st != GRIM_OK || !p.part) return st;
@@ -429,7 +455,7 @@ grim_status grim_layer_norm(const void *x_dev, grim_dtype dt, int64_t ldx, const
                             void *hip_stream) {
     using namespace grim::lm;
     if (!known(dt)) return GRIM_ERR_DTYPE;
-    if (N < 0 || C < 1 || ldx < C || ldy < C || !fits(N, ldx) || !fits(N, ldy) || !(eps >= 0.f) || eps > 3.4e38f) return GRIM_ERR_SHAPE;
+    if (N < 0 || N > kMostRows || C < 1 || ldx < C || ldy < C || !fits(N, ldx) || !fits(N, ldy) || !(eps >= 0.f) || eps > 3.4e38f) return GRIM_ERR_SHAPE;
     if (N == 0) return GRIM_OK;
     if (!x_dev || !y_dev) return GRIM_ERR_NULL;
     const NormParams p{x_dev, gamma_dev, beta_dev, y_dev, mean_dev, rstd_dev, ldx, ldy, N, C, eps,
@@ -452,7 +478,7 @@ grim_status grim_layer_norm_backward(const void *dy_dev, int64_t lddy, const voi
                                      void *workspace, int64_t workspace_bytes, void *hip_stream) {
     using namespace grim::lm;
     if (!known(dt)) return GRIM_ERR_DTYPE;
-    if (N < 0 || C < 1 || lddy < C || ldx < C || (dx_dev && lddx < C) || !fits(N, lddy) || !fits(N, ldx) ||
+    if (N < 0 || N > kMostRows || C < 1 || C > kMostFeatures || lddy < C || ldx < C || (dx_dev && lddx < C) || !fits(N, lddy) || !fits(N, ldx) ||
         (dx_dev && !fits(N, lddx)))
         return GRIM_ERR_SHAPE;
     const bool sums = dgamma_dev || dbeta_dev;

@@ -255,19 +255,37 @@ __global__ void __launch_bounds__(THREADS) rules_columns(RuleParams p, int tiles
     }
 }
 
+// Callers first .. first + count - 1 of a call.
+template <typename T>
+RuleParams callers_of(RuleParams p, bool columns, int64_t first, int64_t count) {
+    p.z = static_cast<const T *>(p.z) + first * (columns ? 1 : p.ldz);
+    p.out = static_cast<T *>(p.out) + first * (columns ? 1 : p.ldo);
+    p.r.history = ahead(p.r.history, first * p.r.ld_history);
+    p.r.history_len = ahead(p.r.history_len, first);
+    p.r.repetition = ahead(p.r.repetition, first);
+    p.r.frequency = ahead(p.r.frequency, first);
+    p.r.presence = ahead(p.r.presence, first);
+    p.r.bias_ids = ahead(p.r.bias_ids, first * p.r.ld_bias);
+    p.r.bias_values = ahead(p.r.bias_values, first * p.r.ld_bias);
+    p.r.allowed = ahead(p.r.allowed, first * p.r.ld_allowed);
+    p.batch = (int32_t)count;
+    return p;
+}
+
 template <typename T, int TILE, int THREADS, bool COLUMNS>
-grim_status rules_launch(const RuleParams &p, hipStream_t stream) {
+grim_status rules_launch(const RuleParams &call, hipStream_t stream) {
     int shift = 0;
     if (COLUMNS)
-        while ((1 << shift) < kMostCallers && (1 << shift) < p.batch) ++shift;    // 16 or 32 bytes of a row
-    const int64_t words = TILE >> shift, tiles = (p.V + words - 1) / words;
-    const int64_t grid = tiles * ((p.batch + (1 << shift) - 1) >> shift);
-    if (grid > kMaxGrid) return GRIM_ERR_SHAPE;
-    const dim3 g((unsigned)grid), b(THREADS);
-    if constexpr (!COLUMNS) hipLaunchKernelGGL((rules_rows<T, TILE, THREADS>), g, b, 0, stream, p, (int)tiles);
-    else if (p.r.nbias <= 128) hipLaunchKernelGGL((rules_columns<T, TILE, THREADS, 128>), g, b, 0, stream, p, (int)tiles, shift);
-    else hipLaunchKernelGGL((rules_columns<T, TILE, THREADS, kMostBias>), g, b, 0, stream, p, (int)tiles, shift);
-    return launched();
+        while ((1 << shift) < kMostCallers && (1 << shift) < call.batch) ++shift;    // 16 or 32 bytes of a row
+    const int64_t words = TILE >> shift, tiles = (call.V + words - 1) / words;       // (up to 2^21: a launch has room for one block's)
+    return in_runs(call.batch, most_groups(THREADS) / tiles << shift, [&](int64_t first, int64_t count) {
+        const RuleParams p = callers_of<T>(call, COLUMNS, first, count);
+        const dim3 g((unsigned)(tiles * ((p.batch + (1 << shift) - 1) >> shift))), b(THREADS);
+        if constexpr (!COLUMNS) hipLaunchKernelGGL((rules_rows<T, TILE, THREADS>), g, b, 0, stream, p, (int)tiles);
+        else if (p.r.nbias <= 128) hipLaunchKernelGGL((rules_columns<T, TILE, THREADS, 128>), g, b, 0, stream, p, (int)tiles, shift);
+        else hipLaunchKernelGGL((rules_columns<T, TILE, THREADS, kMostBias>), g, b, 0, stream, p, (int)tiles, shift);
+        return launched();
+    });
 }
 
 // Tiles of 8192 places, of 2048 where those would leave compute units without one, or in columns, where a tile's chain is longer, with
