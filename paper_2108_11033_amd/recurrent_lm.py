@@ -24,12 +24,19 @@ def _scratch(n: int, device) -> torch.Tensor:
     return torch.empty((max(1, n),), dtype=torch.uint8, device=device)
 
 
+def _fp32(t: torch.Tensor) -> torch.Tensor:
+    """A parameter or state as the kernels read it, whatever type a model holds it in."""
+    return t.detach().float().contiguous()
+
+
 # ---------------------------------------------------------------------------------------------- training
 class LayerNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, gamma, beta):
         x = x.contiguous()
         N, C = x.shape
+        ctx.types = gamma.dtype, beta.dtype
+        gamma, beta = _fp32(gamma), _fp32(beta)
         y, mean, rstd = torch.empty_like(x), x.new_empty(N, dtype=torch.float32), x.new_empty(N, dtype=torch.float32)
         lm.layer_norm(x, DTYPES[x.dtype], C, gamma, beta, EPS, N, C, y, C, mean, rstd, torch.cuda.current_stream())
         ctx.save_for_backward(x, gamma, mean, rstd)
@@ -39,19 +46,21 @@ class LayerNorm(torch.autograd.Function):
     def backward(ctx, dy):
         x, gamma, mean, rstd = ctx.saved_tensors
         N, C = x.shape
-        dx, dgamma, dbeta = torch.empty_like(x), torch.empty_like(gamma), torch.empty_like(gamma)
+        dx, dgamma, dbeta = torch.empty_like(x), torch.empty_like(gamma), torch.empty_like(gamma)      # (sums in fp32)
         lm.layer_norm_backward(dy.contiguous(), C, x, C, DTYPES[x.dtype], gamma, mean, rstd, N, C, dx, C, dgamma, dbeta,
                                _scratch(lm.layer_norm_workspace(N, C), x.device), torch.cuda.current_stream())
-        return dx, dgamma, dbeta
+        return dx, dgamma.to(ctx.types[0]), dbeta.to(ctx.types[1])
 
 
 class GatedRecurrence(torch.autograd.Function):
-    """(outputs, last states) of packed sequences; seq_start is an int32 tensor of their starts and the end."""
+    """(outputs, last states in fp32) of packed sequences; seq_start is an int32 tensor of their starts and the end."""
 
     @staticmethod
     def forward(ctx, gates, bias, h0, seq_start):
         gates = gates.contiguous()
         N, H = gates.shape[0], gates.shape[1] // 3
+        ctx.types = bias.dtype, h0.dtype
+        bias, h0 = _fp32(bias), _fp32(h0)
         y, h_last = gates.new_empty(N, H), torch.empty_like(h0)
         states = _scratch(lm.glr_states(N, H), gates.device)
         lm.glr_sequence(gates, DTYPES[gates.dtype], 3 * H, bias, h0, seq_start, h0.shape[0], N, H, y, H, h_last, states,
@@ -67,7 +76,7 @@ class GatedRecurrence(torch.autograd.Function):
         lm.glr_sequence_backward(gates, DTYPES[gates.dtype], 3 * H, bias, h0, seq_start, h0.shape[0], N, H, states, dy.contiguous(), H,
                                  dh_last.contiguous(), dgates, 3 * H, dbias, dh0, _scratch(lm.glr_workspace(N, H), gates.device),
                                  torch.cuda.current_stream())
-        return dgates, dbias, dh0, None
+        return dgates, dbias.to(ctx.types[0]), dh0.to(ctx.types[1]), None
 
 
 class DistillTopK(torch.autograd.Function):
@@ -164,6 +173,7 @@ class Server:
 
     def __init__(self, model: RecurrentLM, batch: int):
         self.model, self.batch = model, batch
+        self.gammas, self.betas, self.biases = ([_fp32(p) for p in group] for group in (model.gammas, model.betas, model.biases))
         self.packed = {name: self._pack(model, name) for name in model.products()}
         dev = model.embedding.device
         fp32, fp16 = (lambda *s: torch.empty(s, device=dev)), (lambda *s: torch.empty(s, dtype=torch.float16, device=dev))
@@ -182,7 +192,7 @@ class Server:
 
     def _norm(self, x, i, stream):
         """Layer norm of the callers' rows, as the columns of the next product."""
-        lm.layer_norm(x, "f32", x.shape[1], self.model.gammas[i], self.model.betas[i], EPS, self.batch, x.shape[1], self.norm, x.shape[1],
+        lm.layer_norm(x, "f32", x.shape[1], self.gammas[i], self.betas[i], EPS, self.batch, x.shape[1], self.norm, x.shape[1],
                       stream=stream)
         return self.norm.t().to(torch.float16).contiguous()
 
@@ -194,7 +204,7 @@ class Server:
         x = m.embedding[tokens].float()
         for i in range(m.layers):
             binding.spmm(self.packed[f"gates{i}"], self._norm(x, i, stream), b, b, self.gates, b, stream)
-            lm.glr_step(self.gates, b, m.biases[i], self.h[i], b, self.h[i], b, self.y, "f16", b, H, b, stream)
+            lm.glr_step(self.gates, b, self.biases[i], self.h[i], b, self.h[i], b, self.y, "f16", b, H, b, stream)
             binding.spmm(self.packed[f"outs{i}"], self.y, b, b, self.out, b, stream)
             x = x + self.out.t()
         binding.spmm(self.packed["head"], self._norm(x, m.layers, stream), b, b, self.logits, b, stream)
