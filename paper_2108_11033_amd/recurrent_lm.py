@@ -29,6 +29,15 @@ def _fp32(t: torch.Tensor) -> torch.Tensor:
     return t.detach().float().contiguous()
 
 
+def _check(fits: bool, what: str):
+    if not fits:
+        raise ValueError(what)
+
+
+def _whole(t: torch.Tensor) -> bool:
+    return not (t.is_floating_point() or t.is_complex() or t.dtype == torch.bool)
+
+
 # ---------------------------------------------------------------------------------------------- training
 class LayerNorm(torch.autograd.Function):
     @staticmethod
@@ -80,12 +89,21 @@ class GatedRecurrence(torch.autograd.Function):
 
 
 class DistillTopK(torch.autograd.Function):
-    """The sum over rows of weight times the distillation loss.  The gradient is formed with the loss, in one pass over the logits."""
+    """The sum over rows of weight times the distillation loss.  The gradient is formed with the loss, in one pass over the logits; the
+    teacher's logits and the weights get none.  The lists are N x k (numbers of any whole type: those outside 0 .. V-1 are absent), weight N."""
 
     @staticmethod
     def forward(ctx, logits, top_logits, top_ids, temperature, weight):
-        logits = logits.contiguous()
+        _check(logits.dim() == 2, f"logits are rows of a vocabulary, not {tuple(logits.shape)}")
         N, V = logits.shape
+        _check(top_ids.dim() == 2 and top_ids.shape[0] == N and top_logits.shape == top_ids.shape and _whole(top_ids),
+               f"{N} rows of logits with lists of {tuple(top_logits.shape)} logits and {tuple(top_ids.shape)} numbers ({top_ids.dtype})")
+        _check(weight.shape == (N,), f"{N} rows of logits with weights of {tuple(weight.shape)}")
+        logits, top_logits, weight = logits.contiguous(), _fp32(top_logits), _fp32(weight)
+        if top_ids.dtype != torch.int32:                       # (before they are cut to 32 bits)
+            top_ids = top_ids.long()
+            top_ids = torch.where((top_ids >= 0) & (top_ids < V), top_ids, -1).int()
+        top_ids = top_ids.contiguous()
         loss, dz = logits.new_empty(N, dtype=torch.float32), torch.empty_like(logits)
         lm.distill_topk(logits, DTYPES[logits.dtype], V, top_logits, top_ids, top_ids.shape[1], top_ids.shape[1], temperature, weight, N, V,
                         loss, dz, V, _scratch(lm.distill_topk_workspace(N, V), logits.device), torch.cuda.current_stream())

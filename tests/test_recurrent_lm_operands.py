@@ -78,3 +78,47 @@ def test_serving_a_16_bit_model(dtype):
     for _ in range(3):
         assert torch.equal(a.step(tokens), b.step(tokens))
     assert all(torch.equal(x, y) for x, y in zip(a.h, b.h))
+
+
+# ------------------------------------------------------------------------------------------- the teacher's lists
+@pytest.mark.gpu
+def test_lists_of_other_strides_and_types():
+    """The first few of a longer list as topk gives them (rows further apart, 64-bit numbers), a weight for all rows, 16-bit logits of the teacher."""
+    logits, full = _randn(N, V), _randn(N, V, seed=1).topk(3 * K, dim=1)
+    ids, values = full.indices[:, :K], full.values[:, :K]
+    weight = torch.tensor(0.25, device="cuda").expand(N)
+    assert not ids.is_contiguous() and ids.dtype == torch.int64 and weight.stride() == (0,)
+
+    def both(*operands):
+        z = logits.clone().requires_grad_()
+        loss = rl.DistillTopK.apply(z, *operands)
+        loss.backward()
+        return loss.detach(), z.grad
+
+    want = both(values.contiguous(), ids.int().contiguous(), 2.0, torch.full((N,), 0.25, device="cuda"))
+    got = both(values, ids, 2.0, weight)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    half = both(values.bfloat16(), ids, 2.0, weight.bfloat16())
+    want = both(values.bfloat16().float().contiguous(), ids.int().contiguous(), 2.0, torch.full((N,), 0.25, device="cuda"))
+    assert torch.equal(half[0], want[0]) and torch.equal(half[1], want[1])
+
+
+@pytest.mark.gpu
+def test_numbers_beyond_32_bits_are_absent():
+    """An entry outside 0 .. V - 1 is absent, also one whose low 32 bits are a word."""
+    logits, values = _randn(N, V), _randn(N, K, seed=1)
+    ids = torch.arange(K, device="cuda").repeat(N, 1)
+    away = ids.clone()
+    ids[:, 1], ids[:, 3] = -1, -1
+    away[:, 1], away[:, 3] = 2 ** 32 + 5, -2 ** 40
+    weight = torch.ones(N, device="cuda")
+    assert torch.equal(rl.DistillTopK.apply(logits, values, ids, 1.0, weight), rl.DistillTopK.apply(logits, values, away, 1.0, weight))
+
+
+@pytest.mark.parametrize("change", [dict(logits=(V,)), dict(top=(N, K + 1)), dict(top=(N - 1, K)), dict(ids=(N - 1, K)), dict(ids=(N * K,), top=(N * K,)),
+                                    dict(weight=()), dict(weight=(1,)), dict(weight=(N + 1,)), dict(weight=(N, 1)), dict(id_type=torch.float32)])
+def test_lists_that_do_not_fit_are_refused(change):
+    shape = {**dict(logits=(N, V), top=(N, K), ids=(N, K), weight=(N,)), **change}
+    with pytest.raises(ValueError):
+        rl.DistillTopK.apply(torch.zeros(shape["logits"]), torch.zeros(shape["top"]), torch.zeros(shape["ids"], dtype=change.get("id_type", torch.int32)),
+                             1.0, torch.zeros(shape["weight"]))
