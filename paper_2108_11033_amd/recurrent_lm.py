@@ -42,6 +42,8 @@ def _whole(t: torch.Tensor) -> bool:
 class LayerNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, gamma, beta):
+        _check(x.dim() == 2 and gamma.shape == beta.shape == x.shape[1:],
+               f"rows of {tuple(x.shape)} with parameters of {tuple(gamma.shape)} and {tuple(beta.shape)}")
         x = x.contiguous()
         N, C = x.shape
         ctx.types = gamma.dtype, beta.dtype
@@ -62,12 +64,18 @@ class LayerNorm(torch.autograd.Function):
 
 
 class GatedRecurrence(torch.autograd.Function):
-    """(outputs, last states in fp32) of packed sequences; seq_start is an int32 tensor of their starts and the end."""
+    """(outputs, last states in fp32) of packed sequences: gates N x 3H, bias 3H, h0 a row of H per sequence; seq_start holds the sequences'
+    starts and the end, one number more than there are sequences."""
 
     @staticmethod
     def forward(ctx, gates, bias, h0, seq_start):
-        gates = gates.contiguous()
+        _check(gates.dim() == 2 and gates.shape[1] >= 3 and gates.shape[1] % 3 == 0 and bias.shape == gates.shape[1:],
+               f"gates of {tuple(gates.shape)} with biases of {tuple(bias.shape)}")
         N, H = gates.shape[0], gates.shape[1] // 3
+        _check(h0.dim() == 2 and h0.shape[0] >= 1 and h0.shape[1] == H, f"states of {tuple(h0.shape)} for sequences of {H} units")
+        _check(seq_start.shape == (h0.shape[0] + 1,) and _whole(seq_start),
+               f"states of {h0.shape[0]} sequences with starts of {tuple(seq_start.shape)} ({seq_start.dtype})")
+        gates, seq_start = gates.contiguous(), seq_start.int().contiguous()
         ctx.types = bias.dtype, h0.dtype
         bias, h0 = _fp32(bias), _fp32(h0)
         y, h_last = gates.new_empty(N, H), torch.empty_like(h0)

@@ -122,3 +122,31 @@ def test_lists_that_do_not_fit_are_refused(change):
     with pytest.raises(ValueError):
         rl.DistillTopK.apply(torch.zeros(shape["logits"]), torch.zeros(shape["top"]), torch.zeros(shape["ids"], dtype=change.get("id_type", torch.int32)),
                              1.0, torch.zeros(shape["weight"]))
+
+
+# ------------------------------------------------------------------------------------------- the recurrence
+@pytest.mark.gpu
+def test_starts_and_states_of_other_strides_and_types():
+    gates, bias, state = _randn(N, 3 * H), _randn(3 * H), _randn(1, H)
+    seq = torch.tensor([0, 5, 5, N], dtype=torch.int32, device="cuda")
+    want = rl.GatedRecurrence.apply(gates, bias, state.repeat(3, 1), seq)
+    for h0, starts in [(state.expand(3, H), seq.long()), (state.expand(3, H), torch.stack([seq, -seq], 1)[:, 0]),
+                       (torch.cat([state, -state], 0).t().contiguous().t()[:1].expand(3, H), seq)]:
+        got = rl.GatedRecurrence.apply(gates, bias, h0, starts)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("change", [dict(h0=(4, H)), dict(h0=(2, H)), dict(h0=(3, H + 1)), dict(h0=(H,)), dict(h0=(0, H), starts=(1,)), dict(starts=(4, 1)),
+                                    dict(bias=(3 * H + 1,)), dict(bias=(H,)), dict(gates=(N, 3 * H + 1)), dict(gates=(N, 0), bias=(0,), h0=(3, 0)),
+                                    dict(gates=(N * 3 * H,)), dict(start_type=torch.float32)])
+def test_states_that_do_not_fit_the_starts_are_refused(change):
+    shape = {**dict(gates=(N, 3 * H), bias=(3 * H,), h0=(3, H), starts=(4,)), **change}
+    with pytest.raises(ValueError):
+        rl.GatedRecurrence.apply(torch.zeros(shape["gates"]), torch.zeros(shape["bias"]), torch.zeros(shape["h0"]),
+                                 torch.zeros(shape["starts"], dtype=change.get("start_type", torch.int32)))
+
+
+@pytest.mark.parametrize("x,gamma,beta", [((N, H), (H + 1,), (H,)), ((N, H), (H,), (1,)), ((N, H), (1, H), (H,)), ((H,), (H,), (H,)), ((2, N, H), (H,), (H,))])
+def test_parameters_that_do_not_fit_the_rows_are_refused(x, gamma, beta):
+    with pytest.raises(ValueError):
+        rl.LayerNorm.apply(torch.zeros(x), torch.zeros(gamma), torch.zeros(beta))
