@@ -34,6 +34,12 @@ def _check(fits: bool, what: str):
         raise ValueError(what)
 
 
+def _check_place(*tensors: torch.Tensor):
+    """The kernels take addresses: each has to be memory of the GPU that they are launched on."""
+    for t in tensors:
+        _check(t.is_cuda and t.device.index == torch.cuda.current_device(), f"an operand lies on {t.device}, not on the current GPU")
+
+
 def _whole(t: torch.Tensor) -> bool:
     return not (t.is_floating_point() or t.is_complex() or t.dtype == torch.bool)
 
@@ -44,6 +50,7 @@ class LayerNorm(torch.autograd.Function):
     def forward(ctx, x, gamma, beta):
         _check(x.dim() == 2 and gamma.shape == beta.shape == x.shape[1:],
                f"rows of {tuple(x.shape)} with parameters of {tuple(gamma.shape)} and {tuple(beta.shape)}")
+        _check_place(x, gamma, beta)
         x = x.contiguous()
         N, C = x.shape
         ctx.types = gamma.dtype, beta.dtype
@@ -75,6 +82,7 @@ class GatedRecurrence(torch.autograd.Function):
         _check(h0.dim() == 2 and h0.shape[0] >= 1 and h0.shape[1] == H, f"states of {tuple(h0.shape)} for sequences of {H} units")
         _check(seq_start.shape == (h0.shape[0] + 1,) and _whole(seq_start),
                f"states of {h0.shape[0]} sequences with starts of {tuple(seq_start.shape)} ({seq_start.dtype})")
+        _check_place(gates, bias, h0, seq_start)
         gates, seq_start = gates.contiguous(), seq_start.int().contiguous()
         ctx.types = bias.dtype, h0.dtype
         bias, h0 = _fp32(bias), _fp32(h0)
@@ -107,6 +115,7 @@ class DistillTopK(torch.autograd.Function):
         _check(top_ids.dim() == 2 and top_ids.shape[0] == N and top_logits.shape == top_ids.shape and _whole(top_ids),
                f"{N} rows of logits with lists of {tuple(top_logits.shape)} logits and {tuple(top_ids.shape)} numbers ({top_ids.dtype})")
         _check(weight.shape == (N,), f"{N} rows of logits with weights of {tuple(weight.shape)}")
+        _check_place(logits, top_logits, top_ids, weight)
         logits, top_logits, weight = logits.contiguous(), _fp32(top_logits), _fp32(weight)
         if top_ids.dtype != torch.int32:                       # (before they are cut to 32 bits)
             top_ids = top_ids.long()
@@ -198,6 +207,7 @@ class Server:
     """A pruned model for `batch` callers, one token per step.  Products are BCR products in fp16; states stay in fp32."""
 
     def __init__(self, model: RecurrentLM, batch: int):
+        _check_place(*model.parameters())
         self.model, self.batch = model, batch
         self.gammas, self.betas, self.biases = ([_fp32(p) for p in group] for group in (model.gammas, model.betas, model.biases))
         self.packed = {name: self._pack(model, name) for name in model.products()}

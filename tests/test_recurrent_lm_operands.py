@@ -150,3 +150,37 @@ def test_states_that_do_not_fit_the_starts_are_refused(change):
 def test_parameters_that_do_not_fit_the_rows_are_refused(x, gamma, beta):
     with pytest.raises(ValueError):
         rl.LayerNorm.apply(torch.zeros(x), torch.zeros(gamma), torch.zeros(beta))
+
+
+# ------------------------------------------------------------------------------------------- memory that is not the GPU's
+def _calls(device, **elsewhere):
+    """Every function's call on a device, the operands named in `elsewhere` on another."""
+    at = lambda name, t: t.to(elsewhere.get(name, device))
+    seq = torch.tensor([0, N], dtype=torch.int32)
+    norm = [at(n, t) for n, t in [("x", torch.zeros(N, H)), ("gamma", torch.zeros(H)), ("beta", torch.zeros(H))]]
+    glr = [at(n, t) for n, t in [("gates", torch.zeros(N, 3 * H)), ("bias", torch.zeros(3 * H)), ("h0", torch.zeros(1, H)), ("seq_start", seq)]]
+    z, top, ids, weight = [at(n, t) for n, t in [("logits", torch.zeros(N, V)), ("top", torch.zeros(N, K)), ("ids", torch.zeros(N, K, dtype=torch.int32)),
+                                                 ("weight", torch.zeros(N))]]
+    return {"norm": lambda: rl.LayerNorm.apply(*norm), "glr": lambda: rl.GatedRecurrence.apply(*glr),
+            "distill": lambda: rl.DistillTopK.apply(z, top, ids, 1.0, weight)}
+
+
+@pytest.mark.parametrize("name", ["norm", "glr", "distill"])
+def test_operands_in_host_memory_are_refused(name):
+    with pytest.raises(ValueError, match="GPU"):
+        _calls("cpu")[name]()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name,one", [("norm", "gamma"), ("norm", "beta"), ("glr", "bias"), ("glr", "h0"), ("glr", "seq_start"), ("distill", "top"),
+                                      ("distill", "ids"), ("distill", "weight")])
+def test_one_operand_in_host_memory_is_refused(name, one):
+    with pytest.raises(ValueError, match="GPU"):
+        _calls("cuda", **{one: "cpu"})[name]()
+
+
+def test_a_model_in_host_memory_is_not_served():
+    m = rl.RecurrentLM(32, 32, 1)
+    m.prune(16, 32, 8, 16)
+    with pytest.raises(ValueError, match="GPU"):
+        rl.Server(m, 2)
