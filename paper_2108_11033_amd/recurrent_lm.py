@@ -238,6 +238,7 @@ class Server:
         m, b, stream = self.model, self.batch, torch.cuda.current_stream()
         H, V = m.units, self.logits.shape[0]
         x = m.embedding[tokens].float()
+        _check(x.shape == (b, H), f"embeddings of {tuple(x.shape)} for {b} callers: one token of each")
         for i in range(m.layers):
             binding.spmm(self.packed[f"gates{i}"], self._norm(x, i, stream), b, b, self.gates, b, stream)
             lm.glr_step(self.gates, b, self.biases[i], self.h[i], b, self.h[i], b, self.y, "f16", b, H, b, stream)

@@ -184,3 +184,13 @@ def test_a_model_in_host_memory_is_not_served():
     m.prune(16, 32, 8, 16)
     with pytest.raises(ValueError, match="GPU"):
         rl.Server(m, 2)
+
+
+@pytest.mark.gpu
+def test_a_step_takes_one_token_of_each_caller():
+    server = rl.Server(_model(torch.float32, False), 3)
+    for tokens in [[1], [1, 2], [1, 2, 3, 4], [[1, 2, 3]]]:
+        with pytest.raises(ValueError, match="token"):
+            server.step(torch.tensor(tokens, device="cuda"))
+    assert all(not h.any() for h in server.h), "a refused step changed the states"
+    assert rl.generate(server, torch.tensor([1], device="cuda"), 2).shape == (3, 3)       # (one prompt for all callers)
