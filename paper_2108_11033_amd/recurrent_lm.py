@@ -48,12 +48,12 @@ def _whole(t: torch.Tensor) -> bool:
 class LayerNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, gamma, beta):
-        _check(x.dim() == 2 and gamma.shape == beta.shape == x.shape[1:],
+        _check(x.dim() == 2 and gamma.numel() == beta.numel() == x.shape[1],
                f"rows of {tuple(x.shape)} with parameters of {tuple(gamma.shape)} and {tuple(beta.shape)}")
         _check_place(x, gamma, beta)
         x = x.contiguous()
         N, C = x.shape
-        ctx.types = gamma.dtype, beta.dtype
+        ctx.like = [(t.shape, t.dtype) for t in (gamma, beta)]
         gamma, beta = _fp32(gamma), _fp32(beta)
         y, mean, rstd = torch.empty_like(x), x.new_empty(N, dtype=torch.float32), x.new_empty(N, dtype=torch.float32)
         lm.layer_norm(x, DTYPES[x.dtype], C, gamma, beta, EPS, N, C, y, C, mean, rstd, torch.cuda.current_stream())
@@ -67,7 +67,7 @@ class LayerNorm(torch.autograd.Function):
         dx, dgamma, dbeta = torch.empty_like(x), torch.empty_like(gamma), torch.empty_like(gamma)      # (sums in fp32)
         lm.layer_norm_backward(dy.contiguous(), C, x, C, DTYPES[x.dtype], gamma, mean, rstd, N, C, dx, C, dgamma, dbeta,
                                _scratch(lm.layer_norm_workspace(N, C), x.device), torch.cuda.current_stream())
-        return dx, dgamma.to(ctx.types[0]), dbeta.to(ctx.types[1])
+        return dx, *(t.view(shape).to(dtype) for t, (shape, dtype) in zip((dgamma, dbeta), ctx.like))
 
 
 class GatedRecurrence(torch.autograd.Function):
@@ -76,11 +76,11 @@ class GatedRecurrence(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, gates, bias, h0, seq_start):
-        _check(gates.dim() == 2 and gates.shape[1] >= 3 and gates.shape[1] % 3 == 0 and bias.shape == gates.shape[1:],
+        _check(gates.dim() == 2 and gates.shape[1] >= 3 and gates.shape[1] % 3 == 0 and bias.numel() == gates.shape[1],
                f"gates of {tuple(gates.shape)} with biases of {tuple(bias.shape)}")
         N, H = gates.shape[0], gates.shape[1] // 3
-        _check(h0.dim() == 2 and h0.shape[0] >= 1 and h0.shape[1] == H, f"states of {tuple(h0.shape)} for sequences of {H} units")
-        _check(seq_start.shape == (h0.shape[0] + 1,) and _whole(seq_start),
+        _check(h0.dim() >= 1 and h0.shape[0] >= 1 and h0.numel() == h0.shape[0] * H, f"states of {tuple(h0.shape)} for sequences of {H} units")
+        _check(seq_start.numel() == h0.shape[0] + 1 and _whole(seq_start),
                f"states of {h0.shape[0]} sequences with starts of {tuple(seq_start.shape)} ({seq_start.dtype})")
         _check_place(gates, bias, h0, seq_start)
         gates, seq_start = gates.contiguous(), seq_start.int().contiguous()
@@ -114,7 +114,7 @@ class DistillTopK(torch.autograd.Function):
         N, V = logits.shape
         _check(top_ids.dim() == 2 and top_ids.shape[0] == N and top_logits.shape == top_ids.shape and _whole(top_ids),
                f"{N} rows of logits with lists of {tuple(top_logits.shape)} logits and {tuple(top_ids.shape)} numbers ({top_ids.dtype})")
-        _check(weight.shape == (N,), f"{N} rows of logits with weights of {tuple(weight.shape)}")
+        _check(weight.numel() == N, f"{N} rows of logits with weights of {tuple(weight.shape)}")
         _check_place(logits, top_logits, top_ids, weight)
         logits, top_logits, weight = logits.contiguous(), _fp32(top_logits), _fp32(weight)
         if top_ids.dtype != torch.int32:                       # (before they are cut to 32 bits)

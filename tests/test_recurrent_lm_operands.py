@@ -116,7 +116,7 @@ def test_numbers_beyond_32_bits_are_absent():
 
 
 @pytest.mark.parametrize("change", [dict(logits=(V,)), dict(top=(N, K + 1)), dict(top=(N - 1, K)), dict(ids=(N - 1, K)), dict(ids=(N * K,), top=(N * K,)),
-                                    dict(weight=()), dict(weight=(1,)), dict(weight=(N + 1,)), dict(weight=(N, 1)), dict(id_type=torch.float32)])
+                                    dict(weight=()), dict(weight=(1,)), dict(weight=(N + 1,)), dict(id_type=torch.float32)])
 def test_lists_that_do_not_fit_are_refused(change):
     shape = {**dict(logits=(N, V), top=(N, K), ids=(N, K), weight=(N,)), **change}
     with pytest.raises(ValueError):
@@ -136,7 +136,7 @@ def test_starts_and_states_of_other_strides_and_types():
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
 
 
-@pytest.mark.parametrize("change", [dict(h0=(4, H)), dict(h0=(2, H)), dict(h0=(3, H + 1)), dict(h0=(H,)), dict(h0=(0, H), starts=(1,)), dict(starts=(4, 1)),
+@pytest.mark.parametrize("change", [dict(h0=(4, H)), dict(h0=(2, H)), dict(h0=(3, H + 1)), dict(h0=(H,)), dict(h0=(0, H), starts=(1,)), dict(starts=(3, 1)),
                                     dict(bias=(3 * H + 1,)), dict(bias=(H,)), dict(gates=(N, 3 * H + 1)), dict(gates=(N, 0), bias=(0,), h0=(3, 0)),
                                     dict(gates=(N * 3 * H,)), dict(start_type=torch.float32)])
 def test_states_that_do_not_fit_the_starts_are_refused(change):
@@ -146,7 +146,7 @@ def test_states_that_do_not_fit_the_starts_are_refused(change):
                                  torch.zeros(shape["starts"], dtype=change.get("start_type", torch.int32)))
 
 
-@pytest.mark.parametrize("x,gamma,beta", [((N, H), (H + 1,), (H,)), ((N, H), (H,), (1,)), ((N, H), (1, H), (H,)), ((H,), (H,), (H,)), ((2, N, H), (H,), (H,))])
+@pytest.mark.parametrize("x,gamma,beta", [((N, H), (H + 1,), (H,)), ((N, H), (H,), (1,)), ((N, H), (2, H), (H,)), ((H,), (H,), (H,)), ((2, N, H), (H,), (H,))])
 def test_parameters_that_do_not_fit_the_rows_are_refused(x, gamma, beta):
     with pytest.raises(ValueError):
         rl.LayerNorm.apply(torch.zeros(x), torch.zeros(gamma), torch.zeros(beta))
@@ -194,3 +194,23 @@ def test_a_step_takes_one_token_of_each_caller():
             server.step(torch.tensor(tokens, device="cuda"))
     assert all(not h.any() for h in server.h), "a refused step changed the states"
     assert rl.generate(server, torch.tensor([1], device="cuda"), 2).shape == (3, 3)       # (one prompt for all callers)
+
+
+@pytest.mark.gpu
+def test_operands_of_other_shapes_and_the_right_count():
+    """Rows and columns of parameters, weights, starts and states: their numbers count; gradients come in the operands' shapes."""
+    x, gamma, beta, gates, bias, h0 = _randn(N, H), _randn(H, seed=1), _randn(H, seed=2), _randn(N, 3 * H), _randn(3 * H), _randn(3, H)
+    seq, logits, values, weight = torch.tensor([0, 5, 5, N], dtype=torch.int32, device="cuda"), _randn(N, V), _randn(N, K), _randn(N)
+    ids = torch.arange(K, device="cuda").repeat(N, 1)
+
+    def run(*views):
+        leaves = [t.clone().view(*shape).requires_grad_() for t, shape in zip((gamma, beta, bias, h0), views)]
+        y, last = rl.GatedRecurrence.apply(gates, leaves[2], leaves[3], seq.view(views[4]))
+        loss = rl.DistillTopK.apply(logits, values, ids, 2.0, weight.view(views[5]))
+        ((rl.LayerNorm.apply(x, leaves[0], leaves[1]) * x).sum() + (y * x).sum() + last.sum()).backward()
+        assert all(t.grad.shape == t.shape for t in leaves)
+        return [y, last.flatten(), loss] + [t.grad.flatten() for t in leaves]
+
+    plain = run((H,), (H,), (3 * H,), (3, H), (4,), (N,))
+    other = run((1, H), (H, 1), (3, H), (3, 1, H), (4, 1), (N, 1))
+    assert all(torch.equal(a, b) for a, b in zip(plain, other))
