@@ -13,6 +13,7 @@ from __future__ import annotations
 
 import numpy as np
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding, lm
 
@@ -61,6 +62,7 @@ class LayerNorm(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         x, gamma, mean, rstd = ctx.saved_tensors
         N, C = x.shape
@@ -94,6 +96,7 @@ class GatedRecurrence(torch.autograd.Function):
         return y, h_last
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy, dh_last):
         gates, bias, h0, seq_start, states = ctx.saved_tensors
         N, H = gates.shape[0], gates.shape[1] // 3
@@ -128,6 +131,7 @@ class DistillTopK(torch.autograd.Function):
         return loss.sum()
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, upstream):
         return ctx.saved_tensors[0] * upstream, None, None, None, None
 

@@ -214,3 +214,23 @@ def test_operands_of_other_shapes_and_the_right_count():
     plain = run((H,), (H,), (3 * H,), (3, H), (4,), (N,))
     other = run((1, H), (H, 1), (3, H), (3, 1, H), (4, 1), (N, 1))
     assert all(torch.equal(a, b) for a, b in zip(plain, other))
+
+
+# ------------------------------------------------------------------------------------------- second derivatives
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", ["norm", "glr", "distill"])
+def test_second_derivatives_are_refused(name):
+    """The backward passes are kernels without derivatives of their own: what needs one says so, instead of leaving its terms out."""
+    x = _randn(N, {"norm": H, "glr": 3 * H, "distill": V}[name]).requires_grad_()
+    if name == "norm":
+        out = rl.LayerNorm.apply(x, torch.ones(H, device="cuda"), torch.zeros(H, device="cuda"))
+    elif name == "glr":
+        out = rl.GatedRecurrence.apply(x, torch.zeros(3 * H, device="cuda"), torch.zeros(1, H, device="cuda"),
+                                       torch.tensor([0, N], dtype=torch.int32, device="cuda"))[0]
+    else:
+        out = rl.DistillTopK.apply(x, torch.zeros(N, K, device="cuda"), torch.arange(K, device="cuda", dtype=torch.int32).repeat(N, 1), 1.0,
+                                   torch.ones(N, device="cuda"))
+    dx, = torch.autograd.grad(out.square().sum(), x, create_graph=True)
+    assert dx.requires_grad
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        (dx * x).sum().backward()
