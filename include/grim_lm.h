@@ -58,7 +58,8 @@ grim_status grim_layer_norm_backward(const void *dy_dev, int64_t lddy, const voi
  *                  seq_start[0] = 0, ascending, seq_start[nseq] = N.  NULL: one sequence of all rows (nseq = 1).
  *                  The values are read on the GPU only; others than these give undefined results, inside the buffers.
  *   y_dev          N x H of element type dt, rows of ldy; must not overlap the gates
- *   h_last_dev     nseq x H fp32, the states after the last tokens (of an empty sequence: its h0), or NULL
+ *   h_last_dev     nseq x H fp32, the states after the last tokens (of an empty sequence: its h0), or NULL; must not overlap
+ *                  h0 (unlike a step, the call cannot work in place: sequences end and start in different workgroups)
  *   states_dev     grim_glr_states(N, H) bytes of fp32 states for the backward pass, or NULL
  *   workspace      grim_glr_workspace(N, H) bytes, for either direction
  * Backward, for the gradients dy of y and dh_last of h_last (nseq x H fp32, or NULL: zeros): the states are
@@ -67,13 +68,14 @@ grim_status grim_layer_norm_backward(const void *dy_dev, int64_t lddy, const voi
  *     du = G f (1 - f) (h_(t-1) - c)     dc = G (1 - f)     dv = dy h sigmoid(v) (1 - sigmoid(v))     dh0 = f_0 G_0
  *   dgates_dev     N x 3H of element type dt, rows of lddg; must not overlap the inputs
  *   dbias_dev      3H fp32: column sums of the gates' gradient before its rounding, overwritten; or NULL
- *   dh0_dev        nseq x H fp32, overwritten (of an empty sequence: its dh_last); or NULL
+ *   dh0_dev        nseq x H fp32, overwritten (of an empty sequence: its dh_last); or NULL; must not overlap dh_last
  * Infinities and NaN of one sequence do not reach another.
  * grim_glr_step is one token for `batch` callers at once, in the layout of grim_lstm_cell: gates 3H x batch fp32 as
  * grim_bcr_spmv leaves them (ldg >= batch), states H x batch fp32 (h_new_dev may be h_dev itself), y H x batch of element
  * type dt (what the next product reads), or NULL.
  * Errors: NULL, SHAPE (N < 0, N > 2^30, H < 1, H > 2^21, nseq < 1, nseq > 1 without starts, leading dimension or a buffer too small; of
- * the step: H < 1, batch < 0, H * batch > 2^32 - 256, leading dimension too small), DTYPE, DEVICE.
+ * the step: H < 1, batch < 0, H * batch > 2^32 - 256, leading dimension too small), DTYPE, DEVICE, UNSUPPORTED (h_last over h0,
+ * dh0 over dh_last).
  */
 int64_t grim_glr_states(int64_t N, int64_t H);
 int64_t grim_glr_workspace(int64_t N, int64_t H);

@@ -201,6 +201,11 @@ grim_status in_runs(int64_t all, int64_t most, F f) {
 template <typename T>
 T *ahead(T *p, int64_t elements) { return p ? p + elements : p; }
 
+inline bool overlap(const void *a, const void *b, int64_t bytes) {
+    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+    return a && b && (x < y ? y - x : x - y) < (uintptr_t)bytes;
+}
+
 // rows x ld elements stay far below what a 64-bit byte offset holds
 inline bool fits(int64_t rows, int64_t ld) { return ld >= 0 && ld <= (int64_t(1) << 40) && (rows <= 1 || ld <= (int64_t(1) << 56) / rows); }
 

@@ -718,6 +718,8 @@ grim_status grim_glr_sequence(const void *gates_dev, grim_dtype dt, int64_t ldg,
     if (!glr_sizes(N, H, nseq, seq_start_dev) || ldg < 3 * H || ldy < H || !fits(N, ldg) || !fits(N, ldy)) return GRIM_ERR_SHAPE;
     if ((N > 0 && (!gates_dev || !y_dev)) || !workspace) return GRIM_ERR_NULL;
     if (workspace_bytes < grim_glr_workspace(N, H)) return GRIM_ERR_SHAPE;
+    // (the wave that ends a sequence may be done before the one that starts it reads its state)
+    if (overlap(h0_dev, h_last_dev, nseq * H * (int64_t)sizeof(float))) return GRIM_ERR_UNSUPPORTED;
     GlrParams p{};
     p.gates = gates_dev, p.bias = bias_dev, p.h0 = h0_dev, p.seq = seq_start_dev, p.nseq = nseq;
     p.y = y_dev, p.h_last = h_last_dev, p.states = static_cast<float *>(states_dev);
@@ -738,6 +740,7 @@ grim_status grim_glr_sequence_backward(const void *gates_dev, grim_dtype dt, int
         return GRIM_ERR_SHAPE;
     if ((N > 0 && (!gates_dev || !states_dev || !dy_dev || !dgates_dev)) || !workspace) return GRIM_ERR_NULL;
     if (workspace_bytes < grim_glr_workspace(N, H)) return GRIM_ERR_SHAPE;
+    if (overlap(dh_last_dev, dh0_dev, nseq * H * (int64_t)sizeof(float))) return GRIM_ERR_UNSUPPORTED;
     const Cut c = cut_rows(N, H, dt == GRIM_F32, true);
     GlrParams p{};
     p.gates = gates_dev, p.bias = bias_dev, p.h0 = h0_dev, p.seq = seq_start_dev, p.nseq = nseq;

@@ -346,3 +346,41 @@ def test_refusals():
         assert name(step, **kw) == "GRIM_ERR_SHAPE", kw
     from paper_2108_11033_amd import lm
     assert lm._lib().grim_glr_sequence(256, 9, 3 * H, None, None, None, 1, N, H, 512, H, None, None, 768, 1 << 30, None) == 4
+
+
+def test_states_in_place_are_refused():
+    """Workgroups finish at different times: a sequence's last state would take the place of one that another workgroup has yet to read."""
+    N, H, q = 100, 64, 3
+    ws = torch.empty(g.glr_workspace(N, H), dtype=torch.uint8)
+    size = 4 * q * H
+    at = 1 << 20
+
+    def name(fn, *args):
+        with pytest.raises(g.GrimError) as e:
+            fn(*args)
+        return e.value.name
+
+    fwd = lambda h0, h_last: g.glr_sequence(256, "f16", 3 * H, None, h0, 512, q, N, H, 768, H, h_last, None, ws)
+    bwd = lambda dh_last, dh0: g.glr_sequence_backward(256, "f16", 3 * H, None, None, 512, q, N, H, 1024, 1280, H, dh_last, 1536, 3 * H, None, dh0, ws)
+    for fn in (fwd, bwd):
+        for a, b in [(at, at), (at, at + 4), (at + 4, at), (at, at + size - 4), (at + size - 4, at)]:
+            assert name(fn, a, b) == "GRIM_ERR_UNSUPPORTED", (a, b)
+
+
+@pytest.mark.gpu
+def test_states_side_by_side():
+    """The states before and after in halves of one buffer, in either order: neighbours, not in place."""
+    N, H, q, dtype = 900, 64, 3, "f16"
+    starts = [0, 300, 301, 900]
+    seq = torch.tensor(starts, dtype=torch.int32, device="cuda")
+    gates, bias, h0, dy, dh_last = _operands(dtype, N, H, q, 0, 0, 120)
+    want = _train(dtype, gates, bias, h0, seq, q, N, H, dy, dh_last)
+    for first in (0, 1):
+        a, b = torch.zeros(2 * q, H, device="cuda"), torch.zeros(2 * q, H, device="cuda")
+        before, after, d_after, d_before = a[first * q:][:q], a[(1 - first) * q:][:q], b[first * q:][:q], b[(1 - first) * q:][:q]
+        before.copy_(h0), d_after.copy_(dh_last)
+        ws, states = _scratch(g.glr_workspace(N, H)), _scratch(g.glr_states(N, H))
+        y, dg = out_rows(N, H, dtype)[0], out_rows(N, 3 * H, dtype)[0]
+        g.glr_sequence(gates, dtype, 3 * H, bias, before, seq, q, N, H, y, H, after, states, ws)
+        g.glr_sequence_backward(gates, dtype, 3 * H, bias, before, seq, q, N, H, states, dy, dy.stride(0), d_after, dg, 3 * H, None, d_before, ws)
+        assert torch.equal(after, want[1]) and torch.equal(d_before, want[4]) and torch.equal(before, h0) and torch.equal(d_after, dh_last)
