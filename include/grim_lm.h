@@ -13,6 +13,8 @@
  * element type of activations and their gradients (fp32, fp16, bf16); parameters, their gradients, states and statistics are
  * fp32.  Sums, statistics and states are held in fp32, results rounded once (nearest even).  No kernel uses floating-point
  * atomics: a call repeated on the same inputs gives the same bits.  Zero rows are a valid call (row pointers may then be NULL).
+ * Outputs overlap no other operand but where a call says that it works in place, which it does from the same address with the
+ * same leading dimension (another one is refused: SHAPE).
  */
 #ifndef GRIM_LM_H
 #define GRIM_LM_H
@@ -71,7 +73,7 @@ grim_status grim_layer_norm_backward(const void *dy_dev, int64_t lddy, const voi
  *   dh0_dev        nseq x H fp32, overwritten (of an empty sequence: its dh_last); or NULL; must not overlap dh_last
  * Infinities and NaN of one sequence do not reach another.
  * grim_glr_step is one token for `batch` callers at once, in the layout of grim_lstm_cell: gates 3H x batch fp32 as
- * grim_bcr_spmv leaves them (ldg >= batch), states H x batch fp32 (h_new_dev may be h_dev itself), y H x batch of element
+ * grim_bcr_spmv leaves them (ldg >= batch), states H x batch fp32 (h_new_dev may be h_dev itself, same ld), y H x batch of element
  * type dt (what the next product reads), or NULL.
  * Errors: NULL, SHAPE (N < 0, N > 2^30, H < 1, H > 2^21, nseq < 1, nseq > 1 without starts, leading dimension or a buffer too small; of
  * the step: H < 1, batch < 0, H * batch > 2^32 - 256, leading dimension too small), DTYPE, DEVICE, UNSUPPORTED (h_last over h0,

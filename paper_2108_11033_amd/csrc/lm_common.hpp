@@ -206,6 +206,11 @@ inline bool overlap(const void *a, const void *b, int64_t bytes) {
     return a && b && (x < y ? y - x : x - y) < (uintptr_t)bytes;
 }
 
+// an output in its input's place whose rows lie elsewhere
+inline bool moves(const void *in, int64_t ld_in, const void *out, int64_t ld_out, int64_t rows) {
+    return in == out && ld_in != ld_out && rows > 1;
+}
+
 // rows x ld elements stay far below what a 64-bit byte offset holds
 inline bool fits(int64_t rows, int64_t ld) { return ld >= 0 && ld <= (int64_t(1) << 40) && (rows <= 1 || ld <= (int64_t(1) << 56) / rows); }
 

@@ -522,6 +522,7 @@ grim_status grim_distill_topk(const void *z_dev, grim_dtype dt, int64_t ldz, con
     if (k > kMostEntries) return GRIM_ERR_UNSUPPORTED;
     if (N == 0) return GRIM_OK;
     if (!z_dev || !top_logits_dev || !top_ids_dev || !loss_dev || !workspace) return GRIM_ERR_NULL;
+    if (moves(z_dev, ldz, dz_dev, lddz, N)) return GRIM_ERR_SHAPE;
     if (workspace_bytes < grim_distill_topk_workspace(N, V)) return GRIM_ERR_SHAPE;
     const DistillParams p{z_dev, top_logits_dev, weight_dev, top_ids_dev, loss_dev, dz_dev, static_cast<float *>(workspace),
                           ldz, lddz, ldt, N, V, k, 0, temperature, 1.44269504088896340736f / temperature,

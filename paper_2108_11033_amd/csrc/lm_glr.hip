@@ -765,6 +765,7 @@ grim_status grim_glr_step(const float *gates_dev, int64_t ldg, const float *bias
         return GRIM_ERR_SHAPE;
     if (batch == 0) return GRIM_OK;
     if (!gates_dev || !h_dev || !h_new_dev) return GRIM_ERR_NULL;
+    if (moves(h_dev, ldh, h_new_dev, ldh_new, H)) return GRIM_ERR_SHAPE;
     if (H > most_groups(256) * 256 / batch) return GRIM_ERR_SHAPE;
     const GlrStepParams p{gates_dev, bias_dev, h_dev, h_new_dev, y_dev, ldg, ldh, ldh_new, ldy, H, batch};
     const dim3 grid((unsigned)((H * batch + 255) / 256)), block(256);

@@ -458,6 +458,7 @@ grim_status grim_layer_norm(const void *x_dev, grim_dtype dt, int64_t ldx, const
     if (N < 0 || N > kMostRows || C < 1 || ldx < C || ldy < C || !fits(N, ldx) || !fits(N, ldy) || !(eps >= 0.f) || eps > 3.4e38f) return GRIM_ERR_SHAPE;
     if (N == 0) return GRIM_OK;
     if (!x_dev || !y_dev) return GRIM_ERR_NULL;
+    if (moves(x_dev, ldx, y_dev, ldy, N)) return GRIM_ERR_SHAPE;
     const NormParams p{x_dev, gamma_dev, beta_dev, y_dev, mean_dev, rstd_dev, ldx, ldy, N, C, eps,
                        past_caches(2 * N * C * bytes_of(dt))};
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
@@ -484,6 +485,7 @@ grim_status grim_layer_norm_backward(const void *dy_dev, int64_t lddy, const voi
     const bool sums = dgamma_dev || dbeta_dev;
     if (N > 0 && (!dy_dev || !x_dev || !mean_dev || !rstd_dev)) return GRIM_ERR_NULL;
     if (sums && !workspace) return GRIM_ERR_NULL;
+    if (moves(dy_dev, lddy, dx_dev, lddx, N)) return GRIM_ERR_SHAPE;
     if (sums && workspace_bytes < grim_layer_norm_workspace(N, C)) return GRIM_ERR_SHAPE;
     if (!sums && (!dx_dev || N == 0)) return GRIM_OK;
     const NormBackParams p{dy_dev, x_dev, gamma_dev, mean_dev, rstd_dev, dx_dev, sums ? static_cast<float *>(workspace) : nullptr,

@@ -318,6 +318,7 @@ extern "C" grim_status grim_apply_logit_rules(const void *z_dev, grim_dtype dt, 
     if (rules->nbias > 0 && (!rules->bias_ids || !rules->bias_values)) return GRIM_ERR_NULL;
     if (batch == 0) return GRIM_OK;
     if (!z_dev || !out_dev) return GRIM_ERR_NULL;
+    if (moves(z_dev, ldz, out_dev, ldo, rows)) return GRIM_ERR_SHAPE;
     const RuleParams p{z_dev, out_dev, ldz, ldo, V, batch, *rules};
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     return dt == GRIM_F32   ? rules_typed<float>(p, columns != 0, stream)
