@@ -7,7 +7,9 @@
 // between the maximum, the sum and the gradient.  With few rows, or rows that do not fit, a row is cut into slices: a first launch
 // leaves every slice's maximum, sum and share of the loss, and the second joins them and writes the gradient from a second
 // read of z, which a few rows leave in the caches.  Exponents are taken of differences from the maximum, (z - max) / tau, so that
-// masks of the type's lowest value do not overflow on the way.  Measured: 8192 x 32768 bf16 with 64 listed words 216 us (5.0 TB/s, a copy's
+// masks of the type's lowest value do not overflow on the way.  The loss is summed as
+//     w tau sum_i p_i ((top_i - best) - (z_i - max) + tau (log sum_z - log sum_top))
+// whose terms stay numbers where tau^2, or a difference over tau, is none.  Measured: 8192 x 32768 bf16 with 64 listed words 216 us (5.0 TB/s, a copy's
 // rate), 24 x 131075 fp16 in slices 12 (two launches), 1024 x 1000 fp32 5.6.
 #include "lm_common.hpp"
 
@@ -23,7 +25,7 @@ struct DistillParams {
     const int32_t *ids;
     float *loss;
     void *dz;
-    float *part;                // [row][slice][maximum, sum, share of the loss, probability listed in it]
+    float *part;                // [row][slice][maximum, sum, share of the loss / (w tau), probability listed in it]
     int64_t ldz, lddz, ldt, N, V;
     int32_t k, slices;
     float tau, scale;           // scale = log2(e) / tau
@@ -32,12 +34,12 @@ struct DistillParams {
 };
 
 // The teacher's side of a row in LDS, with room for E entries: words (-1: absent), probabilities, the sums of the probabilities of
-// entries that list the same word, the first part of log2 p = (top - best) scale - log2(total), and z at the words.
+// entries that list the same word, below = top - best (log2 p is that times scale, less log2(total)), and z at the words.
 template <int E>
 struct Entries {
     static constexpr int kBits = E <= 64 ? 11 : 13;
     int32_t id[E];
-    float p[E], sum[E], log[E], z[E];
+    float p[E], sum[E], below[E], z[E];
     uint16_t table[1 << kBits];
     float total;                // sum of exponentials (0: nothing is listed; NaN: a listed logit is)
     // (two multiplications with a shift between them: words in even steps spread, whatever the step)
@@ -77,7 +79,7 @@ __device__ __forceinline__ void teacher(const DistillParams &p, int64_t n, const
             const float v = id[b] >= 0 && id[b] < p.V ? listed[b] : -INFINITY;
             e.z[i] = here ? z_at[b] : 0.f;
             e.id[i] = here ? id[b] : -1;
-            e.log[i] = v;
+            e.below[i] = v;
             nan |= v != v;
             m = fmaxf(m, v);
         }
@@ -86,10 +88,10 @@ __device__ __forceinline__ void teacher(const DistillParams &p, int64_t n, const
     if (__any(nan)) m = NAN;
     float s = 0.f;
     for (int i = lane; i < p.k; i += 64) {
-        const float v = e.log[i];
-        const float d = v == -INFINITY ? -INFINITY : (v - m) * p.scale;
-        const float x = v == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(d);
-        e.log[i] = d;
+        const float v = e.below[i];
+        const float d = v - m;                              // (of no use where p is 0)
+        const float x = v == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(d * p.scale);
+        e.below[i] = d;
         e.p[i] = x;
         s += x;
     }
@@ -237,12 +239,12 @@ __global__ void __launch_bounds__(64 * (W + 1)) distill_rows(DistillParams p) {
     const float rsum = 1.f / sum;
     const float factor = weight * p.tau * (total / total);  // (a NaN of the teacher reaches the whole row)
     if (aside) {
-        const float lse = log2f(sum), ltotal = log2f(total);
+        const float lse = p.tau * (kLn2 * log2f(sum)), ltotal = p.tau * (kLn2 * log2f(total));
         float loss = 0.f;
         for (int i = threadIdx.x & 63; i < p.k; i += 64)
-            if (e.p[i] != 0.f) loss += e.p[i] * ((e.log[i] - ltotal) - ((e.z[i] - peak) * p.scale - lse));
+            if (e.p[i] != 0.f) loss += e.p[i] * ((e.below[i] - ltotal) - ((e.z[i] - peak) - lse));
         loss = wave_sum(loss);
-        if (threadIdx.x == TPR) p.loss[n] = weight * p.tau * p.tau * (kLn2 * loss);
+        if (threadIdx.x == TPR) p.loss[n] = weight * p.tau * loss;
     } else if (dz) {
         const float slope = factor * rsum;
         store_rows(p.past, [&](auto past) {
@@ -308,12 +310,12 @@ __global__ void __launch_bounds__(64 * (kSliceWaves + 1)) distill_slices(Distill
         for (int w = 0; w < W; ++w) peak = fmaxf(peak, room[0][w]), sum += room[1][w];
         // (a slice of nothing but -infinity has the sum 0; one NaN makes the sum NaN)
         const float base = peak == -INFINITY ? 0.f : peak;
-        // sum of p (log2 p - (z - peak) scale) over the words in this slice, and of p
+        // sum of p ((top - best) - (z - peak)) over the words in this slice, and of p
         float share = 0.f, there = 0.f;
         for (int i = lane; i < p.k; i += 64) {
             const int32_t id = e.id[i];
             if (id >= lo && id < hi && e.p[i] != 0.f) {
-                share += e.p[i] * (e.log[i] - (e.z[i] - base) * p.scale);
+                share += e.p[i] * (e.below[i] - (e.z[i] - base));
                 there += e.p[i];
             }
         }
@@ -380,15 +382,15 @@ __global__ void __launch_bounds__(64 * (kSliceWaves + 1)) distill_join(DistillPa
         // (z of this slice only: other slices' places may hold their gradient already, where dz is z)
         teacher<true>(p, n, z, lo, hi, e);
         if (s == 0) {
-            // log2 q = (z - base_i) scale + (base_i - peak) scale - log2 sum
-            const float extra = log2f(sum) - log2f(e.total);
+            // z - max = (z - base_i) + (base_i - peak)
+            const float extra = p.tau * (kLn2 * (log2f(sum) - log2f(e.total)));
             float share = 0.f;
             for (int i = lane; i < p.slices; i += 64) {
                 const float base = part[4 * i] == -INFINITY ? 0.f : part[4 * i], there = part[4 * i + 3];
-                if (there != 0.f) share += part[4 * i + 2] + there * ((peak - base) * p.scale + extra);
+                if (there != 0.f) share += part[4 * i + 2] + there * ((peak - base) + extra);
             }
             share = wave_sum(share);
-            if (lane == 0) p.loss[n] = e.total == 0.f ? 0.f : weight * p.tau * p.tau * (kLn2 * share);
+            if (lane == 0) p.loss[n] = e.total == 0.f ? 0.f : weight * p.tau * share;
         }
     }
     if (!dz) return;

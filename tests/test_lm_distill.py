@@ -193,3 +193,37 @@ def test_refusals():
                dict(ws=torch.empty(g.distill_topk_workspace(6, 100) - 1, dtype=torch.uint8))]:
         assert name(**kw) == "GRIM_ERR_SHAPE", kw
     assert name(k=1025, ldt=1025) == "GRIM_ERR_UNSUPPORTED"
+
+
+# temperatures at the ends of their range and between, with weights that keep the results within fp32
+@pytest.mark.gpu
+@pytest.mark.parametrize("N,V", [(5, 50000), (200, 3000)])
+@pytest.mark.parametrize("tau,scale", [(1e-30, 1.0), (1e-30, 1e30), (1e-23, 1.0), (1e-12, 1.0), (1e-3, 1.0), (1e6, 1.0), (1e18, 1.0), (1e19, 0.01), (1e24, 1e-24),
+                                       (1e30, 1e-30), (1e30, 1e-38)])
+def test_temperatures(N, V, tau, scale):
+    k = 7
+    z, top, ids, weight = _operands("f32", N, V, k, 0, 0, 13)
+    weight = (0.5 + weight) * scale
+    z[0, ids[0].long().clamp(0, V - 1)] = -1e4
+    dz = torch.empty(N, V, device="cuda")
+    loss = _run(z, "f32", V, top, ids, tau, weight, N, k, V, dz, V)
+    want, wdz, sl, sdz = reference(z, top, ids, tau, weight)
+    close(loss, want, sl, "f32", "loss")
+    close(dz, wdz, sdz, "f32", "dz")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tau", [0.25, 1.0])
+@pytest.mark.parametrize("N,V", [(3, 50000), (200, 3000)])
+def test_listed_words_of_the_lowest_value(N, V, tau):
+    """The teacher's best word is masked by the type's lowest value: the loss is as large as that, and no infinity."""
+    k = 3
+    z, top, ids, _ = _operands("f32", N, V, k, 0, 0, 14)
+    ids = torch.arange(k, device="cuda", dtype=torch.int32).repeat(N, 1)
+    top[:, 0] = top.amax(1) + 1
+    weight = torch.full((N,), 0.25, device="cuda")
+    z[0, 0] = torch.finfo(torch.float32).min
+    loss = _run(z, "f32", V, top, ids, tau, weight, N, k, V)
+    want, _, sl, _ = reference(z, top, ids, tau, weight)
+    close(loss, want, sl, "f32", "loss")
+    assert torch.isfinite(loss).all() and float(loss[0]) > 1e30
