@@ -7,7 +7,8 @@
  * the current GPU, owned by the caller; a call only enqueues kernels on hip_stream (NULL = the default stream), allocates
  * nothing, never synchronises and may be captured into a graph.  Argument errors are found before anything is enqueued.
  * Calls that need scratch memory take a workspace of at least the number of bytes that the matching *_workspace function
- * returns, 16-byte aligned, contents irrelevant before and after; calls that overlap in time need workspaces of their own.
+ * returns (0 for sizes that the call refuses), 16-byte aligned, contents irrelevant before and after; calls that overlap in
+ * time need workspaces of their own.
  *
  * Tensors are rows of tokens: element (n, c) at n * ld + c, any ld >= the row's length, aligned to an element.  dt is the
  * element type of activations and their gradients (fp32, fp16, bf16); parameters, their gradients, states and statistics are

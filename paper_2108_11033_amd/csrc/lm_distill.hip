@@ -504,7 +504,7 @@ extern "C" {
 
 int64_t grim_distill_topk_workspace(int64_t N, int64_t V) {
     using namespace grim::lm;
-    if (N < 0 || V < 1 || V >= (int64_t)1 << 31) return 0;
+    if (N < 0 || N > kMostRows || V < 1 || V >= (int64_t)1 << 31) return 0;
     // (whichever type comes: of fp32 a slice holds the fewest elements)
     int64_t bytes = 16;
     if (!by_rows<float>(N, V)) bytes += N * slices_of<float>(V) * 16;

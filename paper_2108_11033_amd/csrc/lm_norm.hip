@@ -467,7 +467,7 @@ grim_status grim_layer_norm(const void *x_dev, grim_dtype dt, int64_t ldx, const
 
 int64_t grim_layer_norm_workspace(int64_t N, int64_t C) {
     using namespace grim::lm;
-    if (N < 0 || C < 1) return 0;
+    if (N < 0 || N > kMostRows || C < 1 || C > kMostFeatures) return 0;
     const int64_t a = back_groups_of<float>(N, C), b = back_groups_of<f16>(N, C);
     const int64_t groups = a > b ? a : b;
     return (groups > 0 ? groups : 1) * 2 * C * (int64_t)sizeof(float);
