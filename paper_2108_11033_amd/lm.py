@@ -2,7 +2,8 @@
 distillation from a teacher's top logits, and the rules for the logits of a served step.
 
 Argument marshalling only, as in binding.py: device buffers are anything with a ``data_ptr()`` or a raw address, dtypes are
-"f32" / "f16" / "bf16", leading dimensions count elements, errors are raised as GrimError.
+"f32" / "f16" / "bf16", leading dimensions count elements, errors are raised as GrimError.  A workspace is a buffer with
+``data_ptr()`` and ``nbytes``, or a pair (address, bytes).
 """
 from __future__ import annotations
 
@@ -69,8 +70,15 @@ def _on(stream):
 
 
 def _room(buf):
-    """Address and bytes of a workspace tensor (or None)."""
-    return (None, 0) if buf is None else (_at(buf), buf.nbytes)
+    """Address and bytes of a workspace (or None)."""
+    if buf is None:
+        return None, 0
+    if isinstance(buf, tuple):
+        return _at(buf[0]), buf[1]
+    try:
+        return _at(buf), buf.nbytes
+    except AttributeError:
+        raise TypeError("a workspace has a size: a buffer with nbytes, or (address, bytes)") from None
 
 
 def layer_norm(x, dtype, ldx: int, gamma, beta, eps: float, N: int, C: int, y, ldy: int, mean=None, rstd=None, stream=None):
