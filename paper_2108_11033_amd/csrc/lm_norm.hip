@@ -322,13 +322,17 @@ int threads_per_row(int64_t C) {
     return 0;
 }
 
+// The fewest pieces of a team of TPR threads: what the next smaller team, with `held` pieces each, has no room for.
+constexpr int fewest_pieces(int tpr, int held) { return tpr == 16 ? 1 : held * (tpr / 4) / tpr + 1; }
+
 // The same for the backward pass, whose threads hold five values per element: as many as leave no register spilled.
 template <typename T>
 constexpr int back_pieces(int tpr) { return (tpr == 1024 ? 8 : tpr == 256 && sizeof(T) == 2 ? 32 : 16) / vec_of<T>(); }
+// (16 waves hold no more 16-bit features than 4 do)
 template <typename T>
 int back_threads_per_row(int64_t C) {
     const int64_t V = vec_of<T>();
-    for (int tpr : {16, 64, 256, 1024})
+    for (int tpr : {16, 64, 256, sizeof(T) == 4 ? 1024 : 256})
         if (C >= V && C <= back_pieces<T>(tpr) * tpr * V) return tpr;
     return 0;
 }
@@ -363,12 +367,12 @@ NormParams rows_of(NormParams p, int64_t first, int64_t count) {
 
 template <typename T, int TPR>
 grim_status norm_launch(const NormParams &call, hipStream_t stream) {
-    constexpr int RPG = TPR < 256 ? 256 / TPR : 1, threads = TPR < 256 ? 256 : TPR;
+    constexpr int RPG = TPR < 256 ? 256 / TPR : 1, threads = TPR < 256 ? 256 : TPR, fewest = fewest_pieces(TPR, 4);
     return in_runs(call.N, most_groups(threads) * RPG, [&](int64_t first, int64_t count) {
         const NormParams p = rows_of<T>(call, first, count);
         const dim3 g((unsigned)((p.N + RPG - 1) / RPG)), b(threads);
         switch ((p.C + TPR * vec_of<T>() - 1) / (TPR * vec_of<T>())) {
-            case 1: hipLaunchKernelGGL((norm_rows<T, TPR, 1>), g, b, 0, stream, p); break;
+            case 1: hipLaunchKernelGGL((norm_rows<T, TPR, fewest>), g, b, 0, stream, p); break;
             case 2: hipLaunchKernelGGL((norm_rows<T, TPR, 2>), g, b, 0, stream, p); break;
             case 3: hipLaunchKernelGGL((norm_rows<T, TPR, 3>), g, b, 0, stream, p); break;
             default: hipLaunchKernelGGL((norm_rows<T, TPR, 4>), g, b, 0, stream, p); break;
@@ -395,9 +399,9 @@ template <typename T, int TPR>
 grim_status norm_back_launch(const NormBackParams &p, int64_t groups, hipStream_t stream) {
     const dim3 g((unsigned)groups), b(TPR < 256 ? 64 * kBackWaves : TPR);
     const size_t lds = TPR < 256 && p.part ? 2 * p.C * sizeof(float) : 0;
-    constexpr int most = back_pieces<T>(TPR);
+    constexpr int most = back_pieces<T>(TPR), fewest = fewest_pieces(TPR, back_pieces<T>(TPR / 4));
     switch ((p.C + TPR * vec_of<T>() - 1) / (TPR * vec_of<T>())) {
-        case 1: hipLaunchKernelGGL((norm_back_rows<T, TPR, 1>), g, b, lds, stream, p); break;
+        case 1: hipLaunchKernelGGL((norm_back_rows<T, TPR, fewest>), g, b, lds, stream, p); break;
         case 2: hipLaunchKernelGGL((norm_back_rows<T, TPR, most < 2 ? most : 2>), g, b, lds, stream, p); break;
         case 3: hipLaunchKernelGGL((norm_back_rows<T, TPR, most < 3 ? most : 3>), g, b, lds, stream, p); break;
         default: hipLaunchKernelGGL((norm_back_rows<T, TPR, most>), g, b, lds, stream, p); break;
@@ -426,7 +430,9 @@ grim_status norm_back_typed(const NormBackParams &p, float *dgamma, float *dbeta
             case 16: st = norm_back_launch<T, 16>(p, groups, stream); break;
             case 64: st = norm_back_launch<T, 64>(p, groups, stream); break;
             case 256: st = norm_back_launch<T, 256>(p, groups, stream); break;
-            case 1024: st = norm_back_launch<T, 1024>(p, groups, stream); break;
+            case 1024:
+                if constexpr (sizeof(T) == 4) st = norm_back_launch<T, 1024>(p, groups, stream);
+                break;
             default:
                 if (p.part) {                                               // first: dx may take dy's place
                     const int64_t slab = (p.N + groups - 1) / groups;
