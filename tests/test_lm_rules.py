@@ -167,3 +167,27 @@ def test_refusals():
     assert name(history=768, max_history=2 ** 20 + 1, ld_history=2 ** 21) == "GRIM_ERR_UNSUPPORTED"
     from paper_2108_11033_amd import lm
     assert lm._lib().grim_apply_logit_rules(256, 0, 0, 64, 64, 2, None, 512, 64, None) == 1              # GRIM_ERR_NULL: no rules
+
+
+# Columns of more than 2^22 logits run in tiles of 8192 places, with room for up to 128 biases a caller or for 1024; 2^22 itself is the first such call.
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("V,batch,L,nb", [(131075, 33, 700, 16), (131072, 64, 300, 129), (2 ** 17, 32, 5, 128), (14001, 301, 60, 40), (1400003, 3, 3000, 1024)])
+def test_many_logits_in_columns(dtype, V, batch, L, nb):
+    assert V * batch >= 1 << 22
+    r = _rules(V, batch, L, nb, V + batch)
+    buf, view = _logits(dtype, V, batch, True, 3, V)
+    view[0, 0], view[batch - 1, V - 1] = -math.inf, torch.finfo(TORCH[dtype]).min
+    out, oview = _logits(dtype, V, batch, True, 5, 1)
+    out.fill_(float("nan"))
+    call = lambda to: g.logit_rules(buf, dtype, buf.stride(0), V, batch, to, to.stride(0), columns=True, stream=torch.cuda.current_stream(), **r)
+    call(out)
+    # the same callers' rows a few at a time in 64 bits
+    for b0 in range(0, batch, 16):
+        n = min(16, batch - b0)
+        some = {k: v[b0:b0 + n] if torch.is_tensor(v) else v for k, v in r.items()}
+        want, slack = reference(view[b0:b0 + n].double(), some, n, V)
+        close(oview[b0:b0 + n], want, slack, dtype, f"callers {b0}..")
+    assert torch.isnan(out[:, batch:]).all()
+    call(buf)                                                                                             # in place
+    assert torch.equal(view, oview) and torch.isnan(buf[:, batch:]).all()
