@@ -227,3 +227,10 @@ def test_listed_words_of_the_lowest_value(N, V, tau):
     want, _, sl, _ = reference(z, top, ids, tau, weight)
     close(loss, want, sl, "f32", "loss")
     assert torch.isfinite(loss).all() and float(loss[0]) > 1e30
+
+
+# More rows than compute units of 1793 to 2688 pieces of 16 bytes: rows of eight waves with six pieces a thread.
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,N,V,k", [("bf16", 300, 18001, 64), ("f16", 301, 21503, 100), ("f32", 300, 9001, 65), ("f32", 257, 10752, 16), ("bf16", 270, 14337, 7)])
+def test_many_rows_of_a_middling_vocabulary(dtype, N, V, k):
+    test_loss_and_gradient(dtype, N, V, k)
