@@ -110,7 +110,8 @@ grim_status grim_glr_step(const float *gates_dev, int64_t ldg, const float *bias
  *   workspace      grim_distill_topk_workspace(N, V) bytes
  * The loss is a difference of logarithms in fp32, off by some 2^-20 of weight tau^2: at temperatures far above the spread of
  * the logits that is more than what is left of a loss whose teacher lists all words.
- * z may hold -infinity (words that cannot come: q = 0); a row that holds nothing else, or +infinity or NaN, gives NaN.
+ * z may hold -infinity (words that cannot come: q = 0); a row that holds nothing else, or +infinity or NaN, gives NaN, as does a
+ * listed logit of +infinity or NaN.
  * Errors: NULL, SHAPE (N < 0, N >= 2^31, V < 1, V >= 2^31, k < 1, leading dimension too small, tau outside 1e-30 .. 1e30,
  * workspace too small), DTYPE, DEVICE, UNSUPPORTED (k > 1024).
  */

@@ -28,6 +28,7 @@ constexpr int kWaves = 8;       // waves, and chunks, of a workgroup
 // against 212).
 constexpr int kWavesMaps = 8;
 template <int VEC> constexpr int waves_forward() { return VEC == 1 ? 8 : VEC == 2 ? 6 : 4; }
+// (two 16-bit units a lane backward want a few registers more than the 128 that four waves leave: 4 are spilled, 20 bytes of scratch a lane)
 template <int VEC> constexpr int waves_backward() { return VEC <= 2 ? 4 : 2; }
 // Units of a lane where there are rows enough: 4 bytes, 256 of a row per wave.  (bf16, both directions: 65536 x 1024 555 us with one
 // unit, 479 with two, 490 with four; fp32: 896 with one, 903 with two.)
