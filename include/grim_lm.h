@@ -1,7 +1,8 @@
 /*
  * grim_lm.h -- operators of a recurrent language model around the BCR products of grim_bcr.h: the layer norm between
- * layers, a gated linear recurrence that trains over long sequences and serves token by token, distillation of a pruned
- * student from its teacher's top logits, and the rules applied to the logits of a served step.
+ * layers, a gated linear recurrence that trains over long sequences and serves token by token, distillation of a
+ * pruned student from its teacher's top logits, the clipped policy loss of sampled words, clipping by the norm of all gradients, and
+ * the rules applied to the logits of a served step.
  *
  * Conventions of grim_bcr.h: functions return a grim_status and never throw or abort; *_dev pointers are device memory of
  * the current GPU, owned by the caller; a call only enqueues kernels on hip_stream (NULL = the default stream), allocates
@@ -120,6 +121,72 @@ grim_status grim_distill_topk(const void *z_dev, grim_dtype dt, int64_t ldz, con
                               const int32_t *top_ids_dev, int32_t k, int64_t ldt, float temperature,
                               const float *weight_dev, int64_t N, int64_t V, float *loss_dev, void *dz_dev, int64_t lddz,
                               void *workspace, int64_t workspace_bytes, void *hip_stream);
+
+/*
+ * The clipped policy loss of chosen words, with a KL term against a reference model.  Row n of the logits z has V entries, the word ids[n] was
+ * sampled there.  With the temperature tau, lp = log softmax(z / tau)[id], r = exp(lp - old) and d = ref - lp,
+ *     loss_n = weight_n * (kl * (exp(d) - d - 1) - min(r * A, clamp(r, 1 - clip_low, 1 + clip_high) * A))
+ *     dz_n[j] = weight_n * s * ([j = id] - softmax(z / tau)_j) / tau       (the gradient of sum over n of loss_n)
+ *     s = kl * (1 - exp(d)) - (r * A where r * A <= clamp(r) * A, else 0)
+ * Zero-initialise, then set what is used.
+ */
+typedef struct grim_policy {
+    const int32_t *ids;           /* N; a row whose word lies outside 0 .. V-1 (padding) has loss, logp and gradient 0, whatever z holds */
+    const float *old_logp;        /* N: lp of the policy that sampled the words; NULL: lp itself (r = 1, with the same gradient) */
+    const float *ref_logp;        /* N: lp of the reference; NULL: no KL term, as with kl = 0 */
+    const float *advantage;       /* N: A */
+    const float *weight;          /* N (the mean's 1/N, a loss scale, 0 for padding), or NULL (1); rows of weight 0 have loss and gradient 0 */
+    float temperature, clip_low, clip_high, kl;
+} grim_policy;
+
+/*
+ *   z_dev          N x V of element type dt, rows of ldz
+ *   loss_dev       N fp32, or NULL
+ *   logp_dev       N fp32: lp, of rows of weight 0 too, or NULL.  With neither loss nor gradient asked for, the call scores texts (what old_logp and ref_logp
+ *                  are made of) and needs no advantages.
+ *   dz_dev         N x V of element type dt, rows of lddz, may be z_dev itself (same ld); or NULL
+ *   workspace      grim_policy_loss_workspace(N, V) bytes
+ * z may hold -infinity (words that cannot come); a row that holds nothing else, or +infinity or NaN, gives NaN.  A chosen word of -infinity has lp = -infinity and, with a
+ * KL term, loss infinity and no gradient (NaN).
+ * Errors: NULL, SHAPE (N < 0, N >= 2^31, V < 1, V >= 2^31, leading dimension too small, temperature outside 1e-30 .. 1e30, clip_low outside 0 .. 1, clip_high or
+ * kl negative or above 3e38, workspace too small), DTYPE, DEVICE.
+ */
+int64_t grim_policy_loss_workspace(int64_t N, int64_t V);
+grim_status grim_policy_loss(const void *z_dev, grim_dtype dt, int64_t ldz, const grim_policy *policy, int64_t N, int64_t V, float *loss_dev,
+                             float *logp_dev, void *dz_dev, int64_t lddz, void *workspace, int64_t workspace_bytes, void *hip_stream);
+
+/*
+ * The norm of all gradients of a model, and clipping by it:
+ *     norm = |unscale| * sqrt(sum over all tensors of g^2)        out = g * unscale * min(1, max_norm / norm)
+ * (unscale takes a loss scale back).  Squares are summed in fp64.  A norm that is not finite leaves the gradients unclipped (out = g * unscale): whoever
+ * reads the norm can skip the step.
+ * A list names the gradients of a step.  It is host memory alone, holds no tensor alive and may be made anew for every step; it must not be freed while a call
+ * with it runs on another thread (kernels have copies of it).
+ */
+typedef struct grim_grad {
+    const void *grad;             /* count elements of type dt, one after another, aligned to an element */
+    void *out;                    /* count elements of type out_dt; may be grad itself (same type); NULL in lists that only grim_grad_norm takes */
+    int64_t count;
+    int32_t dt, out_dt;           /* grim_dtype */
+} grim_grad;
+typedef struct grim_grad_list grim_grad_list;
+
+/*
+ * Tensors without elements may be in the list; an empty list has the norm 0.
+ * Errors: NULL, SHAPE (count outside 0 .. 2^20, a tensor of more than 2^40 elements or 100 tensors in a row of more than 2^43, outputs that overlap each other or a gradient other than their own),
+ * DTYPE, ALLOC.
+ */
+grim_status grim_grad_list_create(const grim_grad *grads, int32_t count, grim_grad_list **out);
+void grim_grad_list_free(grim_grad_list *list);
+int64_t grim_grad_workspace(const grim_grad_list *list);
+/*
+ *   norm_dev       1 fp32
+ *   workspace      grim_grad_workspace(list) bytes
+ * Errors: NULL (also: clipping a list without outputs), SHAPE (max_norm negative or NaN, unscale not finite, workspace too small), DEVICE.
+ */
+grim_status grim_grad_norm(const grim_grad_list *list, float unscale, float *norm_dev, void *workspace, int64_t workspace_bytes, void *hip_stream);
+grim_status grim_grad_clip(const grim_grad_list *list, float max_norm, float unscale, float *norm_dev, void *workspace, int64_t workspace_bytes,
+                           void *hip_stream);
 
 /*
  * The rules applied to the logits of a served step, for `batch` callers at once, in this order:

@@ -14,7 +14,8 @@ using bf16 = __bf16;
 using f16 = _Float16;
 
 constexpr int kComputeUnits = 256;
-constexpr int64_t kMostRows = 0x7fffffff;       // of a layer norm, a distillation
+constexpr int64_t kMostRows = 0x7fffffff;       // of a layer norm, a distillation, a policy loss
+constexpr int kMostHeads = 4096, kMostHeadSize = 128;   // of a gated delta rule
 
 // V elements of T as they lie in memory, in words: what waits in registers keeps two 16-bit elements in each.  They are read
 // and written at any address that an element may have: rows may start anywhere (odd widths, leading dimensions and offsets), the

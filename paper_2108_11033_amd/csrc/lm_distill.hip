@@ -11,13 +11,12 @@
 //     w tau sum_i p_i ((top_i - best) - (z_i - max) + tau (log sum_z - log sum_top))
 // whose terms stay numbers where tau^2, or a difference over tau, is none.  Measured: 8192 x 32768 bf16 with 64 listed words 216 us (5.0 TB/s, a copy's
 // rate), 24 x 131075 fp16 in slices 12 (two launches), 1024 x 1000 fp32 5.6.
-#include "lm_common.hpp"
+#include "lm_rows.hpp"
 
 namespace grim {
 namespace lm {
 
 constexpr int kMostEntries = 1024;
-constexpr float kLn2 = 0.69314718055994530942f;
 
 struct DistillParams {
     const void *z;
@@ -143,20 +142,6 @@ __device__ __forceinline__ void teacher(const DistillParams &p, int64_t n, const
     }
 }
 
-template <typename T>
-constexpr int piece() { return 16 / (int)sizeof(T); }
-
-template <typename T>
-__device__ __forceinline__ void zero_row(T *dz, int64_t lo, int64_t hi) {
-    constexpr int V = piece<T>();
-    const float none[V] = {};
-    for (int64_t c = lo + (int64_t)threadIdx.x * V; c < hi; c += (int64_t)blockDim.x * V) {
-        if (c + V <= hi) store(dz + c, none);
-        else
-            for (int j = 0; c + j < hi; ++j) dz[c + j] = (T)0.f;
-    }
-}
-
 // weight tau (q_j - p_j) at the listed words, over what was streamed there.
 template <int E, typename T>
 __device__ __forceinline__ void write_listed(const DistillParams &p, const Entries<E> &e, T *dz, float peak, float rsum, float factor,
@@ -266,31 +251,6 @@ __global__ void __launch_bounds__(64 * (W + 1)) distill_rows(DistillParams p) {
 }
 
 // -------------------------------------------------------------------------------------------------- slices of rows
-constexpr int kSliceWaves = 4, kSlicePer = 4;               // a slice: 4 pieces of 16 bytes a thread
-
-template <typename T>
-constexpr int64_t slice_elements() { return 64 * kSliceWaves * kSlicePer * piece<T>(); }
-
-// The pieces of a slice [lo, hi), element by element at its end.
-template <typename T>
-struct Slice {
-    static constexpr int V = piece<T>();
-    Pack<T, V> raw[kSlicePer];
-    int have[kSlicePer];
-    __device__ __forceinline__ static int64_t at(int64_t lo, int k) { return lo + (int64_t)(k * 64 * kSliceWaves + threadIdx.x) * V; }
-    __device__ __forceinline__ Slice(const T *z, int64_t lo, int64_t hi) {
-#pragma unroll
-        for (int k = 0; k < kSlicePer; ++k) {
-            const int64_t c = at(lo, k), left = hi - c;
-            have[k] = left >= V ? V : left > 0 ? (int)left : 0;
-            if (have[k] == V) raw[k] = load<V>(z + c);
-            else
-#pragma unroll
-                for (int j = 0; j < V; ++j) put(raw[k], j, j < have[k] ? z[c + j] : (T)-INFINITY);
-        }
-    }
-};
-
 // (kSliceWaves waves take the slice, one more the teacher's side meanwhile)
 template <typename T, int E>
 __global__ void __launch_bounds__(64 * (kSliceWaves + 1)) distill_slices(DistillParams p) {
@@ -427,9 +387,6 @@ __global__ void __launch_bounds__(64 * (kSliceWaves + 1)) distill_join(DistillPa
 }
 
 // -------------------------------------------------------------------------------------------------- launches
-template <typename T>
-int64_t slices_of(int64_t V) { return (V + slice_elements<T>() - 1) / slice_elements<T>(); }
-
 // A workgroup per row where its registers hold the row: 18 pieces a thread of 15 waves.
 template <typename T>
 bool row_fits(int64_t V) { return V >= piece<T>() && V <= (int64_t)18 * 960 * piece<T>(); }

@@ -1,5 +1,6 @@
 """ctypes binding of the language-model operators declared in include/grim_lm.h: layer norm, the gated linear recurrence,
-distillation from a teacher's top logits, and the rules for the logits of a served step.
+distillation from a teacher's top logits, the clipped policy loss, clipping by the norm of all gradients, and the rules for the
+logits of a served step.
 
 Argument marshalling only, as in binding.py: device buffers are anything with a ``data_ptr()`` or a raw address, dtypes are
 "f32" / "f16" / "bf16", leading dimensions count elements, errors are raised as GrimError.  A workspace is a buffer with
@@ -14,6 +15,10 @@ from .binding import _DT_CODE, GrimError, _addr, _stream, load_library
 
 # struct grim_logit_rules
 _RULES = struct.Struct("@PPqiiPPPPPqPq")
+# struct grim_policy
+_POLICY = struct.Struct("@PPPPPffff")
+# struct grim_grad
+_GRAD = struct.Struct("@PPqii")
 
 _I64, _I32, _P, _F = ctypes.c_int64, ctypes.c_int32, ctypes.c_void_p, ctypes.c_float
 ARGTYPES = {
@@ -27,6 +32,13 @@ ARGTYPES = {
     "grim_glr_step": [_P, _I64, _P, _P, _I64, _P, _I64, _P, _I32, _I64, _I64, _I32, _P],
     "grim_distill_topk_workspace": [_I64, _I64],
     "grim_distill_topk": [_P, _I32, _I64, _P, _P, _I32, _I64, _F, _P, _I64, _I64, _P, _P, _I64, _P, _I64, _P],
+    "grim_policy_loss_workspace": [_I64, _I64],
+    "grim_policy_loss": [_P, _I32, _I64, _P, _I64, _I64, _P, _P, _P, _I64, _P, _I64, _P],
+    "grim_grad_list_create": [_P, _I32, _P],
+    "grim_grad_list_free": [_P],
+    "grim_grad_workspace": [_P],
+    "grim_grad_norm": [_P, _F, _P, _P, _I64, _P],
+    "grim_grad_clip": [_P, _F, _F, _P, _P, _I64, _P],
     "grim_apply_logit_rules": [_P, _I32, _I32, _I64, _I64, _I32, _P, _P, _I64, _P],
 }
 
@@ -39,7 +51,7 @@ class _Calls:
         for fn_name, types in ARGTYPES.items():
             fn = getattr(lib, fn_name)
             fn.argtypes = types
-            fn.restype = _I64 if fn_name.endswith(("_workspace", "_states")) else _I32
+            fn.restype = None if fn_name.endswith("_free") else _I64 if fn_name.endswith(("_workspace", "_states")) else _I32
             setattr(self, fn_name, fn)
         return getattr(lib, name)
 
@@ -157,6 +169,71 @@ def distill_topk(z, dtype, ldz: int, top_logits, top_ids, k: int, ldt: int, temp
                                   _at(weight), N, V, _at(loss), _at(dz), lddz, ws, room, _on(stream))
     if status:
         raise GrimError(status, "grim_distill_topk")
+
+
+def policy_loss_workspace(N: int, V: int) -> int:
+    """grim_policy_loss_workspace: bytes that policy_loss needs."""
+    return int(_c.grim_policy_loss_workspace(N, V))
+
+
+def policy_loss(z, dtype, ldz: int, ids, N: int, V: int, loss, logp, dz, lddz: int, workspace, *, old_logp=None, ref_logp=None, advantage=None,
+                weight=None, temperature: float = 1.0, clip_low: float = 0.2, clip_high: float = 0.2, kl: float = 0.0, stream=None):
+    """grim_policy_loss: enqueue every row's clipped policy loss, its word's logarithm and the gradient of the losses' sum (each may be None)."""
+    policy = _POLICY.pack(_at(ids) or 0, _at(old_logp) or 0, _at(ref_logp) or 0, _at(advantage) or 0, _at(weight) or 0, temperature, clip_low,
+                          clip_high, kl)
+    ws, room = _room(workspace)
+    status = _c.grim_policy_loss(_at(z), _DT_CODE[dtype], ldz, policy, N, V, _at(loss), _at(logp), _at(dz), lddz, ws, room, _on(stream))
+    if status:
+        raise GrimError(status, "grim_policy_loss")
+
+
+class GradList:
+    """grim_grad_list: the gradients of a step and where their clipped values go (the gradients themselves, if `outs` is None).  Tensors are
+    contiguous, of fp32, fp16 or bf16, all on the GPU that the calls run on; the list keeps them alive.  `workspace`: the bytes that its calls need."""
+
+    def __init__(self, grads, outs=None):
+        self.handle, self.workspace = None, 0
+        self.grads = list(grads)
+        self.outs = self.grads if outs is None else list(outs)
+        if len(self.grads) != len(self.outs) or any(g.numel() != o.numel() for g, o in zip(self.grads, self.outs)):
+            raise ValueError("gradients and outputs differ in number or size")
+        for t in self.grads + self.outs:
+            if not t.is_contiguous():
+                raise ValueError(f"a tensor of {tuple(t.shape)} is not contiguous")
+            if str(t.dtype) not in _NAMES:
+                raise ValueError(f"a tensor of {t.dtype}")
+        code = lambda t: _DT_CODE[_NAMES[str(t.dtype)]]
+        rows = b"".join(_GRAD.pack(_at(g) or 0, _at(o) or 0, g.numel(), code(g), code(o)) for g, o in zip(self.grads, self.outs))
+        handle = _P()
+        status = _c.grim_grad_list_create(rows, len(self.grads), ctypes.byref(handle))
+        if status:
+            raise GrimError(status, "grim_grad_list_create")
+        self.handle = handle
+        self.workspace = int(_c.grim_grad_workspace(handle))
+
+    def __del__(self):
+        handle, self.handle = getattr(self, "handle", None), None
+        if handle:
+            _c.grim_grad_list_free(handle)
+
+
+_NAMES = {"torch.float32": "f32", "torch.float16": "f16", "torch.bfloat16": "bf16"}
+
+
+def grad_norm(grads: GradList, unscale: float, norm, workspace, stream=None):
+    """grim_grad_norm: enqueue norm = |unscale| times the norm of all gradients of the list."""
+    ws, room = _room(workspace)
+    status = _c.grim_grad_norm(grads.handle, unscale, _at(norm), ws, room, _on(stream))
+    if status:
+        raise GrimError(status, "grim_grad_norm")
+
+
+def grad_clip(grads: GradList, max_norm: float, unscale: float, norm, workspace, stream=None):
+    """grim_grad_clip: the same, and enqueue every output = gradient * unscale * min(1, max_norm / norm)."""
+    ws, room = _room(workspace)
+    status = _c.grim_grad_clip(grads.handle, max_norm, unscale, _at(norm), ws, room, _on(stream))
+    if status:
+        raise GrimError(status, "grim_grad_clip")
 
 
 def logit_rules(z, dtype, ldz: int, V: int, batch: int, out, ldo: int, *, columns: bool = False, history=None, ld_history: int = 0,
