@@ -1,7 +1,7 @@
 /*
  * grim_lm.h -- operators of a recurrent language model around the BCR products of grim_bcr.h: the layer norm between
- * layers, a gated linear recurrence that trains over long sequences and serves token by token, distillation of a
- * pruned student from its teacher's top logits, the clipped policy loss of sampled words, clipping by the norm of all gradients, and
+ * layers, a gated linear recurrence and a gated delta rule that train over long sequences and serve token by token, distillation of
+ * a pruned student from its teacher's top logits, the clipped policy loss of sampled words, clipping by the norm of all gradients, and
  * the rules applied to the logits of a served step.
  *
  * Conventions of grim_bcr.h: functions return a grim_status and never throw or abort; *_dev pointers are device memory of
@@ -95,6 +95,43 @@ grim_status grim_glr_sequence_backward(const void *gates_dev, grim_dtype dt, int
 grim_status grim_glr_step(const float *gates_dev, int64_t ldg, const float *bias_dev, const float *h_dev, int64_t ldh,
                           float *h_new_dev, int64_t ldh_new, void *y_dev, grim_dtype dt, int64_t ldy, int64_t H,
                           int32_t batch, void *hip_stream);
+
+/*
+ * Gated delta rule over packed sequences: a recurrent layer whose state is, for each of its heads, a dk x dv matrix S that maps keys to
+ * values.  A token decays the states, looks up what they hold for its key and moves that towards its value:
+ *     D_t = exp(g_t) S_(t-1)     e_t = v_t - D_t' k_t     S_t = D_t + beta_t k_t e_t'     y_t = scale S_t' q_t
+ *   q_dev, k_dev    N x (key_heads dk) of element type dt, rows of ldq, ldk; head h reads key head h / (heads / key_heads).  norm_eps > 0: each head's
+ *                   query and key count divided by sqrt(their squares' sum + norm_eps); 0: as they are (keys longer than one, with beta
+ *                   near 1, make the states grow without bound)
+ *   v_dev           N x (heads dv) of element type dt, rows of ldv
+ *   decay_dev, beta_dev   N x heads fp32, rows of ldg: g (the logarithm of the decay, at most 0; below -10000, -infinity too, it counts as
+ *                   -10000, whose exponential is 0) and beta (in 0 .. 1, or up to 2)
+ *   s0_dev          nseq x heads x dk x dv fp32: the states before the first tokens, or NULL (zeros)
+ *   seq_start_dev   nseq + 1 int32, as of grim_glr_sequence; NULL: one sequence of all rows (nseq = 1)
+ *   y_dev           N x (heads dv) of element type dt, rows of ldy; must not overlap the inputs
+ *   s_last_dev      nseq x heads x dk x dv fp32, the states after the last tokens (of an empty sequence: its s0), or NULL; must not overlap s0
+ *   states_dev      grim_gdr_states(...) bytes for the backward pass, 16-byte aligned, or NULL
+ *   workspace       grim_gdr_workspace(...) bytes
+ * Infinities and NaN reach the tokens of their own sequence and head alone,
+ * there also tokens in front of them.  Products run on the matrix cores with operands in two (fp16, bf16) or three (fp32) bf16 parts, sums in fp32: results are off by some 2^-17
+ * or 2^-23 of the terms' size before their rounding.  Values beyond 3.3e38 count as infinite.
+ * grim_gdr_step is one token for `batch` callers at once, columns as of grim_glr_step: q and k (key_heads dk) x batch, v (heads dv) x batch, g and beta
+ * heads x batch, all fp32; states batch x heads x dk x dv fp32 as the sequence calls have them (s_new_dev may be s_dev itself), y (heads dv) x batch of element
+ * type dt, or NULL.  Its arithmetic is fp32.
+ * Errors: NULL, SHAPE (N < 0, N > 2^30, nseq < 1, nseq > 1 without starts, heads < 1 or > 4096, heads not a multiple of key_heads, dk or dv < 1, leading
+ * dimension or a buffer too small, scale not finite, norm_eps negative), DTYPE, DEVICE, UNSUPPORTED (dk or dv > 128, s_last over s0, s_new over a part of s).
+ */
+int64_t grim_gdr_states(int64_t N, int32_t nseq, int32_t heads, int32_t dk, int32_t dv);
+int64_t grim_gdr_workspace(int64_t N, int32_t nseq, int32_t heads, int32_t key_heads, int32_t dk, int32_t dv);
+grim_status grim_gdr_sequence(const void *q_dev, const void *k_dev, const void *v_dev, grim_dtype dt, int64_t ldq, int64_t ldk, int64_t ldv,
+                              const float *decay_dev, const float *beta_dev, int64_t ldg, const float *s0_dev, const int32_t *seq_start_dev,
+                              int32_t nseq, int64_t N, int32_t heads, int32_t key_heads, int32_t dk, int32_t dv, float scale, float norm_eps,
+                              void *y_dev, int64_t ldy, float *s_last_dev, void *states_dev, void *workspace, int64_t workspace_bytes,
+                              void *hip_stream);
+grim_status grim_gdr_step(const float *q_dev, const float *k_dev, const float *v_dev, int64_t ldq, int64_t ldk, int64_t ldv, const float *decay_dev,
+                          const float *beta_dev, int64_t ldg, const float *s_dev, float *s_new_dev, void *y_dev, grim_dtype dt, int64_t ldy,
+                          int32_t heads, int32_t key_heads, int32_t dk, int32_t dv, float scale, float norm_eps, int32_t batch,
+                          void *hip_stream);
 
 /*
  * Distillation from a teacher's top logits.  Row n of the student's logits z has V entries; the teacher lists k of them,

@@ -1,5 +1,5 @@
-"""ctypes binding of the language-model operators declared in include/grim_lm.h: layer norm, the gated linear recurrence,
-distillation from a teacher's top logits, the clipped policy loss, clipping by the norm of all gradients, and the rules for the
+"""ctypes binding of the language-model operators declared in include/grim_lm.h: layer norm, the gated linear recurrence, the gated
+delta rule, distillation from a teacher's top logits, the clipped policy loss, clipping by the norm of all gradients, and the rules for the
 logits of a served step.
 
 Argument marshalling only, as in binding.py: device buffers are anything with a ``data_ptr()`` or a raw address, dtypes are
@@ -32,6 +32,10 @@ ARGTYPES = {
     "grim_glr_step": [_P, _I64, _P, _P, _I64, _P, _I64, _P, _I32, _I64, _I64, _I32, _P],
     "grim_distill_topk_workspace": [_I64, _I64],
     "grim_distill_topk": [_P, _I32, _I64, _P, _P, _I32, _I64, _F, _P, _I64, _I64, _P, _P, _I64, _P, _I64, _P],
+    "grim_gdr_states": [_I64, _I32, _I32, _I32, _I32],
+    "grim_gdr_workspace": [_I64, _I32, _I32, _I32, _I32, _I32],
+    "grim_gdr_sequence": [_P, _P, _P, _I32, _I64, _I64, _I64, _P, _P, _I64, _P, _P, _I32, _I64, _I32, _I32, _I32, _I32, _F, _F, _P, _I64, _P, _P, _P, _I64, _P],
+    "grim_gdr_step": [_P, _P, _P, _I64, _I64, _I64, _P, _P, _I64, _P, _P, _P, _I32, _I64, _I32, _I32, _I32, _I32, _F, _F, _I32, _P],
     "grim_policy_loss_workspace": [_I64, _I64],
     "grim_policy_loss": [_P, _I32, _I64, _P, _I64, _I64, _P, _P, _P, _I64, _P, _I64, _P],
     "grim_grad_list_create": [_P, _I32, _P],
@@ -169,6 +173,36 @@ def distill_topk(z, dtype, ldz: int, top_logits, top_ids, k: int, ldt: int, temp
                                   _at(weight), N, V, _at(loss), _at(dz), lddz, ws, room, _on(stream))
     if status:
         raise GrimError(status, "grim_distill_topk")
+
+
+def gdr_states(N: int, nseq: int, heads: int, Dk: int, Dv: int) -> int:
+    """grim_gdr_states: bytes that gdr_sequence leaves for its backward pass."""
+    return int(_c.grim_gdr_states(N, nseq, heads, Dk, Dv))
+
+
+def gdr_workspace(N: int, nseq: int, heads: int, key_heads: int, Dk: int, Dv: int) -> int:
+    """grim_gdr_workspace: bytes that either direction of gdr_sequence needs."""
+    return int(_c.grim_gdr_workspace(N, nseq, heads, key_heads, Dk, Dv))
+
+
+def gdr_sequence(q, k, v, dtype, ldq: int, ldk: int, ldv: int, decay, beta, ldg: int, s0, seq_start, nseq: int, N: int, heads: int, key_heads: int,
+                 Dk: int, Dv: int, scale: float, norm_eps: float, y, ldy: int, s_last, states, workspace, stream=None):
+    """grim_gdr_sequence: enqueue the gated delta rule over N packed rows of queries, keys and values.  `decay` holds logarithms.
+    `states` (a buffer of gdr_states bytes, or None) is what the backward pass reads."""
+    ws, room = _room(workspace)
+    status = _c.grim_gdr_sequence(_at(q), _at(k), _at(v), _DT_CODE[dtype], ldq, ldk, ldv, _at(decay), _at(beta), ldg, _at(s0), _at(seq_start), nseq, N,
+                                  heads, key_heads, Dk, Dv, scale, norm_eps, _at(y), ldy, _at(s_last), _at(states), ws, room, _on(stream))
+    if status:
+        raise GrimError(status, "grim_gdr_sequence")
+
+
+def gdr_step(q, k, v, ldq: int, ldk: int, ldv: int, decay, beta, ldg: int, s, s_new, y, dtype, ldy: int, heads: int, key_heads: int,
+             Dk: int, Dv: int, scale: float, norm_eps: float, batch: int, stream=None):
+    """grim_gdr_step: one token of the gated delta rule for `batch` callers; operands in columns, states batch x heads x Dk x Dv."""
+    status = _c.grim_gdr_step(_at(q), _at(k), _at(v), ldq, ldk, ldv, _at(decay), _at(beta), ldg, _at(s), _at(s_new), _at(y), _DT_CODE[dtype], ldy,
+                              heads, key_heads, Dk, Dv, scale, norm_eps, batch, _on(stream))
+    if status:
+        raise GrimError(status, "grim_gdr_step")
 
 
 def policy_loss_workspace(N: int, V: int) -> int:
