@@ -17,29 +17,31 @@ namespace lm {
 
 // M of every chunk and head, and G: a workgroup each.  L by the matrix cores, M by forward substitution: blocks of 16 x 16, those on the diagonal a column a lane, then
 // block by block away from it, M_IJ = Z - M_II beta Z with Z = L_IJ - sum over J <= K < I of L_IK beta M_KJ, in fp32 on the matrix cores.
-template <typename T, int DK>
-__global__ void __launch_bounds__(kGdrThreads) chunk_matrices(GdrParams p) {
+template <typename T, int DK, bool WHOLE>
+__global__ void __launch_bounds__(kMatrixThreads) chunk_matrices(GdrParams p) {
     constexpr int C = Gdr<T>::chunk, PD = Gdr<T>::data, PC = Gdr<T>::comp, TT = C / 32, B = C / 16, LD = C + 4;
-    using Keys = Tile<PD, C, DK>;
+    using Keys = Tile<PD, C, DK, true>;
     constexpr int square = C * LD * 4;
     __shared__ __attribute__((aligned(16))) char lds[square + (Keys::bytes > square ? Keys::bytes : square)];
     __shared__ double G[C];
-    __shared__ float beta[C], rk[C];
+    __shared__ float tokens[3 * C];                          // beta, what keys and queries count with
+    float *beta = tokens, *rk = tokens + C, *rq = tokens + 2 * C;
     float *L = reinterpret_cast<float *>(lds), *M = reinterpret_cast<float *>(lds + square);        // (M after the keys are done with)
     const Keys keys{reinterpret_cast<uint16_t *>(lds + square)};
-    const int64_t place = blockIdx.x / p.heads;
-    const int h = (int)(blockIdx.x % p.heads);
-    const int s = sequence_of<C>(p.seq_start, p.nseq, p.N, place);
+    const uint32_t place = blockIdx.x / (uint32_t)p.heads;
+    const int h = (int)(blockIdx.x % (uint32_t)p.heads);
+    const int s = sequence_of(p.seq_start, p.nseq, p.N, C, place);
     const Span span(p.seq_start, s, p.N);
-    const int64_t first = span.first + (place - (span.first / C + s)) * C;
+    const int64_t first = span.first + (int64_t)(place - place_of(span, s, C)) * C;
+    if (first >= span.end) return;
     const int rows = (int)min((int64_t)C, span.end - first);
-    if (rows <= 0) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l15 = lane & 15, lq = lane >> 4;
-    Rows<T, C, DK> k;
+    Rows<WHOLE, T, kMatrixThreads, C, DK> k, q;
+    q.fetch(static_cast<const T *>(p.q) + first * p.ldq + (int64_t)(h / p.group) * p.dk, p.ldq, rows, p.dk);
     k.fetch(static_cast<const T *>(p.k) + first * p.ldk + (int64_t)(h / p.group) * p.dk, p.ldk, rows, p.dk);
     if (wave == 0) {
         const float g = lane < rows ? p.decay[(first + lane) * p.ldg + h] : 0.f;
-        double sum = g < kLeastDecay ? kLeastDecay : (double)g;
+        double sum = (g < kLeastDecay ? kLeastDecay : (double)g) * 1.44269504088896340736;
 #pragma unroll
         for (int n = 1; n < C; n *= 2) {
             const double before = __shfl_up(sum, n, 64);
@@ -47,7 +49,9 @@ __global__ void __launch_bounds__(kGdrThreads) chunk_matrices(GdrParams p) {
         }
         if (lane < C) G[lane] = sum, beta[lane] = lane < rows ? p.beta[(first + lane) * p.ldg + h] : 0.f;
     }
-    k.place(keys, rk, p.norm_eps, 1.f);
+    k.place(keys, rows, p.dk);
+    k.lengths(rows, p.dk, rk, p.norm_eps, 1.f);
+    q.lengths(rows, p.dk, rq, p.norm_eps, p.scale);
     __syncthreads();
     {
         const int j0 = (wave >> 1) * (C / 2), i0 = (wave & 1) * (C / 2);
@@ -67,10 +71,10 @@ __global__ void __launch_bounds__(kGdrThreads) chunk_matrices(GdrParams p) {
 #pragma unroll
             for (int y = 0; y < TT; ++y) {
                 const int j = j0 + 16 * x + lq * 4, i = i0 + 16 * y + l15;
-                f32x4 v = {};
+                f32x4 v;
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    if (i > j + e) v[e] = expf((float)(G[i] - G[j + e])) * rk[i] * rk[j + e] * acc[x][y][e];
+                    v[e] = i > j + e ? decay_of(G[i] - G[j + e]) * rk[i] * rk[j + e] * acc[x][y][e] : 0.f;
                 *reinterpret_cast<f32x4 *>(L + i * LD + j) = v;
             }
     }
@@ -121,11 +125,20 @@ __global__ void __launch_bounds__(kGdrThreads) chunk_matrices(GdrParams p) {
     }
     const Saved<T> saved(p, place, h);
     if (threadIdx.x < C) saved.G()[threadIdx.x] = G[threadIdx.x];
-    for (int q = threadIdx.x; q < C * C / 8; q += kGdrThreads) {
-        const int i = q / (C / 8), c = q % (C / 8) * 8;
+    if (threadIdx.x < C) {
+        const int i = threadIdx.x;
+        float *to = saved.tokens() + i;
+        const float since = decay_of(G[i]);
+        to[0] = beta[i], to[C] = since * rk[i], to[2 * C] = decay_of(G[C - 1] - G[i]) * rk[i], to[3 * C] = since * rq[i], to[4 * C] = rk[i], to[5 * C] = rq[i];
+    }
+    for (int q = threadIdx.x; q < C * C / 8; q += kMatrixThreads) {
+        const int i = q / (C / 8), c = q % (C / 8) / 4 * 32 + q % 4 * 4;
         float v[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = c / 16 > i / 16 ? 0.f : M[i * LD + c + j];
+        for (int j = 0; j < 8; ++j) {
+            const int at = c + j % 4 + j / 4 * 16;
+            v[j] = at / 16 > i / 16 ? 0.f : M[i * LD + at];
+        }
 #pragma unroll
         for (int t = 0; t < PC; ++t) {
             bf16 part[8];
@@ -137,273 +150,334 @@ __global__ void __launch_bounds__(kGdrThreads) chunk_matrices(GdrParams p) {
 }
 
 // ---------------------------------------------------------------------------------------------------- from chunk to chunk
+// Values in LDS as they come; what a lane of a 16 x 16 result takes of them.
+template <typename T, int ROWS, int COLS>
+struct Values {
+    static constexpr int ld = sizeof(T) == 4 ? COLS + 4 : COLS == 128 ? 144 : COLS + 8, bytes = ROWS * ld * (int)sizeof(T);
+    T *at;
+    __device__ __forceinline__ f32x4 get(int r, int c) const {
+        f32x4 v;
+        if constexpr (sizeof(T) == 4) {
+            const int lane = threadIdx.x & 63;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = at[(r + (lane >> 4) * 4 + e) * ld + c + (lane & 15)];
+        } else {
+            const s16x4 w = turned(reinterpret_cast<const uint16_t *>(at), ld, r, c);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = (float)__builtin_bit_cast(T, (uint16_t)w[e]);
+        }
+        return v;
+    }
+};
+
 // What a workgroup of the walk keeps in LDS.
-template <typename T, int DK>
+template <typename T, int DK, int COLS>
 struct WalkRoom {
     static constexpr int C = Gdr<T>::chunk, PD = Gdr<T>::data, PC = Gdr<T>::comp;
     using Keys = Tile<PD, C, DK>;
-    using States = Tile<PC, DK, kGdrColumns>;
-    using Square = Tile<PC, C, C>;
-    using Columns = Tile<PC, C, kGdrColumns>;
-    static constexpr int keys = 0, queries = keys + Keys::bytes, states = queries + Keys::bytes, square = states + States::bytes,
-                         x = square + Square::bytes, u = x + Columns::bytes, G = u + Columns::bytes, beta = G + C * 8, rk = beta + C * 4, rq = rk + C * 4,
-                         bytes = rq + C * 4;
+    using Queries = Tile<PD, C, DK, true>;
+    using Square = Tile<PC, C, C, true>;
+    using Vals = Values<T, C, COLS>;
+    static constexpr int keys = 0, queries = keys + Keys::bytes, values = queries + Queries::bytes, M = values + Vals::bytes, P = M + Square::bytes, G = P + Square::bytes,
+                         tokens = G + C * 8, bytes = tokens + C * 24;
     static_assert(bytes <= 160 * 1024, "LDS");
 };
 
-// Four elements of a head's row of values from column c; zeros behind its width.
-template <typename T>
-__device__ __forceinline__ Pack<T, 4> fetch4(const T *row, int c, int width) {
-    if (c + 4 <= width) return load<4>(row + c);
-    Pack<T, 4> r;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) put(r, j, c + j < width ? row[c + j] : (T)0.f);
-    return r;
-}
-
-template <typename T>
-__device__ __forceinline__ void store4(T *row, int c, int width, f32x4 v) {
-    if (c + 4 <= width) {
-        const float t[4] = {v[0], v[1], v[2], v[3]};
-        store(row + c, t);
-    } else
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (c + j < width) row[c + j] = (T)v[j];
-}
-
-// A workgroup takes 64 columns of the states of a sequence's head.  Its four waves have a half of the columns and a half of the tokens (of the rows of the states) each.
-// Columns of the states are rows of the results of the products: lanes then have four columns of a token, which lie together in memory and in LDS.
-template <typename T, int DK>
-__global__ void __launch_bounds__(kGdrThreads) walk(GdrParams p) {
-    constexpr int C = Gdr<T>::chunk, PD = Gdr<T>::data, PC = Gdr<T>::comp, TT = C / 32, TD = DK / 32;
-    using Room = WalkRoom<T, DK>;
+// A workgroup takes 16 CT W columns of the states of a run of chunks of a sequence's head.  All that a chunk does to a column of the states stays in that column, so each of its W waves
+// has 16 CT columns to itself from chunk to chunk, in registers: results that are sums over tokens or keys are the next product's operands.  The waves meet only where keys, queries,
+// values and M are placed in LDS and where the products of queries and keys, which all need, are formed.
+// MAPS: no outputs; what every run but a sequence's last does to the states, as S -> A S + B: B's columns (into the places of the states in front of the next run; of a sequence's
+// first run, whose start is known, these are the states themselves) come from a start of zeros, A's from the columns of 1 and values of zero.
+template <typename T, int DK, int W, int CT, bool WHOLE, bool MAPS>
+__global__ void __launch_bounds__(64 * W, 2) walk(GdrParams p) {
+    constexpr int C = Gdr<T>::chunk, PD = Gdr<T>::data, PC = Gdr<T>::comp, THREADS = 64 * W, COLS = 16 * CT * W;
+    constexpr int TT = C / 16, SS = C / 32, DT = DK / 16, DS = DK / 32;     // tiles of tokens, sums over them; of the states' rows
+    using Room = WalkRoom<T, DK, COLS>;
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    const auto tile = [&](int at) { return reinterpret_cast<uint16_t *>(lds + at); };
-    const typename Room::Keys K{tile(Room::keys)}, Q{tile(Room::queries)};
-    const typename Room::States S{tile(Room::states)};
-    const typename Room::Square M{tile(Room::square)};      // then the products of queries and keys
-    const typename Room::Columns X{tile(Room::x)}, U{tile(Room::u)};
+    const typename Room::Keys K{reinterpret_cast<uint16_t *>(lds + Room::keys)};
+    const typename Room::Queries Q{reinterpret_cast<uint16_t *>(lds + Room::queries)};
+    const typename Room::Square M{reinterpret_cast<uint16_t *>(lds + Room::M)}, P{reinterpret_cast<uint16_t *>(lds + Room::P)};
+    const typename Room::Vals V{reinterpret_cast<T *>(lds + Room::values)};
     double *G = reinterpret_cast<double *>(lds + Room::G);
-    float *beta = reinterpret_cast<float *>(lds + Room::beta), *rk = reinterpret_cast<float *>(lds + Room::rk), *rq = reinterpret_cast<float *>(lds + Room::rq);
+    float *tokens = reinterpret_cast<float *>(lds + Room::tokens);
+    const float *beta = tokens, *fk = tokens + C, *fu = tokens + 2 * C, *fq = tokens + 3 * C, *rk = tokens + 4 * C, *rq = tokens + 5 * C;
 
-    int64_t b = blockIdx.x;
-    const int block = (int)(b % p.blocks);
-    b /= p.blocks;
-    const int h = (int)(b % p.heads), s = (int)(b / p.heads);
+    // (the workgroups of a run, whose heads read the same rows, lie together)
+    const uint32_t value_blocks = (p.tiles + CT * W - 1) / (CT * W), blocks = value_blocks + (MAPS ? (DT + CT * W - 1) / (CT * W) : 0), heads = (uint32_t)p.heads;
+    const int block = (int)(blockIdx.x % blocks), h = (int)(blockIdx.x / blocks % heads);
+    const uint32_t run = blockIdx.x / blocks / heads;
+    const int s = sequence_of(p.seq_start, p.nseq, p.N, p.size, run);
     const Span span(p.seq_start, s, p.N);
-    const int64_t place = span.first / C + s;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l15 = lane & 15, lq = lane >> 4;
-    const int v0 = (wave >> 1) * 32, t0 = (wave & 1) * (C / 2), d0 = (wave & 1) * (DK / 2), j0 = (wave >> 1) * (C / 2);
-    const int col = block * kGdrColumns + v0 + lq * 4;      // of the lane's first value
+    const uint32_t r = run - place_of(span, s, p.size);     // of the sequence's runs
+    const int64_t from = span.first + (int64_t)r * p.size, to = min(span.end, from + p.size);
+    if (MAPS ? to >= span.end : from >= to && r > 0) return;            // (an empty sequence has its first run for its last states)
+    const bool map = MAPS && block >= (int)value_blocks;
+    if (map && r == 0) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l15 = lane & 15, g4 = (lane >> 4) * 4;
+    const int tile0 = ((map ? block - (int)value_blocks : block) * W + wave) * CT, tiles = map ? DT : p.tiles, col0 = map ? 0 : block * COLS;
+    const bool idle = tile0 >= tiles;
     const T *q = static_cast<const T *>(p.q) + (int64_t)(h / p.group) * p.dk, *k = static_cast<const T *>(p.k) + (int64_t)(h / p.group) * p.dk;
-    const T *v = static_cast<const T *>(p.v) + (int64_t)h * p.dv;
+    const T *v = static_cast<const T *>(p.v) + (int64_t)h * p.dv + col0;
     T *y = static_cast<T *>(p.y) + (int64_t)h * p.dv;
 
-    f32x4 state[2][TD];
+    f32x4 state[DT][CT];                                    // rows 16 n + g4 .. + 3, column 16 (tile0 + c) + l15
     const int64_t head = ((int64_t)s * p.heads + h) * p.dk;
 #pragma unroll
-    for (int x = 0; x < 2; ++x)
+    for (int n = 0; n < DT; ++n)
 #pragma unroll
-        for (int n = 0; n < TD; ++n) {
-            const int d = d0 + 16 * n + l15;
-            state[x][n] = f32x4{};
-            if (p.s0 && d < p.dk) {
-                float t[4];
-                unpack(fetch4(p.s0 + (head + d) * p.dv, col + 16 * x, p.dv), t);
+        for (int c = 0; c < CT; ++c) {
+            const int d = 16 * n + g4, col = 16 * (tile0 + c) + l15;
+            state[n][c] = f32x4{};
+            if (MAPS && r > 0) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) state[x][n][e] = t[e];
+                for (int e = 0; e < 4; ++e) state[n][c][e] = map && d + e == col ? 1.f : 0.f;
+            } else if (r > 0) {
+                if (tile0 + c < p.tiles) state[n][c] = *reinterpret_cast<const f32x4 *>(p.starts + ((((int64_t)run * p.heads + h) * p.tiles + tile0 + c) * DT + n) * 256 + lane * 4);
+            } else if (p.s0) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) state[n][c][e] = p.s0[(head + min(d + e, p.dk - 1)) * p.dv + min(col, p.dv - 1)];
             }
-            put4(S, d, v0 + 16 * x + lq * 4, state[x][n]);
         }
+#pragma unroll
+    for (int n = 0; n < DT; ++n)
+#pragma unroll
+        for (int c = 0; c < CT; ++c)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                asm volatile("" : "+v"(state[n][c][e]));    // (all are asked for before any is looked at)
+                if (16 * n + g4 + e >= p.dk || 16 * (tile0 + c) + l15 >= (map ? p.dk : p.dv)) state[n][c][e] = 0.f;
+            }
 
     // what the next chunk brings
-    Rows<T, C, DK> kn, qn;
-    Pack<T, 4> vn[2][TT];
-    constexpr int pieces = PC * C * C / 8, MP = (pieces + kGdrThreads - 1) / kGdrThreads;
-    uint4 mn[MP];
+    Rows<WHOLE, T, THREADS, C, DK> kn, qn;
+    Rows<WHOLE, T, THREADS, C, COLS> vn;
+    constexpr int pieces = PC * C * C / 8, MP = (pieces + THREADS - 1) / THREADS, TP = (6 * C + THREADS - 1) / THREADS;
+    u32x4 mn[MP];
     double Gn = 0.;
-    float bn = 0.f;
+    float tn[TP];
+    const int64_t place = place_of(span, s, C) + r * (p.size / C);
     const auto fetch = [&](int64_t n, int64_t first) {
-        const int rows = (int)min((int64_t)C, span.end - first);
+        const int rows = (int)min((int64_t)C, to - first);
         kn.fetch(k + first * p.ldk, p.ldk, rows, p.dk);
-        qn.fetch(q + first * p.ldq, p.ldq, rows, p.dk);
+        if (!MAPS) qn.fetch(q + first * p.ldq, p.ldq, rows, p.dk);
+        vn.fetch(v + first * p.ldv, p.ldv, rows, p.dv - col0);
         const Saved<T> saved(p, place + n, h);
 #pragma unroll
-        for (int i = 0; i < MP; ++i) {
-            const int piece = i * kGdrThreads + (int)threadIdx.x;
-            if (piece < pieces) mn[i] = reinterpret_cast<const uint4 *>(saved.M())[piece];
-        }
-        if (threadIdx.x < C) {
-            Gn = saved.G()[threadIdx.x];
-            bn = (int)threadIdx.x < rows ? p.beta[(first + threadIdx.x) * p.ldg + h] : 0.f;
-        }
+        for (int i = 0; i < MP; ++i) mn[i] = reinterpret_cast<const u32x4 *>(saved.M())[min(i * THREADS + (int)threadIdx.x, pieces - 1)];
+        Gn = saved.G()[threadIdx.x % C];
 #pragma unroll
-        for (int x = 0; x < 2; ++x)
-#pragma unroll
-            for (int t = 0; t < TT; ++t) {
-                const int token = t0 + 16 * t + l15;
-                if (token < rows) vn[x][t] = fetch4(v + (first + token) * p.ldv, col + 16 * x, p.dv);
-                else
-#pragma unroll
-                    for (int i = 0; i < vn[x][t].W; ++i) vn[x][t].w[i] = 0;
-            }
+        for (int i = 0; i < TP; ++i) tn[i] = saved.tokens()[min(i * THREADS + (int)threadIdx.x, 6 * C - 1)];
     };
-    if (span.first < span.end) fetch(0, span.first);
-    for (int64_t n = 0, first = span.first; first < span.end; ++n, first += C) {
-        const int rows = (int)min((int64_t)C, span.end - first);
-        kn.place(K, rk, p.norm_eps, 1.f);
-        qn.place(Q, rq, p.norm_eps, p.scale);
+    if (from < to) fetch(0, from);
+    for (int64_t n = 0, first = from; first < to; ++n, first += C) {
+        const int rows = (int)min((int64_t)C, to - first);
+        kn.place(K, rows, p.dk);
+        if (!MAPS) qn.place(Q, rows, p.dk);
+        vn.keep(V.at, V.ld, map ? 0 : rows, p.dv - col0);
 #pragma unroll
         for (int i = 0; i < MP; ++i) {
-            const int piece = i * kGdrThreads + (int)threadIdx.x, e = piece % (C * C / 8) * 8;
-            if (piece < pieces) *reinterpret_cast<uint4 *>(M.at + piece / (C * C / 8) * M.part + e / C * M.ld + e % C) = mn[i];
+            const int piece = i * THREADS + (int)threadIdx.x, e = piece % (C * C / 8) * 8;
+            if (piece < pieces) *reinterpret_cast<u32x4 *>(M.at + piece / (C * C / 8) * M.part + e / C * M.ld + e % C) = mn[i];
         }
-        if (threadIdx.x < C) G[threadIdx.x] = Gn, beta[threadIdx.x] = bn;
-        f32x4 value[2][TT];
+        if (threadIdx.x < C) G[threadIdx.x] = Gn;
 #pragma unroll
-        for (int x = 0; x < 2; ++x)
-#pragma unroll
-            for (int t = 0; t < TT; ++t) {
-                float u[4];
-                unpack(vn[x][t], u);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) value[x][t][e] = u[e];
-            }
-        if (first + C < span.end) fetch(n + 1, first + C);
-        if (p.states) {
-            float *to = p.states + (((place + n) * p.heads + h) * p.blocks + block) * (DK * kGdrColumns);
-#pragma unroll
-            for (int x = 0; x < 2; ++x)
-#pragma unroll
-                for (int m = 0; m < TD; ++m) *reinterpret_cast<f32x4 *>(to + (d0 + 16 * m + l15) * kGdrColumns + v0 + 16 * x + lq * 4) = state[x][m];
-        }
+        for (int i = 0; i < TP; ++i)
+            if (i * THREADS + (int)threadIdx.x < 6 * C) tokens[i * THREADS + threadIdx.x] = tn[i];
+        if (first + C < to) fetch(n + 1, first + C);
         __syncthreads();
-        f32x4 ks[2][TT] = {}, out[2][TT] = {}, pr[TT][TT] = {};
+        // the products of queries and keys: a wave has the queries of a tile and the keys up to them (of W waves W / TT share them)
+        if (!MAPS) {
+            constexpr int EACH = W >= TT ? W / TT : 1;
 #pragma unroll
-        for (int d = 0; d < DK; d += 32) {
-            Frag<PC> a[2];
-            Frag<PD> bk[TT], bq[TT], aj[TT];
+            for (int t0 = 0; t0 < TT; t0 += W) {
+                const int t = t0 + (EACH > 1 ? wave / EACH : wave);
+                if (t < TT) {
+                    Frag<PD> a[DS];
 #pragma unroll
-            for (int x = 0; x < 2; ++x) a[x] = across(S, v0 + 16 * x, d);
+                    for (int d = 0; d < DS; ++d) a[d] = along(Q, 16 * t, 32 * d);
+                    const int i = 16 * t + l15;
+                    const double Gi = G[i];
+                    const float qi = rq[i];
+                    for (int x = EACH > 1 ? wave % EACH : 0; x < TT; x += EACH) {
+                        if (x / 2 > t / 2) break;           // (nobody reads those)
+                        f32x4 acc = {};
 #pragma unroll
-            for (int t = 0; t < TT; ++t) {
-                bk[t] = along(K, t0 + 16 * t, d), bq[t] = along(Q, t0 + 16 * t, d);
-                if (j0 <= t0) aj[t] = along(K, j0 + 16 * t, d);
-            }
+                        for (int d = 0; d < DS; ++d) acc = multiply(along(K, 16 * x, 32 * d), a[d], acc);
+                        const int j = 16 * x + g4;
 #pragma unroll
-            for (int x = 0; x < 2; ++x)
-#pragma unroll
-                for (int t = 0; t < TT; ++t) ks[x][t] = multiply(a[x], bk[t], ks[x][t]), out[x][t] = multiply(a[x], bq[t], out[x][t]);
-            if (j0 <= t0)
-#pragma unroll
-                for (int x = 0; x < TT; ++x)
-#pragma unroll
-                    for (int t = 0; t < TT; ++t) pr[x][t] = multiply(aj[x], bq[t], pr[x][t]);
-        }
-        float bt[TT], until[TT];
-#pragma unroll
-        for (int t = 0; t < TT; ++t) {
-            const int i = t0 + 16 * t + l15;
-            const float since = expf((float)G[i]);
-            bt[t] = beta[i];
-            until[t] = expf((float)(G[C - 1] - G[i])) * rk[i];
-            const float fk = since * rk[i], fq = since * rq[i];
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) value[x][t][e] -= fk * ks[x][t][e], out[x][t][e] *= fq;
-                put4(X, i, v0 + 16 * x + lq * 4, value[x][t] * bt[t]);
+                        for (int e = 0; e < 4; ++e) acc[e] = i >= j + e ? decay_of(Gi - G[j + e]) * (qi * rk[j + e]) * acc[e] : 0.f;
+                        put4(P, i, j, acc);
+                    }
+                }
             }
         }
-        __syncthreads();
-        f32x4 less[2][TT] = {};
+        f32x4 x[TT][CT] = {}, out[TT][CT] = {};             // tokens x columns, columns x tokens
+        Frag<PC> u[SS][CT];
+        if (!idle) {
+        {
+            Frag<PC> S[DS][CT];
 #pragma unroll
-        for (int j = 0; j < C; j += 32) {
-            if (j >= t0 + C / 2) continue;                  // M is lower
-            Frag<PC> a[2], m[TT];
+            for (int d = 0; d < DS; ++d)
 #pragma unroll
-            for (int x = 0; x < 2; ++x) a[x] = across(X, v0 + 16 * x, j);
+                for (int c = 0; c < CT; ++c) S[d][c] = operand<PC>(state[2 * d][c], state[2 * d + 1][c]);
+            if (!MAPS && p.states)
 #pragma unroll
-            for (int t = 0; t < TT; ++t) m[t] = along(M, t0 + 16 * t, j);
+                for (int d = 0; d < DT; ++d)
 #pragma unroll
-            for (int x = 0; x < 2; ++x)
+                    for (int c = 0; c < CT; ++c)
+                        if (tile0 + c < p.tiles)
+                            *reinterpret_cast<f32x4 *>(p.states + ((((place + n) * p.heads + h) * p.tiles + tile0 + c) * DT + d) * 256 + lane * 4) = state[d][c];
 #pragma unroll
-                for (int t = 0; t < TT; ++t) less[x][t] = multiply(a[x], m[t], less[x][t]);
-        }
-        __syncthreads();
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-#pragma unroll
-            for (int t = 0; t < TT; ++t) {
-                const int i = t0 + 16 * t + l15;
-                const f32x4 u = (value[x][t] - less[x][t]) * bt[t];
-                put4(X, i, v0 + 16 * x + lq * 4, u);
-                put4(U, i, v0 + 16 * x + lq * 4, u * until[t]);
-            }
-        if (j0 <= t0)
-#pragma unroll
-            for (int x = 0; x < TT; ++x)
+            for (int d = 0; d < DS; ++d)
 #pragma unroll
                 for (int t = 0; t < TT; ++t) {
-                    const int j = j0 + 16 * x + lq * 4, i = t0 + 16 * t + l15;
-                    f32x4 w = {};
+                    const Frag<PD> a = along(K, 16 * t, 32 * d);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (i >= j + e) w[e] = expf((float)(G[i] - G[j + e])) * rq[i] * rk[j + e] * pr[x][t][e];
-                    put4(M, i, j, w);
+                    for (int c = 0; c < CT; ++c) x[t][c] = multiply(a, S[d][c], x[t][c]);
+                    if (MAPS) continue;
+                    const Frag<PD> e = along(Q, 16 * t, 32 * d);
+#pragma unroll
+                    for (int c = 0; c < CT; ++c) out[t][c] = multiply(S[d][c], e, out[t][c]);
                 }
-        const float whole = expf((float)G[C - 1]);
-        __syncthreads();
-#pragma unroll
-        for (int j = 0; j < C; j += 32) {
-            if (j >= t0 + C / 2) continue;
-            Frag<PC> a[2], m[TT];
-#pragma unroll
-            for (int x = 0; x < 2; ++x) a[x] = across(X, v0 + 16 * x, j);
-#pragma unroll
-            for (int t = 0; t < TT; ++t) m[t] = along(M, t0 + 16 * t, j);
-#pragma unroll
-            for (int x = 0; x < 2; ++x)
-#pragma unroll
-                for (int t = 0; t < TT; ++t) out[x][t] = multiply(a[x], m[t], out[x][t]);
         }
 #pragma unroll
-        for (int x = 0; x < 2; ++x)
+        for (int t = 0; t < TT; ++t) {
+            const f32x4 f = *reinterpret_cast<const f32x4 *>(fk + 16 * t + g4);
+            const float fo = fq[16 * t + l15];
 #pragma unroll
-            for (int m = 0; m < TD; ++m) state[x][m] *= whole;
+            for (int c = 0; c < CT; ++c) x[t][c] = V.get(16 * t, 16 * (wave * CT + c)) - f * x[t][c], out[t][c] *= fo;
+        }
+        const auto by = [&](const float *factor, f32x4 (&a)[TT][CT]) {
 #pragma unroll
-        for (int j = 0; j < C; j += 32) {
-            Frag<PC> a[2];
+            for (int t = 0; t < SS; ++t) {
+                const f32x4 lo = *reinterpret_cast<const f32x4 *>(factor + 32 * t + g4), hi = *reinterpret_cast<const f32x4 *>(factor + 32 * t + 16 + g4);
 #pragma unroll
-            for (int x = 0; x < 2; ++x) a[x] = across(U, v0 + 16 * x, j);
+                for (int c = 0; c < CT; ++c) u[t][c] = operand<PC>(a[2 * t][c] * lo, a[2 * t + 1][c] * hi);
+            }
+        };
+        by(beta, x);
+        f32x4 less[TT][CT] = {};
 #pragma unroll
-            for (int m = 0; m < TD; ++m) {
-                const Frag<PD> f = across(K, d0 + 16 * m, j);
+        for (int t = 0; t < TT; ++t)
 #pragma unroll
-                for (int x = 0; x < 2; ++x) state[x][m] = multiply(a[x], f, state[x][m]);
+            for (int j = 0; j <= t / 2; ++j) {
+                const Frag<PC> m = along(M, 16 * t, 32 * j);
+#pragma unroll
+                for (int c = 0; c < CT; ++c) less[t][c] = multiply(m, u[j][c], less[t][c]);
+            }
+#pragma unroll
+        for (int t = 0; t < TT; ++t) {
+            const f32x4 bt = *reinterpret_cast<const f32x4 *>(beta + 16 * t + g4);
+#pragma unroll
+            for (int c = 0; c < CT; ++c) x[t][c] = (x[t][c] - less[t][c]) * bt;          // U
+        }
+        by(fu, x);
+        const float whole = decay_of(G[C - 1]);
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+#pragma unroll
+            for (int c = 0; c < CT; ++c) state[d][c] *= whole;
+#pragma unroll
+            for (int j = 0; j < SS; ++j) {
+                const Frag<PD> a = across(K, 16 * d, 32 * j);
+#pragma unroll
+                for (int c = 0; c < CT; ++c) state[d][c] = multiply(a, u[j][c], state[d][c]);
             }
         }
+        if (!MAPS)
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
+            for (int t = 0; t < SS; ++t)
 #pragma unroll
-            for (int t = 0; t < TT; ++t) {
-                const int i = t0 + 16 * t + l15;
-                if (i < rows) store4(y + (first + i) * p.ldy, col + 16 * x, p.dv, out[x][t]);
+                for (int c = 0; c < CT; ++c) u[t][c] = operand<PC>(x[2 * t][c], x[2 * t + 1][c]);
+        }
+        __syncthreads();                                    // (the products of queries and keys are there)
+        if (MAPS || idle) {
+            if (!MAPS) __syncthreads();
+            continue;
+        }
+#pragma unroll
+        for (int t = 0; t < TT; ++t) {
+#pragma unroll
+            for (int j = 0; j <= t / 2; ++j) {
+                const Frag<PC> m = along(P, 16 * t, 32 * j);
+#pragma unroll
+                for (int c = 0; c < CT; ++c) out[t][c] = multiply(u[j][c], m, out[t][c]);
             }
+            const int i = 16 * t + l15;
 #pragma unroll
-            for (int m = 0; m < TD; ++m) put4(S, d0 + 16 * m + l15, v0 + 16 * x + lq * 4, state[x][m]);
+            for (int c = 0; c < CT; ++c)
+                if (i < rows && tile0 + c < p.tiles) leave<WHOLE>(y + (first + i) * p.ldy, 16 * (tile0 + c) + g4, p.dv, out[t][c]);
         }
         __syncthreads();
     }
-    if (!p.s_last) return;
+    if (idle) return;
+    if (MAPS) {
 #pragma unroll
-    for (int x = 0; x < 2; ++x)
+        for (int n = 0; n < DT; ++n)
 #pragma unroll
-        for (int n = 0; n < TD; ++n) {
-            const int d = d0 + 16 * n + l15;
-            if (d < p.dk) store4(p.s_last + (head + d) * p.dv, col + 16 * x, p.dv, state[x][n]);
+            for (int c = 0; c < CT; ++c) {
+                if (tile0 + c >= tiles) continue;
+                if (!map) *reinterpret_cast<f32x4 *>(p.starts + ((((int64_t)(run + 1) * p.heads + h) * p.tiles + tile0 + c) * DT + n) * 256 + lane * 4) = state[n][c];
+                else
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) p.maps[(((int64_t)run * p.heads + h) * DK + 16 * n + g4 + e) * DK + 16 * (tile0 + c) + l15] = state[n][c][e];
+            }
+        return;
+    }
+    if (!p.s_last || to < span.end) return;
+#pragma unroll
+    for (int n = 0; n < DT; ++n)
+#pragma unroll
+        for (int c = 0; c < CT; ++c) {
+            const int d = 16 * n + g4, col = 16 * (tile0 + c) + l15;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (d + e < p.dk && col < p.dv) p.s_last[(head + d + e) * p.dv + col] = state[n][c][e];
         }
+}
+
+// The states in front of every run of a sequence's head, from one to the next: S_(r + 1) = A_r S_r + B_r.  A wave has 16 columns, in registers as above; A comes through LDS.
+template <typename T, int DK>
+__global__ void __launch_bounds__(256) join_runs(GdrParams p) {
+    constexpr int PC = Gdr<T>::comp, DT = DK / 16, DS = DK / 32;
+    using Map = Tile<PC, DK, DK, true>;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const Map A{reinterpret_cast<uint16_t *>(lds)};
+    const uint32_t blocks = (p.tiles + 3) / 4, heads = (uint32_t)p.heads;
+    const int block = (int)(blockIdx.x % blocks), h = (int)(blockIdx.x / blocks % heads), s = (int)(blockIdx.x / blocks / heads);
+    const Span span(p.seq_start, s, p.N);
+    const uint32_t run0 = place_of(span, s, p.size);
+    const int runs = (int)((span.end - span.first + p.size - 1) / p.size);
+    if (runs < 3) return;                                   // (the second run's start is there already)
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tile = block * 4 + wave;
+    const bool idle = tile >= p.tiles;
+    const auto start = [&](int r) { return p.starts + (((int64_t)(run0 + r) * p.heads + h) * p.tiles + (idle ? 0 : tile)) * DT * 256 + lane * 4; };
+    f32x4 state[DT];
+#pragma unroll
+    for (int n = 0; n < DT; ++n) state[n] = *reinterpret_cast<const f32x4 *>(start(1) + n * 256);
+    Rows<true, float, 256, DK, DK> next;
+    next.fetch(p.maps + ((int64_t)(run0 + 1) * p.heads + h) * DK * DK, DK, DK, DK);
+    for (int r = 1; r + 1 < runs; ++r) {
+        next.place(A, DK, DK);
+        if (r + 2 < runs) next.fetch(p.maps + ((int64_t)(run0 + r + 1) * p.heads + h) * DK * DK, DK, DK, DK);
+        f32x4 sum[DT];
+#pragma unroll
+        for (int n = 0; n < DT; ++n) sum[n] = *reinterpret_cast<const f32x4 *>(start(r + 1) + n * 256);
+        __syncthreads();
+        if (!idle) {
+            Frag<PC> S[DS];
+#pragma unroll
+            for (int d = 0; d < DS; ++d) S[d] = operand<PC>(state[2 * d], state[2 * d + 1]);
+#pragma unroll
+            for (int n = 0; n < DT; ++n) {
+#pragma unroll
+                for (int d = 0; d < DS; ++d) sum[n] = multiply(along(A, 16 * n, 32 * d), S[d], sum[n]);
+                state[n] = sum[n];
+                *reinterpret_cast<f32x4 *>(start(r + 1) + n * 256) = sum[n];
+            }
+        }
+        __syncthreads();
+    }
 }
 
 // ---------------------------------------------------------------------------------------------------- launches
@@ -411,42 +485,88 @@ template <typename T>
 int64_t places_of(int64_t N, int32_t nseq) { return N / Gdr<T>::chunk + nseq; }
 
 inline int padded(int dk) { return dk <= 64 ? 64 : 128; }
-inline int blocks_of(int dv) { return (dv + kGdrColumns - 1) / kGdrColumns; }
+inline int tiles_of(int dv) { return (dv + 15) / 16; }
 
 // Bytes of what is kept of the chunks: their matrices, and the states in front of them.
 template <typename T>
 int64_t saved_bytes(int64_t N, int32_t nseq, int32_t heads) { return (places_of<T>(N, nseq) * heads * Saved<T>::bytes + 15) / 16 * 16; }
 template <typename T>
 int64_t states_bytes(int64_t N, int32_t nseq, int32_t heads, int32_t dk, int32_t dv) {
-    return places_of<T>(N, nseq) * heads * blocks_of(dv) * padded(dk) * kGdrColumns * 4;
+    return places_of<T>(N, nseq) * heads * tiles_of(dv) * padded(dk) * 16 * 4;
 }
 
 inline bool gdr_shape(int64_t N, int32_t nseq, int32_t heads, int32_t key_heads, int32_t dk, int32_t dv) {
     return N >= 0 && N <= (int64_t)1 << 30 && nseq >= 1 && heads >= 1 && heads <= kMostHeads && key_heads >= 1 && heads % key_heads == 0 && dk >= 1 && dv >= 1;
 }
 
-template <typename T, int DK>
-grim_status gdr_launch(const GdrParams &p, hipStream_t stream) {
-    const int64_t places = places_of<T>(p.N, p.nseq);
-    if (p.N > 0) {
-        const int64_t each = most_groups(kGdrThreads) / p.heads;
-        if (places > each) return GRIM_ERR_UNSUPPORTED;
-        hipLaunchKernelGGL((chunk_matrices<T, DK>), dim3((unsigned)(places * p.heads)), dim3(kGdrThreads), 0, stream, p);
-        const grim_status st = launched();
-        if (st != GRIM_OK) return st;
-    }
-    constexpr int bytes = WalkRoom<T, DK>::bytes;
-    static const hipError_t grown = hipFuncSetAttribute(reinterpret_cast<const void *>(&walk<T, DK>), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+// Tokens of a run.  Runs are what fills the compute units where sequences and heads are few: as many as there are for two workgroups each, of eight chunks or more (what a run
+// does to the states has to be formed first, which costs more than the run itself, and the runs' maps are joined one after another).
+template <typename T>
+uint32_t run_of(int64_t N, int32_t nseq, int32_t heads, int32_t dv) {
+    constexpr int64_t C = Gdr<T>::chunk, least = 8 * C;
+    const int64_t each = (int64_t)heads * ((tiles_of(dv) + 7) / 8);
+    const int64_t runs = 2 * kComputeUnits / each;
+    if (runs < 2 || N < 2 * least || N / nseq < least) return (uint32_t)1 << 31;
+    const int64_t size = ((N + runs - 1) / runs + C - 1) / C * C;
+    return (uint32_t)(size < least ? least : size);
+}
+inline int64_t runs_of(int64_t N, int32_t nseq, uint32_t size) { return N / size + nseq; }
+
+template <typename T, int DK, int W, int CT, bool WHOLE, bool MAPS>
+grim_status walk_launch(const GdrParams &p, hipStream_t stream) {
+    constexpr int bytes = WalkRoom<T, DK, 16 * CT * W>::bytes;
+    const auto kernel = walk<T, DK, W, CT, WHOLE, MAPS>;
+    static const hipError_t grown = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (grown != hipSuccess) return GRIM_ERR_DEVICE;
-    hipLaunchKernelGGL((walk<T, DK>), dim3((unsigned)((int64_t)p.nseq * p.heads * p.blocks)), dim3(kGdrThreads), bytes, stream, p);
+    const int64_t blocks = (p.tiles + CT * W - 1) / (CT * W) + (MAPS ? (DK / 16 + CT * W - 1) / (CT * W) : 0);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(runs_of(p.N, p.nseq, p.size) * p.heads * blocks)), dim3(64 * W), bytes, stream, p);
     return launched();
 }
 
+template <typename T, int DK, bool WHOLE>
+grim_status gdr_launch(const GdrParams &p, hipStream_t stream) {
+    if (p.N > 0) {
+        const int64_t places = places_of<T>(p.N, p.nseq);
+        if (places > most_groups(kMatrixThreads) / p.heads) return GRIM_ERR_UNSUPPORTED;
+        hipLaunchKernelGGL((chunk_matrices<T, DK, WHOLE>), dim3((unsigned)(places * p.heads)), dim3(kMatrixThreads), 0, stream, p);
+        grim_status st = launched();
+        if (st != GRIM_OK) return st;
+        if (p.size < (uint32_t)p.N) {
+            st = p.tiles <= 4 ? walk_launch<T, DK, 4, 1, WHOLE, true>(p, stream) : walk_launch<T, DK, 8, 1, WHOLE, true>(p, stream);
+            if (st != GRIM_OK) return st;
+            constexpr int bytes = Tile<Gdr<T>::comp, DK, DK, true>::bytes;
+            static const hipError_t grown = hipFuncSetAttribute(reinterpret_cast<const void *>(join_runs<T, DK>), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+            if (grown != hipSuccess) return GRIM_ERR_DEVICE;
+            hipLaunchKernelGGL((join_runs<T, DK>), dim3((unsigned)((int64_t)p.nseq * p.heads * ((p.tiles + 3) / 4))), dim3(256), bytes, stream, p);
+            st = launched();
+            if (st != GRIM_OK) return st;
+        }
+    }
+    return p.tiles <= 4 ? walk_launch<T, DK, 4, 1, WHOLE, false>(p, stream) : walk_launch<T, DK, 8, 1, WHOLE, false>(p, stream);
+}
+
+// What a call keeps of its runs: the states in front of them, and their maps.
+template <typename T>
+int64_t runs_bytes(int64_t N, int32_t nseq, int32_t heads, int32_t dk, int32_t dv) {
+    const uint32_t size = run_of<T>(N, nseq, heads, dv);
+    if (size >= N) return 0;
+    const int64_t d = padded(dk);
+    return runs_of(N, nseq, size) * heads * (tiles_of(dv) * 16 * d + d * d) * 4;
+}
+
+template <typename T>
+int64_t gdr_room(int64_t N, int32_t nseq, int32_t heads, int32_t dk, int32_t dv) { return saved_bytes<T>(N, nseq, heads) + runs_bytes<T>(N, nseq, heads, dk, dv); }
+
 template <typename T>
 grim_status gdr_typed(GdrParams p, void *states, void *workspace, hipStream_t stream) {
+    const int64_t saved = saved_bytes<T>(p.N, p.nseq, p.heads);
     p.saved = static_cast<char *>(states ? states : workspace);
-    if (states) p.states = reinterpret_cast<float *>(p.saved + saved_bytes<T>(p.N, p.nseq, p.heads));
-    return p.dk <= 64 ? gdr_launch<T, 64>(p, stream) : gdr_launch<T, 128>(p, stream);
+    if (states) p.states = reinterpret_cast<float *>(p.saved + saved);
+    p.size = run_of<T>(p.N, p.nseq, p.heads, p.dv);
+    p.starts = reinterpret_cast<float *>(static_cast<char *>(workspace) + saved);
+    p.maps = p.starts + runs_of(p.N, p.nseq, p.size) * p.heads * p.tiles * 16 * padded(p.dk);
+    if (p.dk % 8 == 0 && p.dv % 8 == 0) return p.dk <= 64 ? gdr_launch<T, 64, true>(p, stream) : gdr_launch<T, 128, true>(p, stream);
+    return p.dk <= 64 ? gdr_launch<T, 64, false>(p, stream) : gdr_launch<T, 128, false>(p, stream);
 }
 
 }  // namespace lm
@@ -465,7 +585,7 @@ int64_t grim_gdr_states(int64_t N, int32_t nseq, int32_t heads, int32_t dk, int3
 int64_t grim_gdr_workspace(int64_t N, int32_t nseq, int32_t heads, int32_t key_heads, int32_t dk, int32_t dv) {
     using namespace grim::lm;
     if (!gdr_shape(N, nseq, heads, key_heads, dk, dv) || dk > kMostHeadSize || dv > kMostHeadSize) return 0;
-    const int64_t a = saved_bytes<float>(N, nseq, heads), b = saved_bytes<f16>(N, nseq, heads);
+    const int64_t a = gdr_room<float>(N, nseq, heads, dk, dv), b = gdr_room<f16>(N, nseq, heads, dk, dv);
     return a > b ? a : b;
 }
 
@@ -488,8 +608,8 @@ grim_status grim_gdr_sequence(const void *q_dev, const void *k_dev, const void *
     if (workspace_bytes < grim_gdr_workspace(N, nseq, heads, key_heads, dk, dv) && N > 0) return GRIM_ERR_SHAPE;
     if (N == 0 && !s_last_dev) return GRIM_OK;
     if (s_last_dev && s0_dev && overlap(s0_dev, s_last_dev, (int64_t)nseq * heads * dk * dv * 4)) return GRIM_ERR_UNSUPPORTED;
-    const GdrParams p{q_dev, k_dev, v_dev, decay_dev, beta_dev, s0_dev, seq_start_dev, y_dev, s_last_dev, nullptr, nullptr, ldq, ldk, ldv, ldg, ldy, N, nseq,
-                      heads, heads / key_heads, dk, dv, blocks_of(dv), scale, norm_eps};
+    const GdrParams p{q_dev, k_dev, v_dev, decay_dev, beta_dev, s0_dev, seq_start_dev, y_dev, s_last_dev, nullptr, nullptr, nullptr, nullptr, ldq, ldk, ldv, ldg, ldy, N,
+                      0, nseq, heads, heads / key_heads, dk, dv, tiles_of(dv), scale, norm_eps};
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     return dt == GRIM_F32   ? gdr_typed<float>(p, states_dev, workspace, stream)
            : dt == GRIM_F16 ? gdr_typed<f16>(p, states_dev, workspace, stream)

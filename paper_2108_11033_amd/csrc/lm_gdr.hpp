@@ -14,10 +14,11 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 b16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 template <typename T>
 struct Gdr;
-// chunk: tokens that the matrix form takes at a time.  (In fp32 a chunk of 64 tokens has no room in LDS.)
+// chunk: tokens that the matrix form takes at a time (fewer in fp32, whose products take six times as long)
 template <>
 struct Gdr<bf16> { static constexpr int data = 1, comp = 2, chunk = 64; };
 template <>
@@ -25,48 +26,91 @@ struct Gdr<f16> { static constexpr int data = 2, comp = 2, chunk = 64; };
 template <>
 struct Gdr<float> { static constexpr int data = 3, comp = 3, chunk = 32; };
 
-constexpr int kGdrColumns = 64;                 // columns of the states that a workgroup takes
-constexpr int kGdrThreads = 256;
+constexpr int kMatrixThreads = 256;            // of the kernel that forms the chunks' matrices
 constexpr double kLeastDecay = -10000.;
 
 // ---------------------------------------------------------------------------------------------------- matrices in LDS
-// P parts of ROWS x COLS, rows 16 bytes longer than their elements: the rows that one instruction reads then lie in different banks.
-template <int P, int ROWS, int COLS>
-struct Tile {
-    static constexpr int parts = P, ld = COLS + 8, part = ROWS * ld, bytes = P * part * 2;
-    uint16_t *at;
-};
-
+// Sums run over 32 elements at a time.  A lane of the first operand holds 8 elements of row lane % 16, of the second 8 of column lane % 16; a result's lane
+// has rows (lane / 16) 4 .. + 3 at column lane % 16.  Which 8 of the 32 a lane holds is free as long as both operands agree: here elements 4 g .. 4 g + 3 and
+// 16 + 4 g .. 16 + 4 g + 3, g = lane / 16.  That is what two results of 16 rows above one another leave in a lane, so that a result is the
+// next product's operand (first or second) as it stands, without a way through LDS.
 template <int P>
 struct Frag { s16x8 part[P]; };
 
+// P parts of ROWS x COLS.  Rows are longer than their elements, so that the rows that one access reads lie in different banks.  Measured, in clocks per access of a
+// compute unit of which 8-byte accesses take 1.85 and 16-byte ones 3 at best: rows of 36 or 76 words 8 bytes along the rows 1.85 (40, 72 words 3), transposing reads 3 (40, 72 words 1.85);
+// 16 bytes along the rows (PAIRED: columns stored in the order that a lane reads them in, 32 m + 16 h + 4 g + r at 32 m + 8 g + 4 h + r) 6 with rows of 36 words, 3 of 40 and 72.
+template <int P, int ROWS, int COLS, bool PAIRED = false>
+struct Tile {
+    static constexpr int parts = P, ld = COLS == 128 ? (PAIRED ? 144 : 152) : COLS == 64 ? (PAIRED ? 80 : 72) : 48, part = ROWS * ld, bytes = P * part * 2;
+    uint16_t *at;
+};
+
+__device__ __forceinline__ s16x8 both(s16x4 lo, s16x4 hi) { return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7); }
+
+__device__ __forceinline__ int paired(int c) { return (c & ~31) + 8 * (c >> 2 & 3) + 4 * (c >> 4 & 1) + (c & 3); }
+
 // 16 rows from r, as an operand whose sum runs along them, over elements k .. k + 31.
-template <int P, int R, int C>
-__device__ __forceinline__ Frag<P> along(const Tile<P, R, C> &m, int r, int k) {
+template <int P, int R, int C, bool PAIRED>
+__device__ __forceinline__ Frag<P> along(const Tile<P, R, C, PAIRED> &m, int r, int k) {
     const int lane = threadIdx.x & 63;
     Frag<P> f;
 #pragma unroll
-    for (int p = 0; p < P; ++p)
-        f.part[p] = *reinterpret_cast<const s16x8 *>(m.at + p * m.part + (r + (lane & 15)) * m.ld + k + (lane >> 4) * 8);
-    return f;
-}
-
-// 16 columns from c, as an operand whose sum runs over rows k .. k + 31: the transposing read hands each lane of 16 four rows at one column.
-template <int P, int R, int C>
-__device__ __forceinline__ Frag<P> across(const Tile<P, R, C> &m, int c, int k) {
-    const int lane = threadIdx.x & 63, j = lane & 15;
-    Frag<P> f;
-#pragma unroll
     for (int p = 0; p < P; ++p) {
-        uint16_t *from = m.at + p * m.part + (k + (lane >> 4) * 8 + j / 4) * m.ld + c + (j % 4) * 4;
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)from);
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(from + 4 * m.ld));
-        f.part[p] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        const uint16_t *from = m.at + p * m.part + (r + (lane & 15)) * m.ld + k + (lane >> 4) * (PAIRED ? 8 : 4);
+        if (PAIRED) f.part[p] = *reinterpret_cast<const s16x8 *>(from);
+        else f.part[p] = both(*reinterpret_cast<const s16x4 *>(from), *reinterpret_cast<const s16x4 *>(from + 16));
     }
     return f;
 }
 
-// acc + the 16 x 16 product: a lane has rows (lane / 16) 4 .. + 3 of a's at column lane % 16 of b's.  Small terms first.
+// Four rows from r + (lane / 16) 4 at column c + lane % 16: the transposing read of 16 bits.
+__device__ __forceinline__ s16x4 turned(const uint16_t *at, int ld, int r, int c) {
+    const int lane = threadIdx.x & 63, j = lane & 15;
+    uint16_t *from = const_cast<uint16_t *>(at) + (r + (lane >> 4) * 4 + j / 4) * ld + c + (j % 4) * 4;
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)from);
+}
+
+// 16 columns from c, as an operand whose sum runs over rows k .. k + 31.
+template <int P, int R, int C>
+__device__ __forceinline__ Frag<P> across(const Tile<P, R, C> &m, int c, int k) {
+    Frag<P> f;
+#pragma unroll
+    for (int p = 0; p < P; ++p) f.part[p] = both(turned(m.at + p * m.part, m.ld, k, c), turned(m.at + p * m.part, m.ld, k + 16, c));
+    return f;
+}
+
+// (lo, hi) rounded to bf16, in one word; what is left of them.  (Not by inline asm: the compiler keeps the matrix instructions' results from being read too early
+// only where it knows the reader.)
+__device__ __forceinline__ uint32_t round2(float lo, float hi) {
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    typedef __bf16 b16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{lo, hi}), b16x2));
+}
+template <int V>
+__device__ __forceinline__ void round_off(float (&v)[V], uint32_t (&w)[V / 2], bool more) {
+#pragma unroll
+    for (int j = 0; j < V / 2; ++j) {
+        w[j] = round2(v[2 * j], v[2 * j + 1]);
+        if (more) v[2 * j] -= __builtin_bit_cast(float, w[j] << 16), v[2 * j + 1] -= __builtin_bit_cast(float, w[j] & 0xffff0000u);
+    }
+}
+
+// Two results above one another, as the operand of a sum over their rows.
+template <int P>
+__device__ __forceinline__ Frag<P> operand(f32x4 lo, f32x4 hi) {
+    Frag<P> f;
+    float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+        uint32_t w[4];
+        round_off(v, w, p + 1 < P);
+        __builtin_memcpy(&f.part[p], w, 16);
+    }
+    return f;
+}
+
+// acc + the 16 x 16 product, small terms first.
 template <int PA, int PB>
 __device__ __forceinline__ f32x4 multiply(const Frag<PA> &a, const Frag<PB> &b, f32x4 acc) {
     constexpr int P = PA > PB ? PA : PB;
@@ -80,84 +124,153 @@ __device__ __forceinline__ f32x4 multiply(const Frag<PA> &a, const Frag<PB> &b, 
 }
 
 // Elements c .. c + 3 of row r.
-template <int P, int R, int C>
-__device__ __forceinline__ void put4(const Tile<P, R, C> &m, int r, int c, f32x4 v) {
+template <int P, int R, int C, bool PAIRED>
+__device__ __forceinline__ void put4(const Tile<P, R, C, PAIRED> &m, int r, int c, f32x4 v) {
+    if (PAIRED) c = paired(c);
+    float t[4] = {v[0], v[1], v[2], v[3]};
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-        bf16 h[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            h[j] = (bf16)v[j];
-            if (p + 1 < P) v[j] -= (float)h[j];
-        }
-        s16x4 w;
-        __builtin_memcpy(&w, h, 8);
-        *reinterpret_cast<s16x4 *>(m.at + p * m.part + r * m.ld + c) = w;
+        uint32_t w[2];
+        round_off(t, w, p + 1 < P);
+        s16x4 o;
+        __builtin_memcpy(&o, w, 8);
+        *reinterpret_cast<s16x4 *>(m.at + p * m.part + r * m.ld + c) = o;
     }
 }
 
-template <int P, int R, int C, typename T>
-__device__ __forceinline__ void put8(const Tile<P, R, C> &m, int r, int c, const Pack<T, 8> &raw, const float (&x)[8]) {
-    if constexpr (__is_same(T, bf16) && P == 1) {
-        __builtin_memcpy(m.at + r * m.ld + c, raw.w, 16);
+// Elements c .. c + 7, c a multiple of 8.
+template <int P, int R, int C, bool PAIRED>
+__device__ __forceinline__ void put8(const Tile<P, R, C, PAIRED> &m, int r, int c, s16x8 v, int p = 0) {
+    uint16_t *to = m.at + p * m.part + r * m.ld;
+    if (PAIRED) {
+        *reinterpret_cast<s16x4 *>(to + paired(c)) = __builtin_shufflevector(v, v, 0, 1, 2, 3);
+        *reinterpret_cast<s16x4 *>(to + paired(c) + 8) = __builtin_shufflevector(v, v, 4, 5, 6, 7);
     } else {
-        float v[8];
+        *reinterpret_cast<s16x8 *>(to + c) = v;
+    }
+}
+template <int P, int R, int C, bool PAIRED>
+__device__ __forceinline__ void put8(const Tile<P, R, C, PAIRED> &m, int r, int c, float (&v)[8]) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = x[j];
+    for (int p = 0; p < P; ++p) {
+        uint32_t h[4];
+        round_off(v, h, p + 1 < P);
+        s16x8 w;
+        __builtin_memcpy(&w, h, 16);
+        put8(m, r, c, w, p);
+    }
+}
+
+// V elements from column c of a row of `width` (which may end inside them, or before) without a branch, so that loads do not wait for each other: those that end with the row,
+// which settle() moves to their places when they have come.  WHOLE: the width is a multiple of V.
+template <bool WHOLE, int V, typename T>
+__device__ __forceinline__ Pack<T, V> reach(const T *row, int c, int width) {
+    if (WHOLE || width >= V) return load<V>(row + max(0, min(c, width - V)));
+    Pack<T, V> r = {};
 #pragma unroll
-        for (int p = 0; p < P; ++p) {
-            bf16 h[8];
+    for (int j = 0; j < V; ++j) put(r, j, row[min(c + j, width - 1)]);
+    return r;
+}
+template <bool WHOLE, int V, typename T>
+__device__ __forceinline__ void settle(const Pack<T, V> &raw, int c, int width, bool there, float (&v)[V]) {
+    unpack(raw, v);
+    if (WHOLE) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                h[j] = (bf16)v[j];
-                if (p + 1 < P) v[j] -= (float)h[j];
-            }
-            __builtin_memcpy(m.at + p * m.part + r * m.ld + c, h, 16);
-        }
+        for (int j = 0; j < V; ++j) v[j] = there && c < width ? v[j] : 0.f;
+        return;
+    }
+    const int n = width >= V ? c - max(0, min(c, width - V)) : 0;
+#pragma unroll
+    for (int by = 1; by < V; by *= 2)
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[j] = n & by ? (j + by < V ? v[j + by] : 0.f) : v[j];
+#pragma unroll
+    for (int j = 0; j < V; ++j) v[j] = there && c + j < width ? v[j] : 0.f;
+}
+
+// Elements c .. c + 3 of a row of `width`.
+template <bool WHOLE, bool PAST = false, typename T>
+__device__ __forceinline__ void leave(T *row, int c, int width, f32x4 v) {
+    if (c + 4 <= width) {
+        const float t[4] = {v[0], v[1], v[2], v[3]};
+        store<PAST>(row + c, t);
+    } else if (!WHOLE) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (c + j < width) row[c + j] = (T)v[j];
     }
 }
 
 // Rows of keys or queries on their way to LDS: COLS elements in pieces of 8, dealt to the workgroup's threads; zeros behind the head's
 // width and the last row.
-template <typename T, int ROWS, int COLS>
+template <bool WHOLE, typename T, int THREADS, int ROWS, int COLS>
 struct Rows {
-    static constexpr int per_row = COLS / 8, PER = ROWS * per_row / kGdrThreads;
-    static_assert(PER * kGdrThreads == ROWS * per_row, "whole pieces");
+    static constexpr int per_row = COLS / 8, PER = (ROWS * per_row + THREADS - 1) / THREADS;
+    static constexpr bool even = PER * THREADS == ROWS * per_row;       // else some threads have a piece less
     Pack<T, 8> raw[PER];
-    __device__ __forceinline__ static int row(int k) { return (k * kGdrThreads + (int)threadIdx.x) / per_row; }
-    __device__ __forceinline__ static int col(int k) { return (k * kGdrThreads + (int)threadIdx.x) % per_row * 8; }
+    __device__ __forceinline__ static int row(int k) { return (k * THREADS + (int)threadIdx.x) / per_row; }
+    __device__ __forceinline__ static int col(int k) { return (k * THREADS + (int)threadIdx.x) % per_row * 8; }
     __device__ __forceinline__ void fetch(const T *x, int64_t ld, int rows, int width) {
+#pragma unroll
+        for (int k = 0; k < PER; ++k) raw[k] = reach<WHOLE, 8>(x + min(row(k), rows - 1) * ld, col(k), width);
+    }
+    // Into the tile.
+    template <int P, bool PAIRED>
+    __device__ __forceinline__ void place(const Tile<P, ROWS, COLS, PAIRED> &m, int rows, int width) {
 #pragma unroll
         for (int k = 0; k < PER; ++k) {
             const int r = row(k), c = col(k);
+            if (!even && r >= ROWS) continue;
+            if constexpr (WHOLE && P == 1) {
+                u32x4 w;
 #pragma unroll
-            for (int i = 0; i < raw[k].W; ++i) raw[k].w[i] = 0;
-            if (r >= rows) continue;
-            const T *from = x + r * ld + c;
-            if (c + 8 <= width) raw[k] = load<8>(from);
-            else
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (c + j < width) put(raw[k], j, from[j]);
+                for (int i = 0; i < 4; ++i) w[i] = r < rows && c < width ? raw[k].w[i] : 0u;
+                put8(m, r, c, __builtin_bit_cast(s16x8, w));
+            } else {
+                float v[8];
+                settle<WHOLE>(raw[k], c, width, r < rows, v);
+                put8(m, r, c, v);
+            }
         }
     }
-    // Into the tile; lengths (if asked for): of every row 1 / sqrt(sum of squares + eps), times `factor`; without eps `factor` alone.
-    template <int P>
-    __device__ __forceinline__ void place(const Tile<P, ROWS, COLS> &m, float *lengths, float eps, float factor) {
+    // As they are, to rows of ld elements.
+    __device__ __forceinline__ void keep(T *to, int ld, int rows, int width) {
 #pragma unroll
         for (int k = 0; k < PER; ++k) {
-            float v[8];
-            unpack(raw[k], v);
-            put8(m, row(k), col(k), raw[k], v);
-            if (!lengths) continue;
-            float sq = 0.f;
+            const int r = row(k), c = col(k);
+            if (!even && r >= ROWS) continue;
+            if constexpr (WHOLE) {
+#pragma unroll
+                for (int i = 0; i < raw[k].W; i += 4) {
+                    u32x4 w;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) w[j] = r < rows && c < width ? raw[k].w[i + j] : 0u;
+                    __builtin_memcpy(to + r * ld + c + i * 4 / (int)sizeof(T), &w, 16);
+                }
+            } else {
+                float v[8];
+                settle<WHOLE>(raw[k], c, width, r < rows, v);
+                T t[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) t[j] = (T)v[j];
+                __builtin_memcpy(to + r * ld + c, t, sizeof(t));
+            }
+        }
+    }
+    // Of every row factor / sqrt(sum of squares + eps), without eps `factor` alone; to be called by all lanes.
+    __device__ __forceinline__ void lengths(int rows, int width, float *to, float eps, float factor) {
+        static_assert(even, "whole pieces");
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            float v[8], sq = 0.f;
+            settle<WHOLE>(raw[k], col(k), width, row(k) < rows, v);
 #pragma unroll
             for (int j = 0; j < 8; ++j) sq = __builtin_fmaf(v[j], v[j], sq);
             sq += from_lane<0xb1>(sq);
             sq += from_lane<0x4e>(sq);
             sq += from_lane<0x141>(sq);
             if (per_row == 16) sq += from_lane<0x140>(sq);
-            if (col(k) == 0) lengths[row(k)] = eps > 0.f ? factor / sqrtf(sq + eps) : factor;
+            if (col(k) == 0) to[row(k)] = eps > 0.f ? factor / sqrtf(sq + eps) : factor;
         }
     }
 };
@@ -169,10 +282,13 @@ struct GdrParams {
     const int32_t *seq_start;
     void *y;
     float *s_last;
-    char *saved;                // per chunk and head: what chunk_matrices leaves, and in training the states in front of it
-    float *states;
+    char *saved;                // per chunk and head: what chunk_matrices leaves
+    float *states;              // per chunk and head: the states in front of it, or NULL
+    float *starts;              // per run and head: the states in front of it (of a sequence's first run: not used)
+    float *maps;                // per run and head: dk x dk, what the run makes of the states in front of it, less what it adds
     int64_t ldq, ldk, ldv, ldg, ldy, N;
-    int32_t nseq, heads, group, dk, dv, blocks;         // group: heads of a key head; blocks: of columns of the states
+    uint32_t size;              // tokens of a run
+    int32_t nseq, heads, group, dk, dv, tiles;          // group: heads of a key head; tiles: of 16 columns of the states
     float scale, norm_eps;
 };
 
@@ -186,34 +302,40 @@ struct Span {
     }
 };
 
-// The chunks of all sequences have places in one row: sequence s has the places from first / SIZE + s, one more than it needs at most, and there are
-// N / SIZE + nseq in all.
-template <int SIZE>
-__device__ __forceinline__ int64_t place_of(const int32_t *starts, int s, int64_t N) {
-    return Span(starts, s, N).first / SIZE + s;
-}
+// The chunks (or runs of chunks, of `size` tokens) of all sequences have places in one row: sequence s has the places from first / size + s, one more than it needs at
+// most, and there are N / size + nseq in all.  (N is at most 2^30: 32-bit divisions.)
+__device__ __forceinline__ uint32_t place_of(const Span &span, int s, uint32_t size) { return (uint32_t)span.first / size + s; }
 
-// Which sequence place c belongs to.
-template <int SIZE>
-__device__ __forceinline__ int sequence_of(const int32_t *starts, int nseq, int64_t N, int64_t c) {
-    int lo = 0, hi = nseq - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) / 2;
-        if (place_of<SIZE>(starts, mid, N) <= c) lo = mid;
-        else hi = mid - 1;
+// Which sequence a place belongs to: 64 lanes look at once, so that up to 64 sequences cost one wait for memory, 4096 two.
+__device__ __forceinline__ int sequence_of(const int32_t *starts, int nseq, int64_t N, uint32_t size, uint32_t place) {
+    int lo = 0, left = nseq;
+    while (left > 1) {
+        const int step = (left + 63) / 64, at = lo + (int)(threadIdx.x & 63) * step, in = at < lo + left;
+        const bool before = in && place_of(Span(starts, in ? at : lo, N), at, size) <= place;
+        const int n = __builtin_popcountll(__ballot(before));          // (in ascending order: the first ones)
+        const int next = lo + (n > 0 ? n - 1 : 0) * step;
+        left = min(step, lo + left - next);
+        lo = __builtin_amdgcn_readfirstlane(next);
+        left = __builtin_amdgcn_readfirstlane(left);
     }
     return lo;
 }
 
-// What is kept of a chunk for a head: the matrix M in parts, and the sums of the decays' logarithms in fp64.
+// What is kept of a chunk for a head: the matrix M in parts, columns paired; the running sums of the decays' base-2 logarithms in fp64; and of every token, with r the
+// factors that its key and its query count with (0 behind the last one), beta, the decay since the chunk's start times r_k, the decay until its end times r_k, the
+// decay since its start times r_q, r_k, r_q.
 template <typename T>
 struct Saved {
-    static constexpr int C = Gdr<T>::chunk, P = Gdr<T>::comp, matrix = P * C * C * 2, bytes = matrix + C * 8;
+    static constexpr int C = Gdr<T>::chunk, P = Gdr<T>::comp, matrix = P * C * C * 2, bytes = matrix + C * 32;
     char *at;
     __device__ __forceinline__ Saved(const GdrParams &p, int64_t place, int head) : at(p.saved + (place * p.heads + head) * bytes) {}
     __device__ __forceinline__ uint16_t *M() const { return reinterpret_cast<uint16_t *>(at); }
     __device__ __forceinline__ double *G() const { return reinterpret_cast<double *>(at + matrix); }
+    __device__ __forceinline__ float *tokens() const { return reinterpret_cast<float *>(at + matrix + C * 8); }
 };
+
+// The decay between two places of a chunk.  (The argument's rounding is 2^-24 of it: 8e-7 of a decay to a millionth, less nearer by.)
+__device__ __forceinline__ float decay_of(double from_to) { return __builtin_amdgcn_exp2f((float)from_to); }
 
 }  // namespace lm
 }  // namespace grim

@@ -65,6 +65,20 @@ def test_forward(dtype, starts, heads, key_heads, dk, dv, eps):
     assert torch.equal(c.forward(last=False)[0], y)
 
 
+# sequences that are cut into runs, whose maps are joined: two runs, many, ends and starts next to a cut, sequences of one run among them
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("starts,heads,key_heads,dk,dv", [([0, 1025], 2, 1, 64, 64), ([0, 2500], 1, 1, 128, 128), ([0, 512, 1536, 2049, 3100], 2, 2, 24, 100),
+                                                         ([0, 1600, 1600, 1601], 4, 1, 33, 16), ([0, 100, 3000], 1, 1, 128, 40)])
+def test_runs(dtype, starts, heads, key_heads, dk, dv):
+    c = Call(dtype, starts, heads, key_heads, dk, dv, seed=dk + dv, pad=dv % 3)
+    y, s_last = c.forward()
+    want = c.want()
+    assert untouched(y, c.ybuf)
+    close(s_last, *want["s_last"], "f32", "s_last")
+    close(y, *want["y"], dtype, "y")
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_gates_at_their_ends(dtype):
