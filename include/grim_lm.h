@@ -111,15 +111,19 @@ grim_status grim_glr_step(const float *gates_dev, int64_t ldg, const float *bias
  *   y_dev           N x (heads dv) of element type dt, rows of ldy; must not overlap the inputs
  *   s_last_dev      nseq x heads x dk x dv fp32, the states after the last tokens (of an empty sequence: its s0), or NULL; must not overlap s0
  *   states_dev      grim_gdr_states(...) bytes for the backward pass, 16-byte aligned, or NULL
- *   workspace       grim_gdr_workspace(...) bytes
- * Infinities and NaN reach the tokens of their own sequence and head alone,
+ *   workspace       grim_gdr_workspace(...) bytes, for either direction
+ * Backward, for the gradients dy of y and ds_last of s_last (or NULL: zeros), of the same inputs with the states that the forward call left:
+ *   dq_dev, dk_dev, dv_dev   of element type dt, in the inputs' shapes, rows of lddq, lddk, lddv (those of a key head: sums over the heads that read it)
+ *   ddecay_dev, dbeta_dev    N x heads fp32, rows of lddg (where g counts as -10000 its gradient is 0)
+ *   ds0_dev         nseq x heads x dk x dv fp32 (of an empty sequence: its ds_last), or NULL; must not overlap ds_last
+ * Gradients must not overlap inputs.  Infinities and NaN reach the tokens of their own sequence and head alone (of their own sequence and key head in dq and dk),
  * there also tokens in front of them.  Products run on the matrix cores with operands in two (fp16, bf16) or three (fp32) bf16 parts, sums in fp32: results are off by some 2^-17
  * or 2^-23 of the terms' size before their rounding.  Values beyond 3.3e38 count as infinite.
  * grim_gdr_step is one token for `batch` callers at once, columns as of grim_glr_step: q and k (key_heads dk) x batch, v (heads dv) x batch, g and beta
  * heads x batch, all fp32; states batch x heads x dk x dv fp32 as the sequence calls have them (s_new_dev may be s_dev itself), y (heads dv) x batch of element
  * type dt, or NULL.  Its arithmetic is fp32.
  * Errors: NULL, SHAPE (N < 0, N > 2^30, nseq < 1, nseq > 1 without starts, heads < 1 or > 4096, heads not a multiple of key_heads, dk or dv < 1, leading
- * dimension or a buffer too small, scale not finite, norm_eps negative), DTYPE, DEVICE, UNSUPPORTED (dk or dv > 128, s_last over s0, s_new over a part of s).
+ * dimension or a buffer too small, scale not finite, norm_eps negative), DTYPE, DEVICE, UNSUPPORTED (dk or dv > 128, s_last over s0, ds0 over ds_last, s_new over a part of s).
  */
 int64_t grim_gdr_states(int64_t N, int32_t nseq, int32_t heads, int32_t dk, int32_t dv);
 int64_t grim_gdr_workspace(int64_t N, int32_t nseq, int32_t heads, int32_t key_heads, int32_t dk, int32_t dv);
@@ -128,6 +132,13 @@ grim_status grim_gdr_sequence(const void *q_dev, const void *k_dev, const void *
                               int32_t nseq, int64_t N, int32_t heads, int32_t key_heads, int32_t dk, int32_t dv, float scale, float norm_eps,
                               void *y_dev, int64_t ldy, float *s_last_dev, void *states_dev, void *workspace, int64_t workspace_bytes,
                               void *hip_stream);
+grim_status grim_gdr_sequence_backward(const void *q_dev, const void *k_dev, const void *v_dev, grim_dtype dt, int64_t ldq, int64_t ldk, int64_t ldv,
+                                       const float *decay_dev, const float *beta_dev, int64_t ldg, const float *s0_dev,
+                                       const int32_t *seq_start_dev, int32_t nseq, int64_t N, int32_t heads, int32_t key_heads, int32_t dk,
+                                       int32_t dv, float scale, float norm_eps, const void *states_dev, const void *dy_dev, int64_t lddy,
+                                       const float *ds_last_dev, void *dq_dev, int64_t lddq, void *dk_dev, int64_t lddk, void *dv_dev,
+                                       int64_t lddv, float *ddecay_dev, float *dbeta_dev, int64_t lddg, float *ds0_dev, void *workspace,
+                                       int64_t workspace_bytes, void *hip_stream);
 grim_status grim_gdr_step(const float *q_dev, const float *k_dev, const float *v_dev, int64_t ldq, int64_t ldk, int64_t ldv, const float *decay_dev,
                           const float *beta_dev, int64_t ldg, const float *s_dev, float *s_new_dev, void *y_dev, grim_dtype dt, int64_t ldy,
                           int32_t heads, int32_t key_heads, int32_t dk, int32_t dv, float scale, float norm_eps, int32_t batch,

@@ -9,6 +9,6 @@ from .binding import (  # noqa: F401
     F32, F16, BF16, STATUS_NAMES,
 )
 from .lm import (  # noqa: F401
-    GradList, distill_topk, distill_topk_workspace, gdr_sequence, gdr_states, gdr_step, gdr_workspace, glr_sequence, glr_sequence_backward, glr_states, glr_step, glr_workspace,
+    GradList, distill_topk, distill_topk_workspace, gdr_sequence, gdr_sequence_backward, gdr_states, gdr_step, gdr_workspace, glr_sequence, glr_sequence_backward, glr_states, glr_step, glr_workspace,
     grad_clip, grad_norm, layer_norm, layer_norm_backward, layer_norm_workspace, logit_rules, policy_loss, policy_loss_workspace,
 )

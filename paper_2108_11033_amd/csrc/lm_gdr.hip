@@ -20,7 +20,7 @@ namespace lm {
 template <typename T, int DK, bool WHOLE>
 __global__ void __launch_bounds__(kMatrixThreads) chunk_matrices(GdrParams p) {
     constexpr int C = Gdr<T>::chunk, PD = Gdr<T>::data, PC = Gdr<T>::comp, TT = C / 32, B = C / 16, LD = C + 4;
-    using Keys = Tile<PD, C, DK, true>;
+    using Keys = Tile<PD, C, DK, PAIRED>;
     constexpr int square = C * LD * 4;
     __shared__ __attribute__((aligned(16))) char lds[square + (Keys::bytes > square ? Keys::bytes : square)];
     __shared__ double G[C];
@@ -150,33 +150,13 @@ __global__ void __launch_bounds__(kMatrixThreads) chunk_matrices(GdrParams p) {
 }
 
 // ---------------------------------------------------------------------------------------------------- from chunk to chunk
-// Values in LDS as they come; what a lane of a 16 x 16 result takes of them.
-template <typename T, int ROWS, int COLS>
-struct Values {
-    static constexpr int ld = sizeof(T) == 4 ? COLS + 4 : COLS == 128 ? 144 : COLS + 8, bytes = ROWS * ld * (int)sizeof(T);
-    T *at;
-    __device__ __forceinline__ f32x4 get(int r, int c) const {
-        f32x4 v;
-        if constexpr (sizeof(T) == 4) {
-            const int lane = threadIdx.x & 63;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = at[(r + (lane >> 4) * 4 + e) * ld + c + (lane & 15)];
-        } else {
-            const s16x4 w = turned(reinterpret_cast<const uint16_t *>(at), ld, r, c);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = (float)__builtin_bit_cast(T, (uint16_t)w[e]);
-        }
-        return v;
-    }
-};
-
 // What a workgroup of the walk keeps in LDS.
 template <typename T, int DK, int COLS>
 struct WalkRoom {
     static constexpr int C = Gdr<T>::chunk, PD = Gdr<T>::data, PC = Gdr<T>::comp;
     using Keys = Tile<PD, C, DK>;
-    using Queries = Tile<PD, C, DK, true>;
-    using Square = Tile<PC, C, C, true>;
+    using Queries = Tile<PD, C, DK, PAIRED>;
+    using Square = Tile<PC, C, C, PAIRED>;
     using Vals = Values<T, C, COLS>;
     static constexpr int keys = 0, queries = keys + Keys::bytes, values = queries + Queries::bytes, M = values + Vals::bytes, P = M + Square::bytes, G = P + Square::bytes,
                          tokens = G + C * 8, bytes = tokens + C * 24;
@@ -213,7 +193,7 @@ __global__ void __launch_bounds__(64 * W, 2) walk(GdrParams p) {
     if (MAPS ? to >= span.end : from >= to && r > 0) return;            // (an empty sequence has its first run for its last states)
     const bool map = MAPS && block >= (int)value_blocks;
     if (map && r == 0) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l15 = lane & 15, g4 = (lane >> 4) * 4;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l15 = lane & 15, g4 = (lane >> 4) * 4, own = l15 * 16 + g4;
     const int tile0 = ((map ? block - (int)value_blocks : block) * W + wave) * CT, tiles = map ? DT : p.tiles, col0 = map ? 0 : block * COLS;
     const bool idle = tile0 >= tiles;
     const T *q = static_cast<const T *>(p.q) + (int64_t)(h / p.group) * p.dk, *k = static_cast<const T *>(p.k) + (int64_t)(h / p.group) * p.dk;
@@ -232,7 +212,7 @@ __global__ void __launch_bounds__(64 * W, 2) walk(GdrParams p) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) state[n][c][e] = map && d + e == col ? 1.f : 0.f;
             } else if (r > 0) {
-                if (tile0 + c < p.tiles) state[n][c] = *reinterpret_cast<const f32x4 *>(p.starts + ((((int64_t)run * p.heads + h) * p.tiles + tile0 + c) * DT + n) * 256 + lane * 4);
+                if (tile0 + c < p.tiles) state[n][c] = *reinterpret_cast<const f32x4 *>(p.starts + ((((int64_t)run * p.heads + h) * p.tiles + tile0 + c) * DT + n) * 256 + own);
             } else if (p.s0) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) state[n][c][e] = p.s0[(head + min(d + e, p.dk - 1)) * p.dv + min(col, p.dv - 1)];
@@ -326,7 +306,7 @@ __global__ void __launch_bounds__(64 * W, 2) walk(GdrParams p) {
 #pragma unroll
                     for (int c = 0; c < CT; ++c)
                         if (tile0 + c < p.tiles)
-                            *reinterpret_cast<f32x4 *>(p.states + ((((place + n) * p.heads + h) * p.tiles + tile0 + c) * DT + d) * 256 + lane * 4) = state[d][c];
+                            *reinterpret_cast<f32x4 *>(p.states + ((((place + n) * p.heads + h) * p.tiles + tile0 + c) * DT + d) * 256 + own) = state[d][c];
 #pragma unroll
             for (int d = 0; d < DS; ++d)
 #pragma unroll
@@ -369,7 +349,12 @@ __global__ void __launch_bounds__(64 * W, 2) walk(GdrParams p) {
         for (int t = 0; t < TT; ++t) {
             const f32x4 bt = *reinterpret_cast<const f32x4 *>(beta + 16 * t + g4);
 #pragma unroll
-            for (int c = 0; c < CT; ++c) x[t][c] = (x[t][c] - less[t][c]) * bt;          // U
+            for (int c = 0; c < CT; ++c) {
+                x[t][c] -= less[t][c];
+                if (!MAPS && p.states && tile0 + c < p.tiles)
+                    *reinterpret_cast<f32x4 *>(p.E + ((((place + n) * p.heads + h) * p.tiles + tile0 + c) * TT + t) * 256 + own) = x[t][c];
+                x[t][c] *= bt;                              // U
+            }
         }
         by(fu, x);
         const float whole = decay_of(G[C - 1]);
@@ -417,7 +402,7 @@ __global__ void __launch_bounds__(64 * W, 2) walk(GdrParams p) {
 #pragma unroll
             for (int c = 0; c < CT; ++c) {
                 if (tile0 + c >= tiles) continue;
-                if (!map) *reinterpret_cast<f32x4 *>(p.starts + ((((int64_t)(run + 1) * p.heads + h) * p.tiles + tile0 + c) * DT + n) * 256 + lane * 4) = state[n][c];
+                if (!map) *reinterpret_cast<f32x4 *>(p.starts + ((((int64_t)(run + 1) * p.heads + h) * p.tiles + tile0 + c) * DT + n) * 256 + own) = state[n][c];
                 else
 #pragma unroll
                     for (int e = 0; e < 4; ++e) p.maps[(((int64_t)run * p.heads + h) * DK + 16 * n + g4 + e) * DK + 16 * (tile0 + c) + l15] = state[n][c][e];
@@ -436,82 +421,7 @@ __global__ void __launch_bounds__(64 * W, 2) walk(GdrParams p) {
         }
 }
 
-// The states in front of every run of a sequence's head, from one to the next: S_(r + 1) = A_r S_r + B_r.  A wave has 16 columns, in registers as above; A comes through LDS.
-template <typename T, int DK>
-__global__ void __launch_bounds__(256) join_runs(GdrParams p) {
-    constexpr int PC = Gdr<T>::comp, DT = DK / 16, DS = DK / 32;
-    using Map = Tile<PC, DK, DK, true>;
-    extern __shared__ __attribute__((aligned(16))) char lds[];
-    const Map A{reinterpret_cast<uint16_t *>(lds)};
-    const uint32_t blocks = (p.tiles + 3) / 4, heads = (uint32_t)p.heads;
-    const int block = (int)(blockIdx.x % blocks), h = (int)(blockIdx.x / blocks % heads), s = (int)(blockIdx.x / blocks / heads);
-    const Span span(p.seq_start, s, p.N);
-    const uint32_t run0 = place_of(span, s, p.size);
-    const int runs = (int)((span.end - span.first + p.size - 1) / p.size);
-    if (runs < 3) return;                                   // (the second run's start is there already)
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tile = block * 4 + wave;
-    const bool idle = tile >= p.tiles;
-    const auto start = [&](int r) { return p.starts + (((int64_t)(run0 + r) * p.heads + h) * p.tiles + (idle ? 0 : tile)) * DT * 256 + lane * 4; };
-    f32x4 state[DT];
-#pragma unroll
-    for (int n = 0; n < DT; ++n) state[n] = *reinterpret_cast<const f32x4 *>(start(1) + n * 256);
-    Rows<true, float, 256, DK, DK> next;
-    next.fetch(p.maps + ((int64_t)(run0 + 1) * p.heads + h) * DK * DK, DK, DK, DK);
-    for (int r = 1; r + 1 < runs; ++r) {
-        next.place(A, DK, DK);
-        if (r + 2 < runs) next.fetch(p.maps + ((int64_t)(run0 + r + 1) * p.heads + h) * DK * DK, DK, DK, DK);
-        f32x4 sum[DT];
-#pragma unroll
-        for (int n = 0; n < DT; ++n) sum[n] = *reinterpret_cast<const f32x4 *>(start(r + 1) + n * 256);
-        __syncthreads();
-        if (!idle) {
-            Frag<PC> S[DS];
-#pragma unroll
-            for (int d = 0; d < DS; ++d) S[d] = operand<PC>(state[2 * d], state[2 * d + 1]);
-#pragma unroll
-            for (int n = 0; n < DT; ++n) {
-#pragma unroll
-                for (int d = 0; d < DS; ++d) sum[n] = multiply(along(A, 16 * n, 32 * d), S[d], sum[n]);
-                state[n] = sum[n];
-                *reinterpret_cast<f32x4 *>(start(r + 1) + n * 256) = sum[n];
-            }
-        }
-        __syncthreads();
-    }
-}
-
 // ---------------------------------------------------------------------------------------------------- launches
-template <typename T>
-int64_t places_of(int64_t N, int32_t nseq) { return N / Gdr<T>::chunk + nseq; }
-
-inline int padded(int dk) { return dk <= 64 ? 64 : 128; }
-inline int tiles_of(int dv) { return (dv + 15) / 16; }
-
-// Bytes of what is kept of the chunks: their matrices, and the states in front of them.
-template <typename T>
-int64_t saved_bytes(int64_t N, int32_t nseq, int32_t heads) { return (places_of<T>(N, nseq) * heads * Saved<T>::bytes + 15) / 16 * 16; }
-template <typename T>
-int64_t states_bytes(int64_t N, int32_t nseq, int32_t heads, int32_t dk, int32_t dv) {
-    return places_of<T>(N, nseq) * heads * tiles_of(dv) * padded(dk) * 16 * 4;
-}
-
-inline bool gdr_shape(int64_t N, int32_t nseq, int32_t heads, int32_t key_heads, int32_t dk, int32_t dv) {
-    return N >= 0 && N <= (int64_t)1 << 30 && nseq >= 1 && heads >= 1 && heads <= kMostHeads && key_heads >= 1 && heads % key_heads == 0 && dk >= 1 && dv >= 1;
-}
-
-// Tokens of a run.  Runs are what fills the compute units where sequences and heads are few: as many as there are for two workgroups each, of eight chunks or more (what a run
-// does to the states has to be formed first, which costs more than the run itself, and the runs' maps are joined one after another).
-template <typename T>
-uint32_t run_of(int64_t N, int32_t nseq, int32_t heads, int32_t dv) {
-    constexpr int64_t C = Gdr<T>::chunk, least = 8 * C;
-    const int64_t each = (int64_t)heads * ((tiles_of(dv) + 7) / 8);
-    const int64_t runs = 2 * kComputeUnits / each;
-    if (runs < 2 || N < 2 * least || N / nseq < least) return (uint32_t)1 << 31;
-    const int64_t size = ((N + runs - 1) / runs + C - 1) / C * C;
-    return (uint32_t)(size < least ? least : size);
-}
-inline int64_t runs_of(int64_t N, int32_t nseq, uint32_t size) { return N / size + nseq; }
-
 template <typename T, int DK, int W, int CT, bool WHOLE, bool MAPS>
 grim_status walk_launch(const GdrParams &p, hipStream_t stream) {
     constexpr int bytes = WalkRoom<T, DK, 16 * CT * W>::bytes;
@@ -534,37 +444,27 @@ grim_status gdr_launch(const GdrParams &p, hipStream_t stream) {
         if (p.size < (uint32_t)p.N) {
             st = p.tiles <= 4 ? walk_launch<T, DK, 4, 1, WHOLE, true>(p, stream) : walk_launch<T, DK, 8, 1, WHOLE, true>(p, stream);
             if (st != GRIM_OK) return st;
-            constexpr int bytes = Tile<Gdr<T>::comp, DK, DK, true>::bytes;
-            static const hipError_t grown = hipFuncSetAttribute(reinterpret_cast<const void *>(join_runs<T, DK>), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-            if (grown != hipSuccess) return GRIM_ERR_DEVICE;
-            hipLaunchKernelGGL((join_runs<T, DK>), dim3((unsigned)((int64_t)p.nseq * p.heads * ((p.tiles + 3) / 4))), dim3(256), bytes, stream, p);
-            st = launched();
+            st = join_runs<T, DK, false>(p, stream);
             if (st != GRIM_OK) return st;
         }
     }
     return p.tiles <= 4 ? walk_launch<T, DK, 4, 1, WHOLE, false>(p, stream) : walk_launch<T, DK, 8, 1, WHOLE, false>(p, stream);
 }
 
-// What a call keeps of its runs: the states in front of them, and their maps.
-template <typename T>
-int64_t runs_bytes(int64_t N, int32_t nseq, int32_t heads, int32_t dk, int32_t dv) {
-    const uint32_t size = run_of<T>(N, nseq, heads, dv);
-    if (size >= N) return 0;
-    const int64_t d = padded(dk);
-    return runs_of(N, nseq, size) * heads * (tiles_of(dv) * 16 * d + d * d) * 4;
-}
-
-template <typename T>
-int64_t gdr_room(int64_t N, int32_t nseq, int32_t heads, int32_t dk, int32_t dv) { return saved_bytes<T>(N, nseq, heads) + runs_bytes<T>(N, nseq, heads, dk, dv); }
-
 template <typename T>
 grim_status gdr_typed(GdrParams p, void *states, void *workspace, hipStream_t stream) {
-    const int64_t saved = saved_bytes<T>(p.N, p.nseq, p.heads);
-    p.saved = static_cast<char *>(states ? states : workspace);
-    if (states) p.states = reinterpret_cast<float *>(p.saved + saved);
     p.size = run_of<T>(p.N, p.nseq, p.heads, p.dv);
-    p.starts = reinterpret_cast<float *>(static_cast<char *>(workspace) + saved);
-    p.maps = p.starts + runs_of(p.N, p.nseq, p.size) * p.heads * p.tiles * 16 * padded(p.dk);
+    const GdrRoom<T> room(p.N, p.nseq, p.heads, p.dk, p.dv);
+    char *at = static_cast<char *>(states ? states : workspace);
+    p.saved = at;
+    p.maps = reinterpret_cast<float *>(at + room.saved);
+    if (states) {
+        p.states = reinterpret_cast<float *>(at + room.saved + room.maps);
+        p.E = reinterpret_cast<float *>(at + room.saved + room.maps + room.states);
+        p.starts = static_cast<float *>(workspace);
+    } else {
+        p.starts = reinterpret_cast<float *>(at + room.saved + room.maps);
+    }
     if (p.dk % 8 == 0 && p.dv % 8 == 0) return p.dk <= 64 ? gdr_launch<T, 64, true>(p, stream) : gdr_launch<T, 128, true>(p, stream);
     return p.dk <= 64 ? gdr_launch<T, 64, false>(p, stream) : gdr_launch<T, 128, false>(p, stream);
 }
@@ -577,15 +477,14 @@ extern "C" {
 int64_t grim_gdr_states(int64_t N, int32_t nseq, int32_t heads, int32_t dk, int32_t dv) {
     using namespace grim::lm;
     if (!gdr_shape(N, nseq, heads, 1, dk, dv) || dk > kMostHeadSize || dv > kMostHeadSize) return 0;
-    const int64_t a = saved_bytes<float>(N, nseq, heads) + states_bytes<float>(N, nseq, heads, dk, dv);
-    const int64_t b = saved_bytes<f16>(N, nseq, heads) + states_bytes<f16>(N, nseq, heads, dk, dv);
+    const int64_t a = GdrRoom<float>(N, nseq, heads, dk, dv).kept(), b = GdrRoom<f16>(N, nseq, heads, dk, dv).kept();
     return a > b ? a : b;
 }
 
 int64_t grim_gdr_workspace(int64_t N, int32_t nseq, int32_t heads, int32_t key_heads, int32_t dk, int32_t dv) {
     using namespace grim::lm;
     if (!gdr_shape(N, nseq, heads, key_heads, dk, dv) || dk > kMostHeadSize || dv > kMostHeadSize) return 0;
-    const int64_t a = gdr_room<float>(N, nseq, heads, dk, dv), b = gdr_room<f16>(N, nseq, heads, dk, dv);
+    const int64_t a = GdrRoom<float>(N, nseq, heads, dk, dv).scratch(), b = GdrRoom<f16>(N, nseq, heads, dk, dv).scratch();
     return a > b ? a : b;
 }
 
@@ -595,21 +494,20 @@ grim_status grim_gdr_sequence(const void *q_dev, const void *k_dev, const void *
                               void *y_dev, int64_t ldy, float *s_last_dev, void *states_dev, void *workspace, int64_t workspace_bytes,
                               void *hip_stream) {
     using namespace grim::lm;
-    if (!known(dt)) return GRIM_ERR_DTYPE;
-    if (!gdr_shape(N, nseq, heads, key_heads, dk, dv) || (nseq > 1 && !seq_start_dev) || !(fabsf(scale) < INFINITY) || !(norm_eps >= 0.f) || norm_eps > 3.4e38f)
-        return GRIM_ERR_SHAPE;
-    if (dk > kMostHeadSize || dv > kMostHeadSize) return GRIM_ERR_UNSUPPORTED;
     const int64_t keys = (int64_t)key_heads * dk, values = (int64_t)heads * dv;
+    const grim_status st = gdr_check(dt, N, nseq, seq_start_dev != nullptr, heads, key_heads, dk, dv, scale, norm_eps);
+    if (st != GRIM_OK) return st;
     if (ldq < keys || ldk < keys || ldv < values || ldy < values || ldg < heads || !fits(N, ldq) || !fits(N, ldk) || !fits(N, ldv) || !fits(N, ldy) ||
         !fits(N, ldg))
         return GRIM_ERR_SHAPE;
-    if ((int64_t)nseq * heads > (int64_t)1 << 23) return GRIM_ERR_UNSUPPORTED;
     if (N > 0 && (!q_dev || !k_dev || !v_dev || !decay_dev || !beta_dev || !y_dev || !workspace)) return GRIM_ERR_NULL;
     if (workspace_bytes < grim_gdr_workspace(N, nseq, heads, key_heads, dk, dv) && N > 0) return GRIM_ERR_SHAPE;
     if (N == 0 && !s_last_dev) return GRIM_OK;
     if (s_last_dev && s0_dev && overlap(s0_dev, s_last_dev, (int64_t)nseq * heads * dk * dv * 4)) return GRIM_ERR_UNSUPPORTED;
-    const GdrParams p{q_dev, k_dev, v_dev, decay_dev, beta_dev, s0_dev, seq_start_dev, y_dev, s_last_dev, nullptr, nullptr, nullptr, nullptr, ldq, ldk, ldv, ldg, ldy, N,
-                      0, nseq, heads, heads / key_heads, dk, dv, tiles_of(dv), scale, norm_eps};
+    GdrParams p{};
+    p.q = q_dev, p.k = k_dev, p.v = v_dev, p.decay = decay_dev, p.beta = beta_dev, p.s0 = s0_dev, p.seq_start = seq_start_dev, p.y = y_dev, p.s_last = s_last_dev;
+    p.ldq = ldq, p.ldk = ldk, p.ldv = ldv, p.ldg = ldg, p.ldy = ldy, p.N = N, p.nseq = nseq, p.heads = heads, p.group = heads / key_heads, p.dk = dk, p.dv = dv;
+    p.tiles = tiles_of(dv), p.scale = scale, p.norm_eps = norm_eps;
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     return dt == GRIM_F32   ? gdr_typed<float>(p, states_dev, workspace, stream)
            : dt == GRIM_F16 ? gdr_typed<f16>(p, states_dev, workspace, stream)

@@ -40,9 +40,11 @@ struct Frag { s16x8 part[P]; };
 // P parts of ROWS x COLS.  Rows are longer than their elements, so that the rows that one access reads lie in different banks.  Measured, in clocks per access of a
 // compute unit of which 8-byte accesses take 1.85 and 16-byte ones 3 at best: rows of 36 or 76 words 8 bytes along the rows 1.85 (40, 72 words 3), transposing reads 3 (40, 72 words 1.85);
 // 16 bytes along the rows (PAIRED: columns stored in the order that a lane reads them in, 32 m + 16 h + 4 g + r at 32 m + 8 g + 4 h + r) 6 with rows of 36 words, 3 of 40 and 72.
-template <int P, int ROWS, int COLS, bool PAIRED = false>
+// TURNED: the longer rows with the columns in their own order, for tiles that only transposing reads read.
+enum Order { PLAIN, PAIRED, TURNED };
+template <int P, int ROWS, int COLS, int ORDER = PLAIN>
 struct Tile {
-    static constexpr int parts = P, ld = COLS == 128 ? (PAIRED ? 144 : 152) : COLS == 64 ? (PAIRED ? 80 : 72) : 48, part = ROWS * ld, bytes = P * part * 2;
+    static constexpr int parts = P, ld = COLS == 128 ? (ORDER ? 144 : 152) : COLS == 64 ? (ORDER ? 80 : 72) : 48, part = ROWS * ld, bytes = P * part * 2;
     uint16_t *at;
 };
 
@@ -51,14 +53,14 @@ __device__ __forceinline__ s16x8 both(s16x4 lo, s16x4 hi) { return __builtin_shu
 __device__ __forceinline__ int paired(int c) { return (c & ~31) + 8 * (c >> 2 & 3) + 4 * (c >> 4 & 1) + (c & 3); }
 
 // 16 rows from r, as an operand whose sum runs along them, over elements k .. k + 31.
-template <int P, int R, int C, bool PAIRED>
-__device__ __forceinline__ Frag<P> along(const Tile<P, R, C, PAIRED> &m, int r, int k) {
+template <int P, int R, int C, int ORDER>
+__device__ __forceinline__ Frag<P> along(const Tile<P, R, C, ORDER> &m, int r, int k) {
     const int lane = threadIdx.x & 63;
     Frag<P> f;
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-        const uint16_t *from = m.at + p * m.part + (r + (lane & 15)) * m.ld + k + (lane >> 4) * (PAIRED ? 8 : 4);
-        if (PAIRED) f.part[p] = *reinterpret_cast<const s16x8 *>(from);
+        const uint16_t *from = m.at + p * m.part + (r + (lane & 15)) * m.ld + k + (lane >> 4) * (ORDER == PAIRED ? 8 : 4);
+        if (ORDER == PAIRED) f.part[p] = *reinterpret_cast<const s16x8 *>(from);
         else f.part[p] = both(*reinterpret_cast<const s16x4 *>(from), *reinterpret_cast<const s16x4 *>(from + 16));
     }
     return f;
@@ -71,9 +73,9 @@ __device__ __forceinline__ s16x4 turned(const uint16_t *at, int ld, int r, int c
     return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)from);
 }
 
-// 16 columns from c, as an operand whose sum runs over rows k .. k + 31.
-template <int P, int R, int C>
-__device__ __forceinline__ Frag<P> across(const Tile<P, R, C> &m, int c, int k) {
+// 16 columns from c (as they are stored), as an operand whose sum runs over rows k .. k + 31.
+template <int P, int R, int C, int ORDER>
+__device__ __forceinline__ Frag<P> across(const Tile<P, R, C, ORDER> &m, int c, int k) {
     Frag<P> f;
 #pragma unroll
     for (int p = 0; p < P; ++p) f.part[p] = both(turned(m.at + p * m.part, m.ld, k, c), turned(m.at + p * m.part, m.ld, k + 16, c));
@@ -124,9 +126,9 @@ __device__ __forceinline__ f32x4 multiply(const Frag<PA> &a, const Frag<PB> &b, 
 }
 
 // Elements c .. c + 3 of row r.
-template <int P, int R, int C, bool PAIRED>
-__device__ __forceinline__ void put4(const Tile<P, R, C, PAIRED> &m, int r, int c, f32x4 v) {
-    if (PAIRED) c = paired(c);
+template <int P, int R, int C, int ORDER>
+__device__ __forceinline__ void put4(const Tile<P, R, C, ORDER> &m, int r, int c, f32x4 v) {
+    if (ORDER == PAIRED) c = paired(c);
     float t[4] = {v[0], v[1], v[2], v[3]};
 #pragma unroll
     for (int p = 0; p < P; ++p) {
@@ -139,18 +141,18 @@ __device__ __forceinline__ void put4(const Tile<P, R, C, PAIRED> &m, int r, int 
 }
 
 // Elements c .. c + 7, c a multiple of 8.
-template <int P, int R, int C, bool PAIRED>
-__device__ __forceinline__ void put8(const Tile<P, R, C, PAIRED> &m, int r, int c, s16x8 v, int p = 0) {
+template <int P, int R, int C, int ORDER>
+__device__ __forceinline__ void put8(const Tile<P, R, C, ORDER> &m, int r, int c, s16x8 v, int p = 0) {
     uint16_t *to = m.at + p * m.part + r * m.ld;
-    if (PAIRED) {
+    if (ORDER == PAIRED) {
         *reinterpret_cast<s16x4 *>(to + paired(c)) = __builtin_shufflevector(v, v, 0, 1, 2, 3);
         *reinterpret_cast<s16x4 *>(to + paired(c) + 8) = __builtin_shufflevector(v, v, 4, 5, 6, 7);
     } else {
         *reinterpret_cast<s16x8 *>(to + c) = v;
     }
 }
-template <int P, int R, int C, bool PAIRED>
-__device__ __forceinline__ void put8(const Tile<P, R, C, PAIRED> &m, int r, int c, float (&v)[8]) {
+template <int P, int R, int C, int ORDER>
+__device__ __forceinline__ void put8(const Tile<P, R, C, ORDER> &m, int r, int c, float (&v)[8]) {
 #pragma unroll
     for (int p = 0; p < P; ++p) {
         uint32_t h[4];
@@ -215,8 +217,8 @@ struct Rows {
         for (int k = 0; k < PER; ++k) raw[k] = reach<WHOLE, 8>(x + min(row(k), rows - 1) * ld, col(k), width);
     }
     // Into the tile.
-    template <int P, bool PAIRED>
-    __device__ __forceinline__ void place(const Tile<P, ROWS, COLS, PAIRED> &m, int rows, int width) {
+    template <int P, int ORDER>
+    __device__ __forceinline__ void place(const Tile<P, ROWS, COLS, ORDER> &m, int rows, int width) {
 #pragma unroll
         for (int k = 0; k < PER; ++k) {
             const int r = row(k), c = col(k);
@@ -276,6 +278,7 @@ struct Rows {
 };
 
 // ---------------------------------------------------------------------------------------------------- chunks of sequences
+// Matrices that are kept (states, their gradients, E and its) lie in tiles of 16 x 16, a column's 16 rows one after another: a lane's four in one access.
 struct GdrParams {
     const void *q, *k, *v;
     const float *decay, *beta, *s0;
@@ -283,13 +286,25 @@ struct GdrParams {
     void *y;
     float *s_last;
     char *saved;                // per chunk and head: what chunk_matrices leaves
-    float *states;              // per chunk and head: the states in front of it, or NULL
+    float *states, *E;          // for the backward pass, per chunk and head: the states in front of it, and E; or NULL
     float *starts;              // per run and head: the states in front of it (of a sequence's first run: not used)
     float *maps;                // per run and head: dk x dk, what the run makes of the states in front of it, less what it adds
     int64_t ldq, ldk, ldv, ldg, ldy, N;
     uint32_t size;              // tokens of a run
     int32_t nseq, heads, group, dk, dv, tiles;          // group: heads of a key head; tiles: of 16 columns of the states
     float scale, norm_eps;
+};
+
+// Of the backward pass; p.starts are the gradients of the states behind the runs.
+struct GdrBack {
+    GdrParams p;
+    const void *dy;
+    const float *ds_last;
+    void *dq, *dk, *dv;
+    float *ddecay, *dbeta, *ds0;
+    float *A, *F;               // per chunk and head: the gradient of the states behind it, and of U over what later tokens make of it (lm_gdr_back.hip)
+    int64_t lddy, lddq, lddk, lddv, lddg;
+    int32_t key_heads;
 };
 
 // Sequence s: rows first .. end - 1, in the order of the buffers whatever the starts hold.
@@ -334,8 +349,85 @@ struct Saved {
     __device__ __forceinline__ float *tokens() const { return reinterpret_cast<float *>(at + matrix + C * 8); }
 };
 
+// Values in LDS as they come; what a lane of a 16 x 16 result takes of them.
+template <typename T, int ROWS, int COLS>
+struct Values {
+    static constexpr int ld = sizeof(T) == 4 ? COLS + 4 : COLS == 128 ? 144 : COLS + 8, bytes = ROWS * ld * (int)sizeof(T);
+    T *at;
+    __device__ __forceinline__ f32x4 get(int r, int c) const {
+        f32x4 v;
+        if constexpr (sizeof(T) == 4) {
+            const int lane = threadIdx.x & 63;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = at[(r + (lane >> 4) * 4 + e) * ld + c + (lane & 15)];
+        } else {
+            const s16x4 w = turned(reinterpret_cast<const uint16_t *>(at), ld, r, c);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = (float)__builtin_bit_cast(T, (uint16_t)w[e]);
+        }
+        return v;
+    }
+};
+
 // The decay between two places of a chunk.  (The argument's rounding is 2^-24 of it: 8e-7 of a decay to a millionth, less nearer by.)
 __device__ __forceinline__ float decay_of(double from_to) { return __builtin_amdgcn_exp2f((float)from_to); }
+
+template <typename T>
+int64_t places_of(int64_t N, int32_t nseq) { return N / Gdr<T>::chunk + nseq; }
+
+inline int padded(int dk) { return dk <= 64 ? 64 : 128; }
+inline int tiles_of(int dv) { return (dv + 15) / 16; }
+
+inline bool gdr_shape(int64_t N, int32_t nseq, int32_t heads, int32_t key_heads, int32_t dk, int32_t dv) {
+    return N >= 0 && N <= (int64_t)1 << 30 && nseq >= 1 && heads >= 1 && heads <= kMostHeads && key_heads >= 1 && heads % key_heads == 0 && dk >= 1 && dv >= 1;
+}
+
+inline grim_status gdr_check(grim_dtype dt, int64_t N, int32_t nseq, bool starts, int32_t heads, int32_t key_heads, int32_t dk, int32_t dv, float scale, float eps) {
+    if (!known(dt)) return GRIM_ERR_DTYPE;
+    if (!gdr_shape(N, nseq, heads, key_heads, dk, dv) || (nseq > 1 && !starts) || !(fabsf(scale) < INFINITY) || !(eps >= 0.f) || eps > 3.4e38f) return GRIM_ERR_SHAPE;
+    if (dk > kMostHeadSize || dv > kMostHeadSize || (int64_t)nseq * heads > (int64_t)1 << 23) return GRIM_ERR_UNSUPPORTED;
+    return GRIM_OK;
+}
+
+// Tokens of a run.  Runs are what fills the compute units where sequences and heads are few: as many as there are for two workgroups each, of eight chunks or more (what a run
+// does to the states has to be formed first, which costs more than the run itself, and the runs' maps are joined one after another).
+template <typename T>
+uint32_t run_of(int64_t N, int32_t nseq, int32_t heads, int32_t dv) {
+    constexpr int64_t C = Gdr<T>::chunk, least = 8 * C;
+    const int64_t each = (int64_t)heads * ((tiles_of(dv) + 7) / 8);
+    const int64_t runs = 2 * kComputeUnits / each;
+    if (runs < 2 || N < 2 * least || N / nseq < least) return (uint32_t)1 << 31;
+    const int64_t size = ((N + runs - 1) / runs + C - 1) / C * C;
+    return (uint32_t)(size < least ? least : size);
+}
+inline int64_t runs_of(int64_t N, int32_t nseq, uint32_t size) { return N / size + nseq; }
+
+// Bytes of what a call keeps, section by section: of the chunks their matrices, the states in front of them and E (or their gradients, and E's); of the runs their maps, and
+// the states in front of them (or the gradients behind them).
+template <typename T>
+struct GdrRoom {
+    int64_t saved, maps, states, E, starts;
+    GdrRoom(int64_t N, int32_t nseq, int32_t heads, int32_t dk, int32_t dv) {
+        const int64_t places = places_of<T>(N, nseq) * heads, d = padded(dk), columns = 16 * tiles_of(dv);
+        const uint32_t size = run_of<T>(N, nseq, heads, dv);
+        const int64_t runs = size < N ? runs_of(N, nseq, size) * heads : 0;
+        saved = places * Saved<T>::bytes, states = places * columns * d * 4, E = places * columns * Gdr<T>::chunk * 4;
+        maps = runs * d * d * 4, starts = runs * columns * d * 4;
+    }
+    int64_t kept() const { return saved + maps + states + E; }
+    int64_t scratch() const {                               // forward without keeping, or backward
+        const int64_t forward = saved + maps + starts, backward = starts + states + E;
+        return forward > backward ? forward : backward;
+    }
+};
+
+// S_(r + 1) = A_r S_r + B_r from run to run of every sequence and head; BACK: the gradients, the other way through the transposed maps (lm_gdr_join.hip).
+template <typename T, int DK, bool BACK>
+grim_status join_runs(const GdrParams &p, hipStream_t stream);
+
+// The gradients of queries, keys, decays and betas from what the chunks left (lm_gdr_grad.hip).
+template <typename T, int DK, bool WHOLE>
+grim_status gdr_gradients(const GdrBack &b, hipStream_t stream);
 
 }  // namespace lm
 }  // namespace grim

@@ -1,0 +1,278 @@
+// The gated delta rule over packed sequences, backward: the gradients that mix columns of the states.
+//
+// In the notation of lm_gdr.hip and lm_gdr_back.hip, for every chunk by itself, with keys and queries as they count (r the factor of the raw ones):
+//     dQ   = exp(G) dy S' + dP K          dP_ij =   w_ij dy_i . U_j (i >= j)
+//     dK_r = -exp(G) Y S' + dL K          dL_ij = - w_ij  Y_i . U_j (i > j)
+//     dK_c = dP' Q + dL' K,    dK_e = exp(G_end - G) U A'           dK = dK_r + dK_c + dK_e
+//     dg_i = exp(G_end) <S, A> + sum over j >= i of (dQ . Q + dK_r . K - dK_c . K)_j + sum over j < i of (dK_e . K)_j        dbeta = F . E
+// and back through the division by the lengths.  A workgroup takes a chunk and a key head and goes through the heads that read it, so that
+// their sums need no atomics; a wave has 16 rows of the states (16 elements of keys and queries), whose states come from memory straight into its operands.
+#include "lm_gdr.hpp"
+
+namespace grim {
+namespace lm {
+
+// What a workgroup keeps in LDS: columns of the values VB at a time; dP and dL, in parts and with all factors, come where U, Y and dy were.
+template <typename T, int DK>
+struct GradRoom {
+    static constexpr int C = Gdr<T>::chunk, PD = Gdr<T>::data, PC = Gdr<T>::comp, VB = 64, W = DK / 16;
+    using Keys = Tile<PD, C, DK, TURNED>;
+    using Rows_ = Tile<PD, C, VB, PAIRED>;
+    using Cols = Tile<PC, VB, C, TURNED>;                   // U and Y, a column's tokens in a row
+    using Square = Tile<PC, C, C, TURNED>;
+    static constexpr int keys = 0, queries = keys + Keys::bytes, dy = queries + Keys::bytes, U = dy + Rows_::bytes, Y = U + Cols::bytes, end1 = Y + Cols::bytes;
+    static constexpr int P = dy, L = P + Square::bytes, end2 = L + Square::bytes, G = end1 > end2 ? end1 : end2, tokens = G + C * 8, sums = tokens + C * 24,
+                         states = sums + 2 * W * C * 4, betas = states + W * 4, bytes = betas + W * 16 * 4;
+    static_assert(bytes <= 160 * 1024, "LDS");
+};
+
+// Rows r + lane % 16, elements c + (lane / 16) 4 .. + 3, the parts added up again (exact for 16-bit elements, to 2^-25 in fp32).
+template <int P, int R, int C, int ORDER>
+__device__ __forceinline__ f32x4 elements(const Tile<P, R, C, ORDER> &m, int r, int c) {
+    static_assert(ORDER != PAIRED, "columns in their own order");
+    const int lane = threadIdx.x & 63;
+    f32x4 v = {};
+#pragma unroll
+    for (int p = P - 1; p >= 0; --p) {
+        const s16x4 w = *reinterpret_cast<const s16x4 *>(m.at + p * m.part + (r + (lane & 15)) * m.ld + c + (lane >> 4) * 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] += __builtin_bit_cast(float, (uint32_t)(uint16_t)w[e] << 16);
+    }
+    return v;
+}
+
+template <typename T, int DK, bool WHOLE>
+__global__ void __launch_bounds__(DK * 4, 2) gradients(GdrBack b) {
+    using Room = GradRoom<T, DK>;
+    constexpr int C = Room::C, PD = Room::PD, PC = Room::PC, VB = Room::VB, W = Room::W, THREADS = 64 * W, TT = C / 16, SS = C / 32, DT = DK / 16;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const GdrParams &p = b.p;
+    const typename Room::Keys K{reinterpret_cast<uint16_t *>(lds + Room::keys)}, Q{reinterpret_cast<uint16_t *>(lds + Room::queries)};
+    const typename Room::Rows_ dY{reinterpret_cast<uint16_t *>(lds + Room::dy)};
+    const typename Room::Cols U{reinterpret_cast<uint16_t *>(lds + Room::U)}, Y{reinterpret_cast<uint16_t *>(lds + Room::Y)};
+    const typename Room::Square dP{reinterpret_cast<uint16_t *>(lds + Room::P)}, dL{reinterpret_cast<uint16_t *>(lds + Room::L)};
+    double *G = reinterpret_cast<double *>(lds + Room::G);
+    float *tokens = reinterpret_cast<float *>(lds + Room::tokens), *sums = reinterpret_cast<float *>(lds + Room::sums);
+    float *states = reinterpret_cast<float *>(lds + Room::states), *betas = reinterpret_cast<float *>(lds + Room::betas);
+    const float *beta = tokens, *fk = tokens + C, *fu = tokens + 2 * C, *fq = tokens + 3 * C, *rk = tokens + 4 * C, *rq = tokens + 5 * C;
+
+    const int kh = (int)(blockIdx.x % (uint32_t)b.key_heads);
+    const uint32_t place = blockIdx.x / (uint32_t)b.key_heads;
+    const int s = sequence_of(p.seq_start, p.nseq, p.N, C, place);
+    const Span span(p.seq_start, s, p.N);
+    const int64_t first = span.first + (int64_t)(place - place_of(span, s, C)) * C;
+    if (first >= span.end) return;
+    const int rows = (int)min((int64_t)C, span.end - first);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l15 = lane & 15, g4 = (lane >> 4) * 4, own = l15 * 16 + g4, turned_own = g4 * 16 + l15, d0 = 16 * wave;
+    {
+        Rows<WHOLE, T, THREADS, C, DK> k, q;
+        k.fetch(static_cast<const T *>(p.k) + first * p.ldk + (int64_t)kh * p.dk, p.ldk, rows, p.dk);
+        q.fetch(static_cast<const T *>(p.q) + first * p.ldq + (int64_t)kh * p.dk, p.ldq, rows, p.dk);
+        k.place(K, rows, p.dk);
+        q.place(Q, rows, p.dk);
+    }
+    f32x4 dq[TT] = {}, dk[TT] = {};                         // elements d0 + g4 .. + 3 of token 16 t + l15, sums over the heads
+    for (int h = kh * p.group; h < (kh + 1) * p.group; ++h) {
+        const int64_t chunk = (int64_t)place * p.heads + h;
+        __syncthreads();                                    // (the head before is done with everything)
+        const Saved<T> saved(p, place, h);
+        for (int i = threadIdx.x; i < 6 * C; i += THREADS) tokens[i] = saved.tokens()[i];
+        if (threadIdx.x < C) G[threadIdx.x] = saved.G()[threadIdx.x];
+        f32x4 q[TT] = {}, kr[TT] = {}, ke[TT] = {}, db = {};
+        constexpr int pairs = C == 64 ? 12 : 4, PP = (pairs + W - 1) / W;      // of 16 x 16 of dP and dL that are read
+        f32x4 gp[PP] = {}, gl[PP] = {};
+        const auto pair = [&](int i, int &t, int &j) {
+            const int n = i * W + wave;
+            t = n < 4 ? n / 2 : 2 + (n - 4) / 4, j = n < 4 ? n % 2 : (n - 4) % 4;
+            return n < pairs;
+        };
+        float sa = 0.f;
+        for (int v0 = 0; v0 < p.dv; v0 += VB) {
+            const int tile0 = v0 / 16, there = min(VB / 16, p.tiles - tile0);
+            // operands of the states: row d0 + l15, columns g4 .. + 3 of a tile
+            constexpr int EACH = VB / 16 * TT / W;
+            static_assert(EACH * W == VB / 16 * TT && W % TT == 0, "tiles of U to the waves");
+            f32x4 S[VB / 16], A[VB / 16], e[EACH], f[EACH];
+            Rows<WHOLE, T, THREADS, C, VB> y;
+            y.fetch(static_cast<const T *>(b.dy) + first * b.lddy + (int64_t)h * p.dv + v0, b.lddy, rows, p.dv - v0);
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) {
+                const int n = i * W + wave, v = n / TT, t = n % TT;
+                const int64_t at = ((chunk * p.tiles + tile0 + min(v, there - 1)) * TT + t) * 256 + own;
+                e[i] = *reinterpret_cast<const f32x4 *>(p.E + at), f[i] = *reinterpret_cast<const f32x4 *>(b.F + at);
+            }
+#pragma unroll
+            for (int v = 0; v < VB / 16; ++v)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int64_t at = ((chunk * p.tiles + tile0 + min(v, there - 1)) * DT + wave) * 256 + turned_own + 16 * i;
+                    S[v][i] = p.states[at], A[v][i] = b.A[at];
+                }
+            __syncthreads();                                // (tokens are there; the columns before are done with)
+            y.place(dY, rows, p.dv - v0);
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) {
+                const int n = i * W + wave, v = n / TT, t = n % TT;
+                if (v >= there) e[i] = f[i] = f32x4{};
+                const f32x4 bt = *reinterpret_cast<const f32x4 *>(beta + 16 * t + g4);
+                db += e[i] * f[i];
+                put4(U, 16 * v + l15, 16 * t + g4, e[i] * bt);
+                put4(Y, 16 * v + l15, 16 * t + g4, f[i] * bt);
+            }
+#pragma unroll
+            for (int v = 0; v < VB / 16; ++v) {
+                if (v >= there) S[v] = A[v] = f32x4{};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sa = __builtin_fmaf(S[v][i], A[v][i], sa);
+            }
+            __syncthreads();
+#pragma unroll
+            for (int v = 0; v < VB / 32; ++v) {
+                const Frag<PC> fs = operand<PC>(S[2 * v], S[2 * v + 1]), fa = operand<PC>(A[2 * v], A[2 * v + 1]);
+#pragma unroll
+                for (int t = 0; t < TT; ++t) {
+                    q[t] = multiply(fs, along(dY, 16 * t, 32 * v), q[t]);
+                    kr[t] = multiply(fs, across(Y, 16 * t, 32 * v), kr[t]);
+                    ke[t] = multiply(fa, across(U, 16 * t, 32 * v), ke[t]);
+                }
+#pragma unroll
+                for (int i = 0; i < PP; ++i) {
+                    int t, j;
+                    if (!pair(i, t, j)) continue;
+                    const Frag<PC> u = across(U, 16 * j, 32 * v);
+                    gp[i] = multiply(u, along(dY, 16 * t, 32 * v), gp[i]);
+                    gl[i] = multiply(u, across(Y, 16 * t, 32 * v), gl[i]);
+                }
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < PP; ++i) {
+            int t, j;
+            if (!pair(i, t, j)) continue;
+            t = 16 * t + l15, j = 16 * j + g4;
+            const double Gt = G[t];
+            const float kt = rk[t], qt = rq[t];
+            f32x4 a, c;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float w = t >= j + e ? decay_of(Gt - G[j + e]) * rk[j + e] : 0.f;
+                a[e] = t >= j + e ? w * qt * gp[i][e] : 0.f, c[e] = t > j + e ? -w * kt * gl[i][e] : 0.f;
+            }
+            put4(dP, t, j, a);
+            put4(dL, t, j, c);
+        }
+        __syncthreads();
+        f32x4 kc[TT] = {};
+#pragma unroll
+        for (int t = 0; t < TT; ++t) {
+            q[t] *= fq[16 * t + l15], kr[t] *= -fk[16 * t + l15], ke[t] *= fu[16 * t + l15];
+        }
+#pragma unroll
+        for (int x = 0; x < SS; ++x) {
+            const Frag<PD> fk_ = across(K, d0, 32 * x), fq_ = across(Q, d0, 32 * x);
+#pragma unroll
+            for (int t = 2 * x; t < TT; ++t) {              // (sums over j, 32 of them from 32 x, for the tokens from there on)
+                q[t] = multiply(fk_, along(dP, 16 * t, 32 * x), q[t]);
+                kr[t] = multiply(fk_, along(dL, 16 * t, 32 * x), kr[t]);
+            }
+#pragma unroll
+            for (int j = 0; j < 2 * x + 2; ++j) {           // (sums over t)
+                kc[j] = multiply(fq_, across(dP, 16 * j, 32 * x), kc[j]);
+                kc[j] = multiply(fk_, across(dL, 16 * j, 32 * x), kc[j]);
+            }
+        }
+        // what the decays get of it
+#pragma unroll
+        for (int t = 0; t < TT; ++t) {
+            const f32x4 kv = elements(K, 16 * t, d0), qv = elements(Q, 16 * t, d0);
+            const f32x4 m = q[t] * qv + (kr[t] - kc[t]) * kv, n = ke[t] * kv;
+            const float from_here = across_rows(m[0] + m[1] + (m[2] + m[3]), Add()), before = across_rows(n[0] + n[1] + (n[2] + n[3]), Add());
+            if (lane < 16) sums[wave * C + 16 * t + l15] = from_here, sums[(W + wave) * C + 16 * t + l15] = before;
+            dq[t] += q[t];
+            dk[t] += kr[t] + kc[t] + ke[t];
+        }
+        sa = wave_sum(sa);
+        if (lane == 0) states[wave] = sa;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float one = row_join(db[e], Add());
+            if (l15 == 0) betas[wave * 16 + g4 + e] = one;
+        }
+        __syncthreads();
+        if (wave == 0) {
+            float a = 0.f, n = 0.f, all = 0.f, d = 0.f;
+            const int at = lane % C;
+#pragma unroll
+            for (int w = 0; w < W; ++w) a += sums[w * C + at], n += sums[(W + w) * C + at], all += states[w];
+#pragma unroll
+            for (int w = 0; w < W / TT; ++w) d += betas[(w * TT + at / 16) * 16 + at % 16];
+            float before = n;
+#pragma unroll
+            for (int x = 1; x < C; x *= 2) {
+                const float after = __shfl_down(a, x, C), less = __shfl_up(before, x, C);
+                if (at + x < C) a += after;
+                if (at >= x) before += less;
+            }
+            before = __shfl_up(before, 1, C);
+            if (at == 0) before = 0.f;
+            if (lane < rows) {
+                const int64_t t = first + lane;
+                b.ddecay[t * b.lddg + h] = p.decay[t * p.ldg + h] < kLeastDecay ? 0.f : a + before + decay_of(G[C - 1]) * all;
+                b.dbeta[t * b.lddg + h] = d;
+            }
+        }
+    }
+    // through the division by the lengths: d(x / |x|) = (dx - x (x . dx) / |x|^2) / |x|, of which the last division is made already
+    if (p.norm_eps > 0.f) {
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < TT; ++t) {
+            const f32x4 m = dq[t] * elements(Q, 16 * t, d0), n = dk[t] * elements(K, 16 * t, d0);
+            const float mq = across_rows(m[0] + m[1] + (m[2] + m[3]), Add()), mk = across_rows(n[0] + n[1] + (n[2] + n[3]), Add());
+            if (lane < 16) sums[wave * C + 16 * t + l15] = mq, sums[(W + wave) * C + 16 * t + l15] = mk;
+        }
+        __syncthreads();
+        const float unscale = p.scale != 0.f ? 1.f / p.scale : 0.f;
+#pragma unroll
+        for (int t = 0; t < TT; ++t) {
+            const int i = 16 * t + l15;
+            float mq = 0.f, mk = 0.f;
+#pragma unroll
+            for (int w = 0; w < W; ++w) mq += sums[w * C + i], mk += sums[(W + w) * C + i];
+            const float iq = rq[i] * unscale, ik = rk[i];
+            dq[t] -= elements(Q, 16 * t, d0) * iq * (iq * mq);
+            dk[t] -= elements(K, 16 * t, d0) * ik * (ik * mk);
+        }
+    }
+    T *q_to = static_cast<T *>(b.dq) + first * b.lddq + (int64_t)kh * p.dk, *k_to = static_cast<T *>(b.dk) + first * b.lddk + (int64_t)kh * p.dk;
+#pragma unroll
+    for (int t = 0; t < TT; ++t) {
+        const int i = 16 * t + l15;
+        if (i >= rows) continue;
+        leave<WHOLE>(q_to + i * b.lddq, d0 + g4, p.dk, dq[t]);
+        leave<WHOLE>(k_to + i * b.lddk, d0 + g4, p.dk, dk[t]);
+    }
+}
+
+template <typename T, int DK, bool WHOLE>
+grim_status gdr_gradients(const GdrBack &b, hipStream_t stream) {
+    constexpr int bytes = GradRoom<T, DK>::bytes;
+    const auto kernel = gradients<T, DK, WHOLE>;
+    static const hipError_t grown = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (grown != hipSuccess) return GRIM_ERR_DEVICE;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(places_of<T>(b.p.N, b.p.nseq) * b.key_heads)), dim3(DK * 4), bytes, stream, b);
+    return launched();
+}
+
+#define GRADIENTS(T)                                                                    \
+    template grim_status gdr_gradients<T, 64, false>(const GdrBack &, hipStream_t);     \
+    template grim_status gdr_gradients<T, 64, true>(const GdrBack &, hipStream_t);      \
+    template grim_status gdr_gradients<T, 128, false>(const GdrBack &, hipStream_t);    \
+    template grim_status gdr_gradients<T, 128, true>(const GdrBack &, hipStream_t);
+GRADIENTS(float)
+GRADIENTS(f16)
+GRADIENTS(bf16)
+
+}  // namespace lm
+}  // namespace grim

@@ -35,6 +35,8 @@ ARGTYPES = {
     "grim_gdr_states": [_I64, _I32, _I32, _I32, _I32],
     "grim_gdr_workspace": [_I64, _I32, _I32, _I32, _I32, _I32],
     "grim_gdr_sequence": [_P, _P, _P, _I32, _I64, _I64, _I64, _P, _P, _I64, _P, _P, _I32, _I64, _I32, _I32, _I32, _I32, _F, _F, _P, _I64, _P, _P, _P, _I64, _P],
+    "grim_gdr_sequence_backward": [_P, _P, _P, _I32, _I64, _I64, _I64, _P, _P, _I64, _P, _P, _I32, _I64, _I32, _I32, _I32, _I32, _F, _F, _P, _P, _I64, _P, _P, _I64, _P, _I64, _P, _I64,
+                                   _P, _P, _I64, _P, _P, _I64, _P],
     "grim_gdr_step": [_P, _P, _P, _I64, _I64, _I64, _P, _P, _I64, _P, _P, _P, _I32, _I64, _I32, _I32, _I32, _I32, _F, _F, _I32, _P],
     "grim_policy_loss_workspace": [_I64, _I64],
     "grim_policy_loss": [_P, _I32, _I64, _P, _I64, _I64, _P, _P, _P, _I64, _P, _I64, _P],
@@ -194,6 +196,18 @@ def gdr_sequence(q, k, v, dtype, ldq: int, ldk: int, ldv: int, decay, beta, ldg:
                                   heads, key_heads, Dk, Dv, scale, norm_eps, _at(y), ldy, _at(s_last), _at(states), ws, room, _on(stream))
     if status:
         raise GrimError(status, "grim_gdr_sequence")
+
+
+def gdr_sequence_backward(q, k, v, dtype, ldq: int, ldk: int, ldv: int, decay, beta, ldg: int, s0, seq_start, nseq: int, N: int, heads: int,
+                          key_heads: int, Dk: int, Dv: int, scale: float, norm_eps: float, states, dy, lddy: int, ds_last, dq, lddq: int, dk, lddk: int,
+                          dv, lddv: int, ddecay, dbeta, lddg: int, ds0, workspace, stream=None):
+    """grim_gdr_sequence_backward: the gradients of gdr_sequence's inputs, which `states` was left for; `ds_last` and `ds0` may be None."""
+    ws, room = _room(workspace)
+    status = _c.grim_gdr_sequence_backward(_at(q), _at(k), _at(v), _DT_CODE[dtype], ldq, ldk, ldv, _at(decay), _at(beta), ldg, _at(s0), _at(seq_start),
+                                           nseq, N, heads, key_heads, Dk, Dv, scale, norm_eps, _at(states), _at(dy), lddy, _at(ds_last), _at(dq), lddq,
+                                           _at(dk), lddk, _at(dv), lddv, _at(ddecay), _at(dbeta), lddg, _at(ds0), ws, room, _on(stream))
+    if status:
+        raise GrimError(status, "grim_gdr_sequence_backward")
 
 
 def gdr_step(q, k, v, ldq: int, ldk: int, ldv: int, decay, beta, ldg: int, s, s_new, y, dtype, ldy: int, heads: int, key_heads: int,
