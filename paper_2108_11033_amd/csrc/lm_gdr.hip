@@ -35,7 +35,7 @@ __global__ void __launch_bounds__(kMatrixThreads) chunk_matrices(GdrParams p) {
     const int64_t first = span.first + (int64_t)(place - place_of(span, s, C)) * C;
     if (first >= span.end) return;
     const int rows = (int)min((int64_t)C, span.end - first);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l15 = lane & 15, lq = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l15 = lane & 15, lq = lane >> 4;
     Rows<WHOLE, T, kMatrixThreads, C, DK> k, q;
     q.fetch(static_cast<const T *>(p.q) + first * p.ldq + (int64_t)(h / p.group) * p.dk, p.ldq, rows, p.dk);
     k.fetch(static_cast<const T *>(p.k) + first * p.ldk + (int64_t)(h / p.group) * p.dk, p.ldk, rows, p.dk);
@@ -193,7 +193,7 @@ __global__ void __launch_bounds__(64 * W, 2) walk(GdrParams p) {
     if (MAPS ? to >= span.end : from >= to && r > 0) return;            // (an empty sequence has its first run for its last states)
     const bool map = MAPS && block >= (int)value_blocks;
     if (map && r == 0) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l15 = lane & 15, g4 = (lane >> 4) * 4, own = l15 * 16 + g4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l15 = lane & 15, g4 = (lane >> 4) * 4, own = l15 * 16 + g4;
     const int tile0 = ((map ? block - (int)value_blocks : block) * W + wave) * CT, tiles = map ? DT : p.tiles, col0 = map ? 0 : block * COLS;
     const bool idle = tile0 >= tiles;
     const T *q = static_cast<const T *>(p.q) + (int64_t)(h / p.group) * p.dk, *k = static_cast<const T *>(p.k) + (int64_t)(h / p.group) * p.dk;
@@ -278,6 +278,7 @@ __global__ void __launch_bounds__(64 * W, 2) walk(GdrParams p) {
                     const int i = 16 * t + l15;
                     const double Gi = G[i];
                     const float qi = rq[i];
+#pragma unroll 1
                     for (int x = EACH > 1 ? wave % EACH : 0; x < TT; x += EACH) {
                         if (x / 2 > t / 2) break;           // (nobody reads those)
                         f32x4 acc = {};
@@ -320,6 +321,7 @@ __global__ void __launch_bounds__(64 * W, 2) walk(GdrParams p) {
                     for (int c = 0; c < CT; ++c) out[t][c] = multiply(S[d][c], e, out[t][c]);
                 }
         }
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int t = 0; t < TT; ++t) {
             const f32x4 f = *reinterpret_cast<const f32x4 *>(fk + 16 * t + g4);
@@ -337,6 +339,7 @@ __global__ void __launch_bounds__(64 * W, 2) walk(GdrParams p) {
         };
         by(beta, x);
         f32x4 less[TT][CT] = {};
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int t = 0; t < TT; ++t)
 #pragma unroll
@@ -356,6 +359,7 @@ __global__ void __launch_bounds__(64 * W, 2) walk(GdrParams p) {
                 x[t][c] *= bt;                              // U
             }
         }
+        __builtin_amdgcn_sched_barrier(0);
         by(fu, x);
         const float whole = decay_of(G[C - 1]);
 #pragma unroll
@@ -428,13 +432,15 @@ grim_status walk_launch(const GdrParams &p, hipStream_t stream) {
     const auto kernel = walk<T, DK, W, CT, WHOLE, MAPS>;
     static const hipError_t grown = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (grown != hipSuccess) return GRIM_ERR_DEVICE;
-    const int64_t blocks = (p.tiles + CT * W - 1) / (CT * W) + (MAPS ? (DK / 16 + CT * W - 1) / (CT * W) : 0);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(runs_of(p.N, p.nseq, p.size) * p.heads * blocks)), dim3(64 * W), bytes, stream, p);
+    const int64_t blocks = (p.tiles + CT * W - 1) / (CT * W) + (MAPS ? (DK / 16 + CT * W - 1) / (CT * W) : 0), groups = runs_of(p.N, p.nseq, p.size) * p.heads * blocks;
+    if (groups > most_groups(64 * W)) return GRIM_ERR_UNSUPPORTED;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(64 * W), bytes, stream, p);
     return launched();
 }
 
 template <typename T, int DK, bool WHOLE>
 grim_status gdr_launch(const GdrParams &p, hipStream_t stream) {
+    const bool narrow = DK == 64 && p.tiles <= 4;           // (keys of 128 are too much for the registers of four waves: a second four help with them)
     if (p.N > 0) {
         const int64_t places = places_of<T>(p.N, p.nseq);
         if (places > most_groups(kMatrixThreads) / p.heads) return GRIM_ERR_UNSUPPORTED;
@@ -442,13 +448,13 @@ grim_status gdr_launch(const GdrParams &p, hipStream_t stream) {
         grim_status st = launched();
         if (st != GRIM_OK) return st;
         if (p.size < (uint32_t)p.N) {
-            st = p.tiles <= 4 ? walk_launch<T, DK, 4, 1, WHOLE, true>(p, stream) : walk_launch<T, DK, 8, 1, WHOLE, true>(p, stream);
+            st = narrow ? walk_launch<T, 64, 4, 1, WHOLE, true>(p, stream) : walk_launch<T, DK, 8, 1, WHOLE, true>(p, stream);
             if (st != GRIM_OK) return st;
             st = join_runs<T, DK, false>(p, stream);
             if (st != GRIM_OK) return st;
         }
     }
-    return p.tiles <= 4 ? walk_launch<T, DK, 4, 1, WHOLE, false>(p, stream) : walk_launch<T, DK, 8, 1, WHOLE, false>(p, stream);
+    return narrow ? walk_launch<T, 64, 4, 1, WHOLE, false>(p, stream) : walk_launch<T, DK, 8, 1, WHOLE, false>(p, stream);
 }
 
 template <typename T>

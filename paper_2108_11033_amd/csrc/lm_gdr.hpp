@@ -395,7 +395,7 @@ template <typename T>
 uint32_t run_of(int64_t N, int32_t nseq, int32_t heads, int32_t dv) {
     constexpr int64_t C = Gdr<T>::chunk, least = 8 * C;
     const int64_t each = (int64_t)heads * ((tiles_of(dv) + 7) / 8);
-    const int64_t runs = 2 * kComputeUnits / each;
+    const int64_t runs = (tiles_of(dv) > 4 ? 1 : 2) * kComputeUnits / each;
     if (runs < 2 || N < 2 * least || N / nseq < least) return (uint32_t)1 << 31;
     const int64_t size = ((N + runs - 1) / runs + C - 1) / C * C;
     return (uint32_t)(size < least ? least : size);

@@ -51,7 +51,7 @@ __global__ void __launch_bounds__(64 * W, 2) walk_back(GdrBack b) {
     const uint32_t r = run - place_of(span, s, p.size);
     const int64_t from = span.first + (int64_t)r * p.size, to = min(span.end, from + p.size);
     if (from >= to && (MAPS || r > 0) || MAPS && r == 0) return;            // (an empty sequence has its first run for the gradient of its first states)
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l15 = lane & 15, g4 = (lane >> 4) * 4, own = l15 * 16 + g4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l15 = lane & 15, g4 = (lane >> 4) * 4, own = l15 * 16 + g4;
     const int tile = block * W + wave, col0 = block * COLS;
     const bool idle = tile >= p.tiles;
     const T *q = static_cast<const T *>(p.q) + (int64_t)(h / p.group) * p.dk, *k = static_cast<const T *>(p.k) + (int64_t)(h / p.group) * p.dk;
@@ -142,6 +142,7 @@ __global__ void __launch_bounds__(64 * W, 2) walk_back(GdrBack b) {
             for (int d = 0; d < DS; ++d) a[d] = along(K, 16 * t, 32 * d);
             const double Gj = G[j];
             const float kj = rk[j];
+#pragma unroll 1
             for (int x = wave % EACH; x < TT; x += EACH) {
                 if (x / 2 < t / 2) continue;                // (nobody reads those)
                 f32x4 acc = {};
@@ -171,6 +172,7 @@ __global__ void __launch_bounds__(64 * W, 2) walk_back(GdrBack b) {
             }
 #pragma unroll
             for (int t = 0; t < TT; ++t) x[t] *= *reinterpret_cast<const f32x4 *>(fu + 16 * t + g4);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int t = 0; t < SS; ++t) {
                 const f32x4 lo = V.get(32 * t, 16 * wave), hi = V.get(32 * t + 16, 16 * wave);
@@ -200,6 +202,7 @@ __global__ void __launch_bounds__(64 * W, 2) walk_back(GdrBack b) {
                 for (int i = t / 2; i < SS; ++i) x[t] = multiply(along(P, 16 * t, 32 * i), raw[i], x[t]);          // dU
             by(beta, 1.f);
             f32x4 less[TT] = {};
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int t = 0; t < TT; ++t)
 #pragma unroll
@@ -223,6 +226,7 @@ __global__ void __launch_bounds__(64 * W, 2) walk_back(GdrBack b) {
                     if (i < rows) leave<WHOLE>(dv + (first + i) * b.lddv, 16 * tile + g4, p.dv, out);
                 }
             }
+            __builtin_amdgcn_sched_barrier(0);
             by(fk, -1.f);
 #pragma unroll
             for (int d = 0; d < DT; ++d)
@@ -255,22 +259,24 @@ grim_status back_launch(const GdrBack &b, hipStream_t stream) {
     const auto kernel = walk_back<T, DK, W, WHOLE, MAPS>;
     static const hipError_t grown = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (grown != hipSuccess) return GRIM_ERR_DEVICE;
-    const int64_t blocks = (b.p.tiles + W - 1) / W;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(runs_of(b.p.N, b.p.nseq, b.p.size) * b.p.heads * blocks)), dim3(64 * W), bytes, stream, b);
+    const int64_t groups = runs_of(b.p.N, b.p.nseq, b.p.size) * b.p.heads * ((b.p.tiles + W - 1) / W);
+    if (groups > most_groups(64 * W)) return GRIM_ERR_UNSUPPORTED;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(64 * W), bytes, stream, b);
     return launched();
 }
 
 template <typename T, int DK, bool WHOLE>
 grim_status back_all(const GdrBack &b, hipStream_t stream) {
     const GdrParams &p = b.p;
+    const bool narrow = DK == 64 && p.tiles <= 4;           // (as in the forward pass)
     grim_status st;
     if (p.N > 0 && p.size < (uint32_t)p.N) {
-        st = p.tiles <= 4 ? back_launch<T, DK, 4, WHOLE, true>(b, stream) : back_launch<T, DK, 8, WHOLE, true>(b, stream);
+        st = narrow ? back_launch<T, 64, 4, WHOLE, true>(b, stream) : back_launch<T, DK, 8, WHOLE, true>(b, stream);
         if (st != GRIM_OK) return st;
         st = join_runs<T, DK, true>(p, stream);
         if (st != GRIM_OK) return st;
     }
-    st = p.tiles <= 4 ? back_launch<T, DK, 4, WHOLE, false>(b, stream) : back_launch<T, DK, 8, WHOLE, false>(b, stream);
+    st = narrow ? back_launch<T, 64, 4, WHOLE, false>(b, stream) : back_launch<T, DK, 8, WHOLE, false>(b, stream);
     if (st != GRIM_OK || p.N == 0) return st;
     return gdr_gradients<T, DK, WHOLE>(b, stream);
 }

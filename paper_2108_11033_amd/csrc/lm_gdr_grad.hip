@@ -15,15 +15,31 @@ namespace lm {
 // What a workgroup keeps in LDS: columns of the values VB at a time; dP and dL, in parts and with all factors, come where U, Y and dy were.
 template <typename T, int DK>
 struct GradRoom {
-    static constexpr int C = Gdr<T>::chunk, PD = Gdr<T>::data, PC = Gdr<T>::comp, VB = 64, W = DK / 16;
+    static constexpr int C = Gdr<T>::chunk, PD = Gdr<T>::data, PC = Gdr<T>::comp, VB = 32, W = DK / 16;
     using Keys = Tile<PD, C, DK, TURNED>;
-    using Rows_ = Tile<PD, C, VB, PAIRED>;
+    using Values_ = Tile<PD, C, VB, PAIRED>;
     using Cols = Tile<PC, VB, C, TURNED>;                   // U and Y, a column's tokens in a row
     using Square = Tile<PC, C, C, TURNED>;
-    static constexpr int keys = 0, queries = keys + Keys::bytes, dy = queries + Keys::bytes, U = dy + Rows_::bytes, Y = U + Cols::bytes, end1 = Y + Cols::bytes;
+    static constexpr int keys = 0, queries = keys + Keys::bytes, dy = queries + Keys::bytes, U = dy + Values_::bytes, Y = U + Cols::bytes, end1 = Y + Cols::bytes;
     static constexpr int P = dy, L = P + Square::bytes, end2 = L + Square::bytes, G = end1 > end2 ? end1 : end2, tokens = G + C * 8, sums = tokens + C * 24,
                          states = sums + 2 * W * C * 4, betas = states + W * 4, bytes = betas + W * 16 * 4;
     static_assert(bytes <= 160 * 1024, "LDS");
+};
+
+template <typename T, int DK>
+struct GradTiles {
+    using Room = GradRoom<T, DK>;
+    typename Room::Keys K, Q;
+    typename Room::Values_ dY;
+    typename Room::Cols U, Y;
+    typename Room::Square dP, dL;
+    // (The compiler is kept from seeing that the addresses are the same every time: it holds dozens of them in registers across the loops otherwise, and spills.)
+    __device__ __forceinline__ GradTiles(char *lds) {
+        int again = 0;
+        asm volatile("" : "+s"(again));
+        const auto tile = [&](int at) { return reinterpret_cast<uint16_t *>(lds + again + at); };
+        K.at = tile(Room::keys), Q.at = tile(Room::queries), dY.at = tile(Room::dy), U.at = tile(Room::U), Y.at = tile(Room::Y), dP.at = tile(Room::P), dL.at = tile(Room::L);
+    }
 };
 
 // Rows r + lane % 16, elements c + (lane / 16) 4 .. + 3, the parts added up again (exact for 16-bit elements, to 2^-25 in fp32).
@@ -44,113 +60,136 @@ __device__ __forceinline__ f32x4 elements(const Tile<P, R, C, ORDER> &m, int r, 
 template <typename T, int DK, bool WHOLE>
 __global__ void __launch_bounds__(DK * 4, 2) gradients(GdrBack b) {
     using Room = GradRoom<T, DK>;
-    constexpr int C = Room::C, PD = Room::PD, PC = Room::PC, VB = Room::VB, W = Room::W, THREADS = 64 * W, TT = C / 16, SS = C / 32, DT = DK / 16;
+    constexpr int C = Room::C, PD = Room::PD, PC = Room::PC, VB = Room::VB, W = Room::W, THREADS = 64 * W, TT = C / 16, SS = C / 32, DT = DK / 16, VT = VB / 16;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const GdrParams &p = b.p;
-    const typename Room::Keys K{reinterpret_cast<uint16_t *>(lds + Room::keys)}, Q{reinterpret_cast<uint16_t *>(lds + Room::queries)};
-    const typename Room::Rows_ dY{reinterpret_cast<uint16_t *>(lds + Room::dy)};
-    const typename Room::Cols U{reinterpret_cast<uint16_t *>(lds + Room::U)}, Y{reinterpret_cast<uint16_t *>(lds + Room::Y)};
-    const typename Room::Square dP{reinterpret_cast<uint16_t *>(lds + Room::P)}, dL{reinterpret_cast<uint16_t *>(lds + Room::L)};
     double *G = reinterpret_cast<double *>(lds + Room::G);
     float *tokens = reinterpret_cast<float *>(lds + Room::tokens), *sums = reinterpret_cast<float *>(lds + Room::sums);
     float *states = reinterpret_cast<float *>(lds + Room::states), *betas = reinterpret_cast<float *>(lds + Room::betas);
-    const float *beta = tokens, *fk = tokens + C, *fu = tokens + 2 * C, *fq = tokens + 3 * C, *rk = tokens + 4 * C, *rq = tokens + 5 * C;
+    const float *fk = tokens + C, *fu = tokens + 2 * C, *fq = tokens + 3 * C, *rk = tokens + 4 * C, *rq = tokens + 5 * C;
 
-    const int kh = (int)(blockIdx.x % (uint32_t)b.key_heads);
+    const int kh = (int)(blockIdx.x % (uint32_t)b.key_heads), head0 = kh * p.group, head1 = head0 + p.group;
     const uint32_t place = blockIdx.x / (uint32_t)b.key_heads;
     const int s = sequence_of(p.seq_start, p.nseq, p.N, C, place);
     const Span span(p.seq_start, s, p.N);
     const int64_t first = span.first + (int64_t)(place - place_of(span, s, C)) * C;
     if (first >= span.end) return;
     const int rows = (int)min((int64_t)C, span.end - first);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l15 = lane & 15, g4 = (lane >> 4) * 4, own = l15 * 16 + g4, turned_own = g4 * 16 + l15, d0 = 16 * wave;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l15 = lane & 15, g4 = (lane >> 4) * 4, d0 = 16 * wave;
+    const uint32_t own = l15 * 16 + g4, turned_own = g4 * 16 + l15;
+
+    // what the next VB columns bring (operands of the states: row d0 + l15, columns g4 .. + 3 of a tile), and the next head
+    constexpr int EACH = (VT * TT + W - 1) / W, TP = (6 * C + THREADS - 1) / THREADS;
+    static_assert(W % TT == 0, "a wave has the same tokens of all its tiles of U");
+    const int own_t = wave % TT;
+    f32x4 S[VT], A[VT], e[EACH], f[EACH], bt;
+    Rows<WHOLE, T, THREADS, C, VB> y;
+    float tn[TP];
+    double Gn;
+    float gn;
+    const auto fetch = [&](int h, int v0) {
+        const int64_t chunk = (int64_t)place * p.heads + h;
+        const int tile0 = v0 / 16, there = p.tiles - tile0;
+#pragma unroll
+        for (int v = 0; v < VT; ++v) {
+            const int64_t at = ((chunk * p.tiles + tile0 + min(v, there - 1)) * DT + wave) * 256;
+            const float *from_s = p.states + at, *from_a = b.A + at;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) S[v][i] = from_s[turned_own + 16 * i], A[v][i] = from_a[turned_own + 16 * i];
+        }
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const int64_t at = ((chunk * p.tiles + tile0 + min((i * W + wave) / TT, min(VT, there) - 1)) * TT + own_t) * 256;
+            const float *from_e = p.E + at, *from_f = b.F + at;
+            e[i] = *reinterpret_cast<const f32x4 *>(from_e + own), f[i] = *reinterpret_cast<const f32x4 *>(from_f + own);
+        }
+        y.fetch(static_cast<const T *>(b.dy) + first * b.lddy + (int64_t)h * p.dv + v0, b.lddy, rows, p.dv - v0);
+        const Saved<T> saved(p, place, h);                  // (for all columns, which keeps the loads in one line)
+#pragma unroll
+        for (int i = 0; i < TP; ++i) tn[i] = saved.tokens()[min(i * THREADS + (int)threadIdx.x, 6 * C - 1)];
+        Gn = saved.G()[threadIdx.x % C];
+        gn = p.decay[(first + min(lane, rows - 1)) * p.ldg + h];
+        bt = *reinterpret_cast<const f32x4 *>(saved.tokens() + 16 * own_t + g4);
+    };
     {
         Rows<WHOLE, T, THREADS, C, DK> k, q;
         k.fetch(static_cast<const T *>(p.k) + first * p.ldk + (int64_t)kh * p.dk, p.ldk, rows, p.dk);
         q.fetch(static_cast<const T *>(p.q) + first * p.ldq + (int64_t)kh * p.dk, p.ldq, rows, p.dk);
-        k.place(K, rows, p.dk);
-        q.place(Q, rows, p.dk);
+        fetch(head0, 0);
+        const GradTiles<T, DK> m(lds);
+        k.place(m.K, rows, p.dk);
+        q.place(m.Q, rows, p.dk);
     }
     f32x4 dq[TT] = {}, dk[TT] = {};                         // elements d0 + g4 .. + 3 of token 16 t + l15, sums over the heads
-    for (int h = kh * p.group; h < (kh + 1) * p.group; ++h) {
-        const int64_t chunk = (int64_t)place * p.heads + h;
-        __syncthreads();                                    // (the head before is done with everything)
-        const Saved<T> saved(p, place, h);
-        for (int i = threadIdx.x; i < 6 * C; i += THREADS) tokens[i] = saved.tokens()[i];
-        if (threadIdx.x < C) G[threadIdx.x] = saved.G()[threadIdx.x];
-        f32x4 q[TT] = {}, kr[TT] = {}, ke[TT] = {}, db = {};
-        constexpr int pairs = C == 64 ? 12 : 4, PP = (pairs + W - 1) / W;      // of 16 x 16 of dP and dL that are read
-        f32x4 gp[PP] = {}, gl[PP] = {};
-        const auto pair = [&](int i, int &t, int &j) {
-            const int n = i * W + wave;
-            t = n < 4 ? n / 2 : 2 + (n - 4) / 4, j = n < 4 ? n % 2 : (n - 4) % 4;
-            return n < pairs;
-        };
-        float sa = 0.f;
-        for (int v0 = 0; v0 < p.dv; v0 += VB) {
-            const int tile0 = v0 / 16, there = min(VB / 16, p.tiles - tile0);
-            // operands of the states: row d0 + l15, columns g4 .. + 3 of a tile
-            constexpr int EACH = VB / 16 * TT / W;
-            static_assert(EACH * W == VB / 16 * TT && W % TT == 0, "tiles of U to the waves");
-            f32x4 S[VB / 16], A[VB / 16], e[EACH], f[EACH];
-            Rows<WHOLE, T, THREADS, C, VB> y;
-            y.fetch(static_cast<const T *>(b.dy) + first * b.lddy + (int64_t)h * p.dv + v0, b.lddy, rows, p.dv - v0);
+    constexpr int pairs = C == 64 ? 12 : 4, PP = (pairs + W - 1) / W;          // of 16 x 16 of dP and dL that are read
+    const auto pair = [&](int i, int &t, int &j) {
+        const int n = i * W + wave;
+        t = n < 4 ? n / 2 : 2 + (n - 4) / 4, j = n < 4 ? n % 2 : (n - 4) % 4;
+        return n < pairs;
+    };
+    f32x4 q[TT] = {}, kr[TT] = {}, ke[TT] = {}, gp[PP] = {}, gl[PP] = {}, db = {};
+    float sa = 0.f, g = 0.f;
+    for (int h = head0, v0 = 0; h < head1;) {
+        const bool done = v0 + VB >= p.dv;                  // with the head
+        {
+            const int there = min(VT, p.tiles - v0 / 16);
+            g = gn;
+            const GradTiles<T, DK> m(lds);
+            __syncthreads();                                // (the columns and the head before are done with)
+#pragma unroll
+            for (int i = 0; i < TP; ++i)
+                if (i * THREADS + (int)threadIdx.x < 6 * C) tokens[i * THREADS + threadIdx.x] = tn[i];
+            if (threadIdx.x < C) G[threadIdx.x] = Gn;
+            y.place(m.dY, rows, p.dv - v0);
 #pragma unroll
             for (int i = 0; i < EACH; ++i) {
-                const int n = i * W + wave, v = n / TT, t = n % TT;
-                const int64_t at = ((chunk * p.tiles + tile0 + min(v, there - 1)) * TT + t) * 256 + own;
-                e[i] = *reinterpret_cast<const f32x4 *>(p.E + at), f[i] = *reinterpret_cast<const f32x4 *>(b.F + at);
+                const int v = (i * W + wave) / TT;
+                if (v >= VT) continue;
+                const float in = v < there ? 1.f : 0.f;     // (what is read twice is finite or hurts the head anyway)
+                db += e[i] * f[i] * in;
+                put4(m.U, 16 * v + l15, 16 * own_t + g4, e[i] * (bt * in));
+                put4(m.Y, 16 * v + l15, 16 * own_t + g4, f[i] * (bt * in));
             }
+            if (there < VT) S[1] = A[1] = f32x4{};
 #pragma unroll
-            for (int v = 0; v < VB / 16; ++v)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int64_t at = ((chunk * p.tiles + tile0 + min(v, there - 1)) * DT + wave) * 256 + turned_own + 16 * i;
-                    S[v][i] = p.states[at], A[v][i] = b.A[at];
-                }
-            __syncthreads();                                // (tokens are there; the columns before are done with)
-            y.place(dY, rows, p.dv - v0);
-#pragma unroll
-            for (int i = 0; i < EACH; ++i) {
-                const int n = i * W + wave, v = n / TT, t = n % TT;
-                if (v >= there) e[i] = f[i] = f32x4{};
-                const f32x4 bt = *reinterpret_cast<const f32x4 *>(beta + 16 * t + g4);
-                db += e[i] * f[i];
-                put4(U, 16 * v + l15, 16 * t + g4, e[i] * bt);
-                put4(Y, 16 * v + l15, 16 * t + g4, f[i] * bt);
-            }
-#pragma unroll
-            for (int v = 0; v < VB / 16; ++v) {
-                if (v >= there) S[v] = A[v] = f32x4{};
+            for (int v = 0; v < VT; ++v) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) sa = __builtin_fmaf(S[v][i], A[v][i], sa);
             }
+            const Frag<PC> fs = operand<PC>(S[0], S[1]), fa = operand<PC>(A[0], A[1]);
+            __builtin_amdgcn_sched_barrier(0);
+            if (!done || h + 1 < head1) fetch(done ? h + 1 : h, done ? 0 : v0 + VB);
             __syncthreads();
 #pragma unroll
-            for (int v = 0; v < VB / 32; ++v) {
-                const Frag<PC> fs = operand<PC>(S[2 * v], S[2 * v + 1]), fa = operand<PC>(A[2 * v], A[2 * v + 1]);
+            for (int t = 0; t < TT; ++t) {
+                __builtin_amdgcn_sched_barrier(0);
+                q[t] = multiply(fs, along(m.dY, 16 * t, 0), q[t]);
+                kr[t] = multiply(fs, across(m.Y, 16 * t, 0), kr[t]);
+                ke[t] = multiply(fa, across(m.U, 16 * t, 0), ke[t]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int t = 0; t < TT; ++t) {
-                    q[t] = multiply(fs, along(dY, 16 * t, 32 * v), q[t]);
-                    kr[t] = multiply(fs, across(Y, 16 * t, 32 * v), kr[t]);
-                    ke[t] = multiply(fa, across(U, 16 * t, 32 * v), ke[t]);
-                }
-#pragma unroll
-                for (int i = 0; i < PP; ++i) {
-                    int t, j;
-                    if (!pair(i, t, j)) continue;
-                    const Frag<PC> u = across(U, 16 * j, 32 * v);
-                    gp[i] = multiply(u, along(dY, 16 * t, 32 * v), gp[i]);
-                    gl[i] = multiply(u, across(Y, 16 * t, 32 * v), gl[i]);
-                }
+            for (int i = 0; i < PP; ++i) {
+                int t, j;
+                if (!pair(i, t, j)) continue;
+                __builtin_amdgcn_sched_barrier(0);
+                const Frag<PC> u = across(m.U, 16 * j, 0);
+                gp[i] = multiply(u, along(m.dY, 16 * t, 0), gp[i]);
+                gl[i] = multiply(u, across(m.Y, 16 * t, 0), gl[i]);
             }
         }
+        v0 += VB;
+        if (!done) continue;
+        const GradTiles<T, DK> m(lds);
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < PP; ++i) {
             int t, j;
+            __builtin_amdgcn_sched_barrier(0);
             if (!pair(i, t, j)) continue;
-            t = 16 * t + l15, j = 16 * j + g4;
+            int low = l15, high = g4;
+            asm volatile("" : "+v"(low), "+v"(high));       // (as above: the comparisons too would be kept)
+            t = 16 * t + low, j = 16 * j + high;
             const double Gt = G[t];
             const float kt = rk[t], qt = rq[t];
             f32x4 a, c;
@@ -159,8 +198,8 @@ __global__ void __launch_bounds__(DK * 4, 2) gradients(GdrBack b) {
                 const float w = t >= j + e ? decay_of(Gt - G[j + e]) * rk[j + e] : 0.f;
                 a[e] = t >= j + e ? w * qt * gp[i][e] : 0.f, c[e] = t > j + e ? -w * kt * gl[i][e] : 0.f;
             }
-            put4(dP, t, j, a);
-            put4(dL, t, j, c);
+            put4(m.dP, t, j, a);
+            put4(m.dL, t, j, c);
         }
         __syncthreads();
         f32x4 kc[TT] = {};
@@ -170,24 +209,30 @@ __global__ void __launch_bounds__(DK * 4, 2) gradients(GdrBack b) {
         }
 #pragma unroll
         for (int x = 0; x < SS; ++x) {
-            const Frag<PD> fk_ = across(K, d0, 32 * x), fq_ = across(Q, d0, 32 * x);
+            __builtin_amdgcn_sched_barrier(0);
+            const Frag<PD> fk_ = across(m.K, d0, 32 * x), fq_ = across(m.Q, d0, 32 * x);
 #pragma unroll
             for (int t = 2 * x; t < TT; ++t) {              // (sums over j, 32 of them from 32 x, for the tokens from there on)
-                q[t] = multiply(fk_, along(dP, 16 * t, 32 * x), q[t]);
-                kr[t] = multiply(fk_, along(dL, 16 * t, 32 * x), kr[t]);
+                __builtin_amdgcn_sched_barrier(0);
+                q[t] = multiply(fk_, along(m.dP, 16 * t, 32 * x), q[t]);
+                kr[t] = multiply(fk_, along(m.dL, 16 * t, 32 * x), kr[t]);
             }
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int j = 0; j < 2 * x + 2; ++j) {           // (sums over t)
-                kc[j] = multiply(fq_, across(dP, 16 * j, 32 * x), kc[j]);
-                kc[j] = multiply(fk_, across(dL, 16 * j, 32 * x), kc[j]);
+                __builtin_amdgcn_sched_barrier(0);
+                kc[j] = multiply(fq_, across(m.dP, 16 * j, 32 * x), kc[j]);
+                kc[j] = multiply(fk_, across(m.dL, 16 * j, 32 * x), kc[j]);
             }
         }
         // what the decays get of it
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int t = 0; t < TT; ++t) {
-            const f32x4 kv = elements(K, 16 * t, d0), qv = elements(Q, 16 * t, d0);
-            const f32x4 m = q[t] * qv + (kr[t] - kc[t]) * kv, n = ke[t] * kv;
-            const float from_here = across_rows(m[0] + m[1] + (m[2] + m[3]), Add()), before = across_rows(n[0] + n[1] + (n[2] + n[3]), Add());
+            __builtin_amdgcn_sched_barrier(0);
+            const f32x4 kv = elements(m.K, 16 * t, d0), qv = elements(m.Q, 16 * t, d0);
+            const f32x4 here = q[t] * qv + (kr[t] - kc[t]) * kv, n = ke[t] * kv;
+            const float from_here = across_rows(here[0] + here[1] + (here[2] + here[3]), Add()), before = across_rows(n[0] + n[1] + (n[2] + n[3]), Add());
             if (lane < 16) sums[wave * C + 16 * t + l15] = from_here, sums[(W + wave) * C + 16 * t + l15] = before;
             dq[t] += q[t];
             dk[t] += kr[t] + kc[t] + ke[t];
@@ -218,18 +263,24 @@ __global__ void __launch_bounds__(DK * 4, 2) gradients(GdrBack b) {
             if (at == 0) before = 0.f;
             if (lane < rows) {
                 const int64_t t = first + lane;
-                b.ddecay[t * b.lddg + h] = p.decay[t * p.ldg + h] < kLeastDecay ? 0.f : a + before + decay_of(G[C - 1]) * all;
+                b.ddecay[t * b.lddg + h] = g < kLeastDecay ? 0.f : a + before + decay_of(G[C - 1]) * all;
                 b.dbeta[t * b.lddg + h] = d;
             }
         }
+#pragma unroll
+        for (int t = 0; t < TT; ++t) q[t] = kr[t] = ke[t] = f32x4{};
+#pragma unroll
+        for (int i = 0; i < PP; ++i) gp[i] = gl[i] = f32x4{};
+        db = f32x4{}, sa = 0.f, v0 = 0, ++h;
     }
     // through the division by the lengths: d(x / |x|) = (dx - x (x . dx) / |x|^2) / |x|, of which the last division is made already
     if (p.norm_eps > 0.f) {
+        const GradTiles<T, DK> m(lds);
         __syncthreads();
 #pragma unroll
         for (int t = 0; t < TT; ++t) {
-            const f32x4 m = dq[t] * elements(Q, 16 * t, d0), n = dk[t] * elements(K, 16 * t, d0);
-            const float mq = across_rows(m[0] + m[1] + (m[2] + m[3]), Add()), mk = across_rows(n[0] + n[1] + (n[2] + n[3]), Add());
+            const f32x4 l = dq[t] * elements(m.Q, 16 * t, d0), n = dk[t] * elements(m.K, 16 * t, d0);
+            const float mq = across_rows(l[0] + l[1] + (l[2] + l[3]), Add()), mk = across_rows(n[0] + n[1] + (n[2] + n[3]), Add());
             if (lane < 16) sums[wave * C + 16 * t + l15] = mq, sums[(W + wave) * C + 16 * t + l15] = mk;
         }
         __syncthreads();
@@ -241,8 +292,8 @@ __global__ void __launch_bounds__(DK * 4, 2) gradients(GdrBack b) {
 #pragma unroll
             for (int w = 0; w < W; ++w) mq += sums[w * C + i], mk += sums[(W + w) * C + i];
             const float iq = rq[i] * unscale, ik = rk[i];
-            dq[t] -= elements(Q, 16 * t, d0) * iq * (iq * mq);
-            dk[t] -= elements(K, 16 * t, d0) * ik * (ik * mk);
+            dq[t] -= elements(m.Q, 16 * t, d0) * iq * (iq * mq);
+            dk[t] -= elements(m.K, 16 * t, d0) * ik * (ik * mk);
         }
     }
     T *q_to = static_cast<T *>(b.dq) + first * b.lddq + (int64_t)kh * p.dk, *k_to = static_cast<T *>(b.dk) + first * b.lddk + (int64_t)kh * p.dk;

@@ -30,7 +30,7 @@ __global__ void __launch_bounds__(256) gdr_step(GdrStepParams p) {
     b /= p.blocks;
     const int h = (int)(b % p.heads);
     const int64_t caller = b / p.heads;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, row = threadIdx.x >> 4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, row = threadIdx.x >> 4;
     const int c = block * kStepColumns + col * 4, have = min(p.dv - c, 4);      // (columns of this thread; none or fewer: <= 0)
     const int64_t key = (int64_t)(h / p.group) * p.dk, head = (caller * p.heads + h) * p.dk;
     float q[ROWS], k[ROWS], d[ROWS][4];
