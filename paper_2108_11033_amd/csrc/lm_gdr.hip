@@ -150,17 +150,35 @@ __global__ void __launch_bounds__(kMatrixThreads) chunk_matrices(GdrParams p) {
 }
 
 // ---------------------------------------------------------------------------------------------------- from chunk to chunk
-// What a workgroup of the walk keeps in LDS.
-template <typename T, int DK, int COLS>
+// What a workgroup of the walk keeps in LDS (MAPS: without queries and what is made of them).
+template <typename T, int DK, int COLS, bool MAPS>
 struct WalkRoom {
     static constexpr int C = Gdr<T>::chunk, PD = Gdr<T>::data, PC = Gdr<T>::comp;
     using Keys = Tile<PD, C, DK>;
     using Queries = Tile<PD, C, DK, PAIRED>;
     using Square = Tile<PC, C, C, PAIRED>;
     using Vals = Values<T, C, COLS>;
-    static constexpr int keys = 0, queries = keys + Keys::bytes, values = queries + Queries::bytes, M = values + Vals::bytes, P = M + Square::bytes, G = P + Square::bytes,
-                         tokens = G + C * 8, bytes = tokens + C * 24;
+    static constexpr int keys = 0, values = keys + Keys::bytes, matrix = values + Vals::bytes, decays = matrix + Square::bytes, factors = decays + C * 8, queries = factors + C * 24,
+                         products = queries + Queries::bytes, bytes = MAPS ? queries : products + Square::bytes;
     static_assert(bytes <= 160 * 1024, "LDS");
+    Keys K;
+    Queries Q;
+    Square M, P;
+    Vals V;
+    double *G;
+    float *tokens;
+    const float *beta, *fk, *fu, *fq, *rk, *rq;
+    // (Made for every chunk.  TIGHT: in a way that keeps the compiler from seeing that nothing changes, or it holds dozens of addresses in registers across the loop, and spills.)
+    template <bool TIGHT>
+    __device__ __forceinline__ WalkRoom(char *lds, std::bool_constant<TIGHT>) {
+        int again = 0;
+        if (TIGHT) asm volatile("" : "+s"(again));
+        char *at = lds + again;
+        K.at = reinterpret_cast<uint16_t *>(at + keys), Q.at = reinterpret_cast<uint16_t *>(at + queries);
+        M.at = reinterpret_cast<uint16_t *>(at + matrix), P.at = reinterpret_cast<uint16_t *>(at + products);
+        V.at = reinterpret_cast<T *>(at + values), G = reinterpret_cast<double *>(at + decays), tokens = reinterpret_cast<float *>(at + factors);
+        beta = tokens, fk = tokens + C, fu = tokens + 2 * C, fq = tokens + 3 * C, rk = tokens + 4 * C, rq = tokens + 5 * C;
+    }
 };
 
 // A workgroup takes 16 CT W columns of the states of a run of chunks of a sequence's head.  All that a chunk does to a column of the states stays in that column, so each of its W waves
@@ -169,18 +187,12 @@ struct WalkRoom {
 // MAPS: no outputs; what every run but a sequence's last does to the states, as S -> A S + B: B's columns (into the places of the states in front of the next run; of a sequence's
 // first run, whose start is known, these are the states themselves) come from a start of zeros, A's from the columns of 1 and values of zero.
 template <typename T, int DK, int W, int CT, bool WHOLE, bool MAPS>
-__global__ void __launch_bounds__(64 * W, 2) walk(GdrParams p) {
+__global__ void __launch_bounds__(64 * W, MAPS && W == 8 && WHOLE ? 4 : 2) walk(GdrParams p) {
     constexpr int C = Gdr<T>::chunk, PD = Gdr<T>::data, PC = Gdr<T>::comp, THREADS = 64 * W, COLS = 16 * CT * W;
     constexpr int TT = C / 16, SS = C / 32, DT = DK / 16, DS = DK / 32;     // tiles of tokens, sums over them; of the states' rows
-    using Room = WalkRoom<T, DK, COLS>;
+    constexpr bool TIGHT = MAPS && W == 8 && WHOLE;                  // (128 registers: two workgroups on a compute unit)
+    using Room = WalkRoom<T, DK, COLS, MAPS>;
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    const typename Room::Keys K{reinterpret_cast<uint16_t *>(lds + Room::keys)};
-    const typename Room::Queries Q{reinterpret_cast<uint16_t *>(lds + Room::queries)};
-    const typename Room::Square M{reinterpret_cast<uint16_t *>(lds + Room::M)}, P{reinterpret_cast<uint16_t *>(lds + Room::P)};
-    const typename Room::Vals V{reinterpret_cast<T *>(lds + Room::values)};
-    double *G = reinterpret_cast<double *>(lds + Room::G);
-    float *tokens = reinterpret_cast<float *>(lds + Room::tokens);
-    const float *beta = tokens, *fk = tokens + C, *fu = tokens + 2 * C, *fq = tokens + 3 * C, *rk = tokens + 4 * C, *rq = tokens + 5 * C;
 
     // (the workgroups of a run, whose heads read the same rows, lie together)
     const uint32_t value_blocks = (p.tiles + CT * W - 1) / (CT * W), blocks = value_blocks + (MAPS ? (DT + CT * W - 1) / (CT * W) : 0), heads = (uint32_t)p.heads;
@@ -237,70 +249,57 @@ __global__ void __launch_bounds__(64 * W, 2) walk(GdrParams p) {
     float tn[TP];
     const int64_t place = place_of(span, s, C) + r * (p.size / C);
     const auto fetch = [&](int64_t n, int64_t first) {
-        const int rows = (int)min((int64_t)C, to - first);
+        const int rows = __builtin_amdgcn_readfirstlane((int)min((int64_t)C, to - first));
         kn.fetch(k + first * p.ldk, p.ldk, rows, p.dk);
         if (!MAPS) qn.fetch(q + first * p.ldq, p.ldq, rows, p.dk);
         vn.fetch(v + first * p.ldv, p.ldv, rows, p.dv - col0);
         const Saved<T> saved(p, place + n, h);
+        uint32_t me = threadIdx.x;
+        if (TIGHT) asm volatile("" : "+v"(me));             // (addresses from the chunk's own, not one in 64 bits for each load held across the loop)
 #pragma unroll
-        for (int i = 0; i < MP; ++i) mn[i] = reinterpret_cast<const u32x4 *>(saved.M())[min(i * THREADS + (int)threadIdx.x, pieces - 1)];
-        Gn = saved.G()[threadIdx.x % C];
+        for (int i = 0; i < MP; ++i) mn[i] = reinterpret_cast<const u32x4 *>(saved.M())[min(i * THREADS + me, pieces - 1u)];
+        Gn = saved.G()[me % C];
 #pragma unroll
-        for (int i = 0; i < TP; ++i) tn[i] = saved.tokens()[min(i * THREADS + (int)threadIdx.x, 6 * C - 1)];
+        for (int i = 0; i < TP; ++i) tn[i] = saved.tokens()[min(i * THREADS + me, 6 * C - 1u)];
     };
     if (from < to) fetch(0, from);
     for (int64_t n = 0, first = from; first < to; ++n, first += C) {
-        const int rows = (int)min((int64_t)C, to - first);
-        kn.place(K, rows, p.dk);
-        if (!MAPS) qn.place(Q, rows, p.dk);
-        vn.keep(V.at, V.ld, map ? 0 : rows, p.dv - col0);
+        const int rows = __builtin_amdgcn_readfirstlane((int)min((int64_t)C, to - first));
+        const Room m(lds, std::bool_constant<TIGHT>());
+        kn.place(m.K, rows, p.dk);
+        if (!MAPS) qn.place(m.Q, rows, p.dk);
+        vn.keep(m.V.at, m.V.ld, map ? 0 : rows, p.dv - col0);
 #pragma unroll
         for (int i = 0; i < MP; ++i) {
             const int piece = i * THREADS + (int)threadIdx.x, e = piece % (C * C / 8) * 8;
-            if (piece < pieces) *reinterpret_cast<u32x4 *>(M.at + piece / (C * C / 8) * M.part + e / C * M.ld + e % C) = mn[i];
+            if (piece < pieces) *reinterpret_cast<u32x4 *>(m.M.at + piece / (C * C / 8) * m.M.part + e / C * m.M.ld + e % C) = mn[i];
         }
-        if (threadIdx.x < C) G[threadIdx.x] = Gn;
+        if (threadIdx.x < C) m.G[threadIdx.x] = Gn;
 #pragma unroll
         for (int i = 0; i < TP; ++i)
-            if (i * THREADS + (int)threadIdx.x < 6 * C) tokens[i * THREADS + threadIdx.x] = tn[i];
+            if (i * THREADS + (int)threadIdx.x < 6 * C) m.tokens[i * THREADS + threadIdx.x] = tn[i];
         if (first + C < to) fetch(n + 1, first + C);
         __syncthreads();
-        // the products of queries and keys: a wave has the queries of a tile and the keys up to them (of W waves W / TT share them)
-        if (!MAPS) {
-            constexpr int EACH = W >= TT ? W / TT : 1;
+        if (!MAPS) {                                        // the products of queries and keys
+#pragma unroll W == 4 ? 3 : 1
+            for (int n = 0; n < Lower<C, W>::each; ++n) {
+                int i, j;
+                if (!Lower<C, W>::get(n, wave, i, j)) continue;
+                f32x4 acc = {};
 #pragma unroll
-            for (int t0 = 0; t0 < TT; t0 += W) {
-                const int t = t0 + (EACH > 1 ? wave / EACH : wave);
-                if (t < TT) {
-                    Frag<PD> a[DS];
+                for (int d = 0; d < DS; ++d) acc = multiply(along(m.K, 16 * j, 32 * d), along(m.Q, 16 * i, 32 * d), acc);
+                i = 16 * i + l15, j = 16 * j + g4;
+                const double Gi = m.G[i];
+                const float qi = m.rq[i];
 #pragma unroll
-                    for (int d = 0; d < DS; ++d) a[d] = along(Q, 16 * t, 32 * d);
-                    const int i = 16 * t + l15;
-                    const double Gi = G[i];
-                    const float qi = rq[i];
-#pragma unroll 1
-                    for (int x = EACH > 1 ? wave % EACH : 0; x < TT; x += EACH) {
-                        if (x / 2 > t / 2) break;           // (nobody reads those)
-                        f32x4 acc = {};
-#pragma unroll
-                        for (int d = 0; d < DS; ++d) acc = multiply(along(K, 16 * x, 32 * d), a[d], acc);
-                        const int j = 16 * x + g4;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[e] = i >= j + e ? decay_of(Gi - G[j + e]) * (qi * rk[j + e]) * acc[e] : 0.f;
-                        put4(P, i, j, acc);
-                    }
-                }
+                for (int e = 0; e < 4; ++e) acc[e] = i >= j + e ? decay_of(Gi - m.G[j + e]) * (qi * m.rk[j + e]) * acc[e] : 0.f;
+                put4(m.P, i, j, acc);
             }
         }
         f32x4 x[TT][CT] = {}, out[TT][CT] = {};             // tokens x columns, columns x tokens
         Frag<PC> u[SS][CT];
         if (!idle) {
         {
-            Frag<PC> S[DS][CT];
-#pragma unroll
-            for (int d = 0; d < DS; ++d)
-#pragma unroll
-                for (int c = 0; c < CT; ++c) S[d][c] = operand<PC>(state[2 * d][c], state[2 * d + 1][c]);
             if (!MAPS && p.states)
 #pragma unroll
                 for (int d = 0; d < DT; ++d)
@@ -309,25 +308,30 @@ __global__ void __launch_bounds__(64 * W, 2) walk(GdrParams p) {
                         if (tile0 + c < p.tiles)
                             *reinterpret_cast<f32x4 *>(p.states + ((((place + n) * p.heads + h) * p.tiles + tile0 + c) * DT + d) * 256 + own) = state[d][c];
 #pragma unroll
-            for (int d = 0; d < DS; ++d)
+            for (int d = 0; d < DS; ++d) {
+                if (TIGHT) __builtin_amdgcn_sched_barrier(0);          // (the operands of all d at once are too many)
+                Frag<PC> S[CT];
+#pragma unroll
+                for (int c = 0; c < CT; ++c) S[c] = operand<PC>(state[2 * d][c], state[2 * d + 1][c]);
 #pragma unroll
                 for (int t = 0; t < TT; ++t) {
-                    const Frag<PD> a = along(K, 16 * t, 32 * d);
+                    const Frag<PD> a = along(m.K, 16 * t, 32 * d);
 #pragma unroll
-                    for (int c = 0; c < CT; ++c) x[t][c] = multiply(a, S[d][c], x[t][c]);
+                    for (int c = 0; c < CT; ++c) x[t][c] = multiply(a, S[c], x[t][c]);
                     if (MAPS) continue;
-                    const Frag<PD> e = along(Q, 16 * t, 32 * d);
+                    const Frag<PD> e = along(m.Q, 16 * t, 32 * d);
 #pragma unroll
-                    for (int c = 0; c < CT; ++c) out[t][c] = multiply(S[d][c], e, out[t][c]);
+                    for (int c = 0; c < CT; ++c) out[t][c] = multiply(S[c], e, out[t][c]);
                 }
+            }
         }
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int t = 0; t < TT; ++t) {
-            const f32x4 f = *reinterpret_cast<const f32x4 *>(fk + 16 * t + g4);
-            const float fo = fq[16 * t + l15];
+            const f32x4 f = *reinterpret_cast<const f32x4 *>(m.fk + 16 * t + g4);
+            const float fo = m.fq[16 * t + l15];
 #pragma unroll
-            for (int c = 0; c < CT; ++c) x[t][c] = V.get(16 * t, 16 * (wave * CT + c)) - f * x[t][c], out[t][c] *= fo;
+            for (int c = 0; c < CT; ++c) x[t][c] = m.V.get(16 * t, 16 * (wave * CT + c)) - f * x[t][c], out[t][c] *= fo;
         }
         const auto by = [&](const float *factor, f32x4 (&a)[TT][CT]) {
 #pragma unroll
@@ -337,38 +341,36 @@ __global__ void __launch_bounds__(64 * W, 2) walk(GdrParams p) {
                 for (int c = 0; c < CT; ++c) u[t][c] = operand<PC>(a[2 * t][c] * lo, a[2 * t + 1][c] * hi);
             }
         };
-        by(beta, x);
-        f32x4 less[TT][CT] = {};
+        by(m.beta, x);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int t = 0; t < TT; ++t)
+        for (int t = 0; t < TT; ++t) {
+            f32x4 less[CT] = {};
 #pragma unroll
             for (int j = 0; j <= t / 2; ++j) {
-                const Frag<PC> m = along(M, 16 * t, 32 * j);
+                const Frag<PC> a = along(m.M, 16 * t, 32 * j);
 #pragma unroll
-                for (int c = 0; c < CT; ++c) less[t][c] = multiply(m, u[j][c], less[t][c]);
+                for (int c = 0; c < CT; ++c) less[c] = multiply(a, u[j][c], less[c]);
             }
-#pragma unroll
-        for (int t = 0; t < TT; ++t) {
-            const f32x4 bt = *reinterpret_cast<const f32x4 *>(beta + 16 * t + g4);
+            const f32x4 bt = *reinterpret_cast<const f32x4 *>(m.beta + 16 * t + g4);
 #pragma unroll
             for (int c = 0; c < CT; ++c) {
-                x[t][c] -= less[t][c];
+                x[t][c] -= less[c];
                 if (!MAPS && p.states && tile0 + c < p.tiles)
                     *reinterpret_cast<f32x4 *>(p.E + ((((place + n) * p.heads + h) * p.tiles + tile0 + c) * TT + t) * 256 + own) = x[t][c];
                 x[t][c] *= bt;                              // U
             }
         }
         __builtin_amdgcn_sched_barrier(0);
-        by(fu, x);
-        const float whole = decay_of(G[C - 1]);
+        by(m.fu, x);
+        const float whole = decay_of(m.G[C - 1]);
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
 #pragma unroll
             for (int c = 0; c < CT; ++c) state[d][c] *= whole;
 #pragma unroll
             for (int j = 0; j < SS; ++j) {
-                const Frag<PD> a = across(K, 16 * d, 32 * j);
+                const Frag<PD> a = across(m.K, 16 * d, 32 * j);
 #pragma unroll
                 for (int c = 0; c < CT; ++c) state[d][c] = multiply(a, u[j][c], state[d][c]);
             }
@@ -388,9 +390,9 @@ __global__ void __launch_bounds__(64 * W, 2) walk(GdrParams p) {
         for (int t = 0; t < TT; ++t) {
 #pragma unroll
             for (int j = 0; j <= t / 2; ++j) {
-                const Frag<PC> m = along(P, 16 * t, 32 * j);
+                const Frag<PC> a = along(m.P, 16 * t, 32 * j);
 #pragma unroll
-                for (int c = 0; c < CT; ++c) out[t][c] = multiply(u[j][c], m, out[t][c]);
+                for (int c = 0; c < CT; ++c) out[t][c] = multiply(u[j][c], a, out[t][c]);
             }
             const int i = 16 * t + l15;
 #pragma unroll
@@ -428,7 +430,7 @@ __global__ void __launch_bounds__(64 * W, 2) walk(GdrParams p) {
 // ---------------------------------------------------------------------------------------------------- launches
 template <typename T, int DK, int W, int CT, bool WHOLE, bool MAPS>
 grim_status walk_launch(const GdrParams &p, hipStream_t stream) {
-    constexpr int bytes = WalkRoom<T, DK, 16 * CT * W>::bytes;
+    constexpr int bytes = WalkRoom<T, DK, 16 * CT * W, MAPS>::bytes;
     const auto kernel = walk<T, DK, W, CT, WHOLE, MAPS>;
     static const hipError_t grown = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (grown != hipSuccess) return GRIM_ERR_DEVICE;

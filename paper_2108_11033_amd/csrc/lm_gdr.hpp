@@ -372,6 +372,17 @@ struct Values {
 // The decay between two places of a chunk.  (The argument's rounding is 2^-24 of it: 8e-7 of a decay to a millionth, less nearer by.)
 __device__ __forceinline__ float decay_of(double from_to) { return __builtin_amdgcn_exp2f((float)from_to); }
 
+// The 16 x 16 of a chunk's lower triangle that sums over 32 tokens read (all of a 32 x 32 block on the diagonal), dealt to the W waves of a workgroup: the i-th of a wave, if there is one.
+template <int C, int W>
+struct Lower {
+    static constexpr int count = C == 64 ? 12 : 4, each = (count + W - 1) / W;
+    __device__ __forceinline__ static bool get(int i, int wave, int &row, int &col) {
+        const int n = i * W + wave;
+        row = n < 4 ? n / 2 : 2 + (n - 4) / 4, col = n < 4 ? n % 2 : (n - 4) % 4;
+        return n < count;
+    }
+};
+
 template <typename T>
 int64_t places_of(int64_t N, int32_t nseq) { return N / Gdr<T>::chunk + nseq; }
 

@@ -98,7 +98,7 @@ __global__ void __launch_bounds__(64 * W, 2) walk_back(GdrBack b) {
     const int64_t place = place_of(span, s, C) + r * (p.size / C);
     const auto fetch = [&](int64_t n) {
         const int64_t first = from + n * C;
-        const int rows = (int)min((int64_t)C, to - first);
+        const int rows = __builtin_amdgcn_readfirstlane((int)min((int64_t)C, to - first));
         kn.fetch(k + first * p.ldk, p.ldk, rows, p.dk);
         qn.fetch(q + first * p.ldq, p.ldq, rows, p.dk);
         yn.fetch(dy + first * b.lddy, b.lddy, rows, p.dv - col0);
@@ -113,7 +113,7 @@ __global__ void __launch_bounds__(64 * W, 2) walk_back(GdrBack b) {
     if (chunks > 0) fetch(chunks - 1);
     for (int64_t n = chunks - 1; n >= 0; --n) {
         const int64_t first = from + n * C;
-        const int rows = (int)min((int64_t)C, to - first);
+        const int rows = __builtin_amdgcn_readfirstlane((int)min((int64_t)C, to - first));
         kn.place(K, rows, p.dk);
         qn.place(Q, rows, p.dk);
         yn.keep(V.at, V.ld, rows, p.dv - col0);
@@ -133,26 +133,19 @@ __global__ void __launch_bounds__(64 * W, 2) walk_back(GdrBack b) {
             if (i * THREADS + (int)threadIdx.x < 6 * C) tokens[i * THREADS + threadIdx.x] = tn[i];
         if (n > 0) fetch(n - 1);
         __syncthreads();
-        {   // P: a wave has the keys of a tile and the queries from them on (of W waves W / TT share them)
-            constexpr int EACH = W / TT;
-            static_assert(EACH >= 1, "waves");
-            const int t = wave / EACH, j = 16 * t + l15;    // keys
-            Frag<PD> a[DS];
+#pragma unroll 1
+        for (int n = 0; n < Lower<C, W>::each; ++n) {       // P
+            int i, j;
+            if (!Lower<C, W>::get(n, wave, i, j)) continue;
+            f32x4 acc = {};
 #pragma unroll
-            for (int d = 0; d < DS; ++d) a[d] = along(K, 16 * t, 32 * d);
+            for (int d = 0; d < DS; ++d) acc = multiply(along(Q, 16 * i, 32 * d), along(K, 16 * j, 32 * d), acc);
+            i = 16 * i + g4, j = 16 * j + l15;
             const double Gj = G[j];
             const float kj = rk[j];
-#pragma unroll 1
-            for (int x = wave % EACH; x < TT; x += EACH) {
-                if (x / 2 < t / 2) continue;                // (nobody reads those)
-                f32x4 acc = {};
 #pragma unroll
-                for (int d = 0; d < DS; ++d) acc = multiply(along(Q, 16 * x, 32 * d), a[d], acc);
-                const int i = 16 * x + g4;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[e] = i + e >= j ? decay_of(G[i + e] - Gj) * (rq[i + e] * kj) * acc[e] : 0.f;
-                put4(P, j, i, acc);
-            }
+            for (int e = 0; e < 4; ++e) acc[e] = i + e >= j ? decay_of(G[i + e] - Gj) * (rq[i + e] * kj) * acc[e] : 0.f;
+            put4(P, j, i, acc);
         }
         f32x4 x[TT] = {};
         Frag<PC> u[SS];

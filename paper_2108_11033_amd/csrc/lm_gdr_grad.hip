@@ -22,7 +22,7 @@ struct GradRoom {
     using Square = Tile<PC, C, C, TURNED>;
     static constexpr int keys = 0, queries = keys + Keys::bytes, dy = queries + Keys::bytes, U = dy + Values_::bytes, Y = U + Cols::bytes, end1 = Y + Cols::bytes;
     static constexpr int P = dy, L = P + Square::bytes, end2 = L + Square::bytes, G = end1 > end2 ? end1 : end2, tokens = G + C * 8, sums = tokens + C * 24,
-                         states = sums + 2 * W * C * 4, betas = states + W * 4, bytes = betas + W * 16 * 4;
+                         betas = sums + 2 * W * C * 4, bytes = betas + W * 16 * 4;
     static_assert(bytes <= 160 * 1024, "LDS");
 };
 
@@ -65,7 +65,7 @@ __global__ void __launch_bounds__(DK * 4, 2) gradients(GdrBack b) {
     const GdrParams &p = b.p;
     double *G = reinterpret_cast<double *>(lds + Room::G);
     float *tokens = reinterpret_cast<float *>(lds + Room::tokens), *sums = reinterpret_cast<float *>(lds + Room::sums);
-    float *states = reinterpret_cast<float *>(lds + Room::states), *betas = reinterpret_cast<float *>(lds + Room::betas);
+    float *betas = reinterpret_cast<float *>(lds + Room::betas);
     const float *fk = tokens + C, *fu = tokens + 2 * C, *fq = tokens + 3 * C, *rk = tokens + 4 * C, *rq = tokens + 5 * C;
 
     const int kh = (int)(blockIdx.x % (uint32_t)b.key_heads), head0 = kh * p.group, head1 = head0 + p.group;
@@ -121,12 +121,7 @@ __global__ void __launch_bounds__(DK * 4, 2) gradients(GdrBack b) {
         q.place(m.Q, rows, p.dk);
     }
     f32x4 dq[TT] = {}, dk[TT] = {};                         // elements d0 + g4 .. + 3 of token 16 t + l15, sums over the heads
-    constexpr int pairs = C == 64 ? 12 : 4, PP = (pairs + W - 1) / W;          // of 16 x 16 of dP and dL that are read
-    const auto pair = [&](int i, int &t, int &j) {
-        const int n = i * W + wave;
-        t = n < 4 ? n / 2 : 2 + (n - 4) / 4, j = n < 4 ? n % 2 : (n - 4) % 4;
-        return n < pairs;
-    };
+    constexpr int PP = Lower<C, W>::each;                   // of 16 x 16 of dP and dL
     f32x4 q[TT] = {}, kr[TT] = {}, ke[TT] = {}, gp[PP] = {}, gl[PP] = {}, db = {};
     float sa = 0.f, g = 0.f;
     for (int h = head0, v0 = 0; h < head1;) {
@@ -171,8 +166,7 @@ __global__ void __launch_bounds__(DK * 4, 2) gradients(GdrBack b) {
 #pragma unroll
             for (int i = 0; i < PP; ++i) {
                 int t, j;
-                if (!pair(i, t, j)) continue;
-                __builtin_amdgcn_sched_barrier(0);
+                if (!Lower<C, W>::get(i, wave, t, j)) continue;
                 const Frag<PC> u = across(m.U, 16 * j, 0);
                 gp[i] = multiply(u, along(m.dY, 16 * t, 0), gp[i]);
                 gl[i] = multiply(u, across(m.Y, 16 * t, 0), gl[i]);
@@ -185,8 +179,7 @@ __global__ void __launch_bounds__(DK * 4, 2) gradients(GdrBack b) {
 #pragma unroll
         for (int i = 0; i < PP; ++i) {
             int t, j;
-            __builtin_amdgcn_sched_barrier(0);
-            if (!pair(i, t, j)) continue;
+            if (!Lower<C, W>::get(i, wave, t, j)) continue;
             int low = l15, high = g4;
             asm volatile("" : "+v"(low), "+v"(high));       // (as above: the comparisons too would be kept)
             t = 16 * t + low, j = 16 * j + high;
@@ -213,7 +206,6 @@ __global__ void __launch_bounds__(DK * 4, 2) gradients(GdrBack b) {
             const Frag<PD> fk_ = across(m.K, d0, 32 * x), fq_ = across(m.Q, d0, 32 * x);
 #pragma unroll
             for (int t = 2 * x; t < TT; ++t) {              // (sums over j, 32 of them from 32 x, for the tokens from there on)
-                __builtin_amdgcn_sched_barrier(0);
                 q[t] = multiply(fk_, along(m.dP, 16 * t, 32 * x), q[t]);
                 kr[t] = multiply(fk_, along(m.dL, 16 * t, 32 * x), kr[t]);
             }
@@ -225,20 +217,20 @@ __global__ void __launch_bounds__(DK * 4, 2) gradients(GdrBack b) {
                 kc[j] = multiply(fk_, across(m.dL, 16 * j, 32 * x), kc[j]);
             }
         }
-        // what the decays get of it
+        // what the decays get of it; the last token also exp(G_end) <S, A>, which all get
+        const float all = wave_sum(sa) * decay_of(G[C - 1]);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int t = 0; t < TT; ++t) {
-            __builtin_amdgcn_sched_barrier(0);
             const f32x4 kv = elements(m.K, 16 * t, d0), qv = elements(m.Q, 16 * t, d0);
             const f32x4 here = q[t] * qv + (kr[t] - kc[t]) * kv, n = ke[t] * kv;
-            const float from_here = across_rows(here[0] + here[1] + (here[2] + here[3]), Add()), before = across_rows(n[0] + n[1] + (n[2] + n[3]), Add());
+            float from_here = across_rows(here[0] + here[1] + (here[2] + here[3]), Add());
+            const float before = across_rows(n[0] + n[1] + (n[2] + n[3]), Add());
+            if (16 * t + l15 == C - 1) from_here += all;
             if (lane < 16) sums[wave * C + 16 * t + l15] = from_here, sums[(W + wave) * C + 16 * t + l15] = before;
             dq[t] += q[t];
             dk[t] += kr[t] + kc[t] + ke[t];
         }
-        sa = wave_sum(sa);
-        if (lane == 0) states[wave] = sa;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const float one = row_join(db[e], Add());
@@ -246,13 +238,12 @@ __global__ void __launch_bounds__(DK * 4, 2) gradients(GdrBack b) {
         }
         __syncthreads();
         if (wave == 0) {
-            float a = 0.f, n = 0.f, all = 0.f, d = 0.f;
+            float a = 0.f, before = 0.f, d = 0.f;
             const int at = lane % C;
 #pragma unroll
-            for (int w = 0; w < W; ++w) a += sums[w * C + at], n += sums[(W + w) * C + at], all += states[w];
+            for (int w = 0; w < W; ++w) a += sums[w * C + at], before += sums[(W + w) * C + at];
 #pragma unroll
             for (int w = 0; w < W / TT; ++w) d += betas[(w * TT + at / 16) * 16 + at % 16];
-            float before = n;
 #pragma unroll
             for (int x = 1; x < C; x *= 2) {
                 const float after = __shfl_down(a, x, C), less = __shfl_up(before, x, C);
@@ -263,7 +254,7 @@ __global__ void __launch_bounds__(DK * 4, 2) gradients(GdrBack b) {
             if (at == 0) before = 0.f;
             if (lane < rows) {
                 const int64_t t = first + lane;
-                b.ddecay[t * b.lddg + h] = g < kLeastDecay ? 0.f : a + before + decay_of(G[C - 1]) * all;
+                b.ddecay[t * b.lddg + h] = g < kLeastDecay ? 0.f : a + before;
                 b.dbeta[t * b.lddg + h] = d;
             }
         }
