@@ -117,8 +117,8 @@ grim_status grim_glr_step(const float *gates_dev, int64_t ldg, const float *bias
  *   ddecay_dev, dbeta_dev    N x heads fp32, rows of lddg (where g counts as -10000 its gradient is 0)
  *   ds0_dev         nseq x heads x dk x dv fp32 (of an empty sequence: its ds_last), or NULL; must not overlap ds_last
  * Gradients must not overlap inputs.  Infinities and NaN reach the tokens of their own sequence and head alone (of their own sequence and key head in dq and dk),
- * there also tokens in front of them.  Products run on the matrix cores with operands in two (fp16, bf16) or three (fp32) bf16 parts, sums in fp32: results are off by some 2^-17
- * or 2^-23 of the terms' size before their rounding.  Values beyond 3.3e38 count as infinite.
+ * there also tokens in front of them.  Products run on the matrix cores with operands in up to three bf16 parts, sums in fp32: results are off by some 2^-22 of the
+ * terms' size before their rounding.  Values beyond 3.3e38 count as infinite.
  * grim_gdr_step is one token for `batch` callers at once, columns as of grim_glr_step: q and k (key_heads dk) x batch, v (heads dv) x batch, g and beta
  * heads x batch, all fp32; states batch x heads x dk x dv fp32 as the sequence calls have them (s_new_dev may be s_dev itself), y (heads dv) x batch of element
  * type dt, or NULL.  Its arithmetic is fp32.

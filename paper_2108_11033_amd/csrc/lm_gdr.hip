@@ -131,8 +131,8 @@ __global__ void __launch_bounds__(kMatrixThreads) chunk_matrices(GdrParams p) {
         const float since = decay_of(G[i]);
         to[0] = beta[i], to[C] = since * rk[i], to[2 * C] = decay_of(G[C - 1] - G[i]) * rk[i], to[3 * C] = since * rq[i], to[4 * C] = rk[i], to[5 * C] = rq[i];
     }
-    for (int q = threadIdx.x; q < C * C / 8; q += kMatrixThreads) {
-        const int i = q / (C / 8), c = q % (C / 8) / 4 * 32 + q % 4 * 4;
+    for (int q = threadIdx.x; q < Saved<T>::part / 8; q += kMatrixThreads) {          // four pieces of 8 to a row of 32; first the tall block, then the rest
+        const int i = q < C * 4 ? q / 4 : q / 4 - C + 32, c = (q < C * 4 ? 0 : 32) + q % 4 * 4;
         float v[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -144,7 +144,7 @@ __global__ void __launch_bounds__(kMatrixThreads) chunk_matrices(GdrParams p) {
             bf16 part[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) part[j] = (bf16)v[j], v[j] -= (float)part[j];
-            __builtin_memcpy(saved.M() + t * C * C + q * 8, part, 16);
+            __builtin_memcpy(saved.M() + t * Saved<T>::part + q * 8, part, 16);
         }
     }
 }
@@ -156,7 +156,7 @@ struct WalkRoom {
     static constexpr int C = Gdr<T>::chunk, PD = Gdr<T>::data, PC = Gdr<T>::comp;
     using Keys = Tile<PD, C, DK>;
     using Queries = Tile<PD, C, DK, PAIRED>;
-    using Square = Tile<PC, C, C, PAIRED>;
+    using Square = Triangle<PC, C, PAIRED>;
     using Vals = Values<T, C, COLS>;
     static constexpr int keys = 0, values = keys + Keys::bytes, matrix = values + Vals::bytes, decays = matrix + Square::bytes, factors = decays + C * 8, queries = factors + C * 24,
                          products = queries + Queries::bytes, bytes = MAPS ? queries : products + Square::bytes;
@@ -168,14 +168,9 @@ struct WalkRoom {
     double *G;
     float *tokens;
     const float *beta, *fk, *fu, *fq, *rk, *rq;
-    // (Made for every chunk.  TIGHT: in a way that keeps the compiler from seeing that nothing changes, or it holds dozens of addresses in registers across the loop, and spills.)
-    template <bool TIGHT>
-    __device__ __forceinline__ WalkRoom(char *lds, std::bool_constant<TIGHT>) {
-        int again = 0;
-        if (TIGHT) asm volatile("" : "+s"(again));
-        char *at = lds + again;
+    __device__ __forceinline__ explicit WalkRoom(char *at) {
         K.at = reinterpret_cast<uint16_t *>(at + keys), Q.at = reinterpret_cast<uint16_t *>(at + queries);
-        M.at = reinterpret_cast<uint16_t *>(at + matrix), P.at = reinterpret_cast<uint16_t *>(at + products);
+        M.put(at + matrix), P.put(at + products);
         V.at = reinterpret_cast<T *>(at + values), G = reinterpret_cast<double *>(at + decays), tokens = reinterpret_cast<float *>(at + factors);
         beta = tokens, fk = tokens + C, fu = tokens + 2 * C, fq = tokens + 3 * C, rk = tokens + 4 * C, rq = tokens + 5 * C;
     }
@@ -187,12 +182,12 @@ struct WalkRoom {
 // MAPS: no outputs; what every run but a sequence's last does to the states, as S -> A S + B: B's columns (into the places of the states in front of the next run; of a sequence's
 // first run, whose start is known, these are the states themselves) come from a start of zeros, A's from the columns of 1 and values of zero.
 template <typename T, int DK, int W, int CT, bool WHOLE, bool MAPS>
-__global__ void __launch_bounds__(64 * W, MAPS && W == 8 && WHOLE ? 4 : 2) walk(GdrParams p) {
+__global__ void __launch_bounds__(64 * W, 2) walk(GdrParams p) {
     constexpr int C = Gdr<T>::chunk, PD = Gdr<T>::data, PC = Gdr<T>::comp, THREADS = 64 * W, COLS = 16 * CT * W;
     constexpr int TT = C / 16, SS = C / 32, DT = DK / 16, DS = DK / 32;     // tiles of tokens, sums over them; of the states' rows
-    constexpr bool TIGHT = MAPS && W == 8 && WHOLE;                  // (128 registers: two workgroups on a compute unit)
     using Room = WalkRoom<T, DK, COLS, MAPS>;
     extern __shared__ __attribute__((aligned(16))) char lds[];
+    const Room m(lds);
 
     // (the workgroups of a run, whose heads read the same rows, lie together)
     const uint32_t value_blocks = (p.tiles + CT * W - 1) / (CT * W), blocks = value_blocks + (MAPS ? (DT + CT * W - 1) / (CT * W) : 0), heads = (uint32_t)p.heads;
@@ -243,7 +238,7 @@ __global__ void __launch_bounds__(64 * W, MAPS && W == 8 && WHOLE ? 4 : 2) walk(
     // what the next chunk brings
     Rows<WHOLE, T, THREADS, C, DK> kn, qn;
     Rows<WHOLE, T, THREADS, C, COLS> vn;
-    constexpr int pieces = PC * C * C / 8, MP = (pieces + THREADS - 1) / THREADS, TP = (6 * C + THREADS - 1) / THREADS;
+    constexpr int pieces = PC * Saved<T>::part / 8, MP = (pieces + THREADS - 1) / THREADS, TP = (6 * C + THREADS - 1) / THREADS;
     u32x4 mn[MP];
     double Gn = 0.;
     float tn[TP];
@@ -254,25 +249,22 @@ __global__ void __launch_bounds__(64 * W, MAPS && W == 8 && WHOLE ? 4 : 2) walk(
         if (!MAPS) qn.fetch(q + first * p.ldq, p.ldq, rows, p.dk);
         vn.fetch(v + first * p.ldv, p.ldv, rows, p.dv - col0);
         const Saved<T> saved(p, place + n, h);
-        uint32_t me = threadIdx.x;
-        if (TIGHT) asm volatile("" : "+v"(me));             // (addresses from the chunk's own, not one in 64 bits for each load held across the loop)
 #pragma unroll
-        for (int i = 0; i < MP; ++i) mn[i] = reinterpret_cast<const u32x4 *>(saved.M())[min(i * THREADS + me, pieces - 1u)];
-        Gn = saved.G()[me % C];
+        for (int i = 0; i < MP; ++i) mn[i] = reinterpret_cast<const u32x4 *>(saved.M())[min(i * THREADS + threadIdx.x, pieces - 1u)];
+        Gn = saved.G()[threadIdx.x % C];
 #pragma unroll
-        for (int i = 0; i < TP; ++i) tn[i] = saved.tokens()[min(i * THREADS + me, 6 * C - 1u)];
+        for (int i = 0; i < TP; ++i) tn[i] = saved.tokens()[min(i * THREADS + threadIdx.x, 6 * C - 1u)];
     };
     if (from < to) fetch(0, from);
     for (int64_t n = 0, first = from; first < to; ++n, first += C) {
         const int rows = __builtin_amdgcn_readfirstlane((int)min((int64_t)C, to - first));
-        const Room m(lds, std::bool_constant<TIGHT>());
         kn.place(m.K, rows, p.dk);
         if (!MAPS) qn.place(m.Q, rows, p.dk);
         vn.keep(m.V.at, m.V.ld, map ? 0 : rows, p.dv - col0);
 #pragma unroll
         for (int i = 0; i < MP; ++i) {
-            const int piece = i * THREADS + (int)threadIdx.x, e = piece % (C * C / 8) * 8;
-            if (piece < pieces) *reinterpret_cast<u32x4 *>(m.M.at + piece / (C * C / 8) * m.M.part + e / C * m.M.ld + e % C) = mn[i];
+            const int piece = i * THREADS + (int)threadIdx.x;
+            if (piece < pieces) *reinterpret_cast<u32x4 *>(m.M.piece(piece)) = mn[i];
         }
         if (threadIdx.x < C) m.G[threadIdx.x] = Gn;
 #pragma unroll
@@ -281,7 +273,7 @@ __global__ void __launch_bounds__(64 * W, MAPS && W == 8 && WHOLE ? 4 : 2) walk(
         if (first + C < to) fetch(n + 1, first + C);
         __syncthreads();
         if (!MAPS) {                                        // the products of queries and keys
-#pragma unroll W == 4 ? 3 : 1
+#pragma unroll 1
             for (int n = 0; n < Lower<C, W>::each; ++n) {
                 int i, j;
                 if (!Lower<C, W>::get(n, wave, i, j)) continue;
@@ -309,7 +301,6 @@ __global__ void __launch_bounds__(64 * W, MAPS && W == 8 && WHOLE ? 4 : 2) walk(
                             *reinterpret_cast<f32x4 *>(p.states + ((((place + n) * p.heads + h) * p.tiles + tile0 + c) * DT + d) * 256 + own) = state[d][c];
 #pragma unroll
             for (int d = 0; d < DS; ++d) {
-                if (TIGHT) __builtin_amdgcn_sched_barrier(0);          // (the operands of all d at once are too many)
                 Frag<PC> S[CT];
 #pragma unroll
                 for (int c = 0; c < CT; ++c) S[c] = operand<PC>(state[2 * d][c], state[2 * d + 1][c]);
@@ -450,7 +441,7 @@ grim_status gdr_launch(const GdrParams &p, hipStream_t stream) {
         grim_status st = launched();
         if (st != GRIM_OK) return st;
         if (p.size < (uint32_t)p.N) {
-            st = narrow ? walk_launch<T, 64, 4, 1, WHOLE, true>(p, stream) : walk_launch<T, DK, 8, 1, WHOLE, true>(p, stream);
+            st = walk_launch<T, DK, 4, 1, WHOLE, true>(p, stream);
             if (st != GRIM_OK) return st;
             st = join_runs<T, DK, false>(p, stream);
             if (st != GRIM_OK) return st;

@@ -1,9 +1,10 @@
 // What the kernels of the gated delta rule share: matrices in LDS as sums of bf16 parts, products of them, chunks of packed sequences.
 //
-// A number is held as the sum of P bf16 parts, each the rounding of what the parts before it leave: two parts are off by at most 2^-17 of the number, three
-// by 2^-25 or so.  The product of two numbers takes the parts' products whose numbers add up to less than the larger P, summed in fp32 by the matrix cores.  Operands
-// that come as bf16 are one part, fp16 two, fp32 three, all exact; what is computed between products (states, differences) is two parts where operands are 16 bits
-// wide, whose own roundings are 2^-8 and 2^-11, and three in fp32.  (The fp32 matrix instruction does a sixteenth of the work of the bf16 one.)
+// A number is held as the sum of up to three bf16 parts, each the rounding of what the parts before it leave: three are off by 2^-25 of the number or less.  The product of two
+// numbers takes the parts' products whose numbers add up to two or less, summed in fp32 by the matrix cores: 2^-24 or so, as fp32 itself.  Operands
+// that come as bf16 are one part, fp16 two, fp32 three, all exact but the last; what is computed between products (states, differences) is three.
+// (Two parts for it would be off by 2^-17, which outputs of 16 bits hide but the states and the gates' gradients do not: those were 1e-6 to 6e-6 off in the 2-norm, and are 6e-8 to 4e-7
+// with three.  What that costs: 32768 tokens x 8 heads of 128 x 128 in bf16, both directions, 1077 -> 1262 us.  The fp32 matrix instruction does a sixteenth of the work of the bf16 one.)
 #pragma once
 #include "lm_common.hpp"
 
@@ -18,11 +19,11 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 template <typename T>
 struct Gdr;
-// chunk: tokens that the matrix form takes at a time (fewer in fp32, whose products take six times as long)
+// data: parts of an operand; comp: of what is computed; chunk: tokens that the matrix form takes at a time (fewer in fp32, whose products take up to three times as long)
 template <>
-struct Gdr<bf16> { static constexpr int data = 1, comp = 2, chunk = 64; };
+struct Gdr<bf16> { static constexpr int data = 1, comp = 3, chunk = 64; };
 template <>
-struct Gdr<f16> { static constexpr int data = 2, comp = 2, chunk = 64; };
+struct Gdr<f16> { static constexpr int data = 2, comp = 3, chunk = 64; };
 template <>
 struct Gdr<float> { static constexpr int data = 3, comp = 3, chunk = 32; };
 
@@ -44,7 +45,7 @@ struct Frag { s16x8 part[P]; };
 enum Order { PLAIN, PAIRED, TURNED };
 template <int P, int ROWS, int COLS, int ORDER = PLAIN>
 struct Tile {
-    static constexpr int parts = P, ld = COLS == 128 ? (ORDER ? 144 : 152) : COLS == 64 ? (ORDER ? 80 : 72) : 48, part = ROWS * ld, bytes = P * part * 2;
+    static constexpr int parts = P, ld = COLS == 128 ? (ORDER ? 144 : 152) : COLS == 64 ? (ORDER ? 80 : 72) : 40, part = ROWS * ld, bytes = P * part * 2;
     uint16_t *at;
 };
 
@@ -115,9 +116,8 @@ __device__ __forceinline__ Frag<P> operand(f32x4 lo, f32x4 hi) {
 // acc + the 16 x 16 product, small terms first.
 template <int PA, int PB>
 __device__ __forceinline__ f32x4 multiply(const Frag<PA> &a, const Frag<PB> &b, f32x4 acc) {
-    constexpr int P = PA > PB ? PA : PB;
 #pragma unroll
-    for (int s = P - 1; s >= 0; --s)
+    for (int s = 2; s >= 0; --s)
 #pragma unroll
         for (int i = 0; i < PA; ++i)
             if (s - i >= 0 && s - i < PB)
@@ -161,6 +161,37 @@ __device__ __forceinline__ void put8(const Tile<P, R, C, ORDER> &m, int r, int c
         __builtin_memcpy(&w, h, 16);
         put8(m, r, c, w, p);
     }
+}
+
+// C x C of which the products of chunks need the blocks of 32 x 32 on the diagonal and (C = 64) one beside it: below (UPPER: above) the diagonal.
+template <int P, int C, int ORDER, bool UPPER = false>
+struct Triangle {
+    static constexpr int elements = C * 32 + (C - 32) * 32, bytes = Tile<P, C, 32, ORDER>::bytes + (C > 32 ? Tile<P, 32, 32, ORDER>::bytes : 0);
+    Tile<P, C, 32, ORDER> tall;                             // columns 0 .. 31 of all rows (UPPER: the last 32)
+    Tile<P, 32, 32, ORDER> rest;                            // the other diagonal block
+    __device__ __forceinline__ void put(char *at) {
+        tall.at = reinterpret_cast<uint16_t *>(at), rest.at = reinterpret_cast<uint16_t *>(at + Tile<P, C, 32, ORDER>::bytes);
+    }
+    // Where the n-th 8 elements of what is kept go (not UPPER).
+    __device__ __forceinline__ uint16_t *piece(int n) const {
+        const int p = n / (elements / 8), q = n % (elements / 8), r = q / 4, c = q % 4 * 8;
+        return r < C ? tall.at + p * tall.part + r * tall.ld + c : rest.at + p * rest.part + (r - C) * rest.ld + c;
+    }
+    __device__ __forceinline__ static constexpr bool is_tall(int c) { return UPPER ? c >= C - 32 : c < 32; }
+    __device__ __forceinline__ static constexpr int row(int r) { return UPPER ? r : r - 32; }       // of the rest
+};
+template <int P, int C, int ORDER, bool UPPER>
+__device__ __forceinline__ Frag<P> along(const Triangle<P, C, ORDER, UPPER> &m, int r, int k) {
+    return m.is_tall(k) ? along(m.tall, r, 0) : along(m.rest, m.row(r), 0);
+}
+template <int P, int C, int ORDER, bool UPPER>
+__device__ __forceinline__ Frag<P> across(const Triangle<P, C, ORDER, UPPER> &m, int c, int k) {
+    return m.is_tall(c) ? across(m.tall, c % 32, k) : across(m.rest, c % 32, m.row(k));
+}
+template <int P, int C, int ORDER, bool UPPER>
+__device__ __forceinline__ void put4(const Triangle<P, C, ORDER, UPPER> &m, int r, int c, f32x4 v) {
+    if (m.is_tall(__builtin_amdgcn_readfirstlane(c))) put4(m.tall, r, c % 32, v);         // (the same for all lanes)
+    else put4(m.rest, m.row(r), c % 32, v);
 }
 
 // V elements from column c of a row of `width` (which may end inside them, or before) without a branch, so that loads do not wait for each other: those that end with the row,
@@ -336,12 +367,12 @@ __device__ __forceinline__ int sequence_of(const int32_t *starts, int nseq, int6
     return lo;
 }
 
-// What is kept of a chunk for a head: the matrix M in parts, columns paired; the running sums of the decays' base-2 logarithms in fp64; and of every token, with r the
+// What is kept of a chunk for a head: the matrix M in parts, columns paired, the blocks of Triangle one after another; the running sums of the decays' base-2 logarithms in fp64; and of every token, with r the
 // factors that its key and its query count with (0 behind the last one), beta, the decay since the chunk's start times r_k, the decay until its end times r_k, the
 // decay since its start times r_q, r_k, r_q.
 template <typename T>
 struct Saved {
-    static constexpr int C = Gdr<T>::chunk, P = Gdr<T>::comp, matrix = P * C * C * 2, bytes = matrix + C * 32;
+    static constexpr int C = Gdr<T>::chunk, P = Gdr<T>::comp, part = C * 32 + (C - 32) * 32, matrix = P * part * 2, bytes = matrix + C * 32;
     char *at;
     __device__ __forceinline__ Saved(const GdrParams &p, int64_t place, int head) : at(p.saved + (place * p.heads + head) * bytes) {}
     __device__ __forceinline__ uint16_t *M() const { return reinterpret_cast<uint16_t *>(at); }

@@ -17,8 +17,8 @@ template <typename T, int DK, int COLS>
 struct BackRoom {
     static constexpr int C = Gdr<T>::chunk, PD = Gdr<T>::data, PC = Gdr<T>::comp;
     using Keys = Tile<PD, C, DK>;
-    using Square = Tile<PC, C, C, PAIRED>;                  // P transposed
-    using Matrix = Tile<PC, C, C, TURNED>;
+    using Square = Triangle<PC, C, PAIRED, true>;           // P transposed
+    using Matrix = Triangle<PC, C, TURNED>;
     using Vals = Values<T, C, COLS>;
     static constexpr int keys = 0, queries = keys + Keys::bytes, values = queries + Keys::bytes, M = values + Vals::bytes, P = M + Matrix::bytes, G = P + Square::bytes,
                          tokens = G + C * 8, bytes = tokens + C * 24;
@@ -36,8 +36,9 @@ __global__ void __launch_bounds__(64 * W, 2) walk_back(GdrBack b) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const GdrParams &p = b.p;
     const typename Room::Keys K{reinterpret_cast<uint16_t *>(lds + Room::keys)}, Q{reinterpret_cast<uint16_t *>(lds + Room::queries)};
-    const typename Room::Matrix M{reinterpret_cast<uint16_t *>(lds + Room::M)};
-    const typename Room::Square P{reinterpret_cast<uint16_t *>(lds + Room::P)};
+    typename Room::Matrix M;
+    typename Room::Square P;
+    M.put(lds + Room::M), P.put(lds + Room::P);
     const typename Room::Vals V{reinterpret_cast<T *>(lds + Room::values)};
     double *G = reinterpret_cast<double *>(lds + Room::G);
     float *tokens = reinterpret_cast<float *>(lds + Room::tokens);
@@ -91,7 +92,7 @@ __global__ void __launch_bounds__(64 * W, 2) walk_back(GdrBack b) {
 
     Rows<WHOLE, T, THREADS, C, DK> kn, qn;
     Rows<WHOLE, T, THREADS, C, COLS> yn;
-    constexpr int pieces = PC * C * C / 8, MP = (pieces + THREADS - 1) / THREADS, TP = (6 * C + THREADS - 1) / THREADS;
+    constexpr int pieces = PC * Saved<T>::part / 8, MP = (pieces + THREADS - 1) / THREADS, TP = (6 * C + THREADS - 1) / THREADS;
     u32x4 mn[MP];
     double Gn = 0.;
     float tn[TP];
@@ -119,10 +120,10 @@ __global__ void __launch_bounds__(64 * W, 2) walk_back(GdrBack b) {
         yn.keep(V.at, V.ld, rows, p.dv - col0);
 #pragma unroll
         for (int i = 0; i < MP; ++i) {                      // (from the paired order back into the columns' own)
-            const int piece = i * THREADS + (int)threadIdx.x, e = piece % (C * C / 8) * 8;
+            const int piece = i * THREADS + (int)threadIdx.x;
             if (piece < pieces) {
                 const s16x8 w = __builtin_bit_cast(s16x8, mn[i]);
-                uint16_t *at = M.at + piece / (C * C / 8) * M.part + e / C * M.ld + e % C / 32 * 32 + e % 32 / 2;
+                uint16_t *at = M.piece(piece) - piece % 4 * 4;
                 *reinterpret_cast<s16x4 *>(at) = __builtin_shufflevector(w, w, 0, 1, 2, 3);
                 *reinterpret_cast<s16x4 *>(at + 16) = __builtin_shufflevector(w, w, 4, 5, 6, 7);
             }

@@ -19,7 +19,7 @@ struct GradRoom {
     using Keys = Tile<PD, C, DK, TURNED>;
     using Values_ = Tile<PD, C, VB, PAIRED>;
     using Cols = Tile<PC, VB, C, TURNED>;                   // U and Y, a column's tokens in a row
-    using Square = Tile<PC, C, C, TURNED>;
+    using Square = Triangle<PC, C, TURNED>;
     static constexpr int keys = 0, queries = keys + Keys::bytes, dy = queries + Keys::bytes, U = dy + Values_::bytes, Y = U + Cols::bytes, end1 = Y + Cols::bytes;
     static constexpr int P = dy, L = P + Square::bytes, end2 = L + Square::bytes, G = end1 > end2 ? end1 : end2, tokens = G + C * 8, sums = tokens + C * 24,
                          betas = sums + 2 * W * C * 4, bytes = betas + W * 16 * 4;
@@ -38,7 +38,7 @@ struct GradTiles {
         int again = 0;
         asm volatile("" : "+s"(again));
         const auto tile = [&](int at) { return reinterpret_cast<uint16_t *>(lds + again + at); };
-        K.at = tile(Room::keys), Q.at = tile(Room::queries), dY.at = tile(Room::dy), U.at = tile(Room::U), Y.at = tile(Room::Y), dP.at = tile(Room::P), dL.at = tile(Room::L);
+        K.at = tile(Room::keys), Q.at = tile(Room::queries), dY.at = tile(Room::dy), U.at = tile(Room::U), Y.at = tile(Room::Y), dP.put(lds + again + Room::P), dL.put(lds + again + Room::L);
     }
 };
 

@@ -9,7 +9,7 @@ import math
 
 import torch
 
-UNIT_OF = {"f32": 2.0 ** -22, "f16": 2.0 ** -16, "bf16": 2.0 ** -16}
+UNIT_OF = {"f32": 2.0 ** -22, "f16": 2.0 ** -22, "bf16": 2.0 ** -22}
 COUNT = 16
 CHUNK = {"f32": 32, "f16": 64, "bf16": 64}
 
