@@ -33,12 +33,19 @@ struct GradTiles {
     typename Room::Values_ dY;
     typename Room::Cols U, Y;
     typename Room::Square dP, dL;
+    double *G;
+    float *tokens, *sums, *betas;
+    const float *beta, *fk, *fu, *fq, *rk, *rq;
     // (The compiler is kept from seeing that the addresses are the same every time: it holds dozens of them in registers across the loops otherwise, and spills.)
     __device__ __forceinline__ GradTiles(char *lds) {
         int again = 0;
         asm volatile("" : "+s"(again));
         const auto tile = [&](int at) { return reinterpret_cast<uint16_t *>(lds + again + at); };
         K.at = tile(Room::keys), Q.at = tile(Room::queries), dY.at = tile(Room::dy), U.at = tile(Room::U), Y.at = tile(Room::Y), dP.put(lds + again + Room::P), dL.put(lds + again + Room::L);
+        const auto floats = [&](int at) { return reinterpret_cast<float *>(lds + again + at); };
+        G = reinterpret_cast<double *>(lds + again + Room::G), tokens = floats(Room::tokens), sums = floats(Room::sums), betas = floats(Room::betas);
+        constexpr int C = Room::C;
+        beta = tokens, fk = tokens + C, fu = tokens + 2 * C, fq = tokens + 3 * C, rk = tokens + 4 * C, rq = tokens + 5 * C;
     }
 };
 
@@ -63,10 +70,6 @@ __global__ void __launch_bounds__(DK * 4, 2) gradients(GdrBack b) {
     constexpr int C = Room::C, PD = Room::PD, PC = Room::PC, VB = Room::VB, W = Room::W, THREADS = 64 * W, TT = C / 16, SS = C / 32, DT = DK / 16, VT = VB / 16;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const GdrParams &p = b.p;
-    double *G = reinterpret_cast<double *>(lds + Room::G);
-    float *tokens = reinterpret_cast<float *>(lds + Room::tokens), *sums = reinterpret_cast<float *>(lds + Room::sums);
-    float *betas = reinterpret_cast<float *>(lds + Room::betas);
-    const float *fk = tokens + C, *fu = tokens + 2 * C, *fq = tokens + 3 * C, *rk = tokens + 4 * C, *rq = tokens + 5 * C;
 
     const int kh = (int)(blockIdx.x % (uint32_t)b.key_heads), head0 = kh * p.group, head1 = head0 + p.group;
     const uint32_t place = blockIdx.x / (uint32_t)b.key_heads;
@@ -133,8 +136,8 @@ __global__ void __launch_bounds__(DK * 4, 2) gradients(GdrBack b) {
             __syncthreads();                                // (the columns and the head before are done with)
 #pragma unroll
             for (int i = 0; i < TP; ++i)
-                if (i * THREADS + (int)threadIdx.x < 6 * C) tokens[i * THREADS + threadIdx.x] = tn[i];
-            if (threadIdx.x < C) G[threadIdx.x] = Gn;
+                if (i * THREADS + (int)threadIdx.x < 6 * C) m.tokens[i * THREADS + threadIdx.x] = tn[i];
+            if (threadIdx.x < C) m.G[threadIdx.x] = Gn;
             y.place(m.dY, rows, p.dv - v0);
 #pragma unroll
             for (int i = 0; i < EACH; ++i) {
@@ -175,20 +178,20 @@ __global__ void __launch_bounds__(DK * 4, 2) gradients(GdrBack b) {
         v0 += VB;
         if (!done) continue;
         const GradTiles<T, DK> m(lds);
+        int l15 = threadIdx.x & 15, g4 = (threadIdx.x & 63) / 16 * 4;
+        asm volatile("" : "+v"(l15), "+v"(g4));             // (for the same reason: comparisons too would be kept)
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < PP; ++i) {
             int t, j;
             if (!Lower<C, W>::get(i, wave, t, j)) continue;
-            int low = l15, high = g4;
-            asm volatile("" : "+v"(low), "+v"(high));       // (as above: the comparisons too would be kept)
-            t = 16 * t + low, j = 16 * j + high;
-            const double Gt = G[t];
-            const float kt = rk[t], qt = rq[t];
+            t = 16 * t + l15, j = 16 * j + g4;
+            const double Gt = m.G[t];
+            const float kt = m.rk[t], qt = m.rq[t];
             f32x4 a, c;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float w = t >= j + e ? decay_of(Gt - G[j + e]) * rk[j + e] : 0.f;
+                const float w = t >= j + e ? decay_of(Gt - m.G[j + e]) * m.rk[j + e] : 0.f;
                 a[e] = t >= j + e ? w * qt * gp[i][e] : 0.f, c[e] = t > j + e ? -w * kt * gl[i][e] : 0.f;
             }
             put4(m.dP, t, j, a);
@@ -198,7 +201,7 @@ __global__ void __launch_bounds__(DK * 4, 2) gradients(GdrBack b) {
         f32x4 kc[TT] = {};
 #pragma unroll
         for (int t = 0; t < TT; ++t) {
-            q[t] *= fq[16 * t + l15], kr[t] *= -fk[16 * t + l15], ke[t] *= fu[16 * t + l15];
+            q[t] *= m.fq[16 * t + l15], kr[t] *= -m.fk[16 * t + l15], ke[t] *= m.fu[16 * t + l15];
         }
 #pragma unroll
         for (int x = 0; x < SS; ++x) {
@@ -218,7 +221,7 @@ __global__ void __launch_bounds__(DK * 4, 2) gradients(GdrBack b) {
             }
         }
         // what the decays get of it; the last token also exp(G_end) <S, A>, which all get
-        const float all = wave_sum(sa) * decay_of(G[C - 1]);
+        const float all = wave_sum(sa) * decay_of(m.G[C - 1]);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int t = 0; t < TT; ++t) {
@@ -227,23 +230,23 @@ __global__ void __launch_bounds__(DK * 4, 2) gradients(GdrBack b) {
             float from_here = across_rows(here[0] + here[1] + (here[2] + here[3]), Add());
             const float before = across_rows(n[0] + n[1] + (n[2] + n[3]), Add());
             if (16 * t + l15 == C - 1) from_here += all;
-            if (lane < 16) sums[wave * C + 16 * t + l15] = from_here, sums[(W + wave) * C + 16 * t + l15] = before;
+            if (lane < 16) m.sums[wave * C + 16 * t + l15] = from_here, m.sums[(W + wave) * C + 16 * t + l15] = before;
             dq[t] += q[t];
             dk[t] += kr[t] + kc[t] + ke[t];
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const float one = row_join(db[e], Add());
-            if (l15 == 0) betas[wave * 16 + g4 + e] = one;
+            if (l15 == 0) m.betas[wave * 16 + g4 + e] = one;
         }
         __syncthreads();
         if (wave == 0) {
             float a = 0.f, before = 0.f, d = 0.f;
             const int at = lane % C;
 #pragma unroll
-            for (int w = 0; w < W; ++w) a += sums[w * C + at], before += sums[(W + w) * C + at];
+            for (int w = 0; w < W; ++w) a += m.sums[w * C + at], before += m.sums[(W + w) * C + at];
 #pragma unroll
-            for (int w = 0; w < W / TT; ++w) d += betas[(w * TT + at / 16) * 16 + at % 16];
+            for (int w = 0; w < W / TT; ++w) d += m.betas[(w * TT + at / 16) * 16 + at % 16];
 #pragma unroll
             for (int x = 1; x < C; x *= 2) {
                 const float after = __shfl_down(a, x, C), less = __shfl_up(before, x, C);
@@ -265,14 +268,14 @@ __global__ void __launch_bounds__(DK * 4, 2) gradients(GdrBack b) {
         db = f32x4{}, sa = 0.f, v0 = 0, ++h;
     }
     // through the division by the lengths: d(x / |x|) = (dx - x (x . dx) / |x|^2) / |x|, of which the last division is made already
+    const GradTiles<T, DK> m(lds);
     if (p.norm_eps > 0.f) {
-        const GradTiles<T, DK> m(lds);
         __syncthreads();
 #pragma unroll
         for (int t = 0; t < TT; ++t) {
             const f32x4 l = dq[t] * elements(m.Q, 16 * t, d0), n = dk[t] * elements(m.K, 16 * t, d0);
             const float mq = across_rows(l[0] + l[1] + (l[2] + l[3]), Add()), mk = across_rows(n[0] + n[1] + (n[2] + n[3]), Add());
-            if (lane < 16) sums[wave * C + 16 * t + l15] = mq, sums[(W + wave) * C + 16 * t + l15] = mk;
+            if (lane < 16) m.sums[wave * C + 16 * t + l15] = mq, m.sums[(W + wave) * C + 16 * t + l15] = mk;
         }
         __syncthreads();
         const float unscale = p.scale != 0.f ? 1.f / p.scale : 0.f;
@@ -281,8 +284,8 @@ __global__ void __launch_bounds__(DK * 4, 2) gradients(GdrBack b) {
             const int i = 16 * t + l15;
             float mq = 0.f, mk = 0.f;
 #pragma unroll
-            for (int w = 0; w < W; ++w) mq += sums[w * C + i], mk += sums[(W + w) * C + i];
-            const float iq = rq[i] * unscale, ik = rk[i];
+            for (int w = 0; w < W; ++w) mq += m.sums[w * C + i], mk += m.sums[(W + w) * C + i];
+            const float iq = m.rq[i] * unscale, ik = m.rk[i];
             dq[t] -= elements(m.Q, 16 * t, d0) * iq * (iq * mq);
             dk[t] -= elements(m.K, 16 * t, d0) * ik * (ik * mk);
         }
