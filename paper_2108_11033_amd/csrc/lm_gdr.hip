@@ -181,7 +181,8 @@ struct WalkRoom {
 // values and M are placed in LDS and where the products of queries and keys, which all need, are formed.
 // MAPS: no outputs; what every run but a sequence's last does to the states, as S -> A S + B: B's columns (into the places of the states in front of the next run; of a sequence's
 // first run, whose start is known, these are the states themselves) come from a start of zeros, A's from the columns of 1 and values of zero.
-template <typename T, int DK, int W, int CT, bool WHOLE, bool MAPS>
+// HELP: the second half of the waves has no columns; they form the products of queries and keys.
+template <typename T, int DK, int W, int CT, bool WHOLE, bool MAPS, bool HELP>
 __global__ void __launch_bounds__(64 * W, 2) walk(GdrParams p) {
     constexpr int C = Gdr<T>::chunk, PD = Gdr<T>::data, PC = Gdr<T>::comp, THREADS = 64 * W, COLS = 16 * CT * W;
     constexpr int TT = C / 16, SS = C / 32, DT = DK / 16, DS = DK / 32;     // tiles of tokens, sums over them; of the states' rows
@@ -273,10 +274,13 @@ __global__ void __launch_bounds__(64 * W, 2) walk(GdrParams p) {
         if (first + C < to) fetch(n + 1, first + C);
         __syncthreads();
         if (!MAPS) {                                        // the products of queries and keys
+            constexpr int WORK = HELP ? W / 2 : W, EACH = (Lower<C>::count + WORK - 1) / WORK;
 #pragma unroll 1
-            for (int n = 0; n < Lower<C, W>::each; ++n) {
+            for (int n = 0; n < EACH; ++n) {
+                const int pair = n * WORK + wave - (W - WORK);
+                if (pair < 0 || pair >= Lower<C>::count) break;
                 int i, j;
-                if (!Lower<C, W>::get(n, wave, i, j)) continue;
+                Lower<C>::get(pair, i, j);
                 f32x4 acc = {};
 #pragma unroll
                 for (int d = 0; d < DS; ++d) acc = multiply(along(m.K, 16 * j, 32 * d), along(m.Q, 16 * i, 32 * d), acc);
@@ -419,10 +423,10 @@ __global__ void __launch_bounds__(64 * W, 2) walk(GdrParams p) {
 }
 
 // ---------------------------------------------------------------------------------------------------- launches
-template <typename T, int DK, int W, int CT, bool WHOLE, bool MAPS>
+template <typename T, int DK, int W, int CT, bool WHOLE, bool MAPS, bool HELP = false>
 grim_status walk_launch(const GdrParams &p, hipStream_t stream) {
     constexpr int bytes = WalkRoom<T, DK, 16 * CT * W, MAPS>::bytes;
-    const auto kernel = walk<T, DK, W, CT, WHOLE, MAPS>;
+    const auto kernel = walk<T, DK, W, CT, WHOLE, MAPS, HELP>;
     static const hipError_t grown = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (grown != hipSuccess) return GRIM_ERR_DEVICE;
     const int64_t blocks = (p.tiles + CT * W - 1) / (CT * W) + (MAPS ? (DK / 16 + CT * W - 1) / (CT * W) : 0), groups = runs_of(p.N, p.nseq, p.size) * p.heads * blocks;
@@ -433,7 +437,6 @@ grim_status walk_launch(const GdrParams &p, hipStream_t stream) {
 
 template <typename T, int DK, bool WHOLE>
 grim_status gdr_launch(const GdrParams &p, hipStream_t stream) {
-    const bool narrow = DK == 64 && p.tiles <= 4;           // (keys of 128 are too much for the registers of four waves: a second four help with them)
     if (p.N > 0) {
         const int64_t places = places_of<T>(p.N, p.nseq);
         if (places > most_groups(kMatrixThreads) / p.heads) return GRIM_ERR_UNSUPPORTED;
@@ -447,7 +450,12 @@ grim_status gdr_launch(const GdrParams &p, hipStream_t stream) {
             if (st != GRIM_OK) return st;
         }
     }
-    return narrow ? walk_launch<T, 64, 4, 1, WHOLE, false>(p, stream) : walk_launch<T, DK, 8, 1, WHOLE, false>(p, stream);
+    if (p.tiles > 4) return walk_launch<T, DK, 8, 1, WHOLE, false>(p, stream);
+    // 64 columns: four waves, two such workgroups to a compute unit, or where there are not enough of them (or for keys of 128, which are too much for the registers of four
+    // waves) another four that help: 512 tokens in 8 sequences, 16 heads of 64 x 64 in fp16, 30.0 us -> 25.4; 24007 in 40 sequences, in bf16, 164 with four and 205 with eight.
+    if constexpr (DK == 64)
+        if (runs_of(p.N, p.nseq, p.size) * p.heads > kComputeUnits) return walk_launch<T, DK, 4, 1, WHOLE, false>(p, stream);
+    return walk_launch<T, DK, 8, 1, WHOLE, false, true>(p, stream);
 }
 
 template <typename T>

@@ -403,15 +403,11 @@ struct Values {
 // The decay between two places of a chunk.  (The argument's rounding is 2^-24 of it: 8e-7 of a decay to a millionth, less nearer by.)
 __device__ __forceinline__ float decay_of(double from_to) { return __builtin_amdgcn_exp2f((float)from_to); }
 
-// The 16 x 16 of a chunk's lower triangle that sums over 32 tokens read (all of a 32 x 32 block on the diagonal), dealt to the W waves of a workgroup: the i-th of a wave, if there is one.
-template <int C, int W>
+// The 16 x 16 of a chunk's lower triangle that sums over 32 tokens read (all of a 32 x 32 block on the diagonal).
+template <int C>
 struct Lower {
-    static constexpr int count = C == 64 ? 12 : 4, each = (count + W - 1) / W;
-    __device__ __forceinline__ static bool get(int i, int wave, int &row, int &col) {
-        const int n = i * W + wave;
-        row = n < 4 ? n / 2 : 2 + (n - 4) / 4, col = n < 4 ? n % 2 : (n - 4) % 4;
-        return n < count;
-    }
+    static constexpr int count = C == 64 ? 12 : 4;
+    __device__ __forceinline__ static void get(int n, int &row, int &col) { row = n < 4 ? n / 2 : 2 + (n - 4) / 4, col = n < 4 ? n % 2 : (n - 4) % 4; }
 };
 
 template <typename T>
@@ -431,16 +427,18 @@ inline grim_status gdr_check(grim_dtype dt, int64_t N, int32_t nseq, bool starts
     return GRIM_OK;
 }
 
-// Tokens of a run.  Runs are what fills the compute units where sequences and heads are few: as many as there are for two workgroups each, of eight chunks or more (what a run
-// does to the states has to be formed first, which costs more than the run itself, and the runs' maps are joined one after another).
+// Tokens of a run.  Over runs of s chunks a head of n chunks costs 2 s chunks (what a run does to the states has to be formed first) and n / s steps of the join instead of n chunks,
+// some 5 us each where a step is 1.5 to 2: s is the root of n / 8, or what runs that fill the compute units once (twice where two workgroups share one) come to.  One sequence
+// and 4 heads of 64 x 64 in bf16, runs of 2, 4, 8 chunks: 1024 tokens 38, 48, 70 us, 4096 63, 61, 79, 32768 213, 213, 173 (without runs some 5 us a chunk).
 template <typename T>
 uint32_t run_of(int64_t N, int32_t nseq, int32_t heads, int32_t dv) {
-    constexpr int64_t C = Gdr<T>::chunk, least = 8 * C;
-    const int64_t each = (int64_t)heads * ((tiles_of(dv) + 7) / 8);
-    const int64_t runs = (tiles_of(dv) > 4 ? 1 : 2) * kComputeUnits / each;
-    if (runs < 2 || N < 2 * least || N / nseq < least) return (uint32_t)1 << 31;
-    const int64_t size = ((N + runs - 1) / runs + C - 1) / C * C;
-    return (uint32_t)(size < least ? least : size);
+    constexpr int64_t C = Gdr<T>::chunk;
+    const int64_t mean = N / nseq / C, each = (int64_t)heads * ((tiles_of(dv) + 7) / 8), runs = (tiles_of(dv) > 4 ? 1 : 2) * kComputeUnits / each;
+    if (runs < 2 || mean < 4) return (uint32_t)1 << 31;
+    int64_t size = 2;
+    while (size * size * 8 < mean) ++size;
+    const int64_t fill = ((N + runs - 1) / runs + C - 1) / C;
+    return (uint32_t)((size > fill ? size : fill) * C);
 }
 inline int64_t runs_of(int64_t N, int32_t nseq, uint32_t size) { return N / size + nseq; }
 

@@ -28,7 +28,8 @@ struct BackRoom {
 // A workgroup takes 16 W columns of the states of a run of a sequence's head, its chunks from the last to the first.
 // MAPS: what every run but a sequence's first adds to the gradient of the states in front of it, from a gradient of zeros behind it (of the last run, whose end
 // is known, this is the gradient itself); what it makes of the gradient behind it is its map of the forward pass, transposed.
-template <typename T, int DK, int W, bool WHOLE, bool MAPS>
+// HELP: the second half of the waves has no columns; they form P.
+template <typename T, int DK, int W, bool WHOLE, bool MAPS, bool HELP>
 __global__ void __launch_bounds__(64 * W, 2) walk_back(GdrBack b) {
     constexpr int C = Gdr<T>::chunk, PD = Gdr<T>::data, PC = Gdr<T>::comp, THREADS = 64 * W, COLS = 16 * W;
     constexpr int TT = C / 16, SS = C / 32, DT = DK / 16, DS = DK / 32;
@@ -134,10 +135,13 @@ __global__ void __launch_bounds__(64 * W, 2) walk_back(GdrBack b) {
             if (i * THREADS + (int)threadIdx.x < 6 * C) tokens[i * THREADS + threadIdx.x] = tn[i];
         if (n > 0) fetch(n - 1);
         __syncthreads();
+        constexpr int WORK = HELP ? W / 2 : W, EACH = (Lower<C>::count + WORK - 1) / WORK;
 #pragma unroll 1
-        for (int n = 0; n < Lower<C, W>::each; ++n) {       // P
+        for (int n = 0; n < EACH; ++n) {                    // P
+            const int pair = n * WORK + wave - (W - WORK);
+            if (pair < 0 || pair >= Lower<C>::count) break;
             int i, j;
-            if (!Lower<C, W>::get(n, wave, i, j)) continue;
+            Lower<C>::get(pair, i, j);
             f32x4 acc = {};
 #pragma unroll
             for (int d = 0; d < DS; ++d) acc = multiply(along(Q, 16 * i, 32 * d), along(K, 16 * j, 32 * d), acc);
@@ -247,10 +251,10 @@ __global__ void __launch_bounds__(64 * W, 2) walk_back(GdrBack b) {
 }
 
 // ---------------------------------------------------------------------------------------------------- launches
-template <typename T, int DK, int W, bool WHOLE, bool MAPS>
+template <typename T, int DK, int W, bool WHOLE, bool MAPS, bool HELP = false>
 grim_status back_launch(const GdrBack &b, hipStream_t stream) {
     constexpr int bytes = BackRoom<T, DK, 16 * W>::bytes;
-    const auto kernel = walk_back<T, DK, W, WHOLE, MAPS>;
+    const auto kernel = walk_back<T, DK, W, WHOLE, MAPS, HELP>;
     static const hipError_t grown = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (grown != hipSuccess) return GRIM_ERR_DEVICE;
     const int64_t groups = runs_of(b.p.N, b.p.nseq, b.p.size) * b.p.heads * ((b.p.tiles + W - 1) / W);
@@ -259,18 +263,24 @@ grim_status back_launch(const GdrBack &b, hipStream_t stream) {
     return launched();
 }
 
+template <typename T, int DK, bool WHOLE, bool MAPS>
+grim_status back_walk(const GdrBack &b, hipStream_t stream) {
+    if (b.p.tiles > 4) return back_launch<T, DK, 8, WHOLE, MAPS>(b, stream);
+    if constexpr (DK == 64)                                 // (as in the forward pass)
+        if (runs_of(b.p.N, b.p.nseq, b.p.size) * b.p.heads > kComputeUnits) return back_launch<T, DK, 4, WHOLE, MAPS>(b, stream);
+    return back_launch<T, DK, 8, WHOLE, MAPS, true>(b, stream);
+}
+
 template <typename T, int DK, bool WHOLE>
 grim_status back_all(const GdrBack &b, hipStream_t stream) {
     const GdrParams &p = b.p;
-    const bool narrow = DK == 64 && p.tiles <= 4;           // (as in the forward pass)
-    grim_status st;
     if (p.N > 0 && p.size < (uint32_t)p.N) {
-        st = narrow ? back_launch<T, 64, 4, WHOLE, true>(b, stream) : back_launch<T, DK, 8, WHOLE, true>(b, stream);
+        grim_status st = back_walk<T, DK, WHOLE, true>(b, stream);
         if (st != GRIM_OK) return st;
         st = join_runs<T, DK, true>(p, stream);
         if (st != GRIM_OK) return st;
     }
-    st = narrow ? back_launch<T, 64, 4, WHOLE, false>(b, stream) : back_launch<T, DK, 8, WHOLE, false>(b, stream);
+    const grim_status st = back_walk<T, DK, WHOLE, false>(b, stream);
     if (st != GRIM_OK || p.N == 0) return st;
     return gdr_gradients<T, DK, WHOLE>(b, stream);
 }

@@ -124,7 +124,11 @@ __global__ void __launch_bounds__(DK * 4, 2) gradients(GdrBack b) {
         q.place(m.Q, rows, p.dk);
     }
     f32x4 dq[TT] = {}, dk[TT] = {};                         // elements d0 + g4 .. + 3 of token 16 t + l15, sums over the heads
-    constexpr int PP = Lower<C, W>::each;                   // of 16 x 16 of dP and dL
+    constexpr int PP = (Lower<C>::count + W - 1) / W;       // of 16 x 16 of dP and dL
+    const auto pair = [&](int i, int &t, int &j) {
+        Lower<C>::get(i * W + wave, t, j);
+        return i * W + wave < Lower<C>::count;
+    };
     f32x4 q[TT] = {}, kr[TT] = {}, ke[TT] = {}, gp[PP] = {}, gl[PP] = {}, db = {};
     float sa = 0.f, g = 0.f;
     for (int h = head0, v0 = 0; h < head1;) {
@@ -169,7 +173,7 @@ __global__ void __launch_bounds__(DK * 4, 2) gradients(GdrBack b) {
 #pragma unroll
             for (int i = 0; i < PP; ++i) {
                 int t, j;
-                if (!Lower<C, W>::get(i, wave, t, j)) continue;
+                if (!pair(i, t, j)) continue;
                 const Frag<PC> u = across(m.U, 16 * j, 0);
                 gp[i] = multiply(u, along(m.dY, 16 * t, 0), gp[i]);
                 gl[i] = multiply(u, across(m.Y, 16 * t, 0), gl[i]);
@@ -184,7 +188,7 @@ __global__ void __launch_bounds__(DK * 4, 2) gradients(GdrBack b) {
 #pragma unroll
         for (int i = 0; i < PP; ++i) {
             int t, j;
-            if (!Lower<C, W>::get(i, wave, t, j)) continue;
+            if (!pair(i, t, j)) continue;
             t = 16 * t + l15, j = 16 * j + g4;
             const double Gt = m.G[t];
             const float kt = m.rk[t], qt = m.rq[t];
