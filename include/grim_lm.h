@@ -123,7 +123,8 @@ grim_status grim_glr_step(const float *gates_dev, int64_t ldg, const float *bias
  * heads x batch, all fp32; states batch x heads x dk x dv fp32 as the sequence calls have them (s_new_dev may be s_dev itself), y (heads dv) x batch of element
  * type dt, or NULL.  Its arithmetic is fp32.
  * Errors: NULL, SHAPE (N < 0, N > 2^30, nseq < 1, nseq > 1 without starts, heads < 1 or > 4096, heads not a multiple of key_heads, dk or dv < 1, leading
- * dimension or a buffer too small, scale not finite, norm_eps negative), DTYPE, DEVICE, UNSUPPORTED (dk or dv > 128, s_last over s0, ds0 over ds_last, s_new over a part of s).
+ * dimension or a buffer too small, scale not finite, norm_eps negative), DTYPE, DEVICE, UNSUPPORTED (dk or dv > 128,
+ * (N / 32 + nseq) heads above 2^21, s_last over s0, ds0 over ds_last, s_new over a part of s).
  */
 int64_t grim_gdr_states(int64_t N, int32_t nseq, int32_t heads, int32_t dk, int32_t dv);
 int64_t grim_gdr_workspace(int64_t N, int32_t nseq, int32_t heads, int32_t key_heads, int32_t dk, int32_t dv);

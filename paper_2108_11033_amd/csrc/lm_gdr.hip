@@ -430,7 +430,6 @@ grim_status walk_launch(const GdrParams &p, hipStream_t stream) {
     static const hipError_t grown = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (grown != hipSuccess) return GRIM_ERR_DEVICE;
     const int64_t blocks = (p.tiles + CT * W - 1) / (CT * W) + (MAPS ? (DK / 16 + CT * W - 1) / (CT * W) : 0), groups = runs_of(p.N, p.nseq, p.size) * p.heads * blocks;
-    if (groups > most_groups(64 * W)) return GRIM_ERR_UNSUPPORTED;
     hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(64 * W), bytes, stream, p);
     return launched();
 }
@@ -439,7 +438,6 @@ template <typename T, int DK, bool WHOLE>
 grim_status gdr_launch(const GdrParams &p, hipStream_t stream) {
     if (p.N > 0) {
         const int64_t places = places_of<T>(p.N, p.nseq);
-        if (places > most_groups(kMatrixThreads) / p.heads) return GRIM_ERR_UNSUPPORTED;
         hipLaunchKernelGGL((chunk_matrices<T, DK, WHOLE>), dim3((unsigned)(places * p.heads)), dim3(kMatrixThreads), 0, stream, p);
         grim_status st = launched();
         if (st != GRIM_OK) return st;
@@ -483,14 +481,14 @@ extern "C" {
 
 int64_t grim_gdr_states(int64_t N, int32_t nseq, int32_t heads, int32_t dk, int32_t dv) {
     using namespace grim::lm;
-    if (!gdr_shape(N, nseq, heads, 1, dk, dv) || dk > kMostHeadSize || dv > kMostHeadSize) return 0;
+    if (gdr_check(N, nseq, heads, 1, dk, dv) != GRIM_OK) return 0;
     const int64_t a = GdrRoom<float>(N, nseq, heads, dk, dv).kept(), b = GdrRoom<f16>(N, nseq, heads, dk, dv).kept();
     return a > b ? a : b;
 }
 
 int64_t grim_gdr_workspace(int64_t N, int32_t nseq, int32_t heads, int32_t key_heads, int32_t dk, int32_t dv) {
     using namespace grim::lm;
-    if (!gdr_shape(N, nseq, heads, key_heads, dk, dv) || dk > kMostHeadSize || dv > kMostHeadSize) return 0;
+    if (gdr_check(N, nseq, heads, key_heads, dk, dv) != GRIM_OK) return 0;
     const int64_t a = GdrRoom<float>(N, nseq, heads, dk, dv).scratch(), b = GdrRoom<f16>(N, nseq, heads, dk, dv).scratch();
     return a > b ? a : b;
 }

@@ -420,11 +420,15 @@ inline bool gdr_shape(int64_t N, int32_t nseq, int32_t heads, int32_t key_heads,
     return N >= 0 && N <= (int64_t)1 << 30 && nseq >= 1 && heads >= 1 && heads <= kMostHeads && key_heads >= 1 && heads % key_heads == 0 && dk >= 1 && dv >= 1;
 }
 
+inline grim_status gdr_check(int64_t N, int32_t nseq, int32_t heads, int32_t key_heads, int32_t dk, int32_t dv) {
+    if (!gdr_shape(N, nseq, heads, key_heads, dk, dv)) return GRIM_ERR_SHAPE;
+    // (a launch has fewer than 2^32 threads: of a run 4 workgroups of 256 or one of 512, of a sequence that is long enough for the join, one of 5 chunks, 8 of 512)
+    return dk > kMostHeadSize || dv > kMostHeadSize || (N / 32 + nseq) * heads > (int64_t)1 << 21 ? GRIM_ERR_UNSUPPORTED : GRIM_OK;
+}
 inline grim_status gdr_check(grim_dtype dt, int64_t N, int32_t nseq, bool starts, int32_t heads, int32_t key_heads, int32_t dk, int32_t dv, float scale, float eps) {
     if (!known(dt)) return GRIM_ERR_DTYPE;
-    if (!gdr_shape(N, nseq, heads, key_heads, dk, dv) || (nseq > 1 && !starts) || !(fabsf(scale) < INFINITY) || !(eps >= 0.f) || eps > 3.4e38f) return GRIM_ERR_SHAPE;
-    if (dk > kMostHeadSize || dv > kMostHeadSize || (int64_t)nseq * heads > (int64_t)1 << 23) return GRIM_ERR_UNSUPPORTED;
-    return GRIM_OK;
+    if ((nseq > 1 && !starts) || !(fabsf(scale) < INFINITY) || !(eps >= 0.f) || eps > 3.4e38f) return GRIM_ERR_SHAPE;
+    return gdr_check(N, nseq, heads, key_heads, dk, dv);
 }
 
 // Tokens of a run.  Over runs of s chunks a head of n chunks costs 2 s chunks (what a run does to the states has to be formed first) and n / s steps of the join instead of n chunks,

@@ -258,7 +258,6 @@ grim_status back_launch(const GdrBack &b, hipStream_t stream) {
     static const hipError_t grown = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (grown != hipSuccess) return GRIM_ERR_DEVICE;
     const int64_t groups = runs_of(b.p.N, b.p.nseq, b.p.size) * b.p.heads * ((b.p.tiles + W - 1) / W);
-    if (groups > most_groups(64 * W)) return GRIM_ERR_UNSUPPORTED;
     hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(64 * W), bytes, stream, b);
     return launched();
 }
@@ -289,7 +288,6 @@ template <typename T>
 grim_status back_typed(GdrBack b, const void *states, void *workspace, hipStream_t stream) {
     GdrParams &p = b.p;
     p.size = run_of<T>(p.N, p.nseq, p.heads, p.dv);
-    if (places_of<T>(p.N, p.nseq) > most_groups(64 * 8) / p.heads) return GRIM_ERR_UNSUPPORTED;
     const GdrRoom<T> room(p.N, p.nseq, p.heads, p.dk, p.dv);
     char *kept = static_cast<char *>(const_cast<void *>(states)), *at = static_cast<char *>(workspace);      // (read only)
     p.saved = kept;

@@ -85,7 +85,6 @@ __global__ void __launch_bounds__(DK * 4) join_kernel(GdrParams p) {
 template <typename T, int DK, bool BACK>
 grim_status join_runs(const GdrParams &p, hipStream_t stream) {
     const int64_t groups = (int64_t)p.nseq * p.heads * p.tiles;
-    if (groups > most_groups(DK * 4)) return GRIM_ERR_UNSUPPORTED;
     hipLaunchKernelGGL((join_kernel<T, DK, BACK>), dim3((unsigned)groups), dim3(DK * 4), 0, stream, p);
     return launched();
 }

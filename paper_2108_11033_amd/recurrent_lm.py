@@ -107,6 +107,44 @@ class GatedRecurrence(torch.autograd.Function):
         return dgates, dbias.to(ctx.types[0]), dh0.to(ctx.types[1]), None
 
 
+class GatedDeltaRule(torch.autograd.Function):
+    """(outputs, last states in fp32) of packed sequences: q and k N x key heads x Dk, v N x heads x Dv, decay (logarithms, at most 0) and beta N x heads, s0 sequences x heads x
+    Dk x Dv; seq_start holds the sequences' starts and the end.  norm_eps > 0: queries and keys count divided by their lengths."""
+
+    @staticmethod
+    def forward(ctx, q, k, v, decay, beta, s0, seq_start, scale, norm_eps):
+        _check(q.dim() == v.dim() == 3 and q.shape == k.shape and q.shape[0] == v.shape[0] and q.shape[1] >= 1 and v.shape[1] % q.shape[1] == 0 and q.dtype == k.dtype == v.dtype,
+               f"queries of {tuple(q.shape)}, keys of {tuple(k.shape)} and values of {tuple(v.shape)} ({q.dtype}, {k.dtype}, {v.dtype})")
+        N, hk, Dk = q.shape
+        h, Dv = v.shape[1:]
+        _check(decay.shape == beta.shape == (N, h), f"{N} rows of {h} heads with decays of {tuple(decay.shape)} and betas of {tuple(beta.shape)}")
+        _check(s0.dim() == 4 and s0.shape[0] >= 1 and s0.shape[1:] == (h, Dk, Dv), f"states of {tuple(s0.shape)} for {h} heads of {Dk} x {Dv}")
+        _check(seq_start.numel() == s0.shape[0] + 1 and _whole(seq_start),
+               f"states of {s0.shape[0]} sequences with starts of {tuple(seq_start.shape)} ({seq_start.dtype})")
+        _check_place(q, k, v, decay, beta, s0, seq_start)
+        ctx.types = decay.dtype, beta.dtype, s0.dtype
+        q, k, v, seq_start = q.contiguous(), k.contiguous(), v.contiguous(), seq_start.int().contiguous()
+        decay, beta, s0 = _fp32(decay), _fp32(beta), _fp32(s0)
+        ctx.sizes = (s0.shape[0], N, h, hk, Dk, Dv, scale, norm_eps)
+        y, s_last = torch.empty_like(v), torch.empty_like(s0)
+        states = _scratch(lm.gdr_states(N, s0.shape[0], h, Dk, Dv), q.device)
+        lm.gdr_sequence(q, k, v, DTYPES[q.dtype], hk * Dk, hk * Dk, h * Dv, decay, beta, h, s0, seq_start, *ctx.sizes, y, h * Dv, s_last, states,
+                        _scratch(lm.gdr_workspace(N, s0.shape[0], h, hk, Dk, Dv), q.device), torch.cuda.current_stream())
+        ctx.save_for_backward(q, k, v, decay, beta, s0, seq_start, states)
+        return y, s_last
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy, ds_last):
+        q, k, v, decay, beta, s0, seq_start, states = ctx.saved_tensors
+        nseq, N, h, hk, Dk, Dv = ctx.sizes[:6]
+        dq, dk, dv, ddecay, dbeta, ds0 = (torch.empty_like(t) for t in (q, k, v, decay, beta, s0))
+        lm.gdr_sequence_backward(q, k, v, DTYPES[q.dtype], hk * Dk, hk * Dk, h * Dv, decay, beta, h, s0, seq_start, *ctx.sizes, states, dy.contiguous(), h * Dv,
+                                 ds_last.contiguous(), dq, hk * Dk, dk, hk * Dk, dv, h * Dv, ddecay, dbeta, h, ds0,
+                                 _scratch(lm.gdr_workspace(N, nseq, h, hk, Dk, Dv), q.device), torch.cuda.current_stream())
+        return dq, dk, dv, *(t.to(dtype) for t, dtype in zip((ddecay, dbeta, ds0), ctx.types)), None, None, None
+
+
 class DistillTopK(torch.autograd.Function):
     """The sum over rows of weight times the distillation loss.  The gradient is formed with the loss, in one pass over the logits; the
     teacher's logits and the weights get none.  The lists are N x k (numbers of any whole type: those outside 0 .. V-1 are absent), weight N."""
@@ -134,6 +172,49 @@ class DistillTopK(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, upstream):
         return ctx.saved_tensors[0] * upstream, None, None, None, None
+
+
+class PolicyLoss(torch.autograd.Function):
+    """(the sum over rows of the clipped policy loss, the words' logarithms) of N x V logits.  ids: the sampled words, N (of any whole type; a row whose word lies outside 0 .. V-1 is
+    padding); old_logp and ref_logp: what the policy that sampled them and the reference give them, or None; advantage and weight N.  Only the logits get a gradient, formed with the loss."""
+
+    @staticmethod
+    def forward(ctx, logits, ids, old_logp, ref_logp, advantage, weight, temperature, clip, kl):
+        _check(logits.dim() == 2, f"logits are rows of a vocabulary, not {tuple(logits.shape)}")
+        N, V = logits.shape
+        given = [t for t in (old_logp, ref_logp, advantage, weight) if t is not None]
+        _check(ids.numel() == N and _whole(ids) and all(t.numel() == N for t in given),
+               f"{N} rows of logits with words of {tuple(ids.shape)} ({ids.dtype}) and rows of {[tuple(t.shape) for t in given]}")
+        _check_place(logits, ids, *given)
+        logits = logits.contiguous()
+        if ids.dtype != torch.int32:                           # (before they are cut to 32 bits)
+            ids = ids.long()
+            ids = torch.where((ids >= 0) & (ids < V), ids, -1).int()
+        ids = ids.contiguous()
+        old_logp, ref_logp, advantage, weight = (None if t is None else _fp32(t) for t in (old_logp, ref_logp, advantage, weight))
+        loss, logp, dz = logits.new_empty(N, dtype=torch.float32), logits.new_empty(N, dtype=torch.float32), torch.empty_like(logits)
+        lm.policy_loss(logits, DTYPES[logits.dtype], V, ids, N, V, loss, logp, dz, V, _scratch(lm.policy_loss_workspace(N, V), logits.device), old_logp=old_logp,
+                       ref_logp=ref_logp, advantage=advantage, weight=weight, temperature=temperature, clip_low=clip, clip_high=clip, kl=kl,
+                       stream=torch.cuda.current_stream())
+        ctx.save_for_backward(dz)
+        ctx.mark_non_differentiable(logp)
+        return loss.sum(), logp
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, upstream, _):
+        return ctx.saved_tensors[0] * upstream, None, None, None, None, None, None, None, None
+
+
+def clip_gradients(parameters, max_norm: float, unscale: float = 1.0) -> torch.Tensor:
+    """Every gradient times unscale min(1, max_norm / norm), in place; the norm (of all, unscaled), one number on the GPU."""
+    grads = [p.grad for p in parameters if p.grad is not None]
+    _check_place(*grads)
+    group = lm.GradList(grads)
+    dev = torch.device("cuda", torch.cuda.current_device())
+    norm = torch.empty(1, device=dev)
+    lm.grad_clip(group, max_norm, unscale, norm, _scratch(group.workspace, dev), torch.cuda.current_stream())
+    return norm
 
 
 class RecurrentLM(torch.nn.Module):
@@ -189,8 +270,8 @@ class RecurrentLM(torch.nn.Module):
         return LayerNorm.apply(x, self.gammas[-1], self.betas[-1]) @ self.weight("head").t(), last
 
 
-def distill(student: RecurrentLM, teacher: RecurrentLM, batches, k: int = 16, temperature: float = 2.0, rate: float = 1e-2):
-    """One step of distillation per batch of (tokens, seq_start); the losses."""
+def distill(student: RecurrentLM, teacher: RecurrentLM, batches, k: int = 16, temperature: float = 2.0, rate: float = 1e-2, max_norm: float | None = None):
+    """One step of distillation per batch of (tokens, seq_start), gradients clipped by their norm if max_norm is given; the losses."""
     optimizer = torch.optim.Adam(student.parameters(), lr=rate)
     losses = []
     for tokens, seq_start in batches:
@@ -201,8 +282,33 @@ def distill(student: RecurrentLM, teacher: RecurrentLM, batches, k: int = 16, te
         loss = DistillTopK.apply(logits, top.values.float().contiguous(), top.indices.int().contiguous(), temperature, weight)
         optimizer.zero_grad()
         loss.backward()
+        if max_norm is not None:
+            clip_gradients(student.parameters(), max_norm)
         optimizer.step()
         losses.append(float(loss.detach()))
+    return losses
+
+
+def reinforce(model: RecurrentLM, batches, rate: float = 1e-3, temperature: float = 1.0, clip: float = 0.2, kl: float = 0.05, max_norm: float = 1.0, epochs: int = 2):
+    """Steps of the clipped policy loss per batch of (tokens, seq_start, advantage of every token; the last token of a text is followed by none): the policy that the texts came from,
+    and the reference of the KL term, is the model before the batch's first step.  The losses."""
+    optimizer = torch.optim.Adam(model.parameters(), lr=rate)
+    losses = []
+    for tokens, seq_start, advantage in batches:
+        ends = seq_start[1:].long() - 1
+        words = torch.cat([tokens[1:], tokens[:1]]).int()
+        words[ends[ends >= 0]] = -1                            # (an empty text ends where the one before it does)
+        weight = torch.full((tokens.numel(),), 1.0 / tokens.numel(), device=tokens.device)
+        old = None
+        for _ in range(epochs):
+            logits, _ = model(tokens, seq_start)
+            loss, logp = PolicyLoss.apply(logits, words, old, old, advantage, weight, temperature, clip, kl)
+            old = logp if old is None else old
+            optimizer.zero_grad()
+            loss.backward()
+            clip_gradients(model.parameters(), max_norm)
+            optimizer.step()
+            losses.append(float(loss.detach()))
     return losses
 
 

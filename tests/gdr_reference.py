@@ -1,7 +1,7 @@
 """The gated delta rule token by token in 64 bits, with PyTorch's own gradients of it, and what the kernels' results may be off by.
 
-A product of operands in parts is off by at most u of its terms' 2-norms, u = 2^-16 with two parts (3 x 2^-18 for the parts left out and 64 to 128 additions in fp32)
-and 2^-22 with three.  Keys no longer than one, betas and decays in 0 .. 1 make a token's map of the states a contraction, so that what is off stays
+A product of operands in up to three parts is off by at most u = 2^-22 of its terms' 2-norms (2^-24 for the parts left out; 64 to 128 additions in fp32, whose errors are
+independent of each other, as much again).  Keys no longer than one, betas and decays in 0 .. 1 make a token's map of the states a contraction, so that what is off stays
 that far off: an output is six to nine products away from the inputs (forward and backward), whose errors are independent of each other.  A column j of the states is
 at most R_j = max over its tokens of |S_j| and |v_j| in 2-norm, so states are off by 16 u R_j and y by that times the query's length; a gradient is counted by the
 norms of the factors of its terms in the same way."""
@@ -9,7 +9,7 @@ import math
 
 import torch
 
-UNIT_OF = {"f32": 2.0 ** -22, "f16": 2.0 ** -22, "bf16": 2.0 ** -22}
+UNIT = 2.0 ** -22
 COUNT = 16
 CHUNK = {"f32": 32, "f16": 64, "bf16": 64}
 
@@ -20,7 +20,7 @@ def _normal(x, eps):
 
 def run(q, k, v, decay, beta, s0, starts, heads, key_heads, dk, dv, scale, eps, dy=None, ds_last=None, dtype="f32"):
     """{name: (value, slack)} of y, s_last and (dy given) the gradients; every tensor in 64 bits and shaped as the call has it."""
-    N, nseq, u = q.shape[0], len(starts) - 1, COUNT * UNIT_OF[dtype]
+    N, nseq, u = q.shape[0], len(starts) - 1, COUNT * UNIT
     leaf = lambda t: t.detach().double().clone().requires_grad_(dy is not None)
     q, k, v, decay, beta = (leaf(t) for t in (q, k, v, decay, beta))
     s0 = leaf(s0 if s0 is not None else torch.zeros(nseq, heads, dk, dv, device=q.device))

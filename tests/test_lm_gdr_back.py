@@ -114,6 +114,23 @@ def test_no_tokens():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_rows_behind_the_last_sequence(dtype):
+    """Rows that no sequence has are neither read nor written."""
+    c = Back(dtype, [0, 40, 90], 2, 1, 16, 24, seed=13)
+    whole = {n: t.clone() for n, t in c.backward().items()}
+    y = c.forward()[0].clone()
+    c.seq = torch.tensor([0, 40, 70], dtype=torch.int32, device="cuda")
+    for t in (c.q, c.k, c.v, c.decay, c.beta, c.dy):
+        t[70:] = math.nan
+    cut, _ = c.forward()
+    assert torch.equal(cut[:40], y[:40]) and torch.isfinite(cut[:70]).all() and torch.isnan(cut[70:]).all()
+    got = c.backward()
+    for n in NAMES[:5]:
+        assert torch.isfinite(got[n][:70]).all() and torch.isnan(got[n][70:]).all() and torch.equal(got[n][:40], whole[n][:40]), n
+
+
+@pytest.mark.gpu
 def test_differences():
     """Along a direction, the gradients add up to the difference of the 64-bit formula's results; what the difference of step h is off by is at most what steps h and 2 h differ
     by, and the sums' own errors are their slacks and half a step of their type along the direction."""
@@ -148,7 +165,8 @@ def test_refusals():
                 dict(nseq=0), dict(seq=None), dict(heads=3), dict(key_heads=0), dict(dk=0), dict(dv=0), dict(scale=math.nan), dict(eps=-1.0),
                 dict(room=g.gdr_workspace(100, 2, 4, 2, 16, 8) - 1)):
         assert name(**bad) == "GRIM_ERR_SHAPE", bad
-    assert name(dk=129, ldq=300, ldk=300, lddq=300, lddk=300) == "GRIM_ERR_UNSUPPORTED"
+    assert name(dk=129, ldq=300, ldk=300, lddq=300, lddk=300) == "GRIM_ERR_UNSUPPORTED" and name(N=1 << 24) == "GRIM_ERR_UNSUPPORTED" and name(nseq=1 << 20) == "GRIM_ERR_UNSUPPORTED"
+    assert g.gdr_states(1 << 24, 2, 4, 16, 8) == g.gdr_workspace(1 << 24, 2, 4, 2, 16, 8) == 0
     assert name(ds0=F_) == "GRIM_ERR_UNSUPPORTED" and name(ds0=F_ + 4) == "GRIM_ERR_UNSUPPORTED"
     for bad in (dict(q=None), dict(decay=None), dict(states=None), dict(dy=None), dict(dq=None), dict(dkey=None), dict(dvalue=None), dict(ddecay=None), dict(dbeta=None), dict(ws=None)):
         assert name(**bad) == "GRIM_ERR_NULL", bad
