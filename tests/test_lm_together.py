@@ -74,7 +74,7 @@ def test_a_training_step():
     loss, logp, s_last, norm = _step(p, batch, seq)
     want = _plain(p, batch)
     # three products and a recurrence in fp32 one after another, of 64 to 200 terms: below 1e-4 of the values' size
-    near = lambda a, b: float((a.double() - b).norm()) <= 1e-4 * float(b.norm())
+    near = lambda a, b: float((a.detach().double() - b).norm()) <= 1e-4 * float(b.norm())
     assert near(loss, want[0]) and near(logp, want[1]) and near(s_last, want[2]) and near(norm[0], want[3])
     for n, t in p.items():
         assert float((t.grad.double() - want[4][n]).norm()) <= 2e-4 * float(want[4][n].norm()) + 1e-9, n
