@@ -131,6 +131,30 @@ def test_rows_behind_the_last_sequence(dtype):
 
 
 @pytest.mark.gpu
+def test_rows_far_apart():
+    """Offsets beyond 32 bits: 600 rows of 4 M elements, the operands beside each other in them."""
+    c = Back("bf16", [0, 100, 600], 2, 1, 16, 24, seed=21)
+    near, ld = c.backward(), 4_000_000
+    y, s_last = c.forward()
+    far_in, far_out = (torch.empty(600 * ld, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+
+    def place(buf, at, t):
+        view = buf.as_strided((600, t.shape[1]), (ld, 1), ld - 256 + at)
+        view.copy_(t)
+        return view
+    q, k, v, dy = (place(far_in, 64 * i, t) for i, t in enumerate((c.q, c.k, c.v, c.dy)))
+    Y, dq, dk, dv = (place(far_out, 64 * i, torch.full_like(t, math.nan)) for i, t in enumerate((c.v, c.q, c.k, c.v)))
+    rest = c.head()
+    again = torch.empty_like(s_last)
+    g.gdr_sequence(q, k, v, "bf16", ld, ld, ld, *rest[7:], Y, ld, again, c.states, c.ws)
+    gates = [torch.empty(600, 2, device="cuda") for _ in range(2)]
+    ds0 = torch.empty_like(s_last)
+    g.gdr_sequence_backward(q, k, v, "bf16", ld, ld, ld, *rest[7:], c.states, dy, ld, c.ds_last, dq, ld, dk, ld, dv, ld, *gates, 2, ds0, c.ws)
+    for a, b in ((Y, y), (again, s_last), (dq, near["dq"]), (dk, near["dk"]), (dv, near["dv"]), (gates[0], near["ddecay"]), (gates[1], near["dbeta"]), (ds0, near["ds0"])):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.gpu
 def test_differences():
     """Along a direction, the gradients add up to the difference of the 64-bit formula's results; what the difference of step h is off by is at most what steps h and 2 h differ
     by, and the sums' own errors are their slacks and half a step of their type along the direction."""
