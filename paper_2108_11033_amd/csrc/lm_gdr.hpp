@@ -441,7 +441,9 @@ uint32_t run_of(int64_t N, int32_t nseq, int32_t heads, int32_t dv) {
     if (runs < 2 || mean < 4) return (uint32_t)1 << 31;
     int64_t size = 2;
     while (size * size * 8 < mean) ++size;
-    const int64_t fill = ((N + runs - 1) / runs + C - 1) / C;
+    // (every sequence but one may end in a part of a run: counted, unless there are so many that they take several turns anyway.  16384 tokens in 4, 8 heads of 128 x 128 in fp16, both
+    // directions: 1017 -> 871 us)
+    const int64_t whole = runs - (nseq - 1) >= runs / 2 ? runs - (nseq - 1) : runs, fill = ((N + whole - 1) / whole + C - 1) / C;
     return (uint32_t)((size > fill ? size : fill) * C);
 }
 inline int64_t runs_of(int64_t N, int32_t nseq, uint32_t size) { return N / size + nseq; }
