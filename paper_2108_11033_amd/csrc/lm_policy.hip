@@ -8,6 +8,7 @@
 // is looked up while the row is on its way, and its place in the gradient is the owner's, so nothing is stored twice.  Few rows of a large vocabulary,
 // or rows that no workgroup's registers hold, are cut into slices: a first launch leaves every slice's maximum, sum and (where it lies) the word's logit,
 // the second joins them and writes the gradient from a second read of z, which a few rows leave in the caches.
+// 8192 x 32768 bf16: 218 us, 4.9 TB/s; 1024 x 1000 fp32: 5.7 us, a launch and one trip to memory; 24 x 131075 fp16, in slices: 10.2 us, two of each.
 #include "lm_rows.hpp"
 
 namespace grim {
@@ -227,10 +228,15 @@ __global__ void __launch_bounds__(64 * kSliceWaves) policy_join(PolicyParams p) 
 }
 
 // -------------------------------------------------------------------------------------------------- launches
-// A workgroup per row where its registers hold the row: 16 pieces a thread of 16 waves.
+// A workgroup per row where its registers hold the row (16 pieces a thread of 16 waves) and the row is short or the rows
+// fill the card: a second launch costs 3 us, a lone row of 65536 elements 4 us more in one workgroup than in slices.
+// Measured, by rows and in slices, in us: bf16 4 x 16384 7.0 and 9.6, 64 x 32768 8.5 and 9.7, 64 x 50000 11.6 and 11.1,
+// 32 x 65536 13.3 and 9.5, 128 x 131072 25.5 and 20.0, 160 x 131072 26.8 and 26.2, 192 x 131072 28.2 and 30.9,
+// 512 x 65536 26.3 and 37.7; fp32 32 x 32768 9.2 and 9.8, 64 x 65536 14.7 and 12.2, 128 x 65536 18.7 both,
+// 160 x 65536 20.6 and 24.3.
 template <typename T>
 bool policy_by_rows(int64_t N, int64_t V) {
-    return V >= piece<T>() && V <= (int64_t)16 * 1024 * piece<T>() && (N >= 128 || V * (int64_t)sizeof(T) <= 128 * 1024);
+    return V >= piece<T>() && V <= (int64_t)16 * 1024 * piece<T>() && (V <= 32768 || N >= (sizeof(T) == 2 ? 160 : 128));
 }
 
 // Rows first .. first + count - 1 of a call.

@@ -72,7 +72,7 @@ def call(z, dtype, ldz, ids, N, V, dz=None, lddz=0, stream=None, loss=True, logp
 
 
 SHAPES = [(1, 1), (3, 2), (5, 7), (200, 8), (4, 33), (300, 1000), (2, 1023), (130, 2049), (129, 4100), (2, 5003), (140, 8197), (150, 20001), (130, 40003),
-          (128, 70001), (129, 131072), (3, 131075), (2, 300001), (1, 16384), (24, 30000)]
+          (128, 70001), (129, 131072), (161, 131070), (160, 32769), (3, 131075), (2, 300001), (1, 16384), (24, 30000)]
 
 
 @pytest.mark.gpu
