@@ -17,6 +17,7 @@ namespace lm {
 
 // M of every chunk and head, and G: a workgroup each.  L by the matrix cores, M by forward substitution: blocks of 16 x 16, those on the diagonal a column a lane, then
 // block by block away from it, M_IJ = Z - M_II beta Z with Z = L_IJ - sum over J <= K < I of L_IK beta M_KJ, in fp32 on the matrix cores.
+// Bound by the vector ALUs (two thirds of its time: lengths, decays, substitution, splitting): 4096 chunks of 128-wide heads 56 us, 6640 of 64-wide ones 72.
 template <typename T, int DK, bool WHOLE>
 __global__ void __launch_bounds__(kMatrixThreads) chunk_matrices(GdrParams p) {
     constexpr int C = Gdr<T>::chunk, PD = Gdr<T>::data, PC = Gdr<T>::comp, TT = C / 32, B = C / 16, LD = C + 4;
@@ -179,6 +180,8 @@ struct WalkRoom {
 // A workgroup takes 16 CT W columns of the states of a run of chunks of a sequence's head.  All that a chunk does to a column of the states stays in that column, so each of its W waves
 // has 16 CT columns to itself from chunk to chunk, in registers: results that are sums over tokens or keys are the next product's operands.  The waves meet only where keys, queries,
 // values and M are placed in LDS and where the products of queries and keys, which all need, are formed.
+// A chunk is six phases between barriers, of fetches, LDS reads, matrix and vector work in turn, none of which takes half the time (matrix cores 33 %, vector ALUs 40 %, LDS 40 % of it).  4096
+// chunks of 128 x 128 heads in bf16 with all that the backward pass needs 165 us, 0.73 GB moved at 4.4 TB/s; the maps of their 31 runs 170 us; 64 x 64 heads, 6000 chunks, 163 and 64.
 // MAPS: no outputs; what every run but a sequence's last does to the states, as S -> A S + B: B's columns (into the places of the states in front of the next run; of a sequence's
 // first run, whose start is known, these are the states themselves) come from a start of zeros, A's from the columns of 1 and values of zero.
 // HELP: the second half of the waves has no columns; they form the products of queries and keys.

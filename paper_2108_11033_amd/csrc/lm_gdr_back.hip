@@ -28,6 +28,7 @@ struct BackRoom {
 // A workgroup takes 16 W columns of the states of a run of a sequence's head, its chunks from the last to the first.
 // MAPS: what every run but a sequence's first adds to the gradient of the states in front of it, from a gradient of zeros behind it (of the last run, whose end
 // is known, this is the gradient itself); what it makes of the gradient behind it is its map of the forward pass, transposed.
+// Bound as the forward walk is: 4096 chunks of 128 x 128 heads in bf16 169 us (0.73 GB), the runs' parts 141; 64 x 64 heads, 6000 chunks, 163 and 82.
 // HELP: the second half of the waves has no columns; they form P.
 template <typename T, int DK, int W, bool WHOLE, bool MAPS, bool HELP>
 __global__ void __launch_bounds__(64 * W, 2) walk_back(GdrBack b) {

