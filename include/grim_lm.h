@@ -101,7 +101,7 @@ grim_status grim_glr_step(const float *gates_dev, int64_t ldg, const float *bias
  * values.  A token decays the states, looks up what they hold for its key and moves that towards its value:
  *     D_t = exp(g_t) S_(t-1)     e_t = v_t - D_t' k_t     S_t = D_t + beta_t k_t e_t'     y_t = scale S_t' q_t
  *   q_dev, k_dev    N x (key_heads dk) of element type dt, rows of ldq, ldk; head h reads key head h / (heads / key_heads).  norm_eps > 0: each head's
- *                   query and key count divided by sqrt(their squares' sum + norm_eps); 0: as they are (keys longer than one, with beta
+ *                   query and key count divided by sqrt(their squares' sum in fp32 + norm_eps); 0: as they are (keys longer than one, with beta
  *                   near 1, make the states grow without bound)
  *   v_dev           N x (heads dv) of element type dt, rows of ldv
  *   decay_dev, beta_dev   N x heads fp32, rows of ldg: g (the logarithm of the decay, at most 0; below -10000, -infinity too, it counts as
@@ -121,9 +121,9 @@ grim_status grim_glr_step(const float *gates_dev, int64_t ldg, const float *bias
  * terms' size before their rounding.  Values beyond 3.3e38 count as infinite.
  * grim_gdr_step is one token for `batch` callers at once, columns as of grim_glr_step: q and k (key_heads dk) x batch, v (heads dv) x batch, g and beta
  * heads x batch, all fp32; states batch x heads x dk x dv fp32 as the sequence calls have them (s_new_dev may be s_dev itself), y (heads dv) x batch of element
- * type dt, or NULL.  Its arithmetic is fp32.
+ * type dt, or NULL, not over the inputs.  Its arithmetic is fp32.
  * Errors: NULL, SHAPE (N < 0, N > 2^30, nseq < 1, nseq > 1 without starts, heads < 1 or > 4096, heads not a multiple of key_heads, dk or dv < 1, leading
- * dimension or a buffer too small, scale not finite, norm_eps negative), DTYPE, DEVICE, UNSUPPORTED (dk or dv > 128,
+ * dimension or a buffer too small, scale neither 0 nor 1e-30 .. 1e30 in size, norm_eps neither 0 nor 1e-16 .. 1e30), DTYPE, DEVICE, UNSUPPORTED (dk or dv > 128,
  * (N / 32 + nseq) heads above 2^21, s_last over s0, ds0 over ds_last, s_new over a part of s).
  */
 int64_t grim_gdr_states(int64_t N, int32_t nseq, int32_t heads, int32_t dk, int32_t dv);

@@ -430,8 +430,8 @@ template <typename T, int DK, int W, int CT, bool WHOLE, bool MAPS, bool HELP = 
 grim_status walk_launch(const GdrParams &p, hipStream_t stream) {
     constexpr int bytes = WalkRoom<T, DK, 16 * CT * W, MAPS>::bytes;
     const auto kernel = walk<T, DK, W, CT, WHOLE, MAPS, HELP>;
-    static const hipError_t grown = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (grown != hipSuccess) return GRIM_ERR_DEVICE;
+    static std::atomic<bool> grown{false};
+    if (!lds_of(reinterpret_cast<const void *>(kernel), bytes, grown)) return GRIM_ERR_DEVICE;
     const int64_t blocks = (p.tiles + CT * W - 1) / (CT * W) + (MAPS ? (DK / 16 + CT * W - 1) / (CT * W) : 0), groups = runs_of(p.N, p.nseq, p.size) * p.heads * blocks;
     hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(64 * W), bytes, stream, p);
     return launched();

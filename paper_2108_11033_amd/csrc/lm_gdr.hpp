@@ -6,6 +6,8 @@
 // (Two parts for it would be off by 2^-17, which outputs of 16 bits hide but the states and the gates' gradients do not: those were 1e-6 to 6e-6 off in the 2-norm, and are 6e-8 to 4e-7
 // with three.  What that costs: 32768 tokens x 8 heads of 128 x 128 in bf16, both directions, 1077 -> 1262 us.  The fp32 matrix instruction does a sixteenth of the work of the bf16 one.)
 #pragma once
+#include <atomic>
+
 #include "lm_common.hpp"
 
 namespace grim {
@@ -425,9 +427,13 @@ inline grim_status gdr_check(int64_t N, int32_t nseq, int32_t heads, int32_t key
     // (a launch has fewer than 2^32 threads: of a run 4 workgroups of 256 or one of 512, of a sequence that is long enough for the join, one of 5 chunks, 8 of 512)
     return dk > kMostHeadSize || dv > kMostHeadSize || (N / 32 + nseq) * heads > (int64_t)1 << 21 ? GRIM_ERR_UNSUPPORTED : GRIM_OK;
 }
+// (the lengths' squares, factors of queries and their reciprocals stay far from the ends of fp32)
+inline bool gdr_factors(float scale, float eps) {
+    return (scale == 0.f || (fabsf(scale) >= 1e-30f && fabsf(scale) <= 1e30f)) && (eps == 0.f || (eps >= 1e-16f && eps <= 1e30f));
+}
 inline grim_status gdr_check(grim_dtype dt, int64_t N, int32_t nseq, bool starts, int32_t heads, int32_t key_heads, int32_t dk, int32_t dv, float scale, float eps) {
     if (!known(dt)) return GRIM_ERR_DTYPE;
-    if ((nseq > 1 && !starts) || !(fabsf(scale) < INFINITY) || !(eps >= 0.f) || eps > 3.4e38f) return GRIM_ERR_SHAPE;
+    if ((nseq > 1 && !starts) || !gdr_factors(scale, eps)) return GRIM_ERR_SHAPE;
     return gdr_check(N, nseq, heads, key_heads, dk, dv);
 }
 
@@ -470,6 +476,16 @@ struct GdrRoom {
 // S_(r + 1) = A_r S_r + B_r from run to run of every sequence and head; BACK: the gradients, the other way through the transposed maps (lm_gdr_join.hip).
 template <typename T, int DK, bool BACK>
 grim_status join_runs(const GdrParams &p, hipStream_t stream);
+
+// Raises a kernel's LDS limit, once per process.
+inline bool lds_of(const void *kernel, int bytes, std::atomic<bool> &grown) {
+    if (grown) return true;
+    if (hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess) {
+        (void)hipGetLastError();
+        return false;
+    }
+    return grown = true;
+}
 
 // The gradients of queries, keys, decays and betas from what the chunks left (lm_gdr_grad.hip).
 template <typename T, int DK, bool WHOLE>

@@ -256,8 +256,8 @@ template <typename T, int DK, int W, bool WHOLE, bool MAPS, bool HELP = false>
 grim_status back_launch(const GdrBack &b, hipStream_t stream) {
     constexpr int bytes = BackRoom<T, DK, 16 * W>::bytes;
     const auto kernel = walk_back<T, DK, W, WHOLE, MAPS, HELP>;
-    static const hipError_t grown = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (grown != hipSuccess) return GRIM_ERR_DEVICE;
+    static std::atomic<bool> grown{false};
+    if (!lds_of(reinterpret_cast<const void *>(kernel), bytes, grown)) return GRIM_ERR_DEVICE;
     const int64_t groups = runs_of(b.p.N, b.p.nseq, b.p.size) * b.p.heads * ((b.p.tiles + W - 1) / W);
     hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(64 * W), bytes, stream, b);
     return launched();

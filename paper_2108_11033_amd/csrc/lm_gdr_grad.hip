@@ -311,8 +311,8 @@ template <typename T, int DK, bool WHOLE>
 grim_status gdr_gradients(const GdrBack &b, hipStream_t stream) {
     constexpr int bytes = GradRoom<T, DK>::bytes;
     const auto kernel = gradients<T, DK, WHOLE>;
-    static const hipError_t grown = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (grown != hipSuccess) return GRIM_ERR_DEVICE;
+    static std::atomic<bool> grown{false};
+    if (!lds_of(reinterpret_cast<const void *>(kernel), bytes, grown)) return GRIM_ERR_DEVICE;
     hipLaunchKernelGGL(kernel, dim3((unsigned)(places_of<T>(b.p.N, b.p.nseq) * b.key_heads)), dim3(DK * 4), bytes, stream, b);
     return launched();
 }

@@ -5,7 +5,7 @@
 // Bound by memory: a head's dk x dv states are read once and written once, held in registers between.  The second form of y takes all that has to be summed
 // over the rows of the state (k'D, q'D, q . k and the lengths of q and k) from one pass, so that a workgroup meets at one barrier.
 // 32 callers with 16 heads of 128 x 128: 13.6 us, 4.95 TB/s; one caller with 16 heads of 64 x 64 4.7 us of kernel.
-#include "lm_common.hpp"
+#include "lm_gdr.hpp"
 
 namespace grim {
 namespace lm {
@@ -134,7 +134,7 @@ extern "C" grim_status grim_gdr_step(const float *q_dev, const float *k_dev, con
     using namespace grim::lm;
     if (!known(dt)) return GRIM_ERR_DTYPE;
     if (heads < 1 || heads > kMostHeads || key_heads < 1 || heads % key_heads || dk < 1 || dv < 1 || batch < 0 || ldq < batch || ldk < batch || ldv < batch ||
-        ldg < batch || (y_dev && ldy < batch) || !(fabsf(scale) < INFINITY) || !(norm_eps >= 0.f) || norm_eps > 3.4e38f)
+        ldg < batch || (y_dev && ldy < batch) || !gdr_factors(scale, norm_eps))
         return GRIM_ERR_SHAPE;
     if (dk > kMostHeadSize || dv > kMostHeadSize) return GRIM_ERR_UNSUPPORTED;
     const int64_t rows = (int64_t)heads * kMostHeadSize;

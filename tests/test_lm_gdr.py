@@ -151,7 +151,8 @@ def test_refusals():
             g.gdr_sequence(q, B_, C_, dtype, ldq, ldk, ldv, decay, E_, ldg, s0, seq, nseq, N, heads, key_heads, dk, dv, scale, eps, y, ldy, last, None, (ws, room))
         return e.value.name
     for bad in (dict(ldq=31), dict(ldk=31), dict(ldv=31), dict(ldy=31), dict(ldg=3), dict(N=-1), dict(N=(1 << 30) + 1), dict(nseq=0), dict(seq=None), dict(heads=0), dict(heads=3),
-                dict(heads=4097, key_heads=1, ldg=4097, ldv=40000, ldy=40000), dict(key_heads=0), dict(dk=0), dict(dv=0), dict(scale=math.nan), dict(scale=math.inf), dict(eps=-1.0),
+                dict(heads=4097, key_heads=1, ldg=4097, ldv=40000, ldy=40000), dict(key_heads=0), dict(dk=0), dict(dv=0), dict(scale=math.nan), dict(scale=math.inf), dict(eps=-1.0), dict(scale=1e-31), dict(scale=-1e31),
+                dict(eps=1e-17), dict(eps=1e31),
                 dict(eps=math.nan), dict(room=g.gdr_workspace(100, 2, 4, 2, 16, 8) - 1)):
         assert name(**bad) == "GRIM_ERR_SHAPE", bad
     assert name(dk=129, ldq=300, ldk=300) == "GRIM_ERR_UNSUPPORTED" and name(dv=129, ldv=600, ldy=600) == "GRIM_ERR_UNSUPPORTED"

@@ -186,7 +186,8 @@ def test_refusals():
                                     dkey, lddk, dvalue, lddv, ddecay, dbeta, lddg, ds0, (ws, room))
         return e.value.name
     for bad in (dict(ldq=31), dict(ldk=31), dict(ldv=31), dict(ldg=3), dict(lddy=31), dict(lddq=31), dict(lddk=31), dict(lddv=31), dict(lddg=3), dict(N=-1), dict(N=(1 << 30) + 1),
-                dict(nseq=0), dict(seq=None), dict(heads=3), dict(key_heads=0), dict(dk=0), dict(dv=0), dict(scale=math.nan), dict(eps=-1.0),
+                dict(nseq=0), dict(seq=None), dict(heads=3), dict(key_heads=0), dict(dk=0), dict(dv=0), dict(scale=math.nan), dict(eps=-1.0), dict(scale=1e-31), dict(scale=-1e31),
+                dict(eps=1e-17), dict(eps=1e31),
                 dict(room=g.gdr_workspace(100, 2, 4, 2, 16, 8) - 1)):
         assert name(**bad) == "GRIM_ERR_SHAPE", bad
     assert name(dk=129, ldq=300, ldk=300, lddq=300, lddk=300) == "GRIM_ERR_UNSUPPORTED" and name(N=1 << 24) == "GRIM_ERR_UNSUPPORTED" and name(nseq=1 << 20) == "GRIM_ERR_UNSUPPORTED"

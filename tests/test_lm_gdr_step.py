@@ -104,7 +104,8 @@ def test_refusals():
             g.gdr_step(q, B_, C_, ldq, ldk, ldv, decay, H_, ldg, s, new, y, "f16", ldy, heads, key_heads, dk, dv, scale, eps, batch)
         return e.value.name
     for bad in (dict(ldq=3), dict(ldk=3), dict(ldv=3), dict(ldg=3), dict(ldy=3), dict(heads=0), dict(heads=5), dict(heads=4097, key_heads=1), dict(key_heads=0), dict(dk=0), dict(dv=-1),
-                dict(scale=math.inf), dict(scale=math.nan), dict(eps=-1.0), dict(eps=math.nan), dict(eps=math.inf), dict(batch=-1)):
+                dict(scale=math.inf), dict(scale=math.nan), dict(eps=-1.0), dict(scale=1e-31), dict(scale=-1e31),
+                dict(eps=1e-17), dict(eps=1e31), dict(eps=math.nan), dict(eps=math.inf), dict(batch=-1)):
         assert name(**bad) == "GRIM_ERR_SHAPE", bad
     assert name(dk=129) == "GRIM_ERR_UNSUPPORTED" and name(dv=200) == "GRIM_ERR_UNSUPPORTED" and name(new=D_ + 4) == "GRIM_ERR_UNSUPPORTED"
     for bad in (dict(q=None), dict(s=None), dict(new=None), dict(decay=None)):
