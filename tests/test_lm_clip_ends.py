@@ -1,0 +1,36 @@
+"""grim_grad_clip where the norm, or the factor that it gives, lies at the ends of fp32 (test_lm_clip.py has the bounds)."""
+import math
+
+import pytest
+import torch
+
+import paper_2108_11033_amd as g
+from test_lm_clip import check, clipped
+from lm_helpers import randn
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("unscale", [1.0, 0.5])
+@pytest.mark.parametrize("place", [False, True])
+def test_a_norm_that_fp32_does_not_hold_leaves_gradients_unclipped(unscale, place):
+    """Finite gradients whose norm reads as infinity: whoever skips the step by it finds them as they were."""
+    grads = [torch.full((9000,), 3e38, device="cuda"), randn(1, 77)]
+    before = [t.clone() for t in grads]
+    outs = grads if place else [torch.empty_like(t) for t in grads]
+    norm, _, _ = clipped(g.GradList(grads, outs), 1.0, unscale)
+    assert float(norm) == math.inf
+    assert all(torch.equal(a, b * unscale) for a, b in zip(outs, before))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("max_norm,size", [(1e-3, 1e36), (1e-2, 1e37), (1.0, 3e36), (1e-7, 1e36)])
+def test_factors_that_fp32_does_not_hold(dtype, max_norm, size):
+    """Factors down to 1e-45 and less: the clipped gradients are ordinary numbers, and keep their digits."""
+    grads = [(randn(2, 5000).clamp(-2, 2) * size).to(dtype), (randn(3, 8200).clamp(-2, 2) * size).to(dtype)]
+    for outs in ([torch.empty_like(t, dtype=torch.float32) for t in grads], [torch.empty_like(t) for t in grads]):
+        norm, _, _ = clipped(g.GradList(grads, outs), max_norm, 1.0)
+        check(grads, outs, grads, norm, max_norm, 1.0)
+    before = [t.clone() for t in grads]
+    norm, _, _ = clipped(g.GradList(grads), max_norm, 1.0)
+    check(grads, grads, before, norm, max_norm, 1.0)

@@ -1,0 +1,66 @@
+"""The losses, the clipping and the policy's steps of recurrent_lm.py as a training loop calls them: losses under a scale that the backward pass brings, rows that no sequence has,
+gradients of any strides, and whole steps against PyTorch's own operations in 64 bits."""
+import copy
+import math
+
+import pytest
+import torch
+
+import test_lm_distill
+import test_lm_policy
+from lm_helpers import EPS32, TORCH, close, randn
+from paper_2108_11033_amd import recurrent_lm as rl
+from test_recurrent_lm import _plain_logits
+
+SCALE = 65536.0
+
+
+# ------------------------------------------------------------------------------------------- losses under a scale
+# Gradients whose sizes lie far below the type's smallest number before the scale: a weight of 2^-13 times a share of 2^-12 or less, in fp16 2^-24.  The bounds are those of
+# gradients with the scale in their weights (a power of two, and another factor: one rounding more of the weight).
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("factor", [SCALE, -3000.0])
+def test_policy_gradients_take_the_scale_before_they_are_rounded(dtype, factor, monkeypatch):
+    monkeypatch.setattr(test_lm_policy, "HIGH", test_lm_policy.LOW)
+    N, V, tau, kl = 40, 4099, 2.0, 0.05
+    z, ids, old, ref, A, w = test_lm_policy.operands(dtype, N, V, tau, 0, 0, 17)
+    w = (w * 2.0 ** -13).contiguous()
+    w[7], ids[9] = 0, -1
+    z.requires_grad_()
+    loss, logp = rl.PolicyLoss.apply(z, ids, old, ref, A, w, tau, test_lm_policy.LOW, kl)
+    (loss * factor).backward()
+    wl, wp, _, sl, sp, _ = test_lm_policy.reference(z.detach(), ids, tau, old, ref, A, w, kl)
+    wdz, sdz = test_lm_policy.reference(z.detach(), ids, tau, old, ref, A, w.double() * factor, kl)[2::3]
+    close(logp, wp, sp, "f32", "logp")
+    assert abs(float(loss.detach()) - float(wl.sum())) <= float(sl.sum()) + N * EPS32 * float(wl.abs().sum())
+    close(z.grad, wdz, sdz + EPS32 * wdz.abs(), dtype, "dz")
+    assert z.grad.dtype == TORCH[dtype] and not z.grad[7].any() and not z.grad[9].any()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+def test_policy_gradients_without_weights_twice_and_of_nothing(dtype):
+    N, V = 12, 50
+    z, ids, old, _, A, _ = test_lm_policy.operands(dtype, N, V, 1.0, 0, 0, 19)
+    z.requires_grad_()
+    of = lambda weight: rl.PolicyLoss.apply(z, ids, old, None, A, weight, 1.0, 0.2, 0.0)[0]
+    loss = of(None)
+    one, = torch.autograd.grad(loss, z, retain_graph=True)
+    twice, = torch.autograd.grad(loss, z, torch.tensor(2.0, device="cuda"), retain_graph=True)
+    none, = torch.autograd.grad(loss, z, torch.tensor(0.0, device="cuda"))
+    assert torch.equal(one, torch.autograd.grad(of(torch.ones(N, device="cuda")), z)[0]) and not none.any()
+    large = one.abs() > 2.0 ** -13                                           # (below, fp16 rounds to a fixed step)
+    assert large.any() and torch.equal(twice[large], 2 * one[large])
+
+
+@pytest.mark.gpu
+def test_logits_that_are_others_by_the_backward_pass_are_refused():
+    """What it forms the gradient of 16-bit logits from are the logits that the loss was formed from, or none."""
+    z, ids, old, _, A, _ = test_lm_policy.operands("f16", 12, 50, 1.0, 0, 0, 19)
+    z.requires_grad_()
+    loss = rl.PolicyLoss.apply(z, ids, old, None, A, None, 1.0, 0.2, 0.0)[0]
+    with torch.no_grad():
+        z.add_(1.0)
+    with pytest.raises(RuntimeError, match="inplace"):
+        loss.backward()
