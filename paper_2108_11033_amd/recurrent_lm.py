@@ -146,8 +146,8 @@ class GatedDeltaRule(torch.autograd.Function):
 
 
 class DistillTopK(torch.autograd.Function):
-    """The sum over rows of weight times the distillation loss.  The gradient is formed with the loss, in one pass over the logits; the
-    teacher's logits and the weights get none.  The lists are N x k (numbers of any whole type: those outside 0 .. V-1 are absent), weight N."""
+    """The sum over rows of weight times the distillation loss.  The teacher's logits and the weights get no gradient; that of the logits is formed as PolicyLoss
+    forms it, in fp32 with the loss, in 16 bits after the factor of the backward pass.  The lists are N x k (numbers of any whole type: those outside 0 .. V-1 are absent), weight N."""
 
     @staticmethod
     def forward(ctx, logits, top_logits, top_ids, temperature, weight):
@@ -162,16 +162,30 @@ class DistillTopK(torch.autograd.Function):
             top_ids = top_ids.long()
             top_ids = torch.where((top_ids >= 0) & (top_ids < V), top_ids, -1).int()
         top_ids = top_ids.contiguous()
-        loss, dz = logits.new_empty(N, dtype=torch.float32), torch.empty_like(logits)
-        lm.distill_topk(logits, DTYPES[logits.dtype], V, top_logits, top_ids, top_ids.shape[1], top_ids.shape[1], temperature, weight, N, V,
-                        loss, dz, V, _scratch(lm.distill_topk_workspace(N, V), logits.device), torch.cuda.current_stream())
-        ctx.save_for_backward(dz)
+        ctx.temperature = temperature
+        dz = torch.empty_like(logits) if logits.dtype == torch.float32 else None
+        loss = DistillTopK._call(logits, top_logits, top_ids, temperature, weight, dz)
+        ctx.save_for_backward(*((logits, top_logits, top_ids, weight) if dz is None else (dz,)))
         return loss.sum()
 
     @staticmethod
     @once_differentiable
     def backward(ctx, upstream):
-        return ctx.saved_tensors[0] * upstream, None, None, None, None
+        if len(ctx.saved_tensors) == 1:
+            dz = ctx.saved_tensors[0] * upstream
+        else:
+            logits, top_logits, top_ids, weight = ctx.saved_tensors
+            dz = torch.empty_like(logits)
+            DistillTopK._call(logits, top_logits, top_ids, ctx.temperature, weight * upstream, dz)
+        return dz, None, None, None, None
+
+    @staticmethod
+    def _call(logits, top_logits, top_ids, temperature, weight, dz):
+        N, V = logits.shape
+        loss = logits.new_empty(N, dtype=torch.float32)
+        lm.distill_topk(logits, DTYPES[logits.dtype], V, top_logits, top_ids, top_ids.shape[1], top_ids.shape[1], temperature, weight, N, V,
+                        loss, dz, V, _scratch(lm.distill_topk_workspace(N, V), logits.device), torch.cuda.current_stream())
+        return loss
 
 
 class PolicyLoss(torch.autograd.Function):

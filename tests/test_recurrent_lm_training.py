@@ -64,3 +64,21 @@ def test_logits_that_are_others_by_the_backward_pass_are_refused():
         z.add_(1.0)
     with pytest.raises(RuntimeError, match="inplace"):
         loss.backward()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("factor", [SCALE, -3000.0])
+def test_distillation_gradients_take_the_scale_before_they_are_rounded(dtype, factor):
+    N, V, k, tau = 40, 4099, 16, 2.0
+    z, top, ids, w = test_lm_distill._operands(dtype, N, V, k, 0, 0, 23)
+    w = (w * 2.0 ** -13).contiguous()
+    w[7], ids[9] = 0, -1
+    z.requires_grad_()
+    loss = rl.DistillTopK.apply(z, top, ids, tau, w)
+    (loss * factor).backward()
+    want, _, sl, _ = test_lm_distill.reference(z.detach(), top, ids, tau, w)
+    _, wdz, _, sdz = test_lm_distill.reference(z.detach(), top, ids, tau, w.double() * factor)
+    assert abs(float(loss.detach()) - float(want.sum())) <= float(sl.sum()) + N * EPS32 * float(want.abs().sum())
+    close(z.grad, wdz, sdz + EPS32 * wdz.abs(), dtype, "dz")
+    assert z.grad.dtype == TORCH[dtype] and not z.grad[7].any() and not z.grad[9].any()
