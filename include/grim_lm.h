@@ -107,7 +107,8 @@ grim_status grim_glr_step(const float *gates_dev, int64_t ldg, const float *bias
  *   decay_dev, beta_dev   N x heads fp32, rows of ldg: g (the logarithm of the decay, at most 0; below -10000, -infinity too, it counts as
  *                   -10000, whose exponential is 0) and beta (in 0 .. 1, or up to 2)
  *   s0_dev          nseq x heads x dk x dv fp32: the states before the first tokens, or NULL (zeros)
- *   seq_start_dev   nseq + 1 int32, as of grim_glr_sequence; NULL: one sequence of all rows (nseq = 1)
+ *   seq_start_dev   nseq + 1 int32, as of grim_glr_sequence; NULL: one sequence of all rows (nseq = 1).  Here seq_start[0] may be above 0 and seq_start[nseq] below N: rows
+ *                   that no sequence has are neither read nor written
  *   y_dev           N x (heads dv) of element type dt, rows of ldy; must not overlap the inputs
  *   s_last_dev      nseq x heads x dk x dv fp32, the states after the last tokens (of an empty sequence: its s0), or NULL; must not overlap s0
  *   states_dev      grim_gdr_states(...) bytes for the backward pass, 16-byte aligned, or NULL

@@ -109,7 +109,8 @@ class GatedRecurrence(torch.autograd.Function):
 
 class GatedDeltaRule(torch.autograd.Function):
     """(outputs, last states in fp32) of packed sequences: q and k N x key heads x Dk, v N x heads x Dv, decay (logarithms, at most 0) and beta N x heads, s0 sequences x heads x
-    Dk x Dv; seq_start holds the sequences' starts and the end.  norm_eps > 0: queries and keys count divided by their lengths."""
+    Dk x Dv; seq_start holds the sequences' starts and the end, in ascending order: rows in front of the first start and behind the end (a batch that is padded) have outputs and gradients
+    of 0.  norm_eps > 0: queries and keys count divided by their lengths."""
 
     @staticmethod
     def forward(ctx, q, k, v, decay, beta, s0, seq_start, scale, norm_eps):
@@ -126,7 +127,7 @@ class GatedDeltaRule(torch.autograd.Function):
         q, k, v, seq_start = q.contiguous(), k.contiguous(), v.contiguous(), seq_start.int().contiguous()
         decay, beta, s0 = _fp32(decay), _fp32(beta), _fp32(s0)
         ctx.sizes = (s0.shape[0], N, h, hk, Dk, Dv, scale, norm_eps)
-        y, s_last = torch.empty_like(v), torch.empty_like(s0)
+        y, s_last = torch.zeros_like(v), torch.empty_like(s0)                   # (the kernels leave rows of no sequence as they are)
         states = _scratch(lm.gdr_states(N, s0.shape[0], h, Dk, Dv), q.device)
         lm.gdr_sequence(q, k, v, DTYPES[q.dtype], hk * Dk, hk * Dk, h * Dv, decay, beta, h, s0, seq_start, *ctx.sizes, y, h * Dv, s_last, states,
                         _scratch(lm.gdr_workspace(N, s0.shape[0], h, hk, Dk, Dv), q.device), torch.cuda.current_stream())
@@ -138,7 +139,8 @@ class GatedDeltaRule(torch.autograd.Function):
     def backward(ctx, dy, ds_last):
         q, k, v, decay, beta, s0, seq_start, states = ctx.saved_tensors
         nseq, N, h, hk, Dk, Dv = ctx.sizes[:6]
-        dq, dk, dv, ddecay, dbeta, ds0 = (torch.empty_like(t) for t in (q, k, v, decay, beta, s0))
+        dq, dk, dv, ddecay, dbeta = (torch.zeros_like(t) for t in (q, k, v, decay, beta))
+        ds0 = torch.empty_like(s0)
         lm.gdr_sequence_backward(q, k, v, DTYPES[q.dtype], hk * Dk, hk * Dk, h * Dv, decay, beta, h, s0, seq_start, *ctx.sizes, states, dy.contiguous(), h * Dv,
                                  ds_last.contiguous(), dq, hk * Dk, dk, hk * Dk, dv, h * Dv, ddecay, dbeta, h, ds0,
                                  _scratch(lm.gdr_workspace(N, nseq, h, hk, Dk, Dv), q.device), torch.cuda.current_stream())

@@ -82,3 +82,36 @@ def test_distillation_gradients_take_the_scale_before_they_are_rounded(dtype, fa
     assert abs(float(loss.detach()) - float(want.sum())) <= float(sl.sum()) + N * EPS32 * float(want.abs().sum())
     close(z.grad, wdz, sdz + EPS32 * wdz.abs(), dtype, "dz")
     assert z.grad.dtype == TORCH[dtype] and not z.grad[7].any() and not z.grad[9].any()
+
+
+# ------------------------------------------------------------------------------------------- rows that no sequence has
+@pytest.mark.gpu
+@pytest.mark.parametrize("first,end", [(0, 50), (3, 64), (10, 41)])
+def test_the_delta_rule_leaves_zeros_where_no_sequence_is(first, end):
+    """A batch that is padded to a size: outputs and gradients of the rows before the first sequence and behind the last are 0, whatever their operands, and the memory, held."""
+    N, keys, heads, dk, dv = 64, 1, 2, 16, 24
+    rows = [randn(i, N, *s) for i, s in enumerate([(keys, dk), (keys, dk), (heads, dv)])] + [-randn(5, N, heads).abs(), torch.rand(N, heads, device="cuda")]
+    s0, starts = randn(6, 2, heads, dk, dv), torch.tensor([first, 30, end], device="cuda")
+    dy, ds = randn(7, N, heads, dv), randn(8, 2, heads, dk, dv)
+
+    def call(rows, s0, starts, dy):
+        leaves = [t.clone().requires_grad_() for t in (*rows, s0)]
+        y, s_last = rl.GatedDeltaRule.apply(*leaves, starts, dk ** -0.5, 1e-6)
+        stale = [torch.full((n,), math.nan, device="cuda") for n in [N * keys * dk, N * heads * dv, N * heads] for _ in range(6)]
+        del stale                                                            # what fresh tensors may find in their memory
+        return [y, s_last, *torch.autograd.grad([y, s_last], leaves, [dy, ds])]
+
+    inside = slice(first, end)
+    want = call([t[inside] for t in rows], s0, starts - first, dy[inside])
+    padded = [t.clone() for t in rows]
+    for t in padded:
+        t[:first], t[end:] = math.nan, math.nan
+    dy[:first], dy[end:] = math.nan, math.nan
+    stale = [torch.full((N * heads * dv,), math.nan, device="cuda") for _ in range(6)]
+    del stale
+    got = call(padded, s0, starts, dy)
+    for name, a, b in zip(("y", "s_last", "dq", "dk", "dv", "ddecay", "dbeta", "ds0"), got, want):
+        if a.shape == b.shape:
+            assert torch.equal(a, b), name
+        else:
+            assert torch.equal(a[inside], b) and not a[:first].any() and not a[end:].any(), name
