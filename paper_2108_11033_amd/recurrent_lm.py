@@ -239,7 +239,9 @@ class PolicyLoss(torch.autograd.Function):
 
 
 def clip_gradients(parameters, max_norm: float, unscale: float = 1.0) -> torch.Tensor:
-    """Every gradient times unscale min(1, max_norm / norm), in place; the norm (of all, unscaled), one number on the GPU."""
+    """Every gradient times unscale min(1, max_norm / norm), in place; the norm (of all, unscaled), one number on the GPU.  A parameter, or any number of them."""
+    if isinstance(parameters, torch.Tensor):                   # (whose rows have no gradients of their own)
+        parameters = [parameters]
     grads = [p.grad for p in parameters if p.grad is not None]
     _check_place(*grads)
     group = lm.GradList(grads)

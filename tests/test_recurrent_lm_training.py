@@ -115,3 +115,12 @@ def test_the_delta_rule_leaves_zeros_where_no_sequence_is(first, end):
             assert torch.equal(a, b), name
         else:
             assert torch.equal(a[inside], b) and not a[:first].any() and not a[end:].any(), name
+
+
+# ------------------------------------------------------------------------------------------- clipping
+@pytest.mark.gpu
+def test_one_parameter_is_clipped_too():
+    p = torch.zeros(3, 4, device="cuda", requires_grad=True)
+    p.grad = torch.full((3, 4), 2.0, device="cuda")
+    norm = rl.clip_gradients(p, 1.0)
+    assert abs(float(norm) - math.sqrt(48)) <= 6 * EPS32 * 7 and float((p.grad.double() - 1 / math.sqrt(12)).abs().max()) <= 12 * EPS32
