@@ -238,16 +238,22 @@ class PolicyLoss(torch.autograd.Function):
                        advantage=rows[2], weight=rows[3], temperature=numbers[0], clip_low=numbers[1], clip_high=numbers[1], kl=numbers[2], stream=torch.cuda.current_stream())
 
 
+@torch.no_grad()
 def clip_gradients(parameters, max_norm: float, unscale: float = 1.0) -> torch.Tensor:
     """Every gradient times unscale min(1, max_norm / norm), in place; the norm (of all, unscaled), one number on the GPU.  A parameter, or any number of them."""
     if isinstance(parameters, torch.Tensor):                   # (whose rows have no gradients of their own)
         parameters = [parameters]
     grads = [p.grad for p in parameters if p.grad is not None]
+    _check(len({id(t) for t in grads}) == len(grads), "a gradient is there twice")
     _check_place(*grads)
-    group = lm.GradList(grads)
+    together = [t.contiguous() for t in grads]                 # (copies of those that are not, clipped and copied back)
+    group = lm.GradList(together)
     dev = torch.device("cuda", torch.cuda.current_device())
     norm = torch.empty(1, device=dev)
     lm.grad_clip(group, max_norm, unscale, norm, _scratch(group.workspace, dev), torch.cuda.current_stream())
+    for t, clipped in zip(grads, together):
+        if clipped is not t:
+            t.copy_(clipped)
     return norm
 
 

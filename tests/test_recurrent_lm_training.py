@@ -124,3 +124,34 @@ def test_one_parameter_is_clipped_too():
     p.grad = torch.full((3, 4), 2.0, device="cuda")
     norm = rl.clip_gradients(p, 1.0)
     assert abs(float(norm) - math.sqrt(48)) <= 6 * EPS32 * 7 and float((p.grad.double() - 1 / math.sqrt(12)).abs().max()) <= 12 * EPS32
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_gradients_of_any_strides_are_clipped(dtype):
+    """Gradients of transposed parameters, and parts of a wider buffer: each is clipped where it lies, and nothing around it."""
+    buffer = randn(1, 20, 30).to(TORCH[dtype])
+    around = buffer.clone()
+    grads = [randn(2, 12, 7).to(TORCH[dtype]).t(), buffer[3:9, 5:20], randn(3, 2, 5, 6, 4).to(TORCH[dtype]).to(memory_format=torch.channels_last), randn(4, 33).to(TORCH[dtype])]
+    before = [t.clone() for t in grads]
+    parameters = []
+    for t in grads:
+        parameters.append(torch.zeros_like(t).requires_grad_())
+        parameters[-1].grad = t
+    norm = rl.clip_gradients(parameters, 0.5, unscale=0.25)
+    want = 0.25 * math.sqrt(sum(float((t.double() ** 2).sum()) for t in before))
+    assert abs(float(norm) - want) <= want * 6 * EPS32
+    for p, t, b in zip(parameters, grads, before):
+        assert p.grad is t
+        clipped = b.double() * (0.25 * 0.5 / want)
+        close(t, clipped, clipped.abs() * 10 * EPS32, dtype, f"{tuple(b.shape)}")
+    around[3:9, 5:20] = buffer[3:9, 5:20]
+    assert torch.equal(around, buffer)
+
+
+def test_a_gradient_that_is_there_twice_is_refused():
+    for shape in ((3, 4), (4, 3)):
+        p = torch.zeros(4, 3).t() if shape == (3, 4) else torch.zeros(shape)
+        p.requires_grad_().grad = torch.zeros_like(p)
+        with pytest.raises(ValueError, match="twice"):
+            rl.clip_gradients([p, p], 1.0)
