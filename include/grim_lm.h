@@ -208,7 +208,7 @@ grim_status grim_policy_loss(const void *z_dev, grim_dtype dt, int64_t ldz, cons
 /*
  * The norm of all gradients of a model, and clipping by it:
  *     norm = |unscale| * sqrt(sum over all tensors of g^2)        out = g * unscale * min(1, max_norm / norm)
- * (unscale takes a loss scale back).  Squares are summed in fp64.  A norm that is not finite leaves the gradients unclipped (out = g * unscale): whoever
+ * (unscale takes a loss scale back).  Squares are summed in fp64.  A norm that is not finite in fp32 leaves the gradients unclipped (out = g * unscale): whoever
  * reads the norm can skip the step.
  * A list names the gradients of a step.  It is host memory alone, holds no tensor alive and may be made anew for every step; it must not be freed while a call
  * with it runs on another thread (kernels have copies of it).

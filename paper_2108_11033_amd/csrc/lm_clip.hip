@@ -182,8 +182,8 @@ __global__ void __launch_bounds__(256) scale_grads(const ClipParams p) {
     __shared__ double room[256];
     const double norm = norm_of(p, room);
     if (threadIdx.x == 0 && blockIdx.x == 0 && p.first_group == 0) p.norm[0] = (float)norm;
-    // (a norm that is none leaves the gradients unclipped: whoever reads it can skip the step)
-    const float factor = (float)(norm > p.max_norm && norm < INFINITY ? p.unscale * (p.max_norm / norm) : p.unscale);
+    // (a norm that is none, as it is read in fp32, leaves the gradients unclipped: whoever reads it can skip the step)
+    const float factor = (float)(norm > p.max_norm && (float)norm < INFINITY ? p.unscale * (p.max_norm / norm) : p.unscale);
     for (uint32_t b = blockIdx.x; b < p.runs; b += gridDim.x) {
         const uint32_t r = p.runs - 1 - b;
         const int i = tensor_of(p, r);
