@@ -133,9 +133,20 @@ __global__ void __launch_bounds__(256) sum_squares(const ClipParams p) {
     if (threadIdx.x == 0) p.sums[p.first_group + blockIdx.x] = sum;
 }
 
+// A factor as the product of two numbers, so that one that fp32 does not hold (1e-3 of a norm of 1e38) keeps its digits: below 2^-100 each takes half of its exponent, above the second is 1.
+// (What the first product loses then, at its end, is nothing after the second.)
+struct Factor {
+    float first, second;
+    __device__ __forceinline__ explicit Factor(double f) {
+        const int half = f != 0. && fabs(f) < 0x1p-100 ? ilogb(f) / 2 : 0;
+        first = (float)ldexp(f, -half), second = ldexpf(1.f, half);
+    }
+    __device__ __forceinline__ float times(float v) const { return v * first * second; }
+};
+
 // out = g * factor for a run; a thread reads what it writes, so that out may be g.
 template <typename T, typename O, bool PAST>
-__device__ __forceinline__ void scale_run(const T *g, O *out, int64_t left, float factor) {
+__device__ __forceinline__ void scale_run(const T *g, O *out, int64_t left, Factor factor) {
     // 16 bytes of the wider type, so that an access of a wave is one piece of memory (two halves of 32 bytes a lane instead, bf16 into fp32, 168 M: 265 us)
     constexpr int V = 16 / (int)(sizeof(T) > sizeof(O) ? sizeof(T) : sizeof(O)), PER = kRun / 256 / V;
     if (left >= kRun) {
@@ -147,7 +158,7 @@ __device__ __forceinline__ void scale_run(const T *g, O *out, int64_t left, floa
             float v[V];
             unpack(raw[k], v);
 #pragma unroll
-            for (int j = 0; j < V; ++j) v[j] *= factor;
+            for (int j = 0; j < V; ++j) v[j] = factor.times(v[j]);
             store<PAST>(out + (k * 256 + threadIdx.x) * V, v);
         }
     } else {
@@ -156,10 +167,10 @@ __device__ __forceinline__ void scale_run(const T *g, O *out, int64_t left, floa
             if (c + V <= left) {
                 unpack(load<V>(g + c), v);
 #pragma unroll
-                for (int j = 0; j < V; ++j) v[j] *= factor;
+                for (int j = 0; j < V; ++j) v[j] = factor.times(v[j]);
                 store(out + c, v);
             } else {
-                for (int j = 0; c + j < left; ++j) out[c + j] = (O)((float)g[c + j] * factor);
+                for (int j = 0; c + j < left; ++j) out[c + j] = (O)factor.times((float)g[c + j]);
             }
         }
     }
@@ -183,11 +194,11 @@ __global__ void __launch_bounds__(256) scale_grads(const ClipParams p) {
     const double norm = norm_of(p, room);
     if (threadIdx.x == 0 && blockIdx.x == 0 && p.first_group == 0) p.norm[0] = (float)norm;
     // (a norm that is none, as it is read in fp32, leaves the gradients unclipped: whoever reads it can skip the step)
-    const float factor = (float)(norm > p.max_norm && (float)norm < INFINITY ? p.unscale * (p.max_norm / norm) : p.unscale);
+    const Factor factor(norm > p.max_norm && (float)norm < INFINITY ? p.unscale * (p.max_norm / norm) : p.unscale);
     for (uint32_t b = blockIdx.x; b < p.runs; b += gridDim.x) {
         const uint32_t r = p.runs - 1 - b;
         const int i = tensor_of(p, r);
-        if (factor == 1.f && p.t[i].out == p.t[i].grad) continue;
+        if (factor.first == 1.f && p.t[i].out == p.t[i].grad) continue;
         const uint32_t first = i ? p.t[i - 1].last_run : 0;
         const int64_t at = (int64_t)(r - first) * kRun;
         with_type(p.t[i].dt, [&](auto type) {

@@ -20,3 +20,24 @@ def test_a_norm_that_fp32_does_not_hold_leaves_gradients_unclipped(unscale, plac
     norm, _, _ = clipped(g.GradList(grads, outs), 1.0, unscale)
     assert float(norm) == math.inf
     assert all(torch.equal(a, b * unscale) for a, b in zip(outs, before))
+
+
+def expect(grads, outs, before, norm, max_norm):
+    if math.sqrt(sum(float((t.double() ** 2).sum()) for t in before)) <= torch.finfo(torch.float32).max:
+        check(grads, outs, before, norm, max_norm, 1.0)
+    else:                                                                    # (10^37 times the root of 13200 numbers of about one)
+        assert float(norm) == math.inf and all(torch.equal(a, b.to(a.dtype)) for a, b in zip(outs, before))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("max_norm,size", [(1e-3, 1e36), (1e-2, 1e37), (1.0, 3e36), (1e-7, 1e36)])
+def test_factors_that_fp32_does_not_hold(dtype, max_norm, size):
+    """Factors down to 1e-45 and less: the clipped gradients are ordinary numbers, and keep their digits."""
+    grads = [(randn(2, 5000).clamp(-2, 2) * size).to(dtype), (randn(3, 8200).clamp(-2, 2) * size).to(dtype)]
+    for outs in ([torch.empty_like(t, dtype=torch.float32) for t in grads], [torch.empty_like(t) for t in grads]):
+        norm, _, _ = clipped(g.GradList(grads, outs), max_norm, 1.0)
+        expect(grads, outs, grads, norm, max_norm)
+    before = [t.clone() for t in grads]
+    norm, _, _ = clipped(g.GradList(grads), max_norm, 1.0)
+    expect(grads, grads, before, norm, max_norm)
