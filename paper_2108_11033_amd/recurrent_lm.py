@@ -74,7 +74,7 @@ class LayerNorm(torch.autograd.Function):
 
 class GatedRecurrence(torch.autograd.Function):
     """(outputs, last states in fp32) of packed sequences: gates N x 3H, bias 3H, h0 a row of H per sequence; seq_start holds the sequences'
-    starts and the end, one number more than there are sequences."""
+    starts and the end, one number more than there are sequences: 0 first, ascending, N last."""
 
     @staticmethod
     def forward(ctx, gates, bias, h0, seq_start):
@@ -330,8 +330,9 @@ def distill(student: RecurrentLM, teacher: RecurrentLM, batches, k: int = 16, te
 
 
 def reinforce(model: RecurrentLM, batches, rate: float = 1e-3, temperature: float = 1.0, clip: float = 0.2, kl: float = 0.05, max_norm: float = 1.0, epochs: int = 2):
-    """Steps of the clipped policy loss per batch of (tokens, seq_start, advantage of every token; the last token of a text is followed by none): the policy that the texts came from,
-    and the reference of the KL term, is the model before the batch's first step.  The losses."""
+    """Steps of the clipped policy loss per batch of (tokens, seq_start, advantage): token t + 1 of a text is the word that was sampled after token t, and advantage[t] is that word's (that
+    of a text's last token counts for nothing, as none follows it; the loss is the sum over the words by the number of tokens).  The policy that the texts came from, and the reference of
+    the KL term, is the model before the batch's first step.  The losses."""
     optimizer = torch.optim.Adam(model.parameters(), lr=rate)
     losses = []
     for tokens, seq_start, advantage in batches:

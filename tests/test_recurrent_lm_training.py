@@ -155,3 +155,68 @@ def test_a_gradient_that_is_there_twice_is_refused():
         p.requires_grad_().grad = torch.zeros_like(p)
         with pytest.raises(ValueError, match="twice"):
             rl.clip_gradients([p, p], 1.0)
+
+
+# ------------------------------------------------------------------------------------------- steps of the policy
+LENGTHS = [5, 0, 1, 22, 9, 0]                                                # two empty texts, one of a token
+RATE, CLIP, KL, MOST, TEMPERATURE, EPOCHS = 1.0, 0.02, 0.1, 0.5, 1.5, 3
+
+
+def _policy_operands(device):
+    starts = [sum(LENGTHS[:i]) for i in range(len(LENGTHS) + 1)]
+    gen = torch.Generator().manual_seed(12)
+    model = rl.RecurrentLM(96, 64, 2, 4)
+    return (model.to(device), starts, *(torch.randint(0, 96, (starts[-1],), generator=gen).to(device), torch.randn(starts[-1], generator=gen).to(device)))
+
+
+def _plain_reinforce(model, starts, tokens, advantage):
+    """Steps by the gradient in 64 bits: the losses, every step's ratios and the model after them.  Token t + 1 of a text is the word sampled after token t, whose advantage it has; every
+    token counts 1 / N, a text's last one with a loss of 0."""
+    model, N = copy.deepcopy(model).double(), len(tokens)
+    rows = torch.tensor([t for a, b in zip(starts, starts[1:]) for t in range(a, b - 1)], device=tokens.device)
+    losses, ratios, old = [], [], None
+    for _ in range(EPOCHS):
+        lp = torch.log_softmax(_plain_logits(model, tokens, starts)[rows] / TEMPERATURE, 1)[torch.arange(len(rows)), tokens[rows + 1]]
+        old = lp.detach() if old is None else old
+        r, d, A = torch.exp(lp - old), old - lp, advantage.double()[rows]
+        loss = (KL * (torch.exp(d) - d - 1) - torch.minimum(r * A, r.clamp(1 - CLIP, 1 + CLIP) * A)).sum() / N
+        model.zero_grad()
+        loss.backward()
+        norm = torch.sqrt(sum((p.grad ** 2).sum() for p in model.parameters()))
+        with torch.no_grad():
+            for p in model.parameters():
+                p -= RATE * p.grad * min(1.0, MOST / float(norm))
+        losses.append(float(loss.detach()))
+        ratios.append((r.detach(), float(norm)))
+    return losses, ratios, model
+
+
+def test_the_policys_steps_do_what_they_are_there_for():
+    """Of the 64-bit form alone: the steps leave the clipping's bounds on both sides, no ratio lies so near one that fp32 might see it on the other side, some norms are clipped."""
+    _, ratios, _ = _plain_reinforce(*_policy_operands("cpu"))
+    last, first = ratios[-1][0], ratios[0][0]
+    assert torch.equal(first, torch.ones_like(first)) and bool((last > 1 + CLIP).any()) and bool((last < 1 - CLIP).any())
+    for r, _ in ratios[1:]:
+        assert min(float((r - 1 - CLIP).abs().min()), float((r - 1 + CLIP).abs().min())) > 1e-3 * CLIP
+    assert any(norm > MOST for _, norm in ratios)
+
+
+@pytest.mark.gpu
+def test_the_policys_steps_against_plain_operations(monkeypatch):
+    """With steps by the gradient itself in place of the optimizer's, which divides what is off by what is left of it."""
+    monkeypatch.setattr(torch.optim, "Adam", lambda parameters, lr: torch.optim.SGD(parameters, lr=lr))
+    model, starts, tokens, advantage = _policy_operands("cuda")
+    before = {n: p.detach().double().clone() for n, p in model.named_parameters()}
+    want, ratios, after = _plain_reinforce(model, starts, tokens, advantage)
+    seq = torch.tensor(starts, dtype=torch.int32, device="cuda")
+    got = rl.reinforce(model, [(tokens, seq, advantage)], rate=RATE, temperature=TEMPERATURE, clip=CLIP, kl=KL, max_norm=MOST, epochs=EPOCHS)
+    # two layers of fp32 arithmetic: logits off by less than 1e-4 of their size, gradients by less than 2e-4 of theirs in the 2-norm, and so what each of the steps adds; a loss
+    # is a mean of advantages times ratios that are off by as much as the logits
+    logits = float(_plain_logits(after, tokens, starts).detach().abs().max())
+    assert len(got) == EPOCHS
+    for a, b in zip(got, want):
+        assert abs(a - b) <= 1e-4 * (1 + logits / TEMPERATURE) * float(advantage.abs().mean()), (got, want)
+    for (n, p), (_, q) in zip(model.named_parameters(), after.named_parameters()):
+        moved = q.detach() - before[n]
+        assert float((p.detach().double() - q.detach()).norm()) <= EPOCHS * (2e-4 * float(moved.norm()) + EPS32 * float(q.detach().norm())) + 1e-9, n
+    assert any(float((q.detach() - before[n]).norm()) > 1e-2 for n, q in after.named_parameters())
