@@ -17,7 +17,6 @@
 struct grim_grad_list {
     std::vector<grim_grad> tensors;         // none of them empty
     std::vector<int64_t> last_run;          // of every tensor, in its launch's numbers: one past its last run
-    int64_t elements = 0;
     int64_t workgroups = 0;                 // over all launches
 };
 
@@ -43,7 +42,6 @@ struct ClipParams {
     double unscale, max_norm;
     uint32_t runs, first_group;
     int32_t tensors;
-    bool clip, past;
     TensorArgs t[kTable];
 };
 static_assert(sizeof(ClipParams) <= 4096, "launch arguments");
@@ -298,7 +296,6 @@ grim_status grim_grad_list_create(const grim_grad *grads, int32_t count, grim_gr
             if (runs >= (int64_t)1 << 31) return GRIM_ERR_SHAPE;
             list.tensors.push_back(grads[i]);
             list.last_run.push_back(runs);
-            list.elements += grads[i].count;
             if (grads[i].out) {
                 const uintptr_t at = (uintptr_t)grads[i].out;
                 written.push_back({at, at + (uintptr_t)(grads[i].count * bytes_of((grim_dtype)grads[i].out_dt)), list.tensors.size() - 1});

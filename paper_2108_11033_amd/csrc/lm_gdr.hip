@@ -177,24 +177,24 @@ struct WalkRoom {
     }
 };
 
-// A workgroup takes 16 CT W columns of the states of a run of chunks of a sequence's head.  All that a chunk does to a column of the states stays in that column, so each of its W waves
-// has 16 CT columns to itself from chunk to chunk, in registers: results that are sums over tokens or keys are the next product's operands.  The waves meet only where keys, queries,
+// A workgroup takes 16 W columns of the states of a run of chunks of a sequence's head.  All that a chunk does to a column of the states stays in that column, so each of its W waves
+// has 16 columns to itself from chunk to chunk, in registers: results that are sums over tokens or keys are the next product's operands.  The waves meet only where keys, queries,
 // values and M are placed in LDS and where the products of queries and keys, which all need, are formed.
 // A chunk is six phases between barriers, of fetches, LDS reads, matrix and vector work in turn, none of which takes half the time (matrix cores 33 %, vector ALUs 40 %, LDS 40 % of it).  4096
 // chunks of 128 x 128 heads in bf16 with all that the backward pass needs 165 us, 0.73 GB moved at 4.4 TB/s; the maps of their 31 runs 170 us; 64 x 64 heads, 6000 chunks, 163 and 64.
 // MAPS: no outputs; what every run but a sequence's last does to the states, as S -> A S + B: B's columns (into the places of the states in front of the next run; of a sequence's
 // first run, whose start is known, these are the states themselves) come from a start of zeros, A's from the columns of 1 and values of zero.
 // HELP: the second half of the waves has no columns; they form the products of queries and keys.
-template <typename T, int DK, int W, int CT, bool WHOLE, bool MAPS, bool HELP>
+template <typename T, int DK, int W, bool WHOLE, bool MAPS, bool HELP>
 __global__ void __launch_bounds__(64 * W, 2) walk(GdrParams p) {
-    constexpr int C = Gdr<T>::chunk, PD = Gdr<T>::data, PC = Gdr<T>::comp, THREADS = 64 * W, COLS = 16 * CT * W;
+    constexpr int C = Gdr<T>::chunk, PD = Gdr<T>::data, PC = Gdr<T>::comp, THREADS = 64 * W, COLS = 16 * W;
     constexpr int TT = C / 16, SS = C / 32, DT = DK / 16, DS = DK / 32;     // tiles of tokens, sums over them; of the states' rows
     using Room = WalkRoom<T, DK, COLS, MAPS>;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const Room m(lds);
 
     // (the workgroups of a run, whose heads read the same rows, lie together)
-    const uint32_t value_blocks = (p.tiles + CT * W - 1) / (CT * W), blocks = value_blocks + (MAPS ? (DT + CT * W - 1) / (CT * W) : 0), heads = (uint32_t)p.heads;
+    const uint32_t value_blocks = (p.tiles + W - 1) / W, blocks = value_blocks + (MAPS ? (DT + W - 1) / W : 0), heads = (uint32_t)p.heads;
     const int block = (int)(blockIdx.x % blocks), h = (int)(blockIdx.x / blocks % heads);
     const uint32_t run = blockIdx.x / blocks / heads;
     const int s = sequence_of(p.seq_start, p.nseq, p.N, p.size, run);
@@ -205,39 +205,35 @@ __global__ void __launch_bounds__(64 * W, 2) walk(GdrParams p) {
     const bool map = MAPS && block >= (int)value_blocks;
     if (map && r == 0) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l15 = lane & 15, g4 = (lane >> 4) * 4, own = l15 * 16 + g4;
-    const int tile0 = ((map ? block - (int)value_blocks : block) * W + wave) * CT, tiles = map ? DT : p.tiles, col0 = map ? 0 : block * COLS;
-    const bool idle = tile0 >= tiles;
+    const int tile = (map ? block - (int)value_blocks : block) * W + wave, tiles = map ? DT : p.tiles, col0 = map ? 0 : block * COLS;
+    const bool idle = tile >= tiles;
     const T *q = static_cast<const T *>(p.q) + (int64_t)(h / p.group) * p.dk, *k = static_cast<const T *>(p.k) + (int64_t)(h / p.group) * p.dk;
     const T *v = static_cast<const T *>(p.v) + (int64_t)h * p.dv + col0;
     T *y = static_cast<T *>(p.y) + (int64_t)h * p.dv;
 
-    f32x4 state[DT][CT];                                    // rows 16 n + g4 .. + 3, column 16 (tile0 + c) + l15
+    f32x4 state[DT];                                        // rows 16 n + g4 .. + 3, column 16 tile + l15
     const int64_t head = ((int64_t)s * p.heads + h) * p.dk;
 #pragma unroll
-    for (int n = 0; n < DT; ++n)
+    for (int n = 0; n < DT; ++n) {
+        const int d = 16 * n + g4, col = 16 * tile + l15;
+        state[n] = f32x4{};
+        if (MAPS && r > 0) {
 #pragma unroll
-        for (int c = 0; c < CT; ++c) {
-            const int d = 16 * n + g4, col = 16 * (tile0 + c) + l15;
-            state[n][c] = f32x4{};
-            if (MAPS && r > 0) {
+            for (int e = 0; e < 4; ++e) state[n][e] = map && d + e == col ? 1.f : 0.f;
+        } else if (r > 0) {
+            if (tile < p.tiles) state[n] = *reinterpret_cast<const f32x4 *>(p.starts + ((((int64_t)run * p.heads + h) * p.tiles + tile) * DT + n) * 256 + own);
+        } else if (p.s0) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) state[n][c][e] = map && d + e == col ? 1.f : 0.f;
-            } else if (r > 0) {
-                if (tile0 + c < p.tiles) state[n][c] = *reinterpret_cast<const f32x4 *>(p.starts + ((((int64_t)run * p.heads + h) * p.tiles + tile0 + c) * DT + n) * 256 + own);
-            } else if (p.s0) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) state[n][c][e] = p.s0[(head + min(d + e, p.dk - 1)) * p.dv + min(col, p.dv - 1)];
-            }
+            for (int e = 0; e < 4; ++e) state[n][e] = p.s0[(head + min(d + e, p.dk - 1)) * p.dv + min(col, p.dv - 1)];
         }
+    }
 #pragma unroll
     for (int n = 0; n < DT; ++n)
 #pragma unroll
-        for (int c = 0; c < CT; ++c)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                asm volatile("" : "+v"(state[n][c][e]));    // (all are asked for before any is looked at)
-                if (16 * n + g4 + e >= p.dk || 16 * (tile0 + c) + l15 >= (map ? p.dk : p.dv)) state[n][c][e] = 0.f;
-            }
+        for (int e = 0; e < 4; ++e) {
+            asm volatile("" : "+v"(state[n][e]));           // (all are asked for before any is looked at)
+            if (16 * n + g4 + e >= p.dk || 16 * tile + l15 >= (map ? p.dk : p.dv)) state[n][e] = 0.f;
+        }
 
     // what the next chunk brings
     Rows<WHOLE, T, THREADS, C, DK> kn, qn;
@@ -295,31 +291,24 @@ __global__ void __launch_bounds__(64 * W, 2) walk(GdrParams p) {
                 put4(m.P, i, j, acc);
             }
         }
-        f32x4 x[TT][CT] = {}, out[TT][CT] = {};             // tokens x columns, columns x tokens
-        Frag<PC> u[SS][CT];
+        f32x4 x[TT] = {}, out[TT] = {};                     // tokens x columns, columns x tokens
+        Frag<PC> u[SS];
         if (!idle) {
         {
             if (!MAPS && p.states)
 #pragma unroll
                 for (int d = 0; d < DT; ++d)
-#pragma unroll
-                    for (int c = 0; c < CT; ++c)
-                        if (tile0 + c < p.tiles)
-                            *reinterpret_cast<f32x4 *>(p.states + ((((place + n) * p.heads + h) * p.tiles + tile0 + c) * DT + d) * 256 + own) = state[d][c];
+                    *reinterpret_cast<f32x4 *>(p.states + ((((place + n) * p.heads + h) * p.tiles + tile) * DT + d) * 256 + own) = state[d];
 #pragma unroll
             for (int d = 0; d < DS; ++d) {
-                Frag<PC> S[CT];
-#pragma unroll
-                for (int c = 0; c < CT; ++c) S[c] = operand<PC>(state[2 * d][c], state[2 * d + 1][c]);
+                const Frag<PC> S = operand<PC>(state[2 * d], state[2 * d + 1]);
 #pragma unroll
                 for (int t = 0; t < TT; ++t) {
                     const Frag<PD> a = along(m.K, 16 * t, 32 * d);
-#pragma unroll
-                    for (int c = 0; c < CT; ++c) x[t][c] = multiply(a, S[c], x[t][c]);
+                    x[t] = multiply(a, S, x[t]);
                     if (MAPS) continue;
                     const Frag<PD> e = along(m.Q, 16 * t, 32 * d);
-#pragma unroll
-                    for (int c = 0; c < CT; ++c) out[t][c] = multiply(S[c], e, out[t][c]);
+                    out[t] = multiply(S, e, out[t]);
                 }
             }
         }
@@ -328,56 +317,46 @@ __global__ void __launch_bounds__(64 * W, 2) walk(GdrParams p) {
         for (int t = 0; t < TT; ++t) {
             const f32x4 f = *reinterpret_cast<const f32x4 *>(m.fk + 16 * t + g4);
             const float fo = m.fq[16 * t + l15];
-#pragma unroll
-            for (int c = 0; c < CT; ++c) x[t][c] = m.V.get(16 * t, 16 * (wave * CT + c)) - f * x[t][c], out[t][c] *= fo;
+            x[t] = m.V.get(16 * t, 16 * wave) - f * x[t], out[t] *= fo;
         }
-        const auto by = [&](const float *factor, f32x4 (&a)[TT][CT]) {
+        const auto by = [&](const float *factor, f32x4 (&a)[TT]) {
 #pragma unroll
             for (int t = 0; t < SS; ++t) {
                 const f32x4 lo = *reinterpret_cast<const f32x4 *>(factor + 32 * t + g4), hi = *reinterpret_cast<const f32x4 *>(factor + 32 * t + 16 + g4);
-#pragma unroll
-                for (int c = 0; c < CT; ++c) u[t][c] = operand<PC>(a[2 * t][c] * lo, a[2 * t + 1][c] * hi);
+                u[t] = operand<PC>(a[2 * t] * lo, a[2 * t + 1] * hi);
             }
         };
         by(m.beta, x);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int t = 0; t < TT; ++t) {
-            f32x4 less[CT] = {};
+            f32x4 less = {};
 #pragma unroll
             for (int j = 0; j <= t / 2; ++j) {
                 const Frag<PC> a = along(m.M, 16 * t, 32 * j);
-#pragma unroll
-                for (int c = 0; c < CT; ++c) less[c] = multiply(a, u[j][c], less[c]);
+                less = multiply(a, u[j], less);
             }
             const f32x4 bt = *reinterpret_cast<const f32x4 *>(m.beta + 16 * t + g4);
-#pragma unroll
-            for (int c = 0; c < CT; ++c) {
-                x[t][c] -= less[c];
-                if (!MAPS && p.states && tile0 + c < p.tiles)
-                    *reinterpret_cast<f32x4 *>(p.E + ((((place + n) * p.heads + h) * p.tiles + tile0 + c) * TT + t) * 256 + own) = x[t][c];
-                x[t][c] *= bt;                              // U
-            }
+            x[t] -= less;
+            if (!MAPS && p.states)
+                *reinterpret_cast<f32x4 *>(p.E + ((((place + n) * p.heads + h) * p.tiles + tile) * TT + t) * 256 + own) = x[t];
+            x[t] *= bt;                                     // U
         }
         __builtin_amdgcn_sched_barrier(0);
         by(m.fu, x);
         const float whole = decay_of(m.G[C - 1]);
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
-#pragma unroll
-            for (int c = 0; c < CT; ++c) state[d][c] *= whole;
+            state[d] *= whole;
 #pragma unroll
             for (int j = 0; j < SS; ++j) {
                 const Frag<PD> a = across(m.K, 16 * d, 32 * j);
-#pragma unroll
-                for (int c = 0; c < CT; ++c) state[d][c] = multiply(a, u[j][c], state[d][c]);
+                state[d] = multiply(a, u[j], state[d]);
             }
         }
         if (!MAPS)
 #pragma unroll
-            for (int t = 0; t < SS; ++t)
-#pragma unroll
-                for (int c = 0; c < CT; ++c) u[t][c] = operand<PC>(x[2 * t][c], x[2 * t + 1][c]);
+            for (int t = 0; t < SS; ++t) u[t] = operand<PC>(x[2 * t], x[2 * t + 1]);
         }
         __syncthreads();                                    // (the products of queries and keys are there)
         if (MAPS || idle) {
@@ -389,50 +368,42 @@ __global__ void __launch_bounds__(64 * W, 2) walk(GdrParams p) {
 #pragma unroll
             for (int j = 0; j <= t / 2; ++j) {
                 const Frag<PC> a = along(m.P, 16 * t, 32 * j);
-#pragma unroll
-                for (int c = 0; c < CT; ++c) out[t][c] = multiply(u[j][c], a, out[t][c]);
+                out[t] = multiply(u[j], a, out[t]);
             }
             const int i = 16 * t + l15;
-#pragma unroll
-            for (int c = 0; c < CT; ++c)
-                if (i < rows && tile0 + c < p.tiles) leave<WHOLE>(y + (first + i) * p.ldy, 16 * (tile0 + c) + g4, p.dv, out[t][c]);
+            if (i < rows) leave<WHOLE>(y + (first + i) * p.ldy, 16 * tile + g4, p.dv, out[t]);
         }
         __syncthreads();
     }
     if (idle) return;
     if (MAPS) {
 #pragma unroll
-        for (int n = 0; n < DT; ++n)
+        for (int n = 0; n < DT; ++n) {
+            if (!map) *reinterpret_cast<f32x4 *>(p.starts + ((((int64_t)(run + 1) * p.heads + h) * p.tiles + tile) * DT + n) * 256 + own) = state[n];
+            else
 #pragma unroll
-            for (int c = 0; c < CT; ++c) {
-                if (tile0 + c >= tiles) continue;
-                if (!map) *reinterpret_cast<f32x4 *>(p.starts + ((((int64_t)(run + 1) * p.heads + h) * p.tiles + tile0 + c) * DT + n) * 256 + own) = state[n][c];
-                else
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) p.maps[(((int64_t)run * p.heads + h) * DK + 16 * n + g4 + e) * DK + 16 * (tile0 + c) + l15] = state[n][c][e];
-            }
+                for (int e = 0; e < 4; ++e) p.maps[(((int64_t)run * p.heads + h) * DK + 16 * n + g4 + e) * DK + 16 * tile + l15] = state[n][e];
+        }
         return;
     }
     if (!p.s_last || to < span.end) return;
 #pragma unroll
-    for (int n = 0; n < DT; ++n)
+    for (int n = 0; n < DT; ++n) {
+        const int d = 16 * n + g4, col = 16 * tile + l15;
 #pragma unroll
-        for (int c = 0; c < CT; ++c) {
-            const int d = 16 * n + g4, col = 16 * (tile0 + c) + l15;
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (d + e < p.dk && col < p.dv) p.s_last[(head + d + e) * p.dv + col] = state[n][c][e];
-        }
+        for (int e = 0; e < 4; ++e)
+            if (d + e < p.dk && col < p.dv) p.s_last[(head + d + e) * p.dv + col] = state[n][e];
+    }
 }
 
 // ---------------------------------------------------------------------------------------------------- launches
-template <typename T, int DK, int W, int CT, bool WHOLE, bool MAPS, bool HELP = false>
+template <typename T, int DK, int W, bool WHOLE, bool MAPS, bool HELP = false>
 grim_status walk_launch(const GdrParams &p, hipStream_t stream) {
-    constexpr int bytes = WalkRoom<T, DK, 16 * CT * W, MAPS>::bytes;
-    const auto kernel = walk<T, DK, W, CT, WHOLE, MAPS, HELP>;
+    constexpr int bytes = WalkRoom<T, DK, 16 * W, MAPS>::bytes;
+    const auto kernel = walk<T, DK, W, WHOLE, MAPS, HELP>;
     static std::atomic<bool> grown{false};
     if (!lds_of(reinterpret_cast<const void *>(kernel), bytes, grown)) return GRIM_ERR_DEVICE;
-    const int64_t blocks = (p.tiles + CT * W - 1) / (CT * W) + (MAPS ? (DK / 16 + CT * W - 1) / (CT * W) : 0), groups = runs_of(p.N, p.nseq, p.size) * p.heads * blocks;
+    const int64_t blocks = (p.tiles + W - 1) / W + (MAPS ? (DK / 16 + W - 1) / W : 0), groups = runs_of(p.N, p.nseq, p.size) * p.heads * blocks;
     hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(64 * W), bytes, stream, p);
     return launched();
 }
@@ -445,18 +416,18 @@ grim_status gdr_launch(const GdrParams &p, hipStream_t stream) {
         grim_status st = launched();
         if (st != GRIM_OK) return st;
         if (p.size < (uint32_t)p.N) {
-            st = walk_launch<T, DK, 4, 1, WHOLE, true>(p, stream);
+            st = walk_launch<T, DK, 4, WHOLE, true>(p, stream);
             if (st != GRIM_OK) return st;
             st = join_runs<T, DK, false>(p, stream);
             if (st != GRIM_OK) return st;
         }
     }
-    if (p.tiles > 4) return walk_launch<T, DK, 8, 1, WHOLE, false>(p, stream);
+    if (p.tiles > 4) return walk_launch<T, DK, 8, WHOLE, false>(p, stream);
     // 64 columns: four waves, two such workgroups to a compute unit, or where there are not enough of them (or for keys of 128, which are too much for the registers of four
     // waves) another four that help: 512 tokens in 8 sequences, 16 heads of 64 x 64 in fp16, 30.0 us -> 25.4; 24007 in 40 sequences, in bf16, 164 with four and 205 with eight.
     if constexpr (DK == 64)
-        if (runs_of(p.N, p.nseq, p.size) * p.heads > kComputeUnits) return walk_launch<T, DK, 4, 1, WHOLE, false>(p, stream);
-    return walk_launch<T, DK, 8, 1, WHOLE, false, true>(p, stream);
+        if (runs_of(p.N, p.nseq, p.size) * p.heads > kComputeUnits) return walk_launch<T, DK, 4, WHOLE, false>(p, stream);
+    return walk_launch<T, DK, 8, WHOLE, false, true>(p, stream);
 }
 
 template <typename T>

@@ -224,11 +224,11 @@ __device__ __forceinline__ void settle(const Pack<T, V> &raw, int c, int width, 
 }
 
 // Elements c .. c + 3 of a row of `width`.
-template <bool WHOLE, bool PAST = false, typename T>
+template <bool WHOLE, typename T>
 __device__ __forceinline__ void leave(T *row, int c, int width, f32x4 v) {
     if (c + 4 <= width) {
         const float t[4] = {v[0], v[1], v[2], v[3]};
-        store<PAST>(row + c, t);
+        store(row + c, t);
     } else if (!WHOLE) {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
