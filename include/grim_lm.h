@@ -111,7 +111,7 @@ grim_status grim_glr_step(const float *gates_dev, int64_t ldg, const float *bias
  *                   that no sequence has are neither read nor written
  *   y_dev           N x (heads dv) of element type dt, rows of ldy; must not overlap the inputs
  *   s_last_dev      nseq x heads x dk x dv fp32, the states after the last tokens (of an empty sequence: its s0), or NULL; must not overlap s0
- *   states_dev      grim_gdr_states(...) bytes for the backward pass, 16-byte aligned, or NULL
+ *   states_dev      grim_gdr_states(...) bytes for the backward pass, 16-byte aligned, or NULL.  (Enough for any dt: fp32 keeps half as much again as 16 bits.)
  *   workspace       grim_gdr_workspace(...) bytes, for either direction
  * Backward, for the gradients dy of y and ds_last of s_last (or NULL: zeros), of the same inputs with the states that the forward call left:
  *   dq_dev, dk_dev, dv_dev   of element type dt, in the inputs' shapes, rows of lddq, lddk, lddv (those of a key head: sums over the heads that read it)
@@ -223,7 +223,7 @@ typedef struct grim_grad_list grim_grad_list;
 
 /*
  * Tensors without elements may be in the list; an empty list has the norm 0.
- * Errors: NULL, SHAPE (count outside 0 .. 2^20, a tensor of more than 2^40 elements or 100 tensors in a row of more than 2^43, outputs that overlap each other or a gradient other than their own),
+ * Errors: NULL, SHAPE (count outside 0 .. 2^20, a tensor of more than 2^40 elements or 100 tensors in a row of 2^44 and more, outputs that overlap each other or a gradient other than their own),
  * DTYPE, ALLOC.
  */
 grim_status grim_grad_list_create(const grim_grad *grads, int32_t count, grim_grad_list **out);

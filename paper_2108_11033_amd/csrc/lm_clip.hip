@@ -2,8 +2,8 @@
 //
 //     norm = |unscale| sqrt(sum over all tensors of g^2)        out = g unscale min(1, max_norm / norm)
 //
-// Bound by memory: the gradients are read once for the norm and once more to be scaled (nothing that is on chip holds a model's gradients), the outputs
-// written once.  Squares are summed in fp64, where those of any fp32 number neither overflow nor vanish; of fp16, whose squares are exact in fp32, eight at a
+// Bound by memory: the gradients are read once for the norm and once more to be scaled, the outputs written once.  (Models of up to some 100 MB of gradients would fit the compute units'
+// registers in between, in one launch whose workgroups wait for each other: not built.)  Squares are summed in fp64, where those of any fp32 number neither overflow nor vanish; of fp16, whose squares are exact in fp32, eight at a
 // time in fp32 first.  A workgroup takes runs of a tensor (below) in turn and leaves one sum; the scaling workgroups join these sums themselves, each in the same
 // order, so that no launch stands between, and walk the runs from the last one back: what was read last is still in the last-level cache.
 // Tensors travel as launch arguments: no table on the device has to be written before, and a captured call keeps its own.

@@ -424,7 +424,8 @@ grim_status gdr_launch(const GdrParams &p, hipStream_t stream) {
     }
     if (p.tiles > 4) return walk_launch<T, DK, 8, WHOLE, false>(p, stream);
     // 64 columns: four waves, two such workgroups to a compute unit, or where there are not enough of them (or for keys of 128, which are too much for the registers of four
-    // waves) another four that help: 512 tokens in 8 sequences, 16 heads of 64 x 64 in fp16, 30.0 us -> 25.4; 24007 in 40 sequences, in bf16, 164 with four and 205 with eight.
+    // waves) another four that help: 512 tokens in 8 sequences, 16 heads of 64 x 64 in fp16, 42.1 us with four and 36.1 with eight (with chunk_matrices); 24007 in 40 sequences, in bf16,
+    // both directions, 759 with four and 775 with eight.
     if constexpr (DK == 64)
         if (runs_of(p.N, p.nseq, p.size) * p.heads > kComputeUnits) return walk_launch<T, DK, 4, WHOLE, false>(p, stream);
     return walk_launch<T, DK, 8, WHOLE, false, true>(p, stream);

@@ -370,7 +370,7 @@ __device__ __forceinline__ int sequence_of(const int32_t *starts, int nseq, int6
 }
 
 // What is kept of a chunk for a head: the matrix M in parts, columns paired, the blocks of Triangle one after another; the running sums of the decays' base-2 logarithms in fp64; and of every token, with r the
-// factors that its key and its query count with (0 behind the last one), beta, the decay since the chunk's start times r_k, the decay until its end times r_k, the
+// factors that its key and its query count with, beta (0 behind the last one), the decay since the chunk's start times r_k, the decay until its end times r_k, the
 // decay since its start times r_q, r_k, r_q.
 template <typename T>
 struct Saved {
@@ -439,7 +439,9 @@ inline grim_status gdr_check(grim_dtype dt, int64_t N, int32_t nseq, bool starts
 
 // Tokens of a run.  Over runs of s chunks a head of n chunks costs 2 s chunks (what a run does to the states has to be formed first) and n / s steps of the join instead of n chunks,
 // some 5 us each where a step is 1.5 to 2: s is the root of n / 8, or what runs that fill the compute units once (twice where two workgroups share one) come to.  One sequence
-// and 4 heads of 64 x 64 in bf16, runs of 2, 4, 8 chunks: 1024 tokens 38, 48, 70 us, 4096 63, 61, 79, 32768 213, 213, 173 (without runs some 5 us a chunk).
+// and 4 heads of 64 x 64 in bf16, runs of 2, 4, 8 chunks: 1024 tokens 38, 48, 70 us, 4096 63, 61, 79, 32768 213, 213, 173 (without runs some 5 us a chunk).  The lengths lie on the
+// GPU, so that the mean stands for all of them: a long sequence among many short ones is walked chunk after chunk (32749 tokens in 256 sequences, one of 30000, 8 heads of 128 x 128 in bf16,
+// both directions, 8.6 ms; the 30000 alone 1.2).
 template <typename T>
 uint32_t run_of(int64_t N, int32_t nseq, int32_t heads, int32_t dv) {
     constexpr int64_t C = Gdr<T>::chunk;
