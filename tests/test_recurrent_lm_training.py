@@ -84,6 +84,39 @@ def test_distillation_gradients_take_the_scale_before_they_are_rounded(dtype, fa
     assert z.grad.dtype == TORCH[dtype] and not z.grad[7].any() and not z.grad[9].any()
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+def test_losses_captured_with_their_gradients(dtype):
+    """Both losses, forward and backward, in a graph: every replay, on new logits and under a new scale, gives what eager calls give."""
+    N, V, k = 30, 5000, 8
+    z, ids, old, ref, A, w = test_lm_policy.operands(dtype, N, V, 1.0, 0, 0, 29)
+    _, top, lists, _ = test_lm_distill._operands(dtype, N, V, k, 0, 0, 31)
+    scale = torch.ones((), device="cuda")
+    z.requires_grad_()
+
+    def step():
+        loss, logp = rl.PolicyLoss.apply(z, ids, old, ref, A, w, 1.0, 0.2, 0.05)
+        other = rl.DistillTopK.apply(z, top, lists, 2.0, w)
+        return [loss.detach(), logp, other.detach(), *torch.autograd.grad(loss, z, scale), *torch.autograd.grad(other, z, scale)]
+
+    stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        step()
+    stream.synchronize()
+    with torch.cuda.graph(graph, stream=stream):
+        captured = step()
+    for seed in range(4):
+        with torch.no_grad():
+            z.copy_(randn(seed, N, V))
+            scale.fill_([1.0, SCALE, -3.0, 0.5][seed])
+        graph.replay()
+        torch.cuda.synchronize()
+        for got, want in zip(captured, step()):
+            assert torch.equal(got, want), seed
+        torch.cuda.synchronize()
+
+
 # ------------------------------------------------------------------------------------------- rows that no sequence has
 @pytest.mark.gpu
 @pytest.mark.parametrize("first,end", [(0, 50), (3, 64), (10, 41)])
