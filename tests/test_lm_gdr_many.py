@@ -61,3 +61,25 @@ def test_places_among_many_sequences(nseq):
     close(y, *want["y"], "f32", "y")
     empty = torch.tensor([n == 0 for n in lengths], device="cuda")
     assert torch.equal(s_last[empty], c.s0[empty])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("before,behind,starts,heads,dk,dv", [(333, 500, [0, 900, 2100], 1, 128, 128), (1200, 3, [0, 500, 1300], 4, 40, 33), (70, 65, [0, 1, 1, 30], 2, 64, 64)])
+def test_rows_of_no_sequence_around_runs(dtype, before, behind, starts, heads, dk, dv):
+    """Sequences that start after the first row and end before the last: what is around them is neither read nor written, however they are cut."""
+    c = Back(dtype, starts, heads, 1, dk, dv, seed=dk)
+    want, inside = c.want(dy=c.dy, ds_last=c.ds_last), slice(before, before + starts[-1])
+    p = Back(dtype, [0] * (len(starts) - 1) + [before + starts[-1] + behind], heads, 1, dk, dv, seed=dk)
+    p.seq = torch.tensor(starts, dtype=torch.int32, device="cuda") + before
+    for name in ("q", "k", "v", "decay", "beta", "dy"):
+        getattr(p, name).fill_(float("nan"))
+        getattr(p, name)[inside] = getattr(c, name)
+    p.s0, p.ds_last = c.s0, c.ds_last
+    y, s_last = p.forward()
+    got = dict(p.backward(), y=y)
+    close(s_last, *want["s_last"], "f32", "s_last")
+    close(got.pop("ds0"), *want["ds0"], "f32", "ds0")
+    for name, t in got.items():
+        close(t[inside], *want[name], "f32" if name in ("ddecay", "dbeta") else dtype, name)
+        assert torch.isnan(t[:before]).all() and torch.isnan(t[before + starts[-1]:]).all(), name
